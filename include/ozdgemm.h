@@ -268,6 +268,91 @@ oz_status_t oz_native_dgemm(oz_handle_t handle, void* stream, char transa, char 
                             const double* A, int64_t lda, const double* B, int64_t ldb,
                             double beta, double* C, int64_t ldc);
 
+/* ---- 8-bit block-scaled operands, their products, and rows sorted by group ------------------------
+ *
+ * The same matrix units, used once per product: operands in 8-bit floating point with a scale for each block of
+ * 128 along the contraction, as language models are trained and served with.  Conventions of this part:
+ *   - Matrices are row-major with the contraction contiguous: a product is C = A * B^T with A m x k, B n x k, C m x n.
+ *   - Device pointers owned by the caller, work enqueued on `stream`, nothing allocated, nothing synchronised, as above.
+ *   - Sizes of zero are no errors.  Limits: rows and columns <= 2^24, bytes per row < 2^23, groups <= 1024, choices < 2^30.
+ *   - offsets: device int32[groups + 1], ascending from 0 to at most the number of rows: rows offsets[g] .. offsets[g+1] - 1
+ *     are group g's.  Groups may be empty. */
+typedef enum { OZ_F32 = 0, OZ_BF16 = 1, OZ_F16 = 2, OZ_E4M3 = 3, OZ_E5M2 = 4, OZ_E8M0 = 5 } oz_type_t;
+
+/* A matrix of 8-bit floats with its scales: element (r, c) stands for data * scale of block (r / block_rows, c / 128).
+ * OZ_E8M0 scales are bytes b for 2^(b-127), 255 for NaN: the matrix unit applies them itself.  OZ_F32 scales may have any value. */
+typedef struct {
+    void* data;           /* (r, c) at r*ld + c; 16-byte aligned */
+    void* scale;          /* (i, b) at i*scale_ld + b; 4-byte aligned */
+    int64_t ld;           /* bytes per row, multiple of 16, >= columns */
+    int64_t scale_ld;     /* elements per row of blocks, >= ceil(columns / 128); OZ_E8M0: multiple of 4 */
+    int64_t stride;       /* bytes from one matrix of a batch, or one group's, to the next; multiple of 16 */
+    int64_t scale_stride; /* the same for the scales, in elements; OZ_E8M0: multiple of 4 */
+    int32_t type;         /* OZ_E4M3 or OZ_E5M2 */
+    int32_t scale_type;   /* OZ_E8M0 or OZ_F32 */
+    int32_t block_rows;   /* 1 or 128 */
+    int32_t reserved_;    /* 0 */
+} oz_scaled_t;
+
+/* X (rows x cols, row-major, OZ_F32 / OZ_BF16 / OZ_F16, batch matrices stride_x elements apart) in 8-bit floats: `by_rows` as it is,
+ * `by_columns` transposed (cols x rows), either may be NULL; both have the same block_rows.  The scale of a block is 2^e with the
+ * least e >= -126 that keeps its largest |x| within the type's range (448, 57344), 1 for a block of zeros; values are x 2^-e
+ * rounded to nearest even, the only rounding there is.  A block that holds an infinity or a NaN becomes NaN, with scale NaN.
+ * Columns up to the next multiple of 16 are written, as zeros.
+ *   order (may be NULL; batch 1, block_rows 1): row r is row order[r] / order_div of X (x_rows of them), zeros where order[r] is negative
+ *     or the row is not there.
+ *   offsets (may be NULL; batch 1, block_rows 1): the columns of by_columns are cut into groups: group g's rows of X become columns from
+ *     128 * sum_{g' < g} ceil(count_g' / 128) on, zeros up to the next multiple of 128; rows behind the last group are left out.
+ *     by_columns needs ld >= 128 * w and scale_ld >= w with w = floor((rows + 127 * min(groups, rows)) / 128). */
+oz_status_t oz_quantize(oz_handle_t handle, void* stream, int64_t rows, int64_t cols, const void* X, int64_t ldx, int32_t x_type,
+                        int64_t batch, int64_t stride_x, const int32_t* order, int64_t order_div, int64_t x_rows,
+                        const int32_t* offsets, int64_t groups, const oz_scaled_t* by_rows, const oz_scaled_t* by_columns);
+
+/* C = A B^T (+ C if accumulate), C row-major m x n in OZ_F32, OZ_BF16 or OZ_F16, ldc in elements.  A in OZ_E4M3 or OZ_E5M2, B in OZ_E4M3;
+ * both with scales of one type.  Sums are held in 32 bits and rounded once.  k == 0: C = 0, or C as it is.
+ * workspace: 256-byte aligned, oz_scaled_gemm_workspace_bytes(...) bytes (0: may be NULL): parts of a k that is cut where the output alone
+ * leaves the GPU idle, added in their order. */
+size_t oz_scaled_gemm_workspace_bytes(oz_handle_t handle, int64_t m, int64_t n, int64_t k);
+oz_status_t oz_scaled_gemm(oz_handle_t handle, void* stream, int64_t m, int64_t n, int64_t k, const oz_scaled_t* A, const oz_scaled_t* B,
+                           void* C, int64_t ldc, int32_t c_type, int32_t accumulate, void* workspace, size_t workspace_bytes);
+
+/* Rows in groups: rows offsets[g] .. of C = the same rows of A times B_g^T, B_g at B->data + g * B->stride.  Rows of C behind the last
+ * group are set to zero.  m: rows of A and of C. */
+oz_status_t oz_scaled_gemm_grouped(oz_handle_t handle, void* stream, int64_t groups, const int32_t* offsets, int64_t m, int64_t n, int64_t k,
+                                   const oz_scaled_t* A, const oz_scaled_t* B, void* C, int64_t ldc, int32_t c_type);
+
+/* Contraction in groups: C_g = A_g B_g^T (+ C_g), A_g and B_g the columns that oz_quantize gives group g in by_columns with the
+ * same offsets; C_g at C + g * stride_c elements.  An empty group's C_g is zero, or as it is.  k: columns of A and B, a multiple of 128. */
+oz_status_t oz_scaled_gemm_grouped_k(oz_handle_t handle, void* stream, int64_t groups, const int32_t* offsets, int64_t m, int64_t n, int64_t k,
+                                     const oz_scaled_t* A, const oz_scaled_t* B, void* C, int64_t ldc, int64_t stride_c, int32_t c_type,
+                                     int32_t accumulate);
+
+/* tokens * topk choices, chosen[t * topk + j] the expert that token t takes as its j-th (int32 or int64: id_bytes 4 or 8; a value outside
+ * 0 .. experts-1, such as -1, is a choice that is dropped), sorted by expert, each expert's in their own order:
+ *   offsets int32[experts + 1]   slots offsets[e] .. offsets[e+1] - 1 are expert e's
+ *   order   int32[tokens * topk] slot -> choice, -1 behind the last
+ *   place   int32[tokens * topk] choice -> slot, -1 if dropped
+ * workspace: 256-byte aligned, oz_sort_tokens_workspace_bytes(...) bytes (0: may be NULL). */
+size_t oz_sort_tokens_workspace_bytes(oz_handle_t handle, int64_t tokens, int64_t topk, int64_t experts);
+oz_status_t oz_sort_tokens(oz_handle_t handle, void* stream, int64_t tokens, int64_t topk, int64_t experts, const void* chosen,
+                           int32_t id_bytes, int32_t* offsets, int32_t* order, int32_t* place, void* workspace, size_t workspace_bytes);
+
+/* Y[s] = X[order[s] / order_div] for `slots` rows of `cols` values, zeros where order[s] is negative or X (x_rows rows) has no such row.
+ * type of X and Y: OZ_F32, OZ_BF16 or OZ_F16. */
+oz_status_t oz_gather_rows(oz_handle_t handle, void* stream, int64_t slots, int64_t cols, int32_t type, const void* X, int64_t ldx,
+                           int64_t x_rows, const int32_t* order, int64_t order_div, void* Y, int64_t ldy);
+
+/* Y[t] = sum_j weights[t * topk + j] * X[place[t * topk + j]], j ascending, in 32 bits, rounded once; choices without a row in X (slots rows)
+ * are left out.  weights NULL: all 1 (the gradient of oz_gather_rows).  topk <= 64. */
+oz_status_t oz_combine_rows(oz_handle_t handle, void* stream, int64_t tokens, int64_t topk, int64_t cols, int32_t type, const void* X,
+                            int64_t ldx, int64_t slots, const int32_t* place, const float* weights, void* Y, int64_t ldy);
+
+/* Gradients of oz_combine_rows: dX[place] = weight * dY[t], rows of slots that no choice has (order[s] negative) zero; dweights = <dY[t],
+ * X[place]>, 0 for dropped choices.  dweights NULL, or weights NULL: not computed, or 1. */
+oz_status_t oz_combine_rows_grad(oz_handle_t handle, void* stream, int64_t tokens, int64_t topk, int64_t cols, int32_t type, const void* dY,
+                                 int64_t lddy, const void* X, int64_t ldx, int64_t slots, const int32_t* order, const int32_t* place,
+                                 const float* weights, void* dX, int64_t lddx, float* dweights);
+
 const char* oz_status_string(oz_status_t status);
 
 #ifdef __cplusplus

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "oz_f64_direct.h"
+#include "oz_scaled.h"
 
 // Workspace of oz_dgemm_static: device memory owned by the library, one copy per GPU that loads
 // it, held until the process ends.  In host code this name is only a handle for
@@ -209,6 +210,13 @@ struct StageClock {
 };
 
 }  // namespace
+
+namespace oz {
+
+bool handle_on_device(oz_handle_t h) { return on_handle_device(*h); }
+int handle_compute_units(oz_handle_t h) { return h->num_cu; }
+
+}  // namespace oz
 
 extern "C" {
 

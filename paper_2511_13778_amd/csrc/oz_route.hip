@@ -1,0 +1,355 @@
+// Rows sorted by group (tokens by expert), gathered, and combined back with their weights.
+//
+// Sort: a stable counting sort of the choices by expert.  Within 64 choices the lanes of one expert find each other with one ballot
+// per bit of its number; rank = lanes before, plus what the wave, the waves before and the blocks before counted of that
+// expert.  No atomics: the order is the same in every run.
+// Gather and combine move rows; what bounds them is memory.
+#include "oz_scaled_device.h"
+
+namespace oz {
+
+namespace {
+
+constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
+constexpr int kSortBlock = 4096;          // choices of a workgroup, more where that would be over 256 workgroups
+
+int sort_block(int64_t choices) {
+    const int64_t per = (choices + 255) / 256;
+    return int(per <= kSortBlock ? kSortBlock : (per + kSortThreads - 1) / kSortThreads * kSortThreads);
+}
+
+struct SortArgs {
+    const void* chosen;
+    int32_t *offsets, *order, *place, *counts;      // counts[e * blocks + b]
+    int choices, experts, bits, per_block, blocks;
+    bool wide;
+};
+
+__device__ __forceinline__ int chosen_expert(const SortArgs& p, int i, int end) {
+    if (i >= end) return -1;
+    const int64_t e = p.wide ? static_cast<const int64_t*>(p.chosen)[i] : static_cast<const int32_t*>(p.chosen)[i];
+    return e >= 0 && e < p.experts ? int(e) : -1;
+}
+
+// Lanes of this wave with the same expert (0 for none).
+__device__ __forceinline__ unsigned long long same_expert(int e, int bits) {
+    unsigned long long m = __ballot(e >= 0);
+    for (int b = 0; b < bits; ++b) {
+        const unsigned long long set = __ballot((e >> b) & 1);
+        m &= ((e >> b) & 1) ? set : ~set;
+    }
+    return e >= 0 ? m : 0;
+}
+
+// count[wave][expert] of this block's choices; waves take consecutive parts of it
+__device__ __forceinline__ void count_block(const SortArgs& p, int begin, int end, int32_t* count) {
+    for (int i = threadIdx.x; i < kSortWaves * p.experts; i += kSortThreads) count[i] = 0;
+    __syncthreads();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int per_wave = p.per_block / kSortWaves;
+    int32_t* mine = count + wave * p.experts;
+    const int from = begin + wave * per_wave, to = min(from + per_wave, end);
+    for (int i = from; i < to; i += 64) {
+        const int e = chosen_expert(p, i + lane, to);
+        const unsigned long long m = same_expert(e, p.bits);
+        if (m && (m & ((1ull << lane) - 1)) == 0) mine[e] += __popcll(m);       // one lane per expert
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs p) {
+    extern __shared__ int32_t count[];
+    const int begin = int(blockIdx.x) * p.per_block, end = min(begin + p.per_block, p.choices);
+    count_block(p, begin, end, count);
+    for (int e = threadIdx.x; e < p.experts; e += kSortThreads) {
+        int sum = 0;
+        for (int w = 0; w < kSortWaves; ++w) sum += count[w * p.experts + e];
+        p.counts[int64_t(e) * p.blocks + blockIdx.x] = sum;
+    }
+}
+
+// Where each choice goes.  Every workgroup adds up the counts of all blocks by itself (at most 256 per expert, one wave each).
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs p) {
+    extern __shared__ int32_t count[];                    // [waves][experts], then total and start of each expert
+    __shared__ int32_t wave_total[kSortWaves + 1];
+    int32_t* total = count + kSortWaves * p.experts;      // all choices of an expert, then its first slot
+    int32_t* before = total + p.experts;                  // those in blocks before this one
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, block = blockIdx.x;
+    const int begin = block * p.per_block, end = min(begin + p.per_block, p.choices);
+    count_block(p, begin, end, count);
+    if (p.blocks == 1) {
+        for (int e = threadIdx.x; e < p.experts; e += kSortThreads) {
+            int sum = 0;
+            for (int w = 0; w < kSortWaves; ++w) sum += count[w * p.experts + e];
+            total[e] = sum;
+            before[e] = 0;
+        }
+    } else {
+        for (int e = wave; e < p.experts; e += kSortWaves) {
+            int all = 0, prev = 0;
+            for (int b = lane; b < p.blocks; b += 64) {
+                const int c = p.counts[int64_t(e) * p.blocks + b];
+                all += c;
+                prev += b < block ? c : 0;
+            }
+            for (int d = 1; d < 64; d <<= 1) {
+                all += __shfl_xor(all, d);
+                prev += __shfl_xor(prev, d);
+            }
+            if (lane == 0) {
+                total[e] = all;
+                before[e] = prev;
+            }
+        }
+    }
+    __syncthreads();
+    // exclusive prefix over the experts, 512 at a time
+    int carry = 0;
+    for (int e0 = 0; e0 < p.experts; e0 += kSortThreads) {
+        const int e = e0 + threadIdx.x;
+        const int mine = e < p.experts ? total[e] : 0;
+        int sum = mine;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(sum, d);
+            if (lane >= d) sum += o;
+        }
+        if (lane == 63) wave_total[wave] = sum;
+        __syncthreads();
+        int base = carry;
+        for (int w = 0; w < wave; ++w) base += wave_total[w];
+        for (int w = 0; w < kSortWaves; ++w) carry += wave_total[w];
+        if (e < p.experts) {
+            total[e] = base + sum - mine;
+            if (block == 0) p.offsets[e] = base + sum - mine;
+        }
+        __syncthreads();
+    }
+    const int live = carry;
+    if (block == 0 && threadIdx.x == 0) p.offsets[p.experts] = live;
+    // first slot of each wave's choices
+    for (int e = threadIdx.x; e < p.experts; e += kSortThreads) {
+        int at = total[e] + before[e];
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int c = count[w * p.experts + e];
+            count[w * p.experts + e] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+    const int per_wave = p.per_block / kSortWaves;
+    int32_t* next = count + wave * p.experts;
+    const int from = begin + wave * per_wave, to = min(from + per_wave, end);
+    for (int i0 = from; i0 < to; i0 += 64) {
+        const int i = i0 + lane;
+        const int e = chosen_expert(p, i, to);
+        const unsigned long long m = same_expert(e, p.bits);
+        const unsigned long long lower = m & ((1ull << lane) - 1);
+        int slot = -1;
+        if (m) slot = next[e] + __popcll(lower);
+        __builtin_amdgcn_wave_barrier();
+        if (m && lower == 0) next[e] += __popcll(m);
+        __builtin_amdgcn_wave_barrier();
+        if (i < to) {
+            p.place[i] = slot;
+            if (slot >= 0) p.order[slot] = i;
+            if (i >= live) p.order[i] = -1;
+        }
+    }
+}
+
+// ---- rows ---------------------------------------------------------------------------------------
+
+constexpr int kUnitVecs = 4;              // 16-byte loads a lane has in flight: a wave moves 4 KB of a row
+
+struct GatherArgs {
+    const uint8_t* x;
+    uint8_t* y;
+    int64_t ldx, ldy;                     // bytes
+    const int32_t* order;
+    int order_div, x_rows, slots, row_bytes, pieces;
+};
+
+// A wave per 4 KB of a row.  T: the widest type that every row's address and length is a multiple of.
+template <typename T>
+__global__ __launch_bounds__(256) void gather_rows_kernel(GatherArgs p) {
+    const uint32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int s = int(id / uint32_t(p.pieces)), piece = int(id - uint32_t(s) * uint32_t(p.pieces)), lane = threadIdx.x & 63;
+    if (s >= p.slots) return;
+    const int o = p.order[s], src = o < 0 ? -1 : o / p.order_div;
+    const bool there = src >= 0 && src < p.x_rows;
+    const int from = piece * 4096, to = min(from + 4096, p.row_bytes);
+    const uint8_t* x = p.x + int64_t(there ? src : 0) * p.ldx;
+    uint8_t* y = p.y + int64_t(s) * p.ldy;
+    constexpr int kStep = 64 * int(sizeof(T));
+    for (int at = from + lane * int(sizeof(T)); at < to; at += kStep * kUnitVecs) {
+        T v[kUnitVecs];
+#pragma unroll
+        for (int u = 0; u < kUnitVecs; ++u) {
+            v[u] = T{};
+            if (there && at + u * kStep < to) v[u] = *reinterpret_cast<const T*>(x + at + u * kStep);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnitVecs; ++u)
+            if (at + u * kStep < to) *reinterpret_cast<T*>(y + at + u * kStep) = v[u];
+    }
+}
+
+struct CombineArgs {
+    const void *x, *dy;
+    void *y, *dx;
+    int64_t ldx, ldy, lddy, lddx;
+    const int32_t *order, *place;
+    const float* weights;
+    float* dweights;
+    int tokens, topk, cols, slots, pieces;
+    bool vec;
+};
+
+
+// A wave per 512 columns of a token; the choices' rows four at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs p) {
+    const uint32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int t = int(id / uint32_t(p.pieces)), piece = int(id - uint32_t(t) * uint32_t(p.pieces)), lane = threadIdx.x & 63;
+    if (t >= p.tokens) return;
+    const int col = piece * 512 + lane * 8, have = p.cols - col;
+    const T* x = static_cast<const T*>(p.x);
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int j0 = 0; j0 < p.topk; j0 += 4) {
+        float v[4][8], w[4];
+        bool live[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t c = int64_t(t) * p.topk + j0 + u;
+            const int s = j0 + u < p.topk ? p.place[c] : -1;
+            live[u] = s >= 0 && s < p.slots;
+            w[u] = live[u] && p.weights ? p.weights[c] : 1.0f;
+            if (live[u]) load_row<8>(x + int64_t(s) * p.ldx + col, have, p.vec, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (live[u])
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[u], v[u][i], sum[i]);
+    }
+    store_row<8>(static_cast<T*>(p.y) + int64_t(t) * p.ldy + col, have, p.vec, sum);
+}
+
+// A wave per choice: the choices of a token lie in one workgroup and find its dY in the cache.
+template <typename T>
+__global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs p) {
+    const uint32_t c = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (c >= uint32_t(p.slots)) return;
+    const int s = p.place[c];
+    const bool live = s >= 0 && s < p.slots;
+    const float w = live && p.weights ? p.weights[c] : 1.0f;
+    const T* dy = static_cast<const T*>(p.dy) + int64_t(c / uint32_t(p.topk)) * p.lddy;
+    const T* x = static_cast<const T*>(p.x) + int64_t(live ? s : 0) * p.ldx;
+    T* dx = static_cast<T*>(p.dx) + int64_t(live ? s : 0) * p.lddx;
+    float dot = 0.0f;
+    if (live) {
+        for (int col = lane * 8; col < p.cols; col += 1024) {
+            float g[2][8], v[2][8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int at = col + u * 512;
+                if (at < p.cols) {
+                    load_row<8>(dy + at, p.cols - at, p.vec, g[u]);
+                    if (p.dweights) load_row<8>(x + at, p.cols - at, p.vec, v[u]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int at = col + u * 512;
+                if (at < p.cols) {
+                    float out[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (p.dweights) dot = fmaf(g[u][i], v[u][i], dot);
+                        out[i] = w * g[u][i];
+                    }
+                    store_row<8>(dx + at, p.cols - at, p.vec, out);
+                }
+            }
+        }
+        for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
+    }
+    if (p.dweights && lane == 0) p.dweights[c] = dot;
+    if (p.order[c] < 0) {                 // slot c belongs to no choice
+        const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        T* row = static_cast<T*>(p.dx) + int64_t(c) * p.lddx;
+        for (int col = lane * 8; col < p.cols; col += 512) store_row<8>(row + col, p.cols - col, p.vec, none);
+    }
+}
+
+template <typename T>
+bool aligned16(const void* p, int64_t ld) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * int64_t(sizeof(T)) % 16 == 0;
+}
+
+template <typename T>
+void combine_typed(hipStream_t st, CombineArgs p) {
+    p.vec = aligned16<T>(p.x, p.ldx) && aligned16<T>(p.y, p.ldy);
+    p.pieces = (p.cols + 511) / 512;
+    const int64_t waves = int64_t(p.tokens) * p.pieces;
+    hipLaunchKernelGGL(combine_rows_kernel<T>, dim3(unsigned((waves + 3) / 4)), dim3(256), 0, st, p);
+}
+
+template <typename T>
+void combine_grad_typed(hipStream_t st, CombineArgs p) {
+    p.vec = aligned16<T>(p.dy, p.lddy) && aligned16<T>(p.dx, p.lddx) && (!p.dweights || aligned16<T>(p.x, p.ldx));
+    hipLaunchKernelGGL(combine_grad_kernel<T>, dim3(unsigned((int64_t(p.slots) + 3) / 4)), dim3(256), 0, st, p);
+}
+
+}  // namespace
+
+size_t sort_tokens_bytes(int64_t choices, int64_t experts) {
+    const int64_t per = sort_block(choices), blocks = (choices + per - 1) / per;
+    return blocks > 1 ? size_t(blocks) * size_t(experts) * 4 : 0;
+}
+
+void launch_sort_tokens(hipStream_t st, int choices, int experts, const void* chosen, bool wide, int32_t* offsets, int32_t* order,
+                        int32_t* place, int32_t* ws) {
+    SortArgs p{chosen, offsets, order, place, ws, choices, experts, 0, sort_block(choices), 0, wide};
+    while ((1 << p.bits) < experts) ++p.bits;
+    p.blocks = choices > 0 ? (choices + p.per_block - 1) / p.per_block : 1;
+    if (p.blocks > 1)
+        hipLaunchKernelGGL(sort_count_kernel, dim3(p.blocks), dim3(kSortThreads), size_t(kSortWaves) * experts * 4, st, p);
+    hipLaunchKernelGGL(sort_place_kernel, dim3(p.blocks), dim3(kSortThreads), size_t(kSortWaves + 2) * experts * 4, st, p);
+}
+
+void launch_gather_rows(hipStream_t st, int slots, int cols, int elem_bytes, const void* x, int64_t ldx, int x_rows, const int32_t* order,
+                        int order_div, void* y, int64_t ldy) {
+    GatherArgs p{static_cast<const uint8_t*>(x), static_cast<uint8_t*>(y), ldx * elem_bytes, ldy * elem_bytes, order, order_div, x_rows, slots,
+                 cols * elem_bytes, 0};
+    p.pieces = (p.row_bytes + 4095) / 4096;
+    const uintptr_t all = reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y) | uintptr_t(p.ldx) | uintptr_t(p.ldy) | uintptr_t(p.row_bytes);
+    const dim3 grid(unsigned((int64_t(slots) * p.pieces + 3) / 4));
+    if (all % 16 == 0) hipLaunchKernelGGL(gather_rows_kernel<v4i32>, grid, dim3(256), 0, st, p);
+    else if (all % 4 == 0) hipLaunchKernelGGL(gather_rows_kernel<uint32_t>, grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL(gather_rows_kernel<uint16_t>, grid, dim3(256), 0, st, p);
+}
+
+void launch_combine_rows(hipStream_t st, int tokens, int topk, int cols, int type, const void* x, int64_t ldx, int slots, const int32_t* place,
+                         const float* weights, void* y, int64_t ldy) {
+    CombineArgs p{};
+    p.x = x; p.ldx = ldx; p.y = y; p.ldy = ldy; p.place = place; p.weights = weights;
+    p.tokens = tokens; p.topk = topk; p.cols = cols; p.slots = slots;
+    if (type == OZ_F32) combine_typed<float>(st, p);
+    else if (type == OZ_BF16) combine_typed<bf16_t>(st, p);
+    else combine_typed<f16_t>(st, p);
+}
+
+void launch_combine_grad(hipStream_t st, int tokens, int topk, int cols, int type, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                         int slots, const int32_t* order, const int32_t* place, const float* weights, void* dx, int64_t lddx, float* dweights) {
+    CombineArgs p{};
+    p.dy = dy; p.lddy = lddy; p.x = x; p.ldx = ldx; p.dx = dx; p.lddx = lddx; p.order = order; p.place = place; p.weights = weights;
+    p.dweights = dweights; p.tokens = tokens; p.topk = topk; p.cols = cols; p.slots = slots;
+    if (type == OZ_F32) combine_grad_typed<float>(st, p);
+    else if (type == OZ_BF16) combine_grad_typed<bf16_t>(st, p);
+    else combine_grad_typed<f16_t>(st, p);
+}
+
+}  // namespace oz

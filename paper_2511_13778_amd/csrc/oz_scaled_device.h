@@ -1,0 +1,113 @@
+// Device code that the kernels on 8-bit block-scaled operands and on sorted rows share.
+#pragma once
+
+#include "oz_scaled.h"
+
+namespace oz {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int v4i32 __attribute__((ext_vector_type(4)));
+typedef int v8i32 __attribute__((ext_vector_type(8)));
+
+// A piece of the rows: piece `t` of the groups cut into pieces of SIZE rows, each group for itself; group `groups` holds the rows
+// behind the last one.  blocks_before: 128-row blocks of the groups before.  Called by whole waves; offsets that are not ascending
+// or pass `rows` give wrong pieces, none outside 0 .. rows.
+struct GroupPiece {
+    int group, row, end;      // rows row .. min(row + SIZE, end) - 1; group < 0: no such piece
+    int blocks_before;
+};
+
+__device__ __forceinline__ int clamp_offset(const int32_t* offsets, int g, int rows) { return min(max(offsets[g], 0), rows); }
+
+template <int SIZE>
+__device__ __forceinline__ GroupPiece find_piece(const int32_t* __restrict__ offsets, int groups, int rows, int t) {
+    const int lane = threadIdx.x & 63;
+    int pieces = 0, blocks = 0;               // of the groups before this round's
+    for (int g0 = 0; g0 <= groups; g0 += 64) {
+        const int g = g0 + lane;
+        int lo = 0, hi = 0;
+        if (g <= groups) {
+            lo = clamp_offset(offsets, g, rows);
+            hi = g < groups ? max(lo, clamp_offset(offsets, g + 1, rows)) : rows;
+        }
+        const int mine = (hi - lo + SIZE - 1) / SIZE, blk = (hi - lo + kScaleBlock - 1) / kScaleBlock;
+        int sum = mine, bsum = blk;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(sum, d), ob = __shfl_up(bsum, d);
+            if (lane >= d) { sum += o; bsum += ob; }
+        }
+        const unsigned long long has = __ballot(pieces + sum > t);
+        if (has) {
+            const int src = __ffsll(has) - 1;
+            const int first = pieces + __shfl(sum, src) - __shfl(mine, src);
+            GroupPiece p;
+            p.group = __builtin_amdgcn_readfirstlane(g0 + src);
+            p.row = __builtin_amdgcn_readfirstlane(__shfl(lo, src) + (t - first) * SIZE);
+            p.end = __builtin_amdgcn_readfirstlane(__shfl(hi, src));
+            p.blocks_before = __builtin_amdgcn_readfirstlane(blocks + __shfl(bsum, src) - __shfl(blk, src));
+            return p;
+        }
+        pieces += __shfl(sum, 63);
+        blocks += __shfl(bsum, 63);
+    }
+    return GroupPiece{-1, 0, 0, 0};
+}
+
+// Rows of group g, and the 128-row blocks of the groups before it.
+struct GroupSpan { int count, blocks_before; };
+__device__ __forceinline__ GroupSpan group_span(const int32_t* __restrict__ offsets, int g, int rows) {
+    const int lane = threadIdx.x & 63;
+    int blocks = 0;
+    for (int q = lane; q < g; q += 64) {
+        const int lo = clamp_offset(offsets, q, rows), hi = max(lo, clamp_offset(offsets, q + 1, rows));
+        blocks += (hi - lo + kScaleBlock - 1) / kScaleBlock;
+    }
+    for (int d = 1; d < 64; d <<= 1) blocks += __shfl_xor(blocks, d);
+    const int lo = clamp_offset(offsets, g, rows), hi = max(lo, clamp_offset(offsets, g + 1, rows));
+    return GroupSpan{__builtin_amdgcn_readfirstlane(hi - lo), __builtin_amdgcn_readfirstlane(blocks)};
+}
+
+// ---- elements of 32 and 16 bits; a conversion to fewer bits rounds to nearest even ----------------
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+
+template <typename T>
+__device__ __forceinline__ float to_float(T x) { return static_cast<float>(x); }
+template <typename T>
+__device__ __forceinline__ void put(T* p, float x) { *p = static_cast<T>(x); }
+
+// N consecutive elements as floats: one to N/4 16-byte loads where `vec` says that p is aligned for them and all are there, else one by one
+// with zeros from `have` on.
+template <int N, typename T>
+__device__ __forceinline__ void load_row(const T* __restrict__ p, int have, bool vec, float (&x)[N]) {
+    if (vec && have >= N) {
+        constexpr int kVec = N * int(sizeof(T)) / 16;
+        static_assert(kVec * 16 == N * int(sizeof(T)), "whole 16-byte loads");
+        union { v4i32 v[kVec]; T e[N]; } u;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) u.v[i] = reinterpret_cast<const v4i32*>(p)[i];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = to_float(u.e[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = i < have ? to_float(p[i]) : 0.0f;
+    }
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void store_row(T* __restrict__ p, int have, bool vec, const float (&x)[N]) {
+    if (vec && have >= N) {
+        constexpr int kVec = N * int(sizeof(T)) / 16;
+        union { v4i32 v[kVec]; T e[N]; } u;
+#pragma unroll
+        for (int i = 0; i < N; ++i) put(&u.e[i], x[i]);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) reinterpret_cast<v4i32*>(p)[i] = u.v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < have) put(p + i, x[i]);
+    }
+}
+
+}  // namespace oz

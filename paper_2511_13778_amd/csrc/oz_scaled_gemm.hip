@@ -1,0 +1,185 @@
+// Product of 8-bit block-scaled matrices on tiles of C, tiles of the operands through LDS.
+//
+// A step is a block of 128 of k.  Its rows of A and B (128 bytes each) go from L2 straight into LDS, STAGES - 1 steps ahead;
+// one barrier per step.  A row's eight 16-byte pieces are stored at piece ^ (row & 7), so that the 16 lanes that read the same
+// piece of 16 rows meet different banks.  The scales come in the same way, four blocks at a time, into two buffers of their own.
+#include "oz_scaled_gemm_device.h"
+
+namespace oz {
+
+namespace {
+
+template <int BM, int BN, int WM, int WN, int STAGES, bool A_E5M2, bool E8M0>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel(ScaledGemm g, int tiles_n) {
+    constexpr int WAVES = (BM / WM) * (BN / WN), ROWS = BM + BN;
+    constexpr int COPIES = (ROWS / 8 + WAVES - 1) / WAVES;        // 1 KB each, per wave and step
+    static_assert(ROWS / 8 % WAVES == 0 && BM % 64 == 0 && BN % 64 == 0, "whole transfers");
+    constexpr int STAGE_BYTES = ROWS * kScaleBlock;
+    constexpr int SCALE_BYTES = ROWS * (E8M0 ? 4 : 16);           // four blocks of k
+    constexpr int SCALE_COPIES = ROWS / 64 * (E8M0 ? 1 : 4);
+    constexpr int MT = WM / 16, NT = WN / 16;
+    __shared__ __align__(16) uint8_t lds[STAGES * STAGE_BYTES + 2 * SCALE_BYTES];
+
+    const GemmTile t = locate<BM, BN>(g, int(blockIdx.x) / tiles_n, int(blockIdx.x) % tiles_n, int(blockIdx.y));
+    if (t.none) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % (BM / WM) * WM, wn = wave / (BM / WM) * WN;
+    const int steps = (t.k + kScaleBlock - 1) / kScaleBlock;
+    const int tail = t.k & (kScaleBlock - 1);                     // bytes of the last step if it is not whole
+
+    v4f acc[NT][MT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[j][i] = v4f{0, 0, 0, 0};
+
+    if (steps > 0) {
+        const uint32_t lds0 = lds_address(lds);
+        // transfer x of this wave: rows 8y .. 8y+7 of the stage, y = wave + x * WAVES; lane: row lane/8, piece (lane%8) ^ (row%8)
+        const uint32_t piece = uint32_t((lane & 7) ^ (lane >> 3)) * 16;
+        uint32_t off[COPIES];
+#pragma unroll
+        for (int x = 0; x < COPIES; ++x) {
+            const int y = wave + x * WAVES, r = y * 8 + (lane >> 3);
+            off[x] = y < BM / 8 ? uint32_t(min(r, t.rows - 1)) * uint32_t(g.a.ld) + piece
+                                : uint32_t(min(r - BM, t.cols - 1)) * uint32_t(g.b.ld) + piece;
+        }
+        // behind the end of a row lies nothing that may be read: its pieces come from the step's first one, and are masked
+        const uint32_t back = tail && int(piece) >= tail ? piece : 0;
+        auto copy_step = [&](int s) {
+            const uint32_t to = lds0 + uint32_t(s % STAGES) * STAGE_BYTES;
+            const uint32_t less = s == steps - 1 ? back : 0;
+#pragma unroll
+            for (int x = 0; x < COPIES; ++x) {
+                const int y = wave + x * WAVES;
+                copy16_to_lds((y < BM / 8 ? t.a : t.b) + int64_t(s) * kScaleBlock, off[x] - less, to + uint32_t(y) * 1024);
+            }
+        };
+        // the four blocks of k around block0 + s: dword [row] (E8M0: four bytes), or [block][row]
+        auto copy_scales = [&](int s) {
+            const int four = (t.block0 + s) & ~3;
+            const uint32_t to = lds0 + STAGES * STAGE_BYTES + uint32_t((four >> 2) & 1) * SCALE_BYTES;
+            for (int y = wave; y < SCALE_COPIES; y += WAVES) {
+                const int r0 = (E8M0 ? y : y % (ROWS / 64)) * 64;
+                const bool is_a = r0 < BM;
+                const int r = is_a ? min(t.row + r0 + lane, t.row + t.rows - 1) >> g.a.shift
+                                   : min(t.col + r0 - BM + lane, t.col + t.cols - 1) >> g.b.shift;
+                const int first = is_a ? t.row >> g.a.shift : t.col >> g.b.shift;
+                const int64_t ld = is_a ? g.a.scale_ld : g.b.scale_ld;
+                const int blk = E8M0 ? four : min(max(four + y / (ROWS / 64), t.block0), t.block0 + steps - 1);
+                copy4_to_lds((is_a ? t.sa : t.sb) + (int64_t(first) * ld + blk) * (E8M0 ? 1 : 4),
+                             uint32_t(r - first) * uint32_t(ld) * (E8M0 ? 1u : 4u), to + uint32_t(y) * 256);
+            }
+        };
+        auto copy = [&](int s) {
+            if (s >= steps) return;
+            if (s == 0 || ((t.block0 + s) & 3) == 0) copy_scales(s);
+            copy_step(s);
+        };
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) copy(s);
+
+        const uint32_t sw = uint32_t(lane & 7);
+        const int q = lane >> 4, x16 = lane & 15;
+        // this lane's pieces 2q and 2q+1 of row x16 of a fragment
+        const uint32_t p0 = uint32_t(x16) * kScaleBlock + ((uint32_t(2 * q) ^ sw) * 16), p1 = uint32_t(x16) * kScaleBlock + ((uint32_t(2 * q + 1) ^ sw) * 16);
+        for (int s = 0; s < steps; ++s) {
+            if (s + STAGES - 1 <= steps) wait_copies<COPIES * (STAGES - 2)>();
+            else wait_copies<0>();
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            copy(s + STAGES - 1);
+            const uint8_t* st = lds + (s % STAGES) * STAGE_BYTES;
+            auto fragment = [&](int row0) -> v8i32 {
+                union { v8i32 f; v4i32 h[2]; } u;
+                u.h[0] = *reinterpret_cast<const v4i32*>(st + row0 * kScaleBlock + p0);
+                u.h[1] = *reinterpret_cast<const v4i32*>(st + row0 * kScaleBlock + p1);
+                return u.f;
+            };
+            v8i32 fa[MT], fb[NT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) fa[i] = fragment(wm + i * 16);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) fb[j] = fragment(BM + wn + j * 16);
+            if (tail && s == steps - 1) {
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    const int have = min(max(tail - (q * 32 + w * 4), 0), 4);
+                    const int keep = have == 4 ? -1 : (1 << (8 * have)) - 1;
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) fa[i][w] &= keep;
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) fb[j][w] &= keep;
+                }
+            }
+            const int blk = t.block0 + s;
+            const uint8_t* sc = lds + STAGES * STAGE_BYTES + ((blk >> 2) & 1) * SCALE_BYTES;
+            if constexpr (E8M0) {
+                uint32_t sa[MT], sb[NT];
+                const int shift = (blk & 3) * 8;
+#pragma unroll
+                for (int i = 0; i < MT; ++i) sa[i] = *reinterpret_cast<const uint32_t*>(sc + (wm + i * 16 + x16) * 4) >> shift;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(sc + (BM + wn + j * 16 + x16) * 4) >> shift;
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) acc[j][i] = mfma_e8m0<A_E5M2>(fb[j], fa[i], acc[j][i], sb[j], sa[i]);
+            } else {
+                const float* fs = reinterpret_cast<const float*>(sc) + (blk & 3) * ROWS;
+                float sa[MT];
+                v4f sb[NT];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) sa[i] = fs[wm + i * 16 + x16];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) sb[j] = *reinterpret_cast<const v4f*>(fs + BM + wn + j * 16 + q * 4);
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        const v4f p = mfma_plain<A_E5M2>(fb[j], fa[i]);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[j][i][r] = fmaf(p[r] * sb[j][r], sa[i], acc[j][i][r]);
+                    }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+    }
+
+    const int q = lane >> 4, x16 = lane & 15;
+    const bool vec = aligned_c(g, t.c);
+    if (steps == 0 && g.accumulate) return;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int r = wm + i * 16 + x16;
+        if (r >= t.rows) continue;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int c = wn + j * 16 + q * 4;
+            if (c < t.cols) put4(g, t.c + int64_t(t.row + r) * g.ldc + t.col + c, t.cols - c, vec, acc[j][i]);
+        }
+    }
+}
+
+template <int BM, int BN, int WM, int WN, int STAGES>
+void launch_tiles(hipStream_t st, const ScaledGemm& g) {
+    const int tiles_n = (g.n + BN - 1) / BN;
+    const int64_t tiles_m = g.grouping == Grouping::kRows ? group_pieces(g.m, g.groups, BM) : (g.m + BM - 1) / BM;
+    const dim3 grid(unsigned(tiles_m * tiles_n), g.grouping == Grouping::kContraction ? unsigned(g.groups) : 1u);
+    const dim3 block(64 * (BM / WM) * (BN / WN));
+    if (g.e8m0) {
+        if (g.a_e5m2) hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, true, true>), grid, block, 0, st, g, tiles_n);
+        else hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, false, true>), grid, block, 0, st, g, tiles_n);
+    } else {
+        if (g.a_e5m2) hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, true, false>), grid, block, 0, st, g, tiles_n);
+        else hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, false, false>), grid, block, 0, st, g, tiles_n);
+    }
+}
+
+}  // namespace
+
+size_t scaled_gemm_part_bytes(int64_t, int64_t, int64_t, int) { return 0; }
+
+void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int, float*, size_t) { launch_tiles<128, 128, 64, 64, 4>(st, g); }
+
+}  // namespace oz

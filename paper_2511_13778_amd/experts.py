@@ -1,0 +1,99 @@
+"""Rows sorted by expert and back, on torch tensors: what stands before and behind the experts' products (scaled.gemm_grouped).
+
+A layer whose tokens go to their chosen experts:
+
+    routing = sort_tokens(h, ids, experts)                    # ids: tokens x topk, -1 where a choice is dropped
+    a = scaled.quantize(h, x, routing=routing)                # each choice's row, sorted by expert, in 8-bit floats
+    ys = scaled.gemm_grouped(h, a, w, routing.offsets)
+    y = combine(h, ys, routing, weights)
+
+Everything is enqueued on the current stream; nothing is read back, so no call waits for the GPU.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import ozdgemm as g
+from .scaled import check_ints, check_matrix, float_type, stream_of
+
+
+class Routing:
+    """Where each choice went: offsets (experts + 1: an expert's slots), order (slot -> choice, -1 behind the last), place (choice -> slot, -1
+    if dropped), all int32; choice t * topk + j is token t's j-th."""
+
+    __slots__ = ("offsets", "order", "place", "topk", "tokens")
+
+    def __init__(self, offsets, order, place, topk):
+        check_ints(offsets, "offsets")
+        check_ints(order, "order")
+        check_ints(place, "place", order.numel())
+        if topk < 1 or order.numel() % topk:
+            raise ValueError("%d choices are not %s per token" % (order.numel(), topk))
+        self.offsets, self.order, self.place, self.topk, self.tokens = offsets, order, place, topk, order.numel() // topk
+
+
+def sort_tokens(h: g.Handle, ids, experts: int) -> Routing:
+    """Sorts the choices ids (tokens x topk, int64 or int32) by expert, each expert's in their own order."""
+    if not ids.is_cuda or ids.dim() != 2 or ids.shape[1] < 1 or ids.dtype not in (torch.int64, torch.int32) or not ids.is_contiguous():
+        raise ValueError("ids: contiguous tokens x topk, int64 or int32, on the GPU")
+    tokens, topk = ids.shape
+    n = tokens * topk
+    need = h.sort_tokens_workspace_bytes(tokens, topk, experts)
+    # one allocation for the three tables and the workspace
+    at = [0, experts + 1, experts + 1 + n]
+    ws_at = -(-(at[2] + n) // 64) * 64
+    all_ = torch.empty(ws_at + (need + 3) // 4, dtype=torch.int32, device=ids.device)
+    base = all_.data_ptr()
+    h.call("oz_sort_tokens", stream_of(ids), tokens, topk, experts, ids.data_ptr(), ids.element_size(), base, base + 4 * at[1], base + 4 * at[2],
+           base + 4 * ws_at if need else None, need)
+    return Routing(all_[:experts + 1], all_[at[1]:at[2]], all_[at[2]:at[2] + n].view(tokens, topk), topk)
+
+
+def gather(h: g.Handle, x, routing: Routing, out=None):
+    """Each choice's row of x (tokens x cols), sorted by expert; zeros behind the last."""
+    ldx = check_matrix(x, "x")
+    if x.shape[0] != routing.tokens:
+        raise ValueError("x has %d rows, the routing %d tokens" % (x.shape[0], routing.tokens))
+    slots = routing.order.numel()
+    y = torch.empty((slots, x.shape[1]), dtype=x.dtype, device=x.device) if out is None else out
+    ldy = check_matrix(y, "out")
+    if tuple(y.shape) != (slots, x.shape[1]) or y.dtype != x.dtype:
+        raise ValueError("out: %d x %d of %s" % (slots, x.shape[1], x.dtype))
+    h.call("oz_gather_rows", stream_of(x), slots, x.shape[1], float_type(x.dtype), x.data_ptr(), ldx, x.shape[0], routing.order.data_ptr(),
+           routing.topk, y.data_ptr(), ldy)
+    return y
+
+
+def _weights(weights, routing):
+    if weights is None:
+        return None
+    if not weights.is_cuda or weights.dtype != torch.float32 or not weights.is_contiguous() or weights.numel() != routing.order.numel():
+        raise ValueError("weights: contiguous float32, one per choice, on the GPU")
+    return weights.data_ptr()
+
+
+def combine(h: g.Handle, xs, routing: Routing, weights=None, out=None):
+    """Sum over each token's choices of weight * the choice's row of xs, in 32 bits, rounded once.  Without weights: the gradient of gather."""
+    ldx = check_matrix(xs, "xs")
+    if xs.shape[0] != routing.order.numel():
+        raise ValueError("xs has %d rows, the routing %d slots" % (xs.shape[0], routing.order.numel()))
+    y = torch.empty((routing.tokens, xs.shape[1]), dtype=xs.dtype, device=xs.device) if out is None else out
+    ldy = check_matrix(y, "out")
+    if tuple(y.shape) != (routing.tokens, xs.shape[1]) or y.dtype != xs.dtype:
+        raise ValueError("out: %d x %d of %s" % (routing.tokens, xs.shape[1], xs.dtype))
+    h.call("oz_combine_rows", stream_of(xs), routing.tokens, routing.topk, xs.shape[1], float_type(xs.dtype), xs.data_ptr(), ldx, xs.shape[0],
+           routing.place.data_ptr(), _weights(weights, routing), y.data_ptr(), ldy)
+    return y
+
+
+def combine_backward(h: g.Handle, dy, xs, routing: Routing, weights):
+    """Gradients of combine for dy (tokens x cols): (of xs, of the weights)."""
+    lddy, ldx = check_matrix(dy, "dy"), check_matrix(xs, "xs")
+    if xs.shape != (routing.order.numel(), dy.shape[1]) or dy.shape[0] != routing.tokens or dy.dtype != xs.dtype:
+        raise ValueError("dy %s %s and xs %s %s do not belong to this routing" % (tuple(dy.shape), dy.dtype, tuple(xs.shape), xs.dtype))
+    dxs = torch.empty(xs.shape, dtype=xs.dtype, device=xs.device)
+    dw = torch.empty(weights.shape, dtype=torch.float32, device=xs.device)
+    h.call("oz_combine_rows_grad", stream_of(dy), routing.tokens, routing.topk, dy.shape[1], float_type(dy.dtype), dy.data_ptr(), lddy,
+           xs.data_ptr(), ldx, xs.shape[0], routing.order.data_ptr(), routing.place.data_ptr(), _weights(weights, routing), dxs.data_ptr(),
+           max(dxs.shape[1], 1), dw.data_ptr())
+    return dxs, dw

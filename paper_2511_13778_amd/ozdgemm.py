@@ -47,9 +47,20 @@ class oz_layout_t(C.Structure):
                 ("off_record", C.c_size_t), ("off_tileS", C.c_size_t), ("total_bytes", C.c_size_t)]
 
 
+OZ_F32, OZ_BF16, OZ_F16, OZ_E4M3, OZ_E5M2, OZ_E8M0 = range(6)
+
+
+class oz_scaled_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("ld", C.c_int64), ("scale_ld", C.c_int64),
+                ("stride", C.c_int64), ("scale_stride", C.c_int64), ("type", C.c_int32), ("scale_type", C.c_int32),
+                ("block_rows", C.c_int32), ("reserved_", C.c_int32)]
+
+
 EXPORTS = ("oz_create", "oz_destroy", "oz_default_opts", "oz_set_heuristic",
            "oz_dgemm_workspace_bytes", "oz_dgemm", "oz_dgemm_static", "oz_zgemm_workspace_bytes", "oz_zgemm", "oz_dgemm_strided_batched", "oz_dgemm_layout", "oz_profile_enable",
-           "oz_profile_read", "oz_native_dgemm", "oz_status_string")
+           "oz_profile_read", "oz_native_dgemm", "oz_status_string",
+           "oz_quantize", "oz_scaled_gemm_workspace_bytes", "oz_scaled_gemm", "oz_scaled_gemm_grouped", "oz_scaled_gemm_grouped_k",
+           "oz_sort_tokens_workspace_bytes", "oz_sort_tokens", "oz_gather_rows", "oz_combine_rows", "oz_combine_rows_grad")
 
 _lib = None
 
@@ -107,6 +118,20 @@ def load_library() -> C.CDLL:
     lib.oz_profile_read.restype = C.c_int
     lib.oz_status_string.argtypes = [C.c_int]
     lib.oz_status_string.restype = C.c_char_p
+    P, I, L, S = C.c_void_p, C.c_int32, C.c_int64, C.POINTER(oz_scaled_t)
+    for name, args in (("oz_quantize", [L, L, P, L, I, L, L, P, L, L, P, L, S, S]),
+                       ("oz_scaled_gemm", [L, L, L, S, S, P, L, I, I, P, C.c_size_t]),
+                       ("oz_scaled_gemm_grouped", [L, P, L, L, L, S, S, P, L, I]),
+                       ("oz_scaled_gemm_grouped_k", [L, P, L, L, L, S, S, P, L, L, I, I]),
+                       ("oz_sort_tokens", [L, L, L, P, I, P, P, P, P, C.c_size_t]),
+                       ("oz_gather_rows", [L, L, I, P, L, L, P, L, P, L]),
+                       ("oz_combine_rows", [L, L, L, I, P, L, L, P, P, P, L]),
+                       ("oz_combine_rows_grad", [L, L, L, I, P, L, P, L, L, P, P, P, P, L, P])):
+        getattr(lib, name).argtypes = [H, C.c_void_p] + args
+        getattr(lib, name).restype = C.c_int
+    for name in ("oz_scaled_gemm_workspace_bytes", "oz_sort_tokens_workspace_bytes"):
+        getattr(lib, name).argtypes = [H, L, L, L]
+        getattr(lib, name).restype = C.c_size_t
     _lib = lib
     return lib
 
@@ -220,6 +245,18 @@ class Handle:
                      ldc):
         _check(self.lib.oz_native_dgemm(self._h, stream_ptr, transa.encode(), transb.encode(), m, n, k,
                                         alpha, A_ptr, lda, B_ptr, ldb, beta, C_ptr, ldc), "oz_native_dgemm")
+
+    # 8-bit block-scaled operands and sorted rows: arguments as in include/ozdgemm.h, matrices as oz_scaled_t or None.  The calls
+    # on tensors are in `scaled` and `experts`.
+    def call(self, name, stream_ptr, *args):
+        """Enqueues the entry point `name` (oz_quantize .. oz_combine_rows_grad) on a stream; raises OzError on its status."""
+        _check(getattr(self.lib, name)(self._h, stream_ptr, *args), name)
+
+    def scaled_gemm_workspace_bytes(self, m, n, k) -> int:
+        return self.lib.oz_scaled_gemm_workspace_bytes(self._h, m, n, k)
+
+    def sort_tokens_workspace_bytes(self, tokens, topk, experts) -> int:
+        return self.lib.oz_sort_tokens_workspace_bytes(self._h, tokens, topk, experts)
 
     def profile_enable(self, max_calls: int):
         _check(self.lib.oz_profile_enable(self._h, max_calls), "oz_profile_enable")

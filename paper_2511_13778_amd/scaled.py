@@ -1,0 +1,184 @@
+"""8-bit floating-point matrices with a scale for each block of 128, and their products, on torch tensors.
+
+A matrix is row-major with the contraction contiguous, in float8_e4m3fn or float8_e5m2, with a scale per row and 128 columns
+(block_rows 1: activations, gradients) or per 128 x 128 block (block_rows 128: weights).  Scales are E8M0 bytes (torch.uint8 or
+float8_e8m0fnu: 2^(b - 127), 255 for NaN), which the matrix unit applies itself, or float32 of any value.  Products are
+C = A B^T, so a linear layer is
+
+    x, xt = quantize(h, x, which="both")                      # tokens x in, and its transpose for the weight gradient
+    w, wt = quantize(h, w, block_rows=128, which="both")      # out x in, and its transpose for the input gradient
+    y = gemm(h, x, w)
+    d, dt = quantize(h, dy, dtype=torch.float8_e5m2, which="both")
+    dx, dw = gemm(h, d, wt), gemm(h, dt, xt, dtype=torch.float32)
+
+Everything is enqueued on the current stream of the tensors' device; argument checks of the C ABI (include/ozdgemm.h) raise OzError, those
+made here ValueError.  Calls marshal arguments and allocate outputs; the arithmetic is in the HIP kernels.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import ozdgemm as g
+
+BLOCK = 128
+_FLOAT = {torch.float32: g.OZ_F32, torch.bfloat16: g.OZ_BF16, torch.float16: g.OZ_F16}
+_EIGHT = {torch.float8_e4m3fn: g.OZ_E4M3, torch.float8_e5m2: g.OZ_E5M2}
+_SCALE = {torch.float32: g.OZ_F32, torch.uint8: g.OZ_E8M0, torch.float8_e8m0fnu: g.OZ_E8M0}
+
+
+def float_type(dtype) -> int:
+    if dtype not in _FLOAT:
+        raise ValueError("float32, bfloat16 or float16, not %s" % dtype)
+    return _FLOAT[dtype]
+
+
+def stream_of(t) -> int:
+    """The current stream of the tensor's device, which has to be the current device."""
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def check_matrix(t, what):
+    """A CUDA tensor whose rows are contiguous; its leading dimension in elements."""
+    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s: a matrix on the GPU with contiguous rows, not %s %s of strides %s" % (what, t.device, tuple(t.shape), t.stride()))
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def check_ints(t, what, n=None):
+    if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError("%s: contiguous int32 on the GPU%s, not %s %s %s" % (what, "" if n is None else ", %d of them" % n, t.device, t.dtype, tuple(t.shape)))
+    return t
+
+
+class Scaled:
+    """An 8-bit matrix (rows x ld, or groups x rows x ld; the first `cols` columns count) and its scales ((rows / block_rows) x at
+    least ceil(cols / 128), for each group).  Rows start at multiples of 16 bytes; E8M0 scales' rows at multiples of 4."""
+
+    __slots__ = ("data", "scale", "cols", "block_rows", "desc")
+
+    def __init__(self, data, scale, cols=None, block_rows=1):
+        if data.dtype not in _EIGHT or scale.dtype not in _SCALE:
+            raise ValueError("8-bit floats with uint8, float8_e8m0fnu or float32 scales, not %s with %s" % (data.dtype, scale.dtype))
+        if data.dim() not in (2, 3) or scale.dim() != data.dim() or not data.is_cuda or scale.device != data.device:
+            raise ValueError("matrix and scales: two or three dimensions each, on one GPU")
+        cols = data.shape[-1] if cols is None else cols
+        rows = data.shape[-2]
+        if not 0 <= cols <= data.shape[-1] or block_rows not in (1, BLOCK):
+            raise ValueError("cols %s of %d, block_rows %s" % (cols, data.shape[-1], block_rows))
+        if scale.shape[-2] < -(-rows // block_rows) or scale.shape[-1] < -(-cols // BLOCK) or scale.shape[:-2] != data.shape[:-2]:
+            raise ValueError("scales %s do not cover %d x %d" % (tuple(scale.shape), rows, cols))
+        if (data.shape[-1] > 1 and data.stride(-1) != 1) or (scale.shape[-1] > 1 and scale.stride(-1) != 1):
+            raise ValueError("rows of the matrix and of its scales are contiguous")
+        self.data, self.scale, self.cols, self.block_rows = data, scale, cols, block_rows
+        groups = data.dim() == 3
+        # a single row has no distance to the next one: what the ABI asks of it is taken
+        ld = data.stride(-2) if rows > 1 else -(-data.shape[-1] // 16) * 16
+        sld = scale.stride(-2) if scale.shape[-2] > 1 else -(-scale.shape[-1] // 4) * 4
+        self.desc = g.oz_scaled_t(data.data_ptr(), scale.data_ptr(), ld, sld, data.stride(0) if groups else 0,
+                                  scale.stride(0) if groups else 0, _EIGHT[data.dtype], _SCALE[scale.dtype], block_rows, 0)
+
+    @property
+    def rows(self):
+        return self.data.shape[-2]
+
+    @property
+    def groups(self):
+        return self.data.shape[0] if self.data.dim() == 3 else 1
+
+    def values(self):
+        """The 8-bit numbers, without padding."""
+        return self.data[..., :self.cols]
+
+    def scales(self):
+        """The scales, without padding."""
+        return self.scale[..., :-(-self.cols // BLOCK)]
+
+
+def empty(rows, cols, block_rows=1, dtype=torch.float8_e4m3fn, scale_dtype=torch.uint8, groups=None, device="cuda") -> Scaled:
+    """An uninitialised matrix in the layout that the calls here want."""
+    lead = () if groups is None else (groups,)
+    data = torch.empty(lead + (rows, max(-(-cols // 16) * 16, 16)), dtype=dtype, device=device)
+    scale = torch.empty(lead + (-(-rows // block_rows), max(-(-cols // (4 * BLOCK)) * 4, 4)), dtype=scale_dtype, device=device)
+    return Scaled(data, scale, cols, block_rows)
+
+
+def grouped_columns(rows, groups) -> int:
+    """Columns of the transpose of `rows` rows in groups, each group's padded to whole blocks: what they can be at most."""
+    return (rows + (BLOCK - 1) * min(groups, rows)) // BLOCK * BLOCK
+
+
+def quantize(h: g.Handle, x, dtype=torch.float8_e4m3fn, scale_dtype=torch.uint8, block_rows=1, which="rows", routing=None, offsets=None):
+    """x (matrix, or groups x rows x cols) in 8-bit floats with power-of-two scales: `which` = "rows": as it is, "columns": its transpose,
+    "both": the two from one read, as a pair.  routing (experts.Routing): the tokens' rows in the routing's order, one per choice.
+    offsets: the rows are in groups, and the transpose's columns are cut into whole blocks per group, for gemm_grouped_k."""
+    if which not in ("rows", "columns", "both"):
+        raise ValueError("which: rows, columns or both, not %r" % (which,))
+    if dtype not in _EIGHT or scale_dtype not in _SCALE:
+        raise ValueError("8-bit floats with uint8, float8_e8m0fnu or float32 scales, not %s with %s" % (dtype, scale_dtype))
+    groups = x.shape[0] if x.dim() == 3 else None
+    ldx = check_matrix(x if groups is None else x.flatten(0, 1) if x.is_contiguous() else x[0], "x")
+    x_rows, cols = x.shape[-2:]
+    rows = x_rows if routing is None else routing.order.numel()
+    by_rows = empty(rows, cols, block_rows, dtype, scale_dtype, groups, x.device) if which != "columns" else None
+    by_cols = None
+    if which != "rows":
+        by_cols = empty(cols, rows if offsets is None else grouped_columns(rows, offsets.numel() - 1), block_rows, dtype, scale_dtype, groups, x.device)
+    if offsets is not None:
+        check_ints(offsets, "offsets")
+    h.call("oz_quantize", stream_of(x), rows, cols, x.data_ptr(), ldx, float_type(x.dtype), groups or 1,
+           0 if groups is None else x.stride(0), None if routing is None else routing.order.data_ptr(), 1 if routing is None else routing.topk, x_rows,
+           None if offsets is None else offsets.data_ptr(), 0 if offsets is None else offsets.numel() - 1,
+           None if by_rows is None else by_rows.desc, None if by_cols is None else by_cols.desc)
+    return by_rows if which == "rows" else by_cols if which == "columns" else (by_rows, by_cols)
+
+
+def _output(a, shape, dtype, out, accumulate):
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        return torch.empty(shape, dtype=dtype, device=a.data.device)
+    if tuple(out.shape) != tuple(shape) or out.device != a.data.device or (shape[-1] > 1 and out.stride(-1) != 1):
+        raise ValueError("out: %s with contiguous rows on %s, not %s %s" % (shape, a.data.device, tuple(out.shape), out.device))
+    return out
+
+
+def _ld(c):
+    return c.stride(-2) if c.shape[-2] > 1 else max(c.shape[-1], 1)
+
+
+def _check_product(a, b, groups):
+    if a.cols != b.cols or a.data.dim() != 2 or b.groups != groups or a.data.device != b.data.device:
+        raise ValueError("A %s and B %s with %d and %d columns do not multiply" % (tuple(a.data.shape), tuple(b.data.shape), a.cols, b.cols))
+
+
+def gemm(h: g.Handle, a: Scaled, b: Scaled, dtype=torch.bfloat16, out=None, accumulate=False):
+    """A B^T in `dtype` (or out's), summed in 32 bits; accumulate: added to `out`."""
+    _check_product(a, b, 1)
+    c = _output(a, (a.rows, b.rows), dtype, out, accumulate)
+    need = h.scaled_gemm_workspace_bytes(a.rows, b.rows, a.cols)
+    ws = torch.empty(need, dtype=torch.uint8, device=c.device) if need else None
+    h.call("oz_scaled_gemm", stream_of(c), a.rows, b.rows, a.cols, a.desc, b.desc, c.data_ptr(), _ld(c), float_type(c.dtype), int(accumulate),
+           None if ws is None else ws.data_ptr(), need)
+    return c
+
+
+def gemm_grouped(h: g.Handle, a: Scaled, b: Scaled, offsets, dtype=torch.bfloat16, out=None):
+    """Rows offsets[g] .. offsets[g+1] of A times B_g^T, for every group; zeros behind the last."""
+    groups = check_ints(offsets, "offsets").numel() - 1
+    _check_product(a, b, groups)
+    c = _output(a, (a.rows, b.rows), dtype, out, False)
+    h.call("oz_scaled_gemm_grouped", stream_of(c), groups, offsets.data_ptr(), a.rows, b.rows, a.cols, a.desc, b.desc, c.data_ptr(), _ld(c),
+           float_type(c.dtype))
+    return c
+
+
+def gemm_grouped_k(h: g.Handle, a: Scaled, b: Scaled, offsets, dtype=torch.float32, out=None, accumulate=False):
+    """A_g B_g^T for every group (groups x rows of A x rows of B), A_g and B_g the group's columns as quantize(offsets=...) lays them out."""
+    groups = check_ints(offsets, "offsets").numel() - 1
+    _check_product(a, b, 1)
+    c = _output(a, (groups, a.rows, b.rows), dtype, out, accumulate)
+    h.call("oz_scaled_gemm_grouped_k", stream_of(c), groups, offsets.data_ptr(), a.rows, b.rows, a.cols, a.desc, b.desc, c.data_ptr(),
+           _ld(c), c.stride(0) if groups > 1 else a.rows * _ld(c), float_type(c.dtype), int(accumulate))
+    return c
