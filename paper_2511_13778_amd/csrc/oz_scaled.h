@@ -46,6 +46,8 @@ struct QuantizeCall {
 };
 
 void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int num_cu, float* parts, size_t part_bytes);
+void launch_scaled_gemm_256(hipStream_t st, const ScaledGemm& g);
+bool prepare_scaled_gemm();            // once per process, before the first launch
 size_t scaled_gemm_part_bytes(int64_t m, int64_t n, int64_t k, int num_cu);
 void launch_quantize(hipStream_t st, const QuantizeCall& q);
 

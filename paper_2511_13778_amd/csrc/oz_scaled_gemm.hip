@@ -9,7 +9,7 @@ namespace oz {
 
 namespace {
 
-template <int BM, int BN, int WM, int WN, int STAGES, bool A_E5M2, bool E8M0>
+template <int BM, int BN, int WM, int WN, int STAGES, bool A_E5M2, bool E8M0, bool WIDE>
 __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel(ScaledGemm g, int tiles_n) {
     constexpr int WAVES = (BM / WM) * (BN / WN), ROWS = BM + BN;
     constexpr int COPIES = (ROWS / 8 + WAVES - 1) / WAVES;        // 1 KB each, per wave and step
@@ -121,10 +121,22 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
                 for (int i = 0; i < MT; ++i) sa[i] = *reinterpret_cast<const uint32_t*>(sc + (wm + i * 16 + x16) * 4) >> shift;
 #pragma unroll
                 for (int j = 0; j < NT; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(sc + (BM + wn + j * 16 + x16) * 4) >> shift;
+                if constexpr (WIDE) {
+                    Wide wa[MT], wb[NT];
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
+                    for (int i = 0; i < MT; ++i) wa[i] = widen<A_E5M2>(fa[i], scale_float(sa[i]));
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) acc[j][i] = mfma_e8m0<A_E5M2>(fb[j], fa[i], acc[j][i], sb[j], sa[i]);
+                    for (int j = 0; j < NT; ++j) wb[j] = widen<false>(fb[j], scale_float(sb[j]));
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) acc[j][i] = mfma_wide(wb[j], wa[i], acc[j][i]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) acc[j][i] = mfma_e8m0<A_E5M2>(fb[j], fa[i], acc[j][i], sb[j], sa[i]);
+                }
             } else {
                 const float* fs = reinterpret_cast<const float*>(sc) + (blk & 3) * ROWS;
                 float sa[MT];
@@ -133,11 +145,20 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
                 for (int i = 0; i < MT; ++i) sa[i] = fs[wm + i * 16 + x16];
 #pragma unroll
                 for (int j = 0; j < NT; ++j) sb[j] = *reinterpret_cast<const v4f*>(fs + BM + wn + j * 16 + q * 4);
+                Wide wa[MT], wb[NT];
+                if constexpr (WIDE) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) wa[i] = widen<A_E5M2>(fa[i], 1.0f);
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) wb[j] = widen<false>(fb[j], 1.0f);
+                }
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        const v4f p = mfma_plain<A_E5M2>(fb[j], fa[i]);
+                        v4f p;
+                        if constexpr (WIDE) p = mfma_wide(wb[j], wa[i], v4f{0, 0, 0, 0});
+                        else p = mfma_plain<A_E5M2>(fb[j], fa[i]);
 #pragma unroll
                         for (int r = 0; r < 4; ++r) acc[j][i][r] = fmaf(p[r] * sb[j][r], sa[i], acc[j][i][r]);
                     }
@@ -146,19 +167,10 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
         }
     }
 
-    const int q = lane >> 4, x16 = lane & 15;
-    const bool vec = aligned_c(g, t.c);
     if (steps == 0 && g.accumulate) return;
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int r = wm + i * 16 + x16;
-        if (r >= t.rows) continue;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const int c = wn + j * 16 + q * 4;
-            if (c < t.cols) put4(g, t.c + int64_t(t.row + r) * g.ldc + t.col + c, t.cols - c, vec, acc[j][i]);
-        }
-    }
+    __builtin_amdgcn_s_barrier();        // the other waves have read the last tiles
+    store_results<WIDE ? 4 : 2, 1, MT, NT>(g, acc, lds + wave * (WM * WN * (WIDE ? 4 : 2)), t.c + int64_t(t.row + wm) * g.ldc + t.col + wn,
+                                           t.rows - wm, t.cols - wn);
 }
 
 template <int BM, int BN, int WM, int WN, int STAGES>
@@ -167,19 +179,19 @@ void launch_tiles(hipStream_t st, const ScaledGemm& g) {
     const int64_t tiles_m = g.grouping == Grouping::kRows ? group_pieces(g.m, g.groups, BM) : (g.m + BM - 1) / BM;
     const dim3 grid(unsigned(tiles_m * tiles_n), g.grouping == Grouping::kContraction ? unsigned(g.groups) : 1u);
     const dim3 block(64 * (BM / WM) * (BN / WN));
-    if (g.e8m0) {
-        if (g.a_e5m2) hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, true, true>), grid, block, 0, st, g, tiles_n);
-        else hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, false, true>), grid, block, 0, st, g, tiles_n);
-    } else {
-        if (g.a_e5m2) hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, true, false>), grid, block, 0, st, g, tiles_n);
-        else hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, false, false>), grid, block, 0, st, g, tiles_n);
-    }
+    const int kind = (g.a_e5m2 ? 4 : 0) + (g.e8m0 ? 2 : 0) + (g.c_type == OZ_F32 ? 1 : 0);
+#define OZ_KIND(K) case K: hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, (K & 4) != 0, (K & 2) != 0, (K & 1) != 0>), grid, block, 0, st, g, tiles_n); break;
+    switch (kind) { OZ_KIND(0) OZ_KIND(1) OZ_KIND(2) OZ_KIND(3) OZ_KIND(4) OZ_KIND(5) OZ_KIND(6) OZ_KIND(7) }
+#undef OZ_KIND
 }
 
 }  // namespace
 
 size_t scaled_gemm_part_bytes(int64_t, int64_t, int64_t, int) { return 0; }
 
-void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int, float*, size_t) { launch_tiles<128, 128, 64, 64, 4>(st, g); }
+void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int, float*, size_t) {
+    if (g.e8m0 && g.c_type != OZ_F32 && g.m >= 192 && g.n >= 192) launch_scaled_gemm_256(st, g);
+    else launch_tiles<128, 128, 64, 64, 4>(st, g);
+}
 
 }  // namespace oz

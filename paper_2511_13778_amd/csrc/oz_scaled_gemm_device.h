@@ -37,6 +37,43 @@ __device__ __forceinline__ v4f mfma_plain(v8i32 b, v8i32 a) {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, none, 0, A_E5M2 ? 1 : 0, 0, 0, 0, 0);
 }
 
+// The instruction above keeps a sum of 8-bit products to about 2^-16 of the largest of them (normal data: 1.4e-5 of the result's rms), which
+// a result rounded to 16 bits does not show.  Where C is float32, operands are widened to bfloat16, exactly, for v_mfma_f32_16x16x32_bf16,
+// whose sums keep 32 bits (8e-9 on the same data) at half the rate.  A fragment's 32 bytes per lane make four operands.
+typedef bf16_t v8bf __attribute__((ext_vector_type(8)));
+typedef bf16_t v2bf __attribute__((ext_vector_type(2)));
+template <bool E5M2>
+__device__ __forceinline__ v8bf widen(uint32_t lo, uint32_t hi, float scale) {
+    union { v8bf v; v2bf p[4]; } u;
+    if constexpr (E5M2) {
+        u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, false);
+        u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, true);
+        u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, false);
+        u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, true);
+    } else {
+        u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+        u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+        u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+        u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    }
+    return u.v;
+}
+struct Wide { v8bf part[4]; };
+template <bool E5M2>
+__device__ __forceinline__ Wide widen(const v8i32& f, float scale) {
+    Wide w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w.part[i] = widen<E5M2>(uint32_t(f[2 * i]), uint32_t(f[2 * i + 1]), scale);
+    return w;
+}
+__device__ __forceinline__ v4f mfma_wide(const Wide& b, const Wide& a, v4f c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.part[i], a.part[i], c, 0, 0, 0);
+    return c;
+}
+// An E8M0 scale as the conversion takes it: a float of that exponent.
+__device__ __forceinline__ float scale_float(uint32_t byte) { return __uint_as_float((byte & 0xFFu) << 23); }
+
 // The part of a call that a workgroup works on.  Offsets in bytes / elements are 64-bit, what is left inside a tile 32-bit.
 struct GemmTile {
     const uint8_t *a, *b;         // first row of the tile, first byte of k
@@ -85,36 +122,89 @@ __device__ __forceinline__ GemmTile locate(const ScaledGemm& g, int tile_m, int 
     return t;
 }
 
-// Four consecutive results of one row of C.
-template <typename T>
-__device__ __forceinline__ void put4(T* p, int have, bool vec, bool add, const v4f& x) {
-    typedef T vec_t __attribute__((ext_vector_type(4)));
-    if (vec && have >= 4) {
-        v4f s = x;
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, bool bf16) {
+    union { bf16_t b[2]; f16_t h[2]; uint32_t u; } v;
+    if (bf16) { v.b[0] = bf16_t(lo); v.b[1] = bf16_t(hi); }
+    else { v.h[0] = f16_t(lo); v.h[1] = f16_t(hi); }
+    return v.u;
+}
+
+__device__ __forceinline__ float unpack(uint32_t w, int half, bool bf16) {
+    const uint16_t u = uint16_t(half ? w >> 16 : w);
+    union { uint16_t u; bf16_t b; f16_t h; } v{u};
+    return bf16 ? float(v.b) : float(v.h);
+}
+
+// A wave's results, MT x NT tiles of 16 x 16, to C.  They change places through `lds` (the wave's own, 16 * MT * 16 * NT * ES / PARTS bytes,
+// 16-byte aligned), so that a lane stores 16 bytes of a row; for `accumulate` C comes in the same way first.  A row's 16-byte
+// pieces lie at piece ^ row there: the 16 rows that a wave writes at a time meet different banks.
+//   ES: bytes of an element of C;  rows, cols: how many of the wave's rows and columns there are;  c: element (0, 0)
+template <int ES, int PARTS, int MT, int NT>
+__device__ __forceinline__ void store_results(const ScaledGemm& g, v4f (&acc)[NT][MT], uint8_t* lds, int64_t c, int rows, int cols) {
+    constexpr int kRowBytes = NT * 16 * ES, kPieces = kRowBytes / 16, kMask = kPieces < 16 ? kPieces - 1 : 15;
+    constexpr int kPartRows = MT * 16 / PARTS, kPer = 16 / ES;
+    static_assert(MT % PARTS == 0 && kPartRows * kPieces % 64 == 0, "whole rounds of the wave");
+    const int lane = threadIdx.x & 63, q = lane >> 4, x16 = lane & 15;
+    const bool add = g.accumulate != 0, bf16 = g.c_type == OZ_BF16;
+    uint8_t* const out = static_cast<uint8_t*>(g.c) + c * ES;
+    const int64_t ld = g.ldc * ES;
+    const bool vec = ((uintptr_t(out) | uintptr_t(ld)) & 15) == 0;
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (add) {
-            const vec_t old = *reinterpret_cast<const vec_t*>(p);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] += float(old[i]);
+#pragma unroll 1
+            for (int x = lane; x < kPartRows * kPieces; x += 64) {
+                const int r = x / kPieces, p = x % kPieces, col = (p ^ (r & kMask)) * kPer;
+                const uint8_t* at = out + (part * kPartRows + r) * ld + col * ES;
+                const int have = part * kPartRows + r < rows ? cols - col : 0;
+                v4i32 v = {0, 0, 0, 0};
+                if (vec && have >= kPer) v = *reinterpret_cast<const v4i32*>(at);
+                else
+                    for (int i = 0; i < kPer; ++i) {
+                        if (i >= have) break;
+                        if constexpr (ES == 4) v[i] = reinterpret_cast<const int*>(at)[i];
+                        else v[i >> 1] |= int(uint32_t(reinterpret_cast<const uint16_t*>(at)[i]) << (16 * (i & 1)));
+                    }
+                *reinterpret_cast<v4i32*>(lds + r * kRowBytes + p * 16) = v;
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
-        vec_t out;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) out[i] = T(s[i]);
-        *reinterpret_cast<vec_t*>(p) = out;
-    } else {
+        for (int i = part * (MT / PARTS); i < (part + 1) * (MT / PARTS); ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < have) p[i] = T(add ? x[i] + float(p[i]) : x[i]);
+            for (int j = 0; j < NT; ++j) {
+                uint8_t* row = lds + ((i - part * (MT / PARTS)) * 16 + x16) * kRowBytes;
+                v4f s = acc[j][i];
+                if constexpr (ES == 4) {
+                    v4f* at = reinterpret_cast<v4f*>(row + (((j * 4 + q) ^ (x16 & kMask)) << 4));
+                    if (add) s += *at;
+                    *at = s;
+                } else {
+                    uint2* at = reinterpret_cast<uint2*>(row + (((j * 2 + (q >> 1)) ^ (x16 & kMask)) << 4) + (q & 1) * 8);
+                    if (add) {
+                        const uint2 old = *at;
+                        s += v4f{unpack(old.x, 0, bf16), unpack(old.x, 1, bf16), unpack(old.y, 0, bf16), unpack(old.y, 1, bf16)};
+                    }
+                    *at = make_uint2(pack2(s[0], s[1], bf16), pack2(s[2], s[3], bf16));
+                }
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+        for (int x = lane; x < kPartRows * kPieces; x += 64) {
+            const int r = x / kPieces, p = x % kPieces, col = (p ^ (r & kMask)) * kPer;
+            const int have = part * kPartRows + r < rows ? cols - col : 0;
+            const v4i32 v = *reinterpret_cast<const v4i32*>(lds + r * kRowBytes + p * 16);
+            uint8_t* at = out + (part * kPartRows + r) * ld + col * ES;
+            if (vec && have >= kPer) *reinterpret_cast<v4i32*>(at) = v;
+            else
+                for (int i = 0; i < kPer; ++i) {
+                    if (i >= have) break;
+                    if constexpr (ES == 4) reinterpret_cast<int*>(at)[i] = v[i];
+                    else reinterpret_cast<uint16_t*>(at)[i] = uint16_t(uint32_t(v[i >> 1]) >> (16 * (i & 1)));
+                }
+        }
     }
-}
-__device__ __forceinline__ void put4(const ScaledGemm& g, int64_t at, int have, bool vec, const v4f& x) {
-    const bool add = g.accumulate != 0;
-    if (g.c_type == OZ_F32) put4(static_cast<float*>(g.c) + at, have, vec, add, x);
-    else if (g.c_type == OZ_BF16) put4(static_cast<bf16_t*>(g.c) + at, have, vec, add, x);
-    else put4(static_cast<f16_t*>(g.c) + at, have, vec, add, x);
-}
-__device__ __forceinline__ bool aligned_c(const ScaledGemm& g, int64_t offset) {
-    const int esize = g.c_type == OZ_F32 ? 4 : 2;
-    return ((uintptr_t(g.c) + uintptr_t(offset) * esize) | uintptr_t(g.ldc) * esize) % (4 * esize) == 0;
 }
 
 }  // namespace oz
