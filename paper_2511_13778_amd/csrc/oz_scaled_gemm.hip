@@ -36,23 +36,17 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
     if (steps > 0) {
         const uint32_t lds0 = lds_address(lds);
         // transfer x of this wave: rows 8y .. 8y+7 of the stage, y = wave + x * WAVES; lane: row lane/8, piece (lane%8) ^ (row%8)
-        const uint32_t piece = uint32_t((lane & 7) ^ (lane >> 3)) * 16;
-        uint32_t off[COPIES];
-#pragma unroll
-        for (int x = 0; x < COPIES; ++x) {
-            const int y = wave + x * WAVES, r = y * 8 + (lane >> 3);
-            off[x] = y < BM / 8 ? uint32_t(min(r, t.rows - 1)) * uint32_t(g.a.ld) + piece
-                                : uint32_t(min(r - BM, t.cols - 1)) * uint32_t(g.b.ld) + piece;
-        }
-        // behind the end of a row lies nothing that may be read: its pieces come from the step's first one, and are masked
-        const uint32_t back = tail && int(piece) >= tail ? piece : 0;
+        const uint32_t piece = uint32_t((lane & 7) ^ (lane >> 3)) * 16, lda = uint32_t(g.a.ld), ldb = uint32_t(g.b.ld);
+        const v4i32 src_a = tile_buffer(t.a, uint32_t(t.rows - 1) * lda + uint32_t((t.k + 3) & ~3));
+        const v4i32 src_b = tile_buffer(t.b, uint32_t(t.cols - 1) * ldb + uint32_t((t.k + 3) & ~3));
+        const uint32_t off_a = uint32_t(lane >> 3) * lda + piece, off_b = uint32_t(lane >> 3) * ldb + piece;
         auto copy_step = [&](int s) {
             const uint32_t to = lds0 + uint32_t(s % STAGES) * STAGE_BYTES;
-            const uint32_t less = s == steps - 1 ? back : 0;
 #pragma unroll
             for (int x = 0; x < COPIES; ++x) {
                 const int y = wave + x * WAVES;
-                copy16_to_lds((y < BM / 8 ? t.a : t.b) + int64_t(s) * kScaleBlock, off[x] - less, to + uint32_t(y) * 1024);
+                if (y < BM / 8) copy16_to_lds(src_a, off_a, uint32_t(y * 8) * lda + uint32_t(s) * kScaleBlock, to + uint32_t(y) * 1024);
+                else copy16_to_lds(src_b, off_b, uint32_t(y * 8 - BM) * ldb + uint32_t(s) * kScaleBlock, to + uint32_t(y) * 1024);
             }
         };
         // the four blocks of k around block0 + s: dword [row] (E8M0: four bytes), or [block][row]
@@ -169,7 +163,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
 
     if (steps == 0 && g.accumulate) return;
     __builtin_amdgcn_s_barrier();        // the other waves have read the last tiles
-    store_results<WIDE ? 4 : 2, 1, MT, NT>(g, acc, lds + wave * (WM * WN * (WIDE ? 4 : 2)), t.c + int64_t(t.row + wm) * g.ldc + t.col + wn,
+    store_results<WIDE, 1>(g, acc, lds + wave * (WM * WN * (WIDE ? 4 : 2)), t.c + int64_t(t.row + wm) * g.ldc + t.col + wn,
                                            t.rows - wm, t.cols - wn);
 }
 

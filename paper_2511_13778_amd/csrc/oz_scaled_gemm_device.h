@@ -11,10 +11,18 @@
 
 namespace oz {
 
-// 64 lanes x 16 (4) bytes from global memory into LDS at lds_addr + 16 (4) * lane; the address is a wave-uniform base and a per-lane
-// offset.  The compiler does not see the access: completion is awaited with s_waitcnt vmcnt in the loops.
-__device__ __forceinline__ void copy16_to_lds(const uint8_t* base, uint32_t lane_off, uint32_t lds_addr) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
+// Rows of a tile as a buffer: loads at lane offset + scalar offset from `base` on; dwords from `bytes` on read as zero and touch no
+// memory, so neither rows behind the last nor bytes behind the end of the last row are loaded.
+__device__ __forceinline__ v4i32 tile_buffer(const uint8_t* base, uint32_t bytes) {
+    const uint64_t a = uint64_t(uintptr_t(base));
+    return v4i32{__builtin_amdgcn_readfirstlane(int(uint32_t(a))), __builtin_amdgcn_readfirstlane(int(uint32_t(a >> 32) & 0xFFFFu)),
+                 __builtin_amdgcn_readfirstlane(int(bytes)), 0x00020000};
+}
+// 64 lanes x 16 (4) bytes from memory into LDS at lds_addr + 16 (4) * lane.  The compiler does not see the access: completion is awaited
+// with s_waitcnt vmcnt in the loops.
+__device__ __forceinline__ void copy16_to_lds(const v4i32& buffer, uint32_t lane_off, uint32_t off, uint32_t lds_addr) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :: "s"(lds_addr), "v"(lane_off), "s"(buffer), "s"(off) : "memory");
 }
 __device__ __forceinline__ void copy4_to_lds(const uint8_t* base, uint32_t lane_off, uint32_t lds_addr) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, %2" :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
@@ -122,88 +130,115 @@ __device__ __forceinline__ GemmTile locate(const ScaledGemm& g, int tile_m, int 
     return t;
 }
 
-__device__ __forceinline__ uint32_t pack2(float lo, float hi, bool bf16) {
-    union { bf16_t b[2]; f16_t h[2]; uint32_t u; } v;
-    if (bf16) { v.b[0] = bf16_t(lo); v.b[1] = bf16_t(hi); }
-    else { v.h[0] = f16_t(lo); v.h[1] = f16_t(hi); }
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    typedef T pair __attribute__((ext_vector_type(2)));
+    union { pair p; uint32_t u; } v;
+    v.p = pair{T(lo), T(hi)};
     return v.u;
 }
-
-__device__ __forceinline__ float unpack(uint32_t w, int half, bool bf16) {
-    const uint16_t u = uint16_t(half ? w >> 16 : w);
-    union { uint16_t u; bf16_t b; f16_t h; } v{u};
-    return bf16 ? float(v.b) : float(v.h);
+template <typename T>
+__device__ __forceinline__ v4f unpack4(uint2 w) {
+    typedef T quad __attribute__((ext_vector_type(4)));
+    union { uint2 w; quad q; } v;
+    v.w = w;
+    return v4f{float(v.q[0]), float(v.q[1]), float(v.q[2]), float(v.q[3])};
 }
 
-// A wave's results, MT x NT tiles of 16 x 16, to C.  They change places through `lds` (the wave's own, 16 * MT * 16 * NT * ES / PARTS bytes,
+// A tile whose k is empty, by all of a workgroup: zero, unless it is added to what is there.
+__device__ __forceinline__ void store_nothing(const ScaledGemm& g, const GemmTile& t) {
+    if (g.accumulate) return;
+    for (int r = 0; r < t.rows; ++r)
+        for (int c = threadIdx.x; c < t.cols; c += blockDim.x) {
+            const int64_t at = t.c + int64_t(t.row + r) * g.ldc + t.col + c;
+            if (g.c_type == OZ_F32) static_cast<uint32_t*>(g.c)[at] = 0;
+            else static_cast<uint16_t*>(g.c)[at] = 0;
+        }
+}
+
+// A wave's results, MT x NT tiles of 16 x 16, to C.  They change places through `lds` (the wave's own, 16 * MT * 16 * NT elements / PARTS,
 // 16-byte aligned), so that a lane stores 16 bytes of a row; for `accumulate` C comes in the same way first.  A row's 16-byte
 // pieces lie at piece ^ row there: the 16 rows that a wave writes at a time meet different banks.
-//   ES: bytes of an element of C;  rows, cols: how many of the wave's rows and columns there are;  c: element (0, 0)
-template <int ES, int PARTS, int MT, int NT>
-__device__ __forceinline__ void store_results(const ScaledGemm& g, v4f (&acc)[NT][MT], uint8_t* lds, int64_t c, int rows, int cols) {
-    constexpr int kRowBytes = NT * 16 * ES, kPieces = kRowBytes / 16, kMask = kPieces < 16 ? kPieces - 1 : 15;
+//   rows, cols: how many of the wave's rows and columns there are;  c: element (0, 0)
+template <typename T, bool ADD, int PARTS, int MT, int NT>
+__device__ __forceinline__ void store_typed(const ScaledGemm& g, v4f (&acc)[NT][MT], uint8_t* lds, int64_t c, int rows, int cols) {
+    constexpr int ES = int(sizeof(T)), kRowBytes = NT * 16 * ES, kPieces = kRowBytes / 16, kMask = kPieces < 16 ? kPieces - 1 : 15;
     constexpr int kPartRows = MT * 16 / PARTS, kPer = 16 / ES;
     static_assert(MT % PARTS == 0 && kPartRows * kPieces % 64 == 0, "whole rounds of the wave");
     const int lane = threadIdx.x & 63, q = lane >> 4, x16 = lane & 15;
-    const bool add = g.accumulate != 0, bf16 = g.c_type == OZ_BF16;
     uint8_t* const out = static_cast<uint8_t*>(g.c) + c * ES;
     const int64_t ld = g.ldc * ES;
     const bool vec = ((uintptr_t(out) | uintptr_t(ld)) & 15) == 0;
-#pragma unroll
-    for (int part = 0; part < PARTS; ++part) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (add) {
-#pragma unroll 1
-            for (int x = lane; x < kPartRows * kPieces; x += 64) {
-                const int r = x / kPieces, p = x % kPieces, col = (p ^ (r & kMask)) * kPer;
-                const uint8_t* at = out + (part * kPartRows + r) * ld + col * ES;
-                const int have = part * kPartRows + r < rows ? cols - col : 0;
-                v4i32 v = {0, 0, 0, 0};
-                if (vec && have >= kPer) v = *reinterpret_cast<const v4i32*>(at);
-                else
-                    for (int i = 0; i < kPer; ++i) {
-                        if (i >= have) break;
-                        if constexpr (ES == 4) v[i] = reinterpret_cast<const int*>(at)[i];
-                        else v[i >> 1] |= int(uint32_t(reinterpret_cast<const uint16_t*>(at)[i]) << (16 * (i & 1)));
-                    }
-                *reinterpret_cast<v4i32*>(lds + r * kRowBytes + p * 16) = v;
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        }
-#pragma unroll
-        for (int i = part * (MT / PARTS); i < (part + 1) * (MT / PARTS); ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                uint8_t* row = lds + ((i - part * (MT / PARTS)) * 16 + x16) * kRowBytes;
-                v4f s = acc[j][i];
-                if constexpr (ES == 4) {
-                    v4f* at = reinterpret_cast<v4f*>(row + (((j * 4 + q) ^ (x16 & kMask)) << 4));
-                    if (add) s += *at;
-                    *at = s;
-                } else {
-                    uint2* at = reinterpret_cast<uint2*>(row + (((j * 2 + (q >> 1)) ^ (x16 & kMask)) << 4) + (q & 1) * 8);
-                    if (add) {
-                        const uint2 old = *at;
-                        s += v4f{unpack(old.x, 0, bf16), unpack(old.x, 1, bf16), unpack(old.y, 0, bf16), unpack(old.y, 1, bf16)};
-                    }
-                    *at = make_uint2(pack2(s[0], s[1], bf16), pack2(s[2], s[3], bf16));
-                }
-            }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    // piece x of the part, in the order of LDS: row, column, how many of its elements there are
+    auto each = [&](int part, auto&& f) {
 #pragma unroll 1
         for (int x = lane; x < kPartRows * kPieces; x += 64) {
-            const int r = x / kPieces, p = x % kPieces, col = (p ^ (r & kMask)) * kPer;
+            const int r = x / kPieces, col = ((x % kPieces) ^ (r & kMask)) * kPer;
             const int have = part * kPartRows + r < rows ? cols - col : 0;
-            const v4i32 v = *reinterpret_cast<const v4i32*>(lds + r * kRowBytes + p * 16);
-            uint8_t* at = out + (part * kPartRows + r) * ld + col * ES;
-            if (vec && have >= kPer) *reinterpret_cast<v4i32*>(at) = v;
-            else
-                for (int i = 0; i < kPer; ++i) {
-                    if (i >= have) break;
-                    if constexpr (ES == 4) reinterpret_cast<int*>(at)[i] = v[i];
-                    else reinterpret_cast<uint16_t*>(at)[i] = uint16_t(uint32_t(v[i >> 1]) >> (16 * (i & 1)));
-                }
+            f(reinterpret_cast<v4i32*>(lds + x * 16), reinterpret_cast<T*>(out + (part * kPartRows + r) * ld) + col, have);
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+    // where this lane's results of tile (0, j) lie: tile (i, j) is a constant further
+    uint32_t at[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+        at[j] = ES == 4 ? uint32_t(x16 * kRowBytes + (((j * 4 + q) ^ (x16 & kMask)) << 4))
+                        : uint32_t(x16 * kRowBytes + (((j * 2 + (q >> 1)) ^ (x16 & kMask)) << 4) + (q & 1) * 8);
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+        if constexpr (ADD) {
+            each(part, [&](v4i32* piece, const T* p, int have) {
+                union { v4i32 v; T e[kPer]; } u;
+                u.v = v4i32{0, 0, 0, 0};
+                if (vec && have >= kPer) u.v = *reinterpret_cast<const v4i32*>(p);
+                else
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i)
+                        if (i < have) u.e[i] = p[i];
+                *piece = u.v;
+            });
+        }
+#pragma unroll
+        for (int i = 0; i < MT / PARTS; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                uint8_t* p = lds + at[j] + i * 16 * kRowBytes;
+                v4f s = acc[j][part * (MT / PARTS) + i];
+                if constexpr (ES == 4) {
+                    if constexpr (ADD) s += *reinterpret_cast<const v4f*>(p);
+                    *reinterpret_cast<v4f*>(p) = s;
+                } else {
+                    if constexpr (ADD) s += unpack4<T>(*reinterpret_cast<const uint2*>(p));
+                    *reinterpret_cast<uint2*>(p) = make_uint2(pack2<T>(s[0], s[1]), pack2<T>(s[2], s[3]));
+                }
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        each(part, [&](const v4i32* piece, T* p, int have) {
+            union { v4i32 v; T e[kPer]; } u;
+            u.v = *piece;
+            if (vec && have >= kPer) *reinterpret_cast<v4i32*>(p) = u.v;
+            else
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (i < have) p[i] = u.e[i];
+        });
+    }
+}
+// FLOAT32: C is float32, in PARTS parts; else it has 16 bits.  One copy of the code per type runs: the kernels' own is what fills the
+// instruction cache.
+template <bool FLOAT32, int PARTS, int MT, int NT>
+__device__ __forceinline__ void store_results(const ScaledGemm& g, v4f (&acc)[NT][MT], uint8_t* lds, int64_t c, int rows, int cols) {
+    const bool add = g.accumulate != 0;
+    if constexpr (FLOAT32) {
+        if (add) store_typed<float, true, PARTS>(g, acc, lds, c, rows, cols);
+        else store_typed<float, false, PARTS>(g, acc, lds, c, rows, cols);
+    } else if (g.c_type == OZ_BF16) {
+        if (add) store_typed<bf16_t, true, PARTS>(g, acc, lds, c, rows, cols);
+        else store_typed<bf16_t, false, PARTS>(g, acc, lds, c, rows, cols);
+    } else {
+        if (add) store_typed<f16_t, true, PARTS>(g, acc, lds, c, rows, cols);
+        else store_typed<f16_t, false, PARTS>(g, acc, lds, c, rows, cols);
     }
 }
 
