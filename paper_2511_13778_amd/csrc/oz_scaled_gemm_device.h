@@ -169,6 +169,7 @@ __device__ __forceinline__ void store_typed(const ScaledGemm& g, v4f (&acc)[NT][
     uint8_t* const out = static_cast<uint8_t*>(g.c) + c * ES;
     const int64_t ld = g.ldc * ES;
     const bool vec = ((uintptr_t(out) | uintptr_t(ld)) & 15) == 0;
+    const bool whole = vec && rows >= MT * 16 && cols >= NT * 16;
     // piece x of the part, in the order of LDS: row, column, how many of its elements there are
     auto each = [&](int part, auto&& f) {
 #pragma unroll 1
@@ -214,15 +215,35 @@ __device__ __forceinline__ void store_typed(const ScaledGemm& g, v4f (&acc)[NT][
                 }
             }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        each(part, [&](const v4i32* piece, T* p, int have) {
-            union { v4i32 v; T e[kPer]; } u;
-            u.v = *piece;
-            if (vec && have >= kPer) *reinterpret_cast<v4i32*>(p) = u.v;
-            else
+        if (whole) {
+            // nothing to check, eight pieces of a lane on their way together
+            constexpr int kRounds = kPartRows * kPieces / 64, kBatch = kRounds % 8 == 0 ? 8 : kRounds;
+            constexpr int kStepRows = 64 / kPieces > 0 ? 64 / kPieces : 1;
+            static_assert(64 % kPieces == 0 && kStepRows <= kMask + 1, "a round is whole rows");
+            const int r0 = lane / kPieces;
+#pragma unroll 1
+            for (int x = 0; x < kRounds; x += kBatch) {
+                v4i32 v[kBatch];
 #pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    if (i < have) p[i] = u.e[i];
-        });
+                for (int u = 0; u < kBatch; ++u) v[u] = *reinterpret_cast<const v4i32*>(lds + (x + u) * 1024 + lane * 16);
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    const int r = (x + u) * kStepRows + r0;
+                    *reinterpret_cast<v4i32*>(out + (part * kPartRows + r) * ld + (((lane % kPieces) ^ (r & kMask)) << 4)) = v[u];
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        } else {
+            each(part, [&](const v4i32* piece, T* p, int have) {
+                union { v4i32 v; T e[kPer]; } u;
+                u.v = *piece;
+                if (vec && have >= kPer) *reinterpret_cast<v4i32*>(p) = u.v;
+                else
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i)
+                        if (i < have) p[i] = u.e[i];
+            });
+        }
     }
 }
 // FLOAT32: C is float32, in PARTS parts; else it has 16 bits.  One copy of the code per type runs: the kernels' own is what fills the
