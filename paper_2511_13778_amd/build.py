@@ -14,7 +14,7 @@ PROBE_LIB = os.path.join(HERE, "liboz_probe.so")      # measurement probes: sepa
 PROBE_SOURCES = ["oz_probe.hip"]
 SOURCES = ["oz_api.hip", "oz_scan.hip", "oz_esc.hip", "oz_slice.hip", "oz_esc_slice.hip", "oz_gemm_i8.hip", "oz_gemm_few.hip", "oz_gemm_small.hip", "oz_gemm_mid.hip",
            "oz_recompose.hip", "oz_dgemm_f64.hip", "oz_dgemm_f64_direct.hip", "oz_complex.hip",
-           "oz_scaled_api.hip", "oz_quantize.hip", "oz_scaled_gemm.hip", "oz_scaled_gemm_256.hip", "oz_route.hip"]
+           "oz_scaled_api.hip", "oz_quantize.hip", "oz_scaled_gemm.hip", "oz_scaled_gemm_256.hip", "oz_scaled_gemm_few.hip", "oz_route.hip"]
 # packed FP32 instructions are switched off for all device code (known-bad on the test machines)
 # -ffp-contract=off: the FP64 epilogues round every product and sum separately, as the header specifies;
 # hipcc's default would fuse a*b + c into one rounding.

@@ -47,6 +47,7 @@ struct QuantizeCall {
 
 void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int num_cu, float* parts, size_t part_bytes);
 void launch_scaled_gemm_256(hipStream_t st, const ScaledGemm& g);
+void launch_scaled_gemm_few(hipStream_t st, const ScaledGemm& g, int rows, int waves);
 bool prepare_scaled_gemm();            // once per process, before the first launch
 size_t scaled_gemm_part_bytes(int64_t m, int64_t n, int64_t k, int num_cu);
 void launch_quantize(hipStream_t st, const QuantizeCall& q);

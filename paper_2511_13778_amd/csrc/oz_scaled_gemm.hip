@@ -163,8 +163,8 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
 
     if (steps == 0 && g.accumulate) return;
     __builtin_amdgcn_s_barrier();        // the other waves have read the last tiles
-    store_results<WIDE, 1>(g, acc, lds + wave * (WM * WN * (WIDE ? 4 : 2)), t.c + int64_t(t.row + wm) * g.ldc + t.col + wn,
-                                           t.rows - wm, t.cols - wn);
+    constexpr int kWaveBytes = WM * WN * (WIDE ? 4 : 2), kParts = kWaveBytes * WAVES <= int(sizeof(lds)) ? 1 : kWaveBytes * WAVES <= 2 * int(sizeof(lds)) ? 2 : 4;
+    store_results<WIDE, kParts>(g, acc, lds + wave * (kWaveBytes / kParts), t.c + int64_t(t.row + wm) * g.ldc + t.col + wn, t.rows - wm, t.cols - wn);
 }
 
 template <int BM, int BN, int WM, int WN, int STAGES>
@@ -183,9 +183,19 @@ void launch_tiles(hipStream_t st, const ScaledGemm& g) {
 
 size_t scaled_gemm_part_bytes(int64_t, int64_t, int64_t, int) { return 0; }
 
-void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int, float*, size_t) {
-    if (g.e8m0 && g.c_type != OZ_F32 && g.m >= 192 && g.n >= 192) launch_scaled_gemm_256(st, g);
-    else launch_tiles<128, 128, 64, 64, 4>(st, g);
+void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int num_cu, float*, size_t) {
+    // rows that read an operand B together, on average
+    const int64_t rows = g.grouping == Grouping::kRows ? (int64_t(g.m) + g.groups - 1) / g.groups : g.m;
+    if (g.grouping != Grouping::kContraction && rows <= 64) {
+        const int fours = (g.k + 511) / 512;
+        launch_scaled_gemm_few(st, g, int(rows), fours <= 4 ? 4 : fours <= 8 ? 8 : 16);
+        return;
+    }
+    const int64_t tiles256 = ((g.m + 255) / 256) * int64_t((g.n + 255) / 256) * (g.grouping == Grouping::kContraction ? g.groups : 1);
+    const int64_t tiles128 = ((g.m + 127) / 128) * int64_t((g.n + 127) / 128) * (g.grouping == Grouping::kContraction ? g.groups : 1);
+    if (g.e8m0 && g.c_type != OZ_F32 && tiles256 >= num_cu * 3 / 4) launch_scaled_gemm_256(st, g);
+    else if (tiles128 >= num_cu) launch_tiles<128, 128, 64, 64, 2>(st, g);
+    else launch_tiles<64, 64, 32, 32, 2>(st, g);
 }
 
 }  // namespace oz

@@ -145,6 +145,29 @@ __device__ __forceinline__ v4f unpack4(uint2 w) {
     return v4f{float(v.q[0]), float(v.q[1]), float(v.q[2]), float(v.q[3])};
 }
 
+// Four consecutive results of one row of C.
+template <typename T>
+__device__ __forceinline__ void put4(T* p, int have, bool add, v4f s) {
+    typedef T quad __attribute__((ext_vector_type(4)));
+    if (have >= 4 && reinterpret_cast<uintptr_t>(p) % sizeof(quad) == 0) {
+        quad* at = reinterpret_cast<quad*>(p);
+        if (add) {
+            const quad old = *at;
+            s += v4f{float(old[0]), float(old[1]), float(old[2]), float(old[3])};
+        }
+        *at = quad{T(s[0]), T(s[1]), T(s[2]), T(s[3])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) p[i] = T(add ? s[i] + float(p[i]) : s[i]);
+    }
+}
+__device__ __forceinline__ void put4(const ScaledGemm& g, int64_t at, int have, const v4f& s) {
+    if (g.c_type == OZ_F32) put4(static_cast<float*>(g.c) + at, have, g.accumulate != 0, s);
+    else if (g.c_type == OZ_BF16) put4(static_cast<bf16_t*>(g.c) + at, have, g.accumulate != 0, s);
+    else put4(static_cast<f16_t*>(g.c) + at, have, g.accumulate != 0, s);
+}
+
 // A tile whose k is empty, by all of a workgroup: zero, unless it is added to what is there.
 __device__ __forceinline__ void store_nothing(const ScaledGemm& g, const GemmTile& t) {
     if (g.accumulate) return;
@@ -218,8 +241,8 @@ __device__ __forceinline__ void store_typed(const ScaledGemm& g, v4f (&acc)[NT][
         if (whole) {
             // nothing to check, eight pieces of a lane on their way together
             constexpr int kRounds = kPartRows * kPieces / 64, kBatch = kRounds % 8 == 0 ? 8 : kRounds;
-            constexpr int kStepRows = 64 / kPieces > 0 ? 64 / kPieces : 1;
-            static_assert(64 % kPieces == 0 && kStepRows <= kMask + 1, "a round is whole rows");
+            constexpr int kStepRows = 64 / kPieces;
+            static_assert(64 % kPieces == 0, "a round is whole rows");
             const int r0 = lane / kPieces;
 #pragma unroll 1
             for (int x = 0; x < kRounds; x += kBatch) {

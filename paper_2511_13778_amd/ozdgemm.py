@@ -250,7 +250,9 @@ class Handle:
     # on tensors are in `scaled` and `experts`.
     def call(self, name, stream_ptr, *args):
         """Enqueues the entry point `name` (oz_quantize .. oz_combine_rows_grad) on a stream; raises OzError on its status."""
-        _check(getattr(self.lib, name)(self._h, stream_ptr, *args), name)
+        status = getattr(self.lib, name)(self._h, stream_ptr, *args)
+        if status:
+            raise OzError(status, name)
 
     def scaled_gemm_workspace_bytes(self, m, n, k) -> int:
         return self.lib.oz_scaled_gemm_workspace_bytes(self._h, m, n, k)

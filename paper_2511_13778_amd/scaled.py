@@ -36,14 +36,17 @@ def float_type(dtype) -> int:
 
 def stream_of(t) -> int:
     """The current stream of the tensor's device, which has to be the current device."""
-    return torch.cuda.current_stream(t.device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
 def check_matrix(t, what):
     """A CUDA tensor whose rows are contiguous; its leading dimension in elements."""
-    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s: a matrix on the GPU with contiguous rows, not %s %s of strides %s" % (what, t.device, tuple(t.shape), t.stride()))
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+    if t.is_cuda and t.dim() == 2:
+        ld, step = t.stride()
+        rows, cols = t.shape
+        if step == 1 or cols <= 1:
+            return ld if rows > 1 else max(cols, 1)
+    raise ValueError("%s: a matrix on the GPU with contiguous rows, not %s %s of strides %s" % (what, t.device, tuple(t.shape), t.stride()))
 
 
 def check_ints(t, what, n=None):
@@ -89,19 +92,29 @@ class Scaled:
 
     def values(self):
         """The 8-bit numbers, without padding."""
-        return self.data[..., :self.cols]
+        return self.data if self.data.shape[-1] == self.cols else self.data[..., :self.cols]
 
     def scales(self):
         """The scales, without padding."""
-        return self.scale[..., :-(-self.cols // BLOCK)]
+        blocks = -(-self.cols // BLOCK)
+        return self.scale if self.scale.shape[-1] == blocks else self.scale[..., :blocks]
 
 
 def empty(rows, cols, block_rows=1, dtype=torch.float8_e4m3fn, scale_dtype=torch.uint8, groups=None, device="cuda") -> Scaled:
     """An uninitialised matrix in the layout that the calls here want."""
-    lead = () if groups is None else (groups,)
-    data = torch.empty(lead + (rows, max(-(-cols // 16) * 16, 16)), dtype=dtype, device=device)
-    scale = torch.empty(lead + (-(-rows // block_rows), max(-(-cols // (4 * BLOCK)) * 4, 4)), dtype=scale_dtype, device=device)
-    return Scaled(data, scale, cols, block_rows)
+    ld, blocks, high = max(-(-cols // 16) * 16, 16), max(-(-cols // (4 * BLOCK)) * 4, 4), -(-rows // block_rows)
+    m = Scaled.__new__(Scaled)          # sizes and types are right by construction
+    m.cols, m.block_rows = cols, block_rows
+    if groups is None:
+        m.data = torch.empty((rows, ld), dtype=dtype, device=device)
+        m.scale = torch.empty((high, blocks), dtype=scale_dtype, device=device)
+        m.desc = g.oz_scaled_t(m.data.data_ptr(), m.scale.data_ptr(), ld, blocks, 0, 0, _EIGHT[dtype], _SCALE[scale_dtype], block_rows, 0)
+    else:
+        m.data = torch.empty((groups, rows, ld), dtype=dtype, device=device)
+        m.scale = torch.empty((groups, high, blocks), dtype=scale_dtype, device=device)
+        m.desc = g.oz_scaled_t(m.data.data_ptr(), m.scale.data_ptr(), ld, blocks, rows * ld, high * blocks, _EIGHT[dtype], _SCALE[scale_dtype],
+                               block_rows, 0)
+    return m
 
 
 def grouped_columns(rows, groups) -> int:
@@ -117,19 +130,24 @@ def quantize(h: g.Handle, x, dtype=torch.float8_e4m3fn, scale_dtype=torch.uint8,
         raise ValueError("which: rows, columns or both, not %r" % (which,))
     if dtype not in _EIGHT or scale_dtype not in _SCALE:
         raise ValueError("8-bit floats with uint8, float8_e8m0fnu or float32 scales, not %s with %s" % (dtype, scale_dtype))
-    groups = x.shape[0] if x.dim() == 3 else None
-    ldx = check_matrix(x if groups is None else x.flatten(0, 1) if x.is_contiguous() else x[0], "x")
-    x_rows, cols = x.shape[-2:]
-    rows = x_rows if routing is None else routing.order.numel()
-    by_rows = empty(rows, cols, block_rows, dtype, scale_dtype, groups, x.device) if which != "columns" else None
-    by_cols = None
+    if x.dim() == 3:
+        groups, stride = x.shape[0], x.stride(0)
+        ldx = check_matrix(x[0], "x") if groups else x.shape[2]
+        x_rows, cols = x.shape[1:]
+    else:
+        groups, stride = None, 0
+        ldx = check_matrix(x, "x")
+        x_rows, cols = x.shape
+    order, topk, rows = (None, 1, x_rows) if routing is None else (routing.order.data_ptr(), routing.topk, routing.order.numel())
+    ends, sections = (None, 0) if offsets is None else (check_ints(offsets, "offsets").data_ptr(), offsets.numel() - 1)
+    device = x.device
+    by_rows = by_cols = None
+    if which != "columns":
+        by_rows = empty(rows, cols, block_rows, dtype, scale_dtype, groups, device)
     if which != "rows":
-        by_cols = empty(cols, rows if offsets is None else grouped_columns(rows, offsets.numel() - 1), block_rows, dtype, scale_dtype, groups, x.device)
-    if offsets is not None:
-        check_ints(offsets, "offsets")
-    h.call("oz_quantize", stream_of(x), rows, cols, x.data_ptr(), ldx, float_type(x.dtype), groups or 1,
-           0 if groups is None else x.stride(0), None if routing is None else routing.order.data_ptr(), 1 if routing is None else routing.topk, x_rows,
-           None if offsets is None else offsets.data_ptr(), 0 if offsets is None else offsets.numel() - 1,
+        by_cols = empty(cols, rows if ends is None else grouped_columns(rows, sections), block_rows, dtype, scale_dtype, groups, device)
+    h.call("oz_quantize", torch._C._cuda_getCurrentRawStream(device.index), rows, cols, x.data_ptr(), ldx, float_type(x.dtype),
+           1 if groups is None else groups, stride, order, topk, x_rows, ends, sections,
            None if by_rows is None else by_rows.desc, None if by_cols is None else by_cols.desc)
     return by_rows if which == "rows" else by_cols if which == "columns" else (by_rows, by_cols)
 
@@ -156,10 +174,11 @@ def _check_product(a, b, groups):
 def gemm(h: g.Handle, a: Scaled, b: Scaled, dtype=torch.bfloat16, out=None, accumulate=False):
     """A B^T in `dtype` (or out's), summed in 32 bits; accumulate: added to `out`."""
     _check_product(a, b, 1)
-    c = _output(a, (a.rows, b.rows), dtype, out, accumulate)
-    need = h.scaled_gemm_workspace_bytes(a.rows, b.rows, a.cols)
+    m, n, k = a.data.shape[0], b.data.shape[-2], a.cols
+    c = _output(a, (m, n), dtype, out, accumulate)
+    need = h.scaled_gemm_workspace_bytes(m, n, k)
     ws = torch.empty(need, dtype=torch.uint8, device=c.device) if need else None
-    h.call("oz_scaled_gemm", stream_of(c), a.rows, b.rows, a.cols, a.desc, b.desc, c.data_ptr(), _ld(c), float_type(c.dtype), int(accumulate),
+    h.call("oz_scaled_gemm", stream_of(c), m, n, k, a.desc, b.desc, c.data_ptr(), _ld(c), float_type(c.dtype), int(accumulate),
            None if ws is None else ws.data_ptr(), need)
     return c
 
