@@ -46,7 +46,9 @@ struct QuantizeCall {
 };
 
 void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int num_cu, float* parts, size_t part_bytes);
-void launch_scaled_gemm_256(hipStream_t st, const ScaledGemm& g);
+void launch_scaled_gemm_big(hipStream_t st, const ScaledGemm& g, bool wide);       // wide: tiles of 256 x 256, else 256 x 128
+void launch_scaled_gemm_big_f32(hipStream_t st, const ScaledGemm& g);
+bool prepare_scaled_gemm_f32();
 void launch_scaled_gemm_few(hipStream_t st, const ScaledGemm& g, int rows, int waves);
 bool prepare_scaled_gemm();            // once per process, before the first launch
 size_t scaled_gemm_part_bytes(int64_t m, int64_t n, int64_t k, int num_cu);

@@ -121,10 +121,14 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
                     for (int i = 0; i < MT; ++i) wa[i] = widen<A_E5M2>(fa[i], scale_float(sa[i]));
 #pragma unroll
                     for (int j = 0; j < NT; ++j) wb[j] = widen<false>(fb[j], scale_float(sb[j]));
+                    // a tile's four instructions apart from each other: each waits for the one before it
 #pragma unroll
-                    for (int j = 0; j < NT; ++j)
+                    for (int w = 0; w < 4; ++w)
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) acc[j][i] = mfma_wide(wb[j], wa[i], acc[j][i]);
+                        for (int j = 0; j < NT; ++j)
+#pragma unroll
+                            for (int i = 0; i < MT; ++i)
+                                acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j].part[w], wa[i].part[w], acc[j][i], 0, 0, 0);
                 } else {
 #pragma unroll
                     for (int j = 0; j < NT; ++j)
@@ -147,15 +151,23 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
                     for (int j = 0; j < NT; ++j) wb[j] = widen<false>(fb[j], 1.0f);
                 }
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
+                for (int j = 0; j < NT; ++j) {
+                    v4f p[MT];
+                    if constexpr (WIDE) {
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        v4f p;
-                        if constexpr (WIDE) p = mfma_wide(wb[j], wa[i], v4f{0, 0, 0, 0});
-                        else p = mfma_plain<A_E5M2>(fb[j], fa[i]);
+                        for (int w = 0; w < 4; ++w)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[j][i][r] = fmaf(p[r] * sb[j][r], sa[i], acc[j][i][r]);
+                            for (int i = 0; i < MT; ++i)
+                                p[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j].part[w], wa[i].part[w], w == 0 ? v4f{0, 0, 0, 0} : p[i], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) p[i] = mfma_plain<A_E5M2>(fb[j], fa[i]);
                     }
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[j][i][r] = fmaf(p[i][r] * sb[j][r], sa[i], acc[j][i][r]);
+                }
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
@@ -193,7 +205,8 @@ void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int num_cu, float*,
     }
     const int64_t tiles256 = ((g.m + 255) / 256) * int64_t((g.n + 255) / 256) * (g.grouping == Grouping::kContraction ? g.groups : 1);
     const int64_t tiles128 = ((g.m + 127) / 128) * int64_t((g.n + 127) / 128) * (g.grouping == Grouping::kContraction ? g.groups : 1);
-    if (g.e8m0 && g.c_type != OZ_F32 && tiles256 >= num_cu * 3 / 4) launch_scaled_gemm_256(st, g);
+    const int64_t tall = ((g.m + 255) / 256) * int64_t((g.n + 127) / 128) * (g.grouping == Grouping::kContraction ? g.groups : 1);
+    if (g.c_type != OZ_F32 && tall >= num_cu * 3 / 4) launch_scaled_gemm_big(st, g, tiles256 >= num_cu * 3 / 4);
     else if (tiles128 >= num_cu) launch_tiles<128, 128, 64, 64, 2>(st, g);
     else launch_tiles<64, 64, 32, 32, 2>(st, g);
 }
