@@ -30,6 +30,8 @@ struct ScaledGemm {
     int groups;
     Grouping grouping;
     bool a_e5m2, e8m0;
+    bool wide;            // the caller's C is float32: operands are widened for 32-bit sums
+    int parts;            // k is cut into so many; C is then a float32 plane of m x n for each
 };
 
 struct QuantizeCall {
@@ -45,13 +47,13 @@ struct QuantizeCall {
     bool tiles;                            // 128 rows share a scale
 };
 
-void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int num_cu, float* parts, size_t part_bytes);
+void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int num_cu, float* planes);
 void launch_scaled_gemm_big(hipStream_t st, const ScaledGemm& g, bool wide);       // wide: tiles of 256 x 256, else 256 x 128
 void launch_scaled_gemm_big_f32(hipStream_t st, const ScaledGemm& g);
 bool prepare_scaled_gemm_f32();
 void launch_scaled_gemm_few(hipStream_t st, const ScaledGemm& g, int rows, int waves);
 bool prepare_scaled_gemm();            // once per process, before the first launch
-size_t scaled_gemm_part_bytes(int64_t m, int64_t n, int64_t k, int num_cu);
+size_t scaled_gemm_part_bytes(int64_t m, int64_t n, int64_t k, int num_cu);      // of the planes of a product without groups
 void launch_quantize(hipStream_t st, const QuantizeCall& q);
 
 void launch_sort_tokens(hipStream_t st, int choices, int experts, const void* chosen, bool wide, int32_t* offsets, int32_t* order,

@@ -57,8 +57,10 @@ oz_status_t gemm(oz_handle_t h, void* stream, Grouping grouping, int64_t groups,
     if (by_k && (k % kScaleBlock != 0 || A->block_rows != 1 || B->block_rows != 1)) return OZ_ERR_ARG;
     if (m == 0 || n == 0) return OZ_OK;
     if (!C || !is_aligned(C, uintptr_t(esize))) return OZ_ERR_ARG;
-    // workgroups of the smallest tiles there are
-    if (((m + 15) / 16 + (by_rows ? groups + 1 : 0)) * ((n + 63) / 64) > kMaxGrid) return OZ_ERR_ARG;
+    // workgroups: of 1024 threads on 16 columns for few rows, else of 256 on at least 64 x 64
+    const bool few = (by_rows ? (m + groups - 1) / groups : m) <= 64;
+    const int64_t tile = few ? 16 : 64;
+    if (((m + tile - 1) / tile + (by_rows ? groups + 1 : 0)) * ((n + tile - 1) / tile) > (few ? kMaxGrid / 4 : kMaxGrid)) return OZ_ERR_ARG;
     const size_t need = grouping == Grouping::kNone ? oz_scaled_gemm_workspace_bytes(h, m, n, k) : 0;
     if (need > 0 && (!ws || !is_aligned(ws, kWorkspaceAlign) || ws_bytes < need)) return OZ_ERR_WORKSPACE;
     if (!handle_on_device(h)) return OZ_ERR_DEVICE;
@@ -78,7 +80,9 @@ oz_status_t gemm(oz_handle_t h, void* stream, Grouping grouping, int64_t groups,
     g.grouping = grouping;
     g.a_e5m2 = A->type == OZ_E5M2;
     g.e8m0 = A->scale_type == OZ_E8M0;
-    launch_scaled_gemm(static_cast<hipStream_t>(stream), g, handle_compute_units(h), static_cast<float*>(ws), need);
+    g.wide = c_type == OZ_F32;
+    g.parts = 1;
+    launch_scaled_gemm(static_cast<hipStream_t>(stream), g, handle_compute_units(h), static_cast<float*>(ws));
     return hipGetLastError() == hipSuccess ? OZ_OK : OZ_ERR_HIP;
 }
 

@@ -3,6 +3,8 @@
 // A step is a block of 128 of k.  Its rows of A and B (128 bytes each) go from L2 straight into LDS, STAGES - 1 steps ahead;
 // one barrier per step.  A row's eight 16-byte pieces are stored at piece ^ (row & 7), so that the 16 lanes that read the same
 // piece of 16 rows meet different banks.  The scales come in the same way, four blocks at a time, into two buffers of their own.
+#include <algorithm>
+
 #include "oz_scaled_gemm_device.h"
 
 namespace oz {
@@ -175,40 +177,111 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
 
     if (steps == 0 && g.accumulate) return;
     __builtin_amdgcn_s_barrier();        // the other waves have read the last tiles
-    constexpr int kWaveBytes = WM * WN * (WIDE ? 4 : 2), kParts = kWaveBytes * WAVES <= int(sizeof(lds)) ? 1 : kWaveBytes * WAVES <= 2 * int(sizeof(lds)) ? 2 : 4;
-    store_results<WIDE, kParts>(g, acc, lds + wave * (kWaveBytes / kParts), t.c + int64_t(t.row + wm) * g.ldc + t.col + wn, t.rows - wm, t.cols - wn);
+    constexpr int kWaveBytes = int(sizeof(lds)) / WAVES / 1024 * 1024;
+    store_results<WIDE, BM == 64, kWaveBytes>(g, acc, lds + wave * kWaveBytes, t.c + int64_t(t.row + wm) * g.ldc + t.col + wn, t.rows - wm,
+                                              t.cols - wn);
+}
+
+// C = the parts' planes, in their order (+ C).  Four results a thread.
+__global__ __launch_bounds__(256) void add_planes_kernel(ScaledGemm g, const float* __restrict__ planes, int parts, int quads) {
+    const uint32_t x = blockIdx.x * 256 + threadIdx.x;
+    const int r = int(x / uint32_t(quads)), c = int(x % uint32_t(quads)) * 4;
+    if (r >= g.m) return;
+    const int have = min(4, g.n - c);
+    const int64_t at = int64_t(r) * g.n + c, plane = int64_t(g.m) * g.n;
+    v4f s = {0, 0, 0, 0};
+    if (have == 4 && g.n % 4 == 0) {
+#pragma unroll 8
+        for (int p = 0; p < parts; ++p) s += *reinterpret_cast<const v4f*>(planes + p * plane + at);
+    } else {
+        for (int p = 0; p < parts; ++p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < have) s[i] += planes[p * plane + at + i];
+    }
+    put4(g, int64_t(r) * g.ldc + c, have, s);
 }
 
 template <int BM, int BN, int WM, int WN, int STAGES>
 void launch_tiles(hipStream_t st, const ScaledGemm& g) {
     const int tiles_n = (g.n + BN - 1) / BN;
     const int64_t tiles_m = g.grouping == Grouping::kRows ? group_pieces(g.m, g.groups, BM) : (g.m + BM - 1) / BM;
-    const dim3 grid(unsigned(tiles_m * tiles_n), g.grouping == Grouping::kContraction ? unsigned(g.groups) : 1u);
+    const dim3 grid(unsigned(tiles_m * tiles_n), g.grouping == Grouping::kContraction ? unsigned(g.groups) : unsigned(g.parts));
     const dim3 block(64 * (BM / WM) * (BN / WN));
-    const int kind = (g.a_e5m2 ? 4 : 0) + (g.e8m0 ? 2 : 0) + (g.c_type == OZ_F32 ? 1 : 0);
+    const int kind = (g.a_e5m2 ? 4 : 0) + (g.e8m0 ? 2 : 0) + (g.wide ? 1 : 0);
 #define OZ_KIND(K) case K: hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, (K & 4) != 0, (K & 2) != 0, (K & 1) != 0>), grid, block, 0, st, g, tiles_n); break;
     switch (kind) { OZ_KIND(0) OZ_KIND(1) OZ_KIND(2) OZ_KIND(3) OZ_KIND(4) OZ_KIND(5) OZ_KIND(6) OZ_KIND(7) }
 #undef OZ_KIND
 }
 
+
+// How a product without groups is computed, by its sizes alone.
+enum class Route { kFew, kTiles64, kTiles128, kTall, kBig };
+struct Plan {
+    Route route;
+    int parts;         // of k
+    int waves;         // kFew
+};
+
+inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+Plan plan_of(int64_t m, int64_t n, int64_t k, int64_t groups, int num_cu) {
+    const int64_t blocks = up(k, kScaleBlock);
+    if (m <= 64) {
+        const int64_t strips = up(n, 16), fours = up(blocks, 4);
+        int64_t parts = std::min<int64_t>(num_cu / std::max<int64_t>(strips, 1), fours / 8);
+        parts = std::max<int64_t>(1, std::min<int64_t>(parts, 16));
+        const int64_t each = up(fours, parts);
+        return Plan{Route::kFew, int(parts), each <= 4 ? 4 : each <= 8 ? 8 : 16};
+    }
+    if (up(m, 256) * up(n, 256) * groups >= num_cu * 3 / 4) return Plan{Route::kBig, 1, 0};
+    if (up(m, 256) * up(n, 128) * groups >= num_cu * 3 / 4) return Plan{Route::kTall, 1, 0};
+    if (up(m, 128) * up(n, 128) * groups >= num_cu) return Plan{Route::kTiles128, 1, 0};
+    const int64_t tiles = up(m, 64) * up(n, 64) * groups;
+    int64_t parts = 1;
+    if (tiles * 4 <= num_cu * 3) parts = std::max<int64_t>(1, std::min<int64_t>({2 * num_cu / tiles, blocks / 4, 16}));
+    return Plan{Route::kTiles64, int(parts), 0};
+}
+
 }  // namespace
 
-size_t scaled_gemm_part_bytes(int64_t, int64_t, int64_t, int) { return 0; }
+size_t scaled_gemm_part_bytes(int64_t m, int64_t n, int64_t k, int num_cu) {
+    if (m == 0 || n == 0 || k == 0) return 0;
+    const Plan p = plan_of(m, n, k, 1, num_cu);
+    return p.parts > 1 ? size_t(p.parts) * size_t(m) * size_t(n) * 4 : 0;
+}
 
-void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int num_cu, float*, size_t) {
+void launch_scaled_gemm(hipStream_t st, const ScaledGemm& call, int num_cu, float* planes) {
+    ScaledGemm g = call;
     // rows that read an operand B together, on average
-    const int64_t rows = g.grouping == Grouping::kRows ? (int64_t(g.m) + g.groups - 1) / g.groups : g.m;
-    if (g.grouping != Grouping::kContraction && rows <= 64) {
-        const int fours = (g.k + 511) / 512;
-        launch_scaled_gemm_few(st, g, int(rows), fours <= 4 ? 4 : fours <= 8 ? 8 : 16);
-        return;
+    const int64_t rows = g.grouping == Grouping::kRows ? up(g.m, g.groups) : g.m;
+    const bool by_k = g.grouping == Grouping::kContraction;
+    Plan p = plan_of(g.grouping == Grouping::kRows && rows > 64 ? g.m : by_k ? std::max<int64_t>(rows, 65) : rows, g.n, g.k, by_k ? g.groups : 1, num_cu);
+    if (g.grouping != Grouping::kNone) {
+        // groups of fewer rows than a tall tile leave most of it empty
+        if (!by_k && rows < 192 && (p.route == Route::kBig || p.route == Route::kTall)) p.route = Route::kTiles128;
+        p.parts = 1;
+        if (p.route == Route::kFew) p.waves = up(g.k, 512) <= 4 ? 4 : up(g.k, 512) <= 8 ? 8 : 16;
     }
-    const int64_t tiles256 = ((g.m + 255) / 256) * int64_t((g.n + 255) / 256) * (g.grouping == Grouping::kContraction ? g.groups : 1);
-    const int64_t tiles128 = ((g.m + 127) / 128) * int64_t((g.n + 127) / 128) * (g.grouping == Grouping::kContraction ? g.groups : 1);
-    const int64_t tall = ((g.m + 255) / 256) * int64_t((g.n + 127) / 128) * (g.grouping == Grouping::kContraction ? g.groups : 1);
-    if (g.c_type != OZ_F32 && tall >= num_cu * 3 / 4) launch_scaled_gemm_big(st, g, tiles256 >= num_cu * 3 / 4);
-    else if (tiles128 >= num_cu) launch_tiles<128, 128, 64, 64, 2>(st, g);
-    else launch_tiles<64, 64, 32, 32, 2>(st, g);
+    if (p.parts > 1) {
+        g.parts = p.parts;
+        g.c = planes;
+        g.ldc = g.n;
+        g.c_type = OZ_F32;
+        g.accumulate = 0;
+    }
+    switch (p.route) {
+        case Route::kFew: launch_scaled_gemm_few(st, g, int(rows), p.waves); break;
+        case Route::kTiles64: launch_tiles<64, 64, 32, 32, 4>(st, g); break;
+        case Route::kTiles128: launch_tiles<128, 128, 64, 64, 2>(st, g); break;
+        default:
+            if (g.wide) launch_tiles<128, 128, 64, 64, 2>(st, g);
+            else launch_scaled_gemm_big(st, g, p.route == Route::kBig);
+    }
+    if (p.parts > 1) {
+        const int quads = int(up(g.n, 4));
+        hipLaunchKernelGGL(add_planes_kernel, dim3(unsigned(up(int64_t(g.m) * quads, 256))), dim3(256), 0, st, call, planes, p.parts, quads);
+    }
 }
 
 }  // namespace oz

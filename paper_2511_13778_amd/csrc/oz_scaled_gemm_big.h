@@ -357,7 +357,7 @@ __global__ __launch_bounds__(256, 1) void scaled_gemm_big_kernel(ScaledGemm g, i
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[j][i] = v4f{each[j][i][0], each[j][i][1], each[j][i][2], each[j][i][3]};
     }
-    store_results<false, 1>(g, acc, lds + wave * (128 * 32 * NB * 2), t.c + int64_t(t.row + wm) * g.ldc + t.col + wn, t.rows - wm, t.cols - wn);
+    store_results<false, false, 128 * 32 * NB * 2>(g, acc, lds + wave * (128 * 32 * NB * 2), t.c + int64_t(t.row + wm) * g.ldc + t.col + wn, t.rows - wm, t.cols - wn);
 }
 
 template <int NB, Scales SC>

@@ -119,6 +119,11 @@ __device__ __forceinline__ GemmTile locate(const ScaledGemm& g, int tile_m, int 
         t.block0 = s.blocks_before;
         t.c = int64_t(group) * g.stride_c;
         if (t.block0 + (t.k + kScaleBlock - 1) / kScaleBlock > g.k / kScaleBlock) t.k = 0;       // offsets that do not fit the columns
+    } else if (g.parts > 1) {             // `group`: a part of k
+        const int fours = (g.k + 4 * kScaleBlock - 1) / (4 * kScaleBlock);        // whole words of E8M0 scales
+        t.block0 = int(int64_t(fours) * group / g.parts) * 4;
+        t.k = min(g.k, int(int64_t(fours) * (group + 1) / g.parts) * 4 * kScaleBlock) - t.block0 * kScaleBlock;
+        t.c = int64_t(group) * g.m * g.n;
     }
     t.rows = min(TM, row_end - t.row);
     const int64_t k0 = int64_t(t.block0) * kScaleBlock;
@@ -269,14 +274,22 @@ __device__ __forceinline__ void store_typed(const ScaledGemm& g, v4f (&acc)[NT][
         }
     }
 }
-// FLOAT32: C is float32, in PARTS parts; else it has 16 bits.  One copy of the code per type runs: the kernels' own is what fills the
-// instruction cache.
-template <bool FLOAT32, int PARTS, int MT, int NT>
+// WIDE: C is float32; else it has 16 bits, or is a plane of float32 for a part of k (CUT: such calls reach this kernel).  `lds` holds
+// BYTES.  One copy of the code per type runs: the kernels' own is what fills the instruction cache.
+template <bool WIDE, bool CUT, int BYTES, int MT, int NT>
 __device__ __forceinline__ void store_results(const ScaledGemm& g, v4f (&acc)[NT][MT], uint8_t* lds, int64_t c, int rows, int cols) {
+    constexpr int kSize = MT * NT * 256;
+    constexpr int P4 = kSize * 4 <= BYTES ? 1 : kSize * 2 <= BYTES ? 2 : 4, P2 = kSize * 2 <= BYTES ? 1 : 2;
+    static_assert(kSize * 4 / P4 <= BYTES && kSize * 2 / P2 <= BYTES, "room for a part");
     const bool add = g.accumulate != 0;
-    if constexpr (FLOAT32) {
-        if (add) store_typed<float, true, PARTS>(g, acc, lds, c, rows, cols);
-        else store_typed<float, false, PARTS>(g, acc, lds, c, rows, cols);
+    if constexpr (WIDE) {
+        if (add) store_typed<float, true, P4>(g, acc, lds, c, rows, cols);
+        else store_typed<float, false, P4>(g, acc, lds, c, rows, cols);
+        return;
+    }
+    constexpr int PARTS = P2;
+    if (CUT && g.c_type == OZ_F32) {
+        store_typed<float, false, P4>(g, acc, lds, c, rows, cols);
     } else if (g.c_type == OZ_BF16) {
         if (add) store_typed<bf16_t, true, PARTS>(g, acc, lds, c, rows, cols);
         else store_typed<bf16_t, false, PARTS>(g, acc, lds, c, rows, cols);

@@ -20,7 +20,7 @@ __global__ __launch_bounds__(MT == 1 ? 1024 : 512) void scaled_gemm_few_kernel(S
     extern __shared__ __align__(16) float sums[];                 // [wave][row][16]
     constexpr int kB = kFew<MT>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = int(blockDim.x) >> 6;
-    const GemmTile t = locate<MT * 16, 16>(g, int(blockIdx.x) / strips, int(blockIdx.x) % strips, 0);
+    const GemmTile t = locate<MT * 16, 16>(g, int(blockIdx.x) / strips, int(blockIdx.x) % strips, int(blockIdx.y));
     if (t.none) return;
     const int q = lane >> 4, x16 = lane & 15;
     const int blocks = (t.k + kScaleBlock - 1) / kScaleBlock, tail = t.k & (kScaleBlock - 1);
@@ -33,10 +33,10 @@ __global__ __launch_bounds__(MT == 1 ? 1024 : 512) void scaled_gemm_few_kernel(S
     const __amdgpu_buffer_rsrc_t buf_b = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(t.b), 0, int(uint32_t(t.cols - 1) * ldb + bytes), 0x00020000);
     const uint32_t lane_a = uint32_t(x16) * lda + uint32_t(q) * 32, lane_b = uint32_t(x16) * ldb + uint32_t(q) * 32;
     // rows of scales: a lane's own row of each fragment
-    const uint8_t* row_sb = t.sb + int64_t((t.col + min(x16, t.cols - 1)) >> g.b.shift) * g.b.scale_ld * (E8M0 ? 1 : 4);
+    const uint8_t* row_sb = t.sb + (int64_t((t.col + min(x16, t.cols - 1)) >> g.b.shift) * g.b.scale_ld + t.block0) * (E8M0 ? 1 : 4);
     const uint8_t* row_sa[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) row_sa[i] = t.sa + int64_t((t.row + min(i * 16 + x16, t.rows - 1)) >> g.a.shift) * g.a.scale_ld * (E8M0 ? 1 : 4);
+    for (int i = 0; i < MT; ++i) row_sa[i] = t.sa + (int64_t((t.row + min(i * 16 + x16, t.rows - 1)) >> g.a.shift) * g.a.scale_ld + t.block0) * (E8M0 ? 1 : 4);
 
     for (int b0 = wave * kB; b0 < blocks; b0 += waves * kB) {
         union Frag { v8i32 f; v4i32 h[2]; };
@@ -120,9 +120,9 @@ void launch_rows(hipStream_t st, const ScaledGemm& g, int waves) {
     const int strips = (g.n + 15) / 16;
     const int64_t tiles_m = g.grouping == Grouping::kRows ? group_pieces(g.m, g.groups, MT * 16) : (g.m + MT * 16 - 1) / (MT * 16);
     waves = MT == 1 || waves < 8 ? waves : 8;
-    const dim3 grid(unsigned(tiles_m * strips)), block(64 * waves);
+    const dim3 grid(unsigned(tiles_m * strips), unsigned(g.parts)), block(64 * waves);
     const size_t lds = size_t(waves) * MT * 16 * 16 * 4;
-    const int kind = (g.a_e5m2 ? 4 : 0) + (g.e8m0 ? 2 : 0) + (g.c_type == OZ_F32 ? 1 : 0);
+    const int kind = (g.a_e5m2 ? 4 : 0) + (g.e8m0 ? 2 : 0) + (g.wide ? 1 : 0);
 #define OZ_KIND(K) case K: hipLaunchKernelGGL((scaled_gemm_few_kernel<MT, (K & 4) != 0, (K & 2) != 0, (K & 1) != 0>), grid, block, lds, st, g, strips); break;
     switch (kind) { OZ_KIND(0) OZ_KIND(1) OZ_KIND(2) OZ_KIND(3) OZ_KIND(4) OZ_KIND(5) OZ_KIND(6) OZ_KIND(7) }
 #undef OZ_KIND

@@ -84,6 +84,59 @@ def test_product(h, m, n, k, scale, out):
         close(scaled.gemm(h, a, b, dtype=out), exact, size, k)
 
 
+# sizes that fill the chip with tiles of 256 x 256, 256 x 128 and 128 x 128, ragged, of one step to many, odd and even in number; and few tiles with a
+# long k, which is cut
+@pytest.mark.parametrize("scale", [torch.uint8, torch.float32])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("m,n,k", [(3700, 3650, 100), (3600, 3700, 256), (3601, 3841, 777), (2500, 2600, 128), (2305, 2590, 1290), (2600, 2500, 640), (2100, 2000, 300),
+                                   (100, 300, 9000), (300, 70, 20001), (65, 65, 4096), (40, 200, 16500)])
+def test_product_large(h, m, n, k, scale, out):
+    from paper_2511_13778_amd import scaled
+    for a_type, rows_b in ((E4M3, 128), (E5M2, 1)):
+        a, b = matrix(m + k, m, k, a_type, scale, spread=0.5), matrix(n, n, k, E4M3, scale, rows_b, spread=0.5)
+        if scale == torch.uint8:
+            a.scale -= 6                                        # within float16's range
+        else:
+            a.scale *= 2.0 ** -6
+        da, db = dense(a), dense(b)
+        exact, size = da @ db.t(), da.abs() @ db.abs().t()
+        got = scaled.gemm(h, a, b, dtype=out)
+        close(got, exact, size, k)
+        if out != torch.float16:
+            c = got.clone()
+            scaled.gemm(h, a, b, out=c, accumulate=True)
+            close(c, exact + got.double(), size + got.double().abs(), k)
+
+
+@pytest.mark.parametrize("scale", [torch.uint8, torch.float32])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+def test_groups_large(h, scale, out):
+    # groups that fill tall tiles, and one that ends inside each kind of tile
+    from paper_2511_13778_amd import scaled
+    counts, k, n = [700, 0, 1500, 257, 3, 900, 640], 500, 2700
+    offsets = torch.tensor([sum(counts[:i]) for i in range(len(counts) + 1)], dtype=torch.int32, device="cuda")
+    a, b = matrix(5, sum(counts) + 9, k, E4M3, scale), matrix(6, n, k, E4M3, scale, 128, groups=len(counts))
+    got = scaled.gemm_grouped(h, a, b, offsets, dtype=out)
+    da, db = dense(a), dense(b)
+    for e, c in enumerate(counts):
+        rows = slice(int(offsets[e]), int(offsets[e]) + c)
+        if c:
+            close(got[rows], da[rows] @ db[e].t(), da[rows].abs() @ db[e].abs().t(), k)
+    assert not got[sum(counts):].any()
+    r = gen(2)
+    y, x = torch.randn((sum(counts), 1500), generator=r, device="cuda"), torch.randn((sum(counts), 1400), generator=r, device="cuda")
+    qa, qb = (scaled.quantize(h, v, E4M3, scale, which="columns", offsets=offsets) for v in (y, x))
+    got = scaled.gemm_grouped_k(h, qa, qb, offsets, dtype=out)
+    for e, c in enumerate(counts):
+        part = slice(int(offsets[e]), int(offsets[e]) + c)
+        if c:
+            (qy, ey), (qx, ex) = ref.quantize(y[part].t(), E4M3, 1), ref.quantize(x[part].t(), E4M3, 1)
+            dy, dx = (q * ref.power(v).repeat_interleave(128, 1)[:, :c] for q, v in ((qy, ey), (qx, ex)))
+            close(got[e], dy @ dx.t(), dy.abs() @ dx.abs().t(), c)
+        else:
+            assert not got[e].any()
+
+
 @pytest.mark.parametrize("scale", [torch.uint8, torch.float32])
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("m,n,k,pad", [(5, 70, 200, 1), (130, 260, 500, 3), (300, 290, 777, 2), (512, 512, 256, 0)])
