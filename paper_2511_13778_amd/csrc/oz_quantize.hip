@@ -118,11 +118,11 @@ struct TileArgs {
 // A tile of 128 x 128: rows, columns or the whole share a scale; written as it is and transposed from one read.
 // Thread (g, l): rows 8g .. 8g+7, columns 8l .. 8l+7, in registers throughout; the transposed bytes change places through LDS.
 // grid (row tiles, column tiles, batch)
-constexpr int kPitch = kScaleBlock + 16;      // bytes of a transposed row in LDS: 16-byte reads, the rows in different banks
+// There the eight bytes of thread (g, l) lie at place g ^ l of their row: the 16 rows that lanes write at a time meet different banks.
 template <typename T, bool ROWS_E5M2, bool COLS_E5M2, bool SHARED>
 __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
-    __shared__ uint32_t col_top[16][kScaleBlock];
-    __shared__ __align__(16) uint8_t turned[kScaleBlock * kPitch];
+    __shared__ __align__(16) uint32_t col_top[16][kScaleBlock];
+    __shared__ __align__(16) uint8_t turned[kScaleBlock * kScaleBlock];
     const int g = threadIdx.x >> 4, l = threadIdx.x & 15;
     int row0 = int(blockIdx.x) * kScaleBlock, end = p.rows, out_col = row0;
     bool cols_too = p.by_cols.data != nullptr;
@@ -197,13 +197,15 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
     }
     if (!cols_too) return;                       // the same for all of a workgroup
     if constexpr (!SHARED) {
+        uint32_t tops[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            uint32_t top = 0;
+            tops[j] = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, mag(x[i][j]));
-            col_top[g][l * 8 + j] = top;
+            for (int i = 0; i < 8; ++i) tops[j] = max(tops[j], mag(x[i][j]));
         }
+#pragma unroll
+        for (int j = 0; j < 8; j += 4) *reinterpret_cast<uint4*>(&col_top[g][l * 8 + j]) = make_uint4(tops[j], tops[j + 1], tops[j + 2], tops[j + 3]);
         __syncthreads();
         if (threadIdx.x < kScaleBlock) {
             uint32_t top = 0;
@@ -216,14 +218,20 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
         }
         __syncthreads();
     }
+    uint32_t tops[8];
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) {
+        const uint4 v = SHARED ? make_uint4(shared_top, shared_top, shared_top, shared_top) : *reinterpret_cast<const uint4*>(&col_top[0][l * 8 + j]);
+        tops[j] = v.x; tops[j + 1] = v.y; tops[j + 2] = v.z; tops[j + 3] = v.w;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const Scale s = scale_of<COLS_E5M2>(SHARED ? shared_top : col_top[0][l * 8 + j]);
+        const Scale s = scale_of<COLS_E5M2>(tops[j]);
         uint32_t w[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             w[i] = pack4<COLS_E5M2>(x[4 * i][j] * s.mul, x[4 * i + 1][j] * s.mul, x[4 * i + 2][j] * s.mul, x[4 * i + 3][j] * s.mul);
-        *reinterpret_cast<uint2*>(turned + (l * 8 + j) * kPitch + g * 8) = make_uint2(w[0], w[1]);
+        *reinterpret_cast<uint2*>(turned + (l * 8 + j) * kScaleBlock + (g ^ l) * 8) = make_uint2(w[0], w[1]);
     }
     __syncthreads();
     // columns to write: all 128 of a group's block, else what is there, up to a multiple of 16
@@ -233,8 +241,11 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
     for (int i = 0; i < 4; ++i) {
         const int q = i * 256 + threadIdx.x, tr = q >> 3, piece = (q & 7) * 16;
         const int c = int(blockIdx.y) * kScaleBlock + tr;
+        // eight bytes 2p at place 2p ^ l, 2p+1 beside it: in turned order where l is odd
+        const int tl = tr >> 3;
+        const v4i32 v = *reinterpret_cast<const v4i32*>(turned + tr * kScaleBlock + (((q & 7) * 2) ^ (tl & 14)) * 8);
         if (c < p.cols && piece < wide)
-            *reinterpret_cast<v4i32*>(out + int64_t(c) * p.by_cols.ld + out_col + piece) = *reinterpret_cast<const v4i32*>(turned + tr * kPitch + piece);
+            *reinterpret_cast<v4i32*>(out + int64_t(c) * p.by_cols.ld + out_col + piece) = (tl & 1) ? v4i32{v[2], v[3], v[0], v[1]} : v;
     }
 }
 

@@ -11,25 +11,22 @@ namespace oz {
 namespace {
 
 constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
-constexpr int kSortBlock = 4096;          // choices of a workgroup, more where that would be over 256 workgroups
+constexpr int kRounds = 8;                // 64s of choices that a wave has on their way at a time
 
+// Choices of a workgroup: all of them up to 4096, which one launch sorts; else 1024 (two rounds of a wave), more where that would be over
+// 256 workgroups.
 int sort_block(int64_t choices) {
+    if (choices <= kSortThreads * kRounds) return kSortThreads * kRounds;
     const int64_t per = (choices + 255) / 256;
-    return int(per <= kSortBlock ? kSortBlock : (per + kSortThreads - 1) / kSortThreads * kSortThreads);
+    return int(per <= 2 * kSortThreads ? 2 * kSortThreads : (per + kSortThreads - 1) / kSortThreads * kSortThreads);
 }
 
 struct SortArgs {
     const void* chosen;
-    int32_t *offsets, *order, *place, *counts;      // counts[e * blocks + b]
+    int32_t *offsets, *order, *place, *counts;      // counts[block][expert]
     int choices, experts, bits, per_block, blocks;
     bool wide;
 };
-
-__device__ __forceinline__ int chosen_expert(const SortArgs& p, int i, int end) {
-    if (i >= end) return -1;
-    const int64_t e = p.wide ? static_cast<const int64_t*>(p.chosen)[i] : static_cast<const int32_t*>(p.chosen)[i];
-    return e >= 0 && e < p.experts ? int(e) : -1;
-}
 
 // Lanes of this wave with the same expert (0 for none).
 __device__ __forceinline__ unsigned long long same_expert(int e, int bits) {
@@ -41,43 +38,81 @@ __device__ __forceinline__ unsigned long long same_expert(int e, int bits) {
     return e >= 0 ? m : 0;
 }
 
+// f(index, expert or -1, lanes with the same expert) for this wave's choices, 64 at a time, in their order; all lanes come along, also those
+// behind the last.
+template <typename F>
+__device__ __forceinline__ void each_choice(const SortArgs& p, int from, int to, F&& f) {
+    const int lane = threadIdx.x & 63;
+    for (int i0 = from; i0 < to; i0 += 64 * kRounds) {
+        int e[kRounds];
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u) {
+            const int i = i0 + u * 64 + lane;
+            int64_t id = -1;
+            if (i < to) id = p.wide ? static_cast<const int64_t*>(p.chosen)[i] : int64_t(static_cast<const int32_t*>(p.chosen)[i]);
+            e[u] = id >= 0 && id < p.experts ? int(id) : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u)
+            if (i0 + u * 64 < to) f(i0 + u * 64 + lane, e[u], same_expert(e[u], p.bits));
+    }
+}
+
+__device__ __forceinline__ void wave_part(const SortArgs& p, int& from, int& to) {
+    const int begin = int(blockIdx.x) * p.per_block, end = min(begin + p.per_block, p.choices), per_wave = p.per_block / kSortWaves;
+    from = begin + int(threadIdx.x >> 6) * per_wave;
+    to = min(from + per_wave, end);
+}
+
 // count[wave][expert] of this block's choices; waves take consecutive parts of it
-__device__ __forceinline__ void count_block(const SortArgs& p, int begin, int end, int32_t* count) {
+__device__ __forceinline__ void count_block(const SortArgs& p, int32_t* count) {
     for (int i = threadIdx.x; i < kSortWaves * p.experts; i += kSortThreads) count[i] = 0;
     __syncthreads();
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int per_wave = p.per_block / kSortWaves;
-    int32_t* mine = count + wave * p.experts;
-    const int from = begin + wave * per_wave, to = min(from + per_wave, end);
-    for (int i = from; i < to; i += 64) {
-        const int e = chosen_expert(p, i + lane, to);
-        const unsigned long long m = same_expert(e, p.bits);
-        if (m && (m & ((1ull << lane) - 1)) == 0) mine[e] += __popcll(m);       // one lane per expert
+    int from, to;
+    wave_part(p, from, to);
+    int32_t* mine = count + int(threadIdx.x >> 6) * p.experts;
+    const unsigned long long below = (1ull << (threadIdx.x & 63)) - 1;
+    each_choice(p, from, to, [&](int, int e, unsigned long long m) {
+        if (m && (m & below) == 0) mine[e] += __popcll(m);       // one lane per expert
         __builtin_amdgcn_wave_barrier();
-    }
+    });
     __syncthreads();
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs p) {
     extern __shared__ int32_t count[];
-    const int begin = int(blockIdx.x) * p.per_block, end = min(begin + p.per_block, p.choices);
-    count_block(p, begin, end, count);
+    count_block(p, count);
     for (int e = threadIdx.x; e < p.experts; e += kSortThreads) {
         int sum = 0;
         for (int w = 0; w < kSortWaves; ++w) sum += count[w * p.experts + e];
-        p.counts[int64_t(e) * p.blocks + blockIdx.x] = sum;
+        p.counts[int64_t(blockIdx.x) * p.experts + e] = sum;
     }
 }
 
-// Where each choice goes.  Every workgroup adds up the counts of all blocks by itself (at most 256 per expert, one wave each).
+// Where each choice goes.  Every workgroup adds up the counts of all blocks by itself: its waves take an eighth of the blocks each.
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs p) {
-    extern __shared__ int32_t count[];                    // [waves][experts], then total and start of each expert
-    __shared__ int32_t wave_total[kSortWaves + 1];
+    extern __shared__ int32_t count[];                    // [waves][experts], then the tables below
+    __shared__ int32_t wave_total[kSortWaves];
     int32_t* total = count + kSortWaves * p.experts;      // all choices of an expert, then its first slot
     int32_t* before = total + p.experts;                  // those in blocks before this one
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, block = blockIdx.x;
-    const int begin = block * p.per_block, end = min(begin + p.per_block, p.choices);
-    count_block(p, begin, end, count);
+    if (p.blocks > 1) {
+        for (int e = threadIdx.x; e < 2 * p.experts; e += kSortThreads) total[e] = 0;
+        __syncthreads();
+        const int share = (p.blocks + kSortWaves - 1) / kSortWaves, b0 = wave * share, b1 = min(b0 + share, p.blocks);
+        for (int e = lane; e < p.experts; e += 64) {
+            int all = 0, prev = 0;
+#pragma unroll 8
+            for (int b = b0; b < b1; ++b) {
+                const int c = p.counts[int64_t(b) * p.experts + e];
+                all += c;
+                prev += b < block ? c : 0;
+            }
+            atomicAdd(&total[e], all);                    // whole numbers: in any order the same
+            atomicAdd(&before[e], prev);
+        }
+    }
+    count_block(p, count);
     if (p.blocks == 1) {
         for (int e = threadIdx.x; e < p.experts; e += kSortThreads) {
             int sum = 0;
@@ -85,25 +120,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs p) {
             total[e] = sum;
             before[e] = 0;
         }
-    } else {
-        for (int e = wave; e < p.experts; e += kSortWaves) {
-            int all = 0, prev = 0;
-            for (int b = lane; b < p.blocks; b += 64) {
-                const int c = p.counts[int64_t(e) * p.blocks + b];
-                all += c;
-                prev += b < block ? c : 0;
-            }
-            for (int d = 1; d < 64; d <<= 1) {
-                all += __shfl_xor(all, d);
-                prev += __shfl_xor(prev, d);
-            }
-            if (lane == 0) {
-                total[e] = all;
-                before[e] = prev;
-            }
-        }
+        __syncthreads();
     }
-    __syncthreads();
     // exclusive prefix over the experts, 512 at a time
     int carry = 0;
     for (int e0 = 0; e0 < p.experts; e0 += kSortThreads) {
@@ -120,42 +138,36 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs p) {
         for (int w = 0; w < wave; ++w) base += wave_total[w];
         for (int w = 0; w < kSortWaves; ++w) carry += wave_total[w];
         if (e < p.experts) {
-            total[e] = base + sum - mine;
-            if (block == 0) p.offsets[e] = base + sum - mine;
+            const int first = base + sum - mine;
+            if (block == 0) p.offsets[e] = first;
+            // first slot of each wave's choices
+            int at = first + before[e];
+            for (int w = 0; w < kSortWaves; ++w) {
+                const int c = count[w * p.experts + e];
+                count[w * p.experts + e] = at;
+                at += c;
+            }
         }
         __syncthreads();
     }
     const int live = carry;
     if (block == 0 && threadIdx.x == 0) p.offsets[p.experts] = live;
-    // first slot of each wave's choices
-    for (int e = threadIdx.x; e < p.experts; e += kSortThreads) {
-        int at = total[e] + before[e];
-        for (int w = 0; w < kSortWaves; ++w) {
-            const int c = count[w * p.experts + e];
-            count[w * p.experts + e] = at;
-            at += c;
-        }
-    }
-    __syncthreads();
-    const int per_wave = p.per_block / kSortWaves;
     int32_t* next = count + wave * p.experts;
-    const int from = begin + wave * per_wave, to = min(from + per_wave, end);
-    for (int i0 = from; i0 < to; i0 += 64) {
-        const int i = i0 + lane;
-        const int e = chosen_expert(p, i, to);
-        const unsigned long long m = same_expert(e, p.bits);
-        const unsigned long long lower = m & ((1ull << lane) - 1);
+    int from, to;
+    wave_part(p, from, to);
+    const unsigned long long below = (1ull << lane) - 1;
+    each_choice(p, from, to, [&](int i, int e, unsigned long long m) {
         int slot = -1;
-        if (m) slot = next[e] + __popcll(lower);
+        if (m) slot = next[e] + __popcll(m & below);
         __builtin_amdgcn_wave_barrier();
-        if (m && lower == 0) next[e] += __popcll(m);
+        if (m && (m & below) == 0) next[e] += __popcll(m);
         __builtin_amdgcn_wave_barrier();
         if (i < to) {
             p.place[i] = slot;
             if (slot >= 0) p.order[slot] = i;
             if (i >= live) p.order[i] = -1;
         }
-    }
+    });
 }
 
 // ---- rows ---------------------------------------------------------------------------------------
