@@ -337,10 +337,10 @@ size_t oz_sort_tokens_workspace_bytes(oz_handle_t handle, int64_t tokens, int64_
 oz_status_t oz_sort_tokens(oz_handle_t handle, void* stream, int64_t tokens, int64_t topk, int64_t experts, const void* chosen,
                            int32_t id_bytes, int32_t* offsets, int32_t* order, int32_t* place, void* workspace, size_t workspace_bytes);
 
-/* Y[s] = X[order[s] / order_div] for `slots` rows of `cols` values, zeros where order[s] is negative or X (x_rows rows) has no such row.
- * type of X and Y: OZ_F32, OZ_BF16 or OZ_F16. */
-oz_status_t oz_gather_rows(oz_handle_t handle, void* stream, int64_t slots, int64_t cols, int32_t type, const void* X, int64_t ldx,
-                           int64_t x_rows, const int32_t* order, int64_t order_div, void* Y, int64_t ldy);
+/* Y[place[t * topk + j]] = X[t] for every choice that has a place: rows of `cols` values sorted by expert; rows s of Y (tokens * topk of
+ * them) with order[s] negative become zero.  type of X and Y: OZ_F32, OZ_BF16 or OZ_F16.  topk <= 64. */
+oz_status_t oz_gather_rows(oz_handle_t handle, void* stream, int64_t tokens, int64_t topk, int64_t cols, int32_t type, const void* X,
+                           int64_t ldx, const int32_t* order, const int32_t* place, void* Y, int64_t ldy);
 
 /* Y[t] = sum_j weights[t * topk + j] * X[place[t * topk + j]], j ascending, in 32 bits, rounded once; choices without a row in X (slots rows)
  * are left out.  weights NULL: all 1 (the gradient of oz_gather_rows).  topk <= 64. */

@@ -178,32 +178,44 @@ struct GatherArgs {
     const uint8_t* x;
     uint8_t* y;
     int64_t ldx, ldy;                     // bytes
-    const int32_t* order;
-    int order_div, x_rows, slots, row_bytes, pieces;
+    const int32_t *order, *place;
+    int tokens, topk, row_bytes, pieces;
+    int per;                              // choices of a token that a wave writes
 };
 
-// A wave per 4 KB of a row.  T: the widest type that every row's address and length is a multiple of.
+// A wave per 4 KB of a token's row, which it reads once and writes for each choice: from the slots' side every choice would read it again,
+// long after it has left L2 (65536 slots of 4 KB 76 us that way, 61 this).  Few tokens have a wave per choice (33 tokens with 8
+// choices 2.7 us, 5 with one wave for all).  grid.y: choices / per.  T: the widest type that every row's address and length is a multiple of.
 template <typename T>
 __global__ __launch_bounds__(256) void gather_rows_kernel(GatherArgs p) {
     const uint32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int s = int(id / uint32_t(p.pieces)), piece = int(id - uint32_t(s) * uint32_t(p.pieces)), lane = threadIdx.x & 63;
-    if (s >= p.slots) return;
-    const int o = p.order[s], src = o < 0 ? -1 : o / p.order_div;
-    const bool there = src >= 0 && src < p.x_rows;
-    const int from = piece * 4096, to = min(from + 4096, p.row_bytes);
-    const uint8_t* x = p.x + int64_t(there ? src : 0) * p.ldx;
-    uint8_t* y = p.y + int64_t(s) * p.ldy;
+    const int t = int(id / uint32_t(p.pieces)), piece = int(id - uint32_t(t) * uint32_t(p.pieces)), lane = threadIdx.x & 63;
+    if (t >= p.tokens) return;
+    const int slots = p.tokens * p.topk, from = piece * 4096, to = min(from + 4096, p.row_bytes);
+    const uint8_t* x = p.x + int64_t(t) * p.ldx;
     constexpr int kStep = 64 * int(sizeof(T));
     for (int at = from + lane * int(sizeof(T)); at < to; at += kStep * kUnitVecs) {
         T v[kUnitVecs];
 #pragma unroll
         for (int u = 0; u < kUnitVecs; ++u) {
             v[u] = T{};
-            if (there && at + u * kStep < to) v[u] = *reinterpret_cast<const T*>(x + at + u * kStep);
+            if (at + u * kStep < to) v[u] = *reinterpret_cast<const T*>(x + at + u * kStep);
         }
+        for (int j = int(blockIdx.y) * p.per; j < min((int(blockIdx.y) + 1) * p.per, p.topk); ++j) {
+            const int c = t * p.topk + j, s = p.place[c];
+            if (s >= 0 && s < slots) {
+                uint8_t* y = p.y + int64_t(s) * p.ldy + at;
 #pragma unroll
-        for (int u = 0; u < kUnitVecs; ++u)
-            if (at + u * kStep < to) *reinterpret_cast<T*>(y + at + u * kStep) = v[u];
+                for (int u = 0; u < kUnitVecs; ++u)
+                    if (at + u * kStep < to) __builtin_nontemporal_store(v[u], reinterpret_cast<T*>(y + u * kStep));
+            }
+            if (p.order[c] < 0) {         // slot c belongs to no choice
+                uint8_t* y = p.y + int64_t(c) * p.ldy + at;
+#pragma unroll
+                for (int u = 0; u < kUnitVecs; ++u)
+                    if (at + u * kStep < to) *reinterpret_cast<T*>(y + u * kStep) = T{};
+            }
+        }
     }
 }
 
@@ -237,7 +249,7 @@ __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs p) {
             const int s = j0 + u < p.topk ? p.place[c] : -1;
             live[u] = s >= 0 && s < p.slots;
             w[u] = live[u] && p.weights ? p.weights[c] : 1.0f;
-            if (live[u]) load_row<8>(x + int64_t(s) * p.ldx + col, have, p.vec, v[u]);
+            if (live[u]) load_row<8, true>(x + int64_t(s) * p.ldx + col, have, p.vec, v[u]);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -269,7 +281,7 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs p) {
                 const int at = col + u * 512;
                 if (at < p.cols) {
                     load_row<8>(dy + at, p.cols - at, p.vec, g[u]);
-                    if (p.dweights) load_row<8>(x + at, p.cols - at, p.vec, v[u]);
+                    if (p.dweights) load_row<8, true>(x + at, p.cols - at, p.vec, v[u]);
                 }
             }
 #pragma unroll
@@ -282,7 +294,7 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs p) {
                         if (p.dweights) dot = fmaf(g[u][i], v[u][i], dot);
                         out[i] = w * g[u][i];
                     }
-                    store_row<8>(dx + at, p.cols - at, p.vec, out);
+                    store_row<8, true>(dx + at, p.cols - at, p.vec, out);
                 }
             }
         }
@@ -332,13 +344,14 @@ void launch_sort_tokens(hipStream_t st, int choices, int experts, const void* ch
     hipLaunchKernelGGL(sort_place_kernel, dim3(p.blocks), dim3(kSortThreads), size_t(kSortWaves + 2) * experts * 4, st, p);
 }
 
-void launch_gather_rows(hipStream_t st, int slots, int cols, int elem_bytes, const void* x, int64_t ldx, int x_rows, const int32_t* order,
-                        int order_div, void* y, int64_t ldy) {
-    GatherArgs p{static_cast<const uint8_t*>(x), static_cast<uint8_t*>(y), ldx * elem_bytes, ldy * elem_bytes, order, order_div, x_rows, slots,
-                 cols * elem_bytes, 0};
+void launch_gather_rows(hipStream_t st, int tokens, int topk, int cols, int elem_bytes, const void* x, int64_t ldx, const int32_t* order,
+                        const int32_t* place, void* y, int64_t ldy) {
+    GatherArgs p{static_cast<const uint8_t*>(x), static_cast<uint8_t*>(y), ldx * elem_bytes, ldy * elem_bytes, order, place, tokens, topk,
+                 cols * elem_bytes, 0, topk};
     p.pieces = (p.row_bytes + 4095) / 4096;
+    if (int64_t(tokens) * p.pieces < 4096) p.per = 1;
     const uintptr_t all = reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y) | uintptr_t(p.ldx) | uintptr_t(p.ldy) | uintptr_t(p.row_bytes);
-    const dim3 grid(unsigned((int64_t(slots) * p.pieces + 3) / 4));
+    const dim3 grid(unsigned((int64_t(tokens) * p.pieces + 3) / 4), unsigned(topk / p.per));
     if (all % 16 == 0) hipLaunchKernelGGL(gather_rows_kernel<v4i32>, grid, dim3(256), 0, st, p);
     else if (all % 4 == 0) hipLaunchKernelGGL(gather_rows_kernel<uint32_t>, grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL(gather_rows_kernel<uint16_t>, grid, dim3(256), 0, st, p);

@@ -59,8 +59,8 @@ void launch_quantize(hipStream_t st, const QuantizeCall& q);
 void launch_sort_tokens(hipStream_t st, int choices, int experts, const void* chosen, bool wide, int32_t* offsets, int32_t* order,
                         int32_t* place, int32_t* ws);
 size_t sort_tokens_bytes(int64_t choices, int64_t experts);
-void launch_gather_rows(hipStream_t st, int slots, int cols, int elem_bytes, const void* x, int64_t ldx, int x_rows, const int32_t* order,
-                        int order_div, void* y, int64_t ldy);
+void launch_gather_rows(hipStream_t st, int tokens, int topk, int cols, int elem_bytes, const void* x, int64_t ldx, const int32_t* order,
+                        const int32_t* place, void* y, int64_t ldy);
 void launch_combine_rows(hipStream_t st, int tokens, int topk, int cols, int type, const void* x, int64_t ldx, int slots, const int32_t* place,
                          const float* weights, void* y, int64_t ldy);
 void launch_combine_grad(hipStream_t st, int tokens, int topk, int cols, int type, const void* dy, int64_t lddy, const void* x, int64_t ldx,

@@ -180,15 +180,16 @@ oz_status_t oz_sort_tokens(oz_handle_t h, void* stream, int64_t tokens, int64_t 
     return hipGetLastError() == hipSuccess ? OZ_OK : OZ_ERR_HIP;
 }
 
-oz_status_t oz_gather_rows(oz_handle_t h, void* stream, int64_t slots, int64_t cols, int32_t type, const void* X, int64_t ldx, int64_t x_rows,
-                           const int32_t* order, int64_t order_div, void* Y, int64_t ldy) {
+oz_status_t oz_gather_rows(oz_handle_t h, void* stream, int64_t tokens, int64_t topk, int64_t cols, int32_t type, const void* X, int64_t ldx,
+                           const int32_t* order, const int32_t* place, void* Y, int64_t ldy) {
     const int esize = elem_bytes(type);
-    if (!h || esize == 0 || !rows_ok(x_rows, cols, X, ldx, esize) || !rows_ok(slots, cols, Y, ldy, esize)) return OZ_ERR_ARG;
-    if (order_div < 1 || order_div > kMaxChoices || (slots > 0 && !order)) return OZ_ERR_ARG;
+    if (!h || esize == 0 || topk < 0 || topk > 64 || !rows_ok(tokens, cols, X, ldx, esize) || tokens * topk >= kMaxChoices) return OZ_ERR_ARG;
+    const int64_t slots = tokens * topk;
+    if (!rows_ok(slots, cols, Y, ldy, esize) || (slots > 0 && (!order || !place))) return OZ_ERR_ARG;
     if (slots == 0 || cols == 0) return OZ_OK;
-    if (slots * ((cols * esize + 4095) / 4096) > 4 * kMaxGrid) return OZ_ERR_ARG;
+    if (tokens * ((cols * esize + 4095) / 4096) > 4 * kMaxGrid) return OZ_ERR_ARG;
     if (!handle_on_device(h)) return OZ_ERR_DEVICE;
-    launch_gather_rows(static_cast<hipStream_t>(stream), int(slots), int(cols), esize, X, ldx, int(x_rows), order, int(order_div), Y, ldy);
+    launch_gather_rows(static_cast<hipStream_t>(stream), int(tokens), int(topk), int(cols), esize, X, ldx, order, place, Y, ldy);
     return hipGetLastError() == hipSuccess ? OZ_OK : OZ_ERR_HIP;
 }
 

@@ -77,15 +77,15 @@ template <typename T>
 __device__ __forceinline__ void put(T* p, float x) { *p = static_cast<T>(x); }
 
 // N consecutive elements as floats: one to N/4 16-byte loads where `vec` says that p is aligned for them and all are there, else one by one
-// with zeros from `have` on.
-template <int N, typename T>
+// with zeros from `have` on.  STREAM: read (written) once, past the caches.
+template <int N, bool STREAM = false, typename T>
 __device__ __forceinline__ void load_row(const T* __restrict__ p, int have, bool vec, float (&x)[N]) {
     if (vec && have >= N) {
         constexpr int kVec = N * int(sizeof(T)) / 16;
         static_assert(kVec * 16 == N * int(sizeof(T)), "whole 16-byte loads");
         union { v4i32 v[kVec]; T e[N]; } u;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) u.v[i] = reinterpret_cast<const v4i32*>(p)[i];
+        for (int i = 0; i < kVec; ++i) u.v[i] = STREAM ? __builtin_nontemporal_load(reinterpret_cast<const v4i32*>(p) + i) : reinterpret_cast<const v4i32*>(p)[i];
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = to_float(u.e[i]);
     } else {
@@ -94,7 +94,7 @@ __device__ __forceinline__ void load_row(const T* __restrict__ p, int have, bool
     }
 }
 
-template <int N, typename T>
+template <int N, bool STREAM = false, typename T>
 __device__ __forceinline__ void store_row(T* __restrict__ p, int have, bool vec, const float (&x)[N]) {
     if (vec && have >= N) {
         constexpr int kVec = N * int(sizeof(T)) / 16;
@@ -102,7 +102,10 @@ __device__ __forceinline__ void store_row(T* __restrict__ p, int have, bool vec,
 #pragma unroll
         for (int i = 0; i < N; ++i) put(&u.e[i], x[i]);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) reinterpret_cast<v4i32*>(p)[i] = u.v[i];
+        for (int i = 0; i < kVec; ++i) {
+            if constexpr (STREAM) __builtin_nontemporal_store(u.v[i], reinterpret_cast<v4i32*>(p) + i);
+            else reinterpret_cast<v4i32*>(p)[i] = u.v[i];
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)

@@ -59,8 +59,8 @@ def gather(h: g.Handle, x, routing: Routing, out=None):
     ldy = check_matrix(y, "out")
     if tuple(y.shape) != (slots, x.shape[1]) or y.dtype != x.dtype:
         raise ValueError("out: %d x %d of %s" % (slots, x.shape[1], x.dtype))
-    h.call("oz_gather_rows", stream_of(x), slots, x.shape[1], float_type(x.dtype), x.data_ptr(), ldx, x.shape[0], routing.order.data_ptr(),
-           routing.topk, y.data_ptr(), ldy)
+    h.call("oz_gather_rows", stream_of(x), routing.tokens, routing.topk, x.shape[1], float_type(x.dtype), x.data_ptr(), ldx,
+           routing.order.data_ptr(), routing.place.data_ptr(), y.data_ptr(), ldy)
     return y
 
 

@@ -124,7 +124,7 @@ def load_library() -> C.CDLL:
                        ("oz_scaled_gemm_grouped", [L, P, L, L, L, S, S, P, L, I]),
                        ("oz_scaled_gemm_grouped_k", [L, P, L, L, L, S, S, P, L, L, I, I]),
                        ("oz_sort_tokens", [L, L, L, P, I, P, P, P, P, C.c_size_t]),
-                       ("oz_gather_rows", [L, L, I, P, L, L, P, L, P, L]),
+                       ("oz_gather_rows", [L, L, L, I, P, L, P, P, P, L]),
                        ("oz_combine_rows", [L, L, L, I, P, L, L, P, P, P, L]),
                        ("oz_combine_rows_grad", [L, L, L, I, P, L, P, L, L, P, P, P, P, L, P])):
         getattr(lib, name).argtypes = [H, C.c_void_p] + args
