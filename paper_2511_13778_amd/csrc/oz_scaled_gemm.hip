@@ -3,16 +3,15 @@
 // A step is a block of 128 of k.  Its rows of A and B (128 bytes each) go from L2 straight into LDS, STAGES - 1 steps ahead;
 // one barrier per step.  A row's eight 16-byte pieces are stored at piece ^ (row & 7), so that the 16 lanes that read the same
 // piece of 16 rows meet different banks.  The scales come in the same way, four blocks at a time, into two buffers of their own.
-#include <algorithm>
-
 #include "oz_scaled_gemm_device.h"
+#include "oz_scaled_plan.h"
 
 namespace oz {
 
 namespace {
 
 template <int BM, int BN, int WM, int WN, int STAGES, bool A_E5M2, bool E8M0, bool WIDE>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel(ScaledGemm g, int tiles_n) {
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel(ScaledGemm g, int tiles_m, int tiles_n) {
     constexpr int WAVES = (BM / WM) * (BN / WN), ROWS = BM + BN;
     constexpr int COPIES = (ROWS / 8 + WAVES - 1) / WAVES;        // 1 KB each, per wave and step
     static_assert(ROWS / 8 % WAVES == 0 && BM % 64 == 0 && BN % 64 == 0, "whole transfers");
@@ -22,7 +21,8 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
     constexpr int MT = WM / 16, NT = WN / 16;
     __shared__ __align__(16) uint8_t lds[STAGES * STAGE_BYTES + 2 * SCALE_BYTES];
 
-    const GemmTile t = locate<BM, BN>(g, int(blockIdx.x) / tiles_n, int(blockIdx.x) % tiles_n, int(blockIdx.y));
+    const TilePlace place = tile_place(tiles_m, tiles_n);
+    const GemmTile t = locate<BM, BN>(g, place.m, place.n, int(blockIdx.y));
     if (t.none) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % (BM / WM) * WM, wn = wave / (BM / WM) * WN;
@@ -209,60 +209,24 @@ void launch_tiles(hipStream_t st, const ScaledGemm& g) {
     const dim3 grid(unsigned(tiles_m * tiles_n), g.grouping == Grouping::kContraction ? unsigned(g.groups) : unsigned(g.parts));
     const dim3 block(64 * (BM / WM) * (BN / WN));
     const int kind = (g.a_e5m2 ? 4 : 0) + (g.e8m0 ? 2 : 0) + (g.wide ? 1 : 0);
-#define OZ_KIND(K) case K: hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, (K & 4) != 0, (K & 2) != 0, (K & 1) != 0>), grid, block, 0, st, g, tiles_n); break;
+#define OZ_KIND(K) case K: hipLaunchKernelGGL((scaled_gemm_kernel<BM, BN, WM, WN, STAGES, (K & 4) != 0, (K & 2) != 0, (K & 1) != 0>), grid, block, 0, st, g, int(tiles_m), tiles_n); break;
     switch (kind) { OZ_KIND(0) OZ_KIND(1) OZ_KIND(2) OZ_KIND(3) OZ_KIND(4) OZ_KIND(5) OZ_KIND(6) OZ_KIND(7) }
 #undef OZ_KIND
 }
 
 
-// How a product without groups is computed, by its sizes alone.
-enum class Route { kFew, kTiles64, kTiles128, kTall, kBig };
-struct Plan {
-    Route route;
-    int parts;         // of k
-    int waves;         // kFew
-};
-
-inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-Plan plan_of(int64_t m, int64_t n, int64_t k, int64_t groups, int num_cu) {
-    const int64_t blocks = up(k, kScaleBlock);
-    if (m <= 64) {
-        const int64_t strips = up(n, 16), fours = up(blocks, 4);
-        int64_t parts = std::min<int64_t>(num_cu / std::max<int64_t>(strips, 1), fours / 8);
-        parts = std::max<int64_t>(1, std::min<int64_t>(parts, 16));
-        const int64_t each = up(fours, parts);
-        return Plan{Route::kFew, int(parts), each <= 4 ? 4 : each <= 8 ? 8 : 16};
-    }
-    if (up(m, 256) * up(n, 256) * groups >= num_cu * 3 / 4) return Plan{Route::kBig, 1, 0};
-    if (up(m, 256) * up(n, 128) * groups >= num_cu * 3 / 4) return Plan{Route::kTall, 1, 0};
-    if (up(m, 128) * up(n, 128) * groups >= num_cu) return Plan{Route::kTiles128, 1, 0};
-    const int64_t tiles = up(m, 64) * up(n, 64) * groups;
-    int64_t parts = 1;
-    if (tiles * 4 <= num_cu * 3) parts = std::max<int64_t>(1, std::min<int64_t>({2 * num_cu / tiles, blocks / 4, 16}));
-    return Plan{Route::kTiles64, int(parts), 0};
-}
-
 }  // namespace
 
 size_t scaled_gemm_part_bytes(int64_t m, int64_t n, int64_t k, int num_cu) {
     if (m == 0 || n == 0 || k == 0) return 0;
-    const Plan p = plan_of(m, n, k, 1, num_cu);
+    const ScaledPlan p = cut_plan(m, n, k, num_cu);
     return p.parts > 1 ? size_t(p.parts) * size_t(m) * size_t(n) * 4 : 0;
 }
 
 void launch_scaled_gemm(hipStream_t st, const ScaledGemm& call, int num_cu, float* planes) {
     ScaledGemm g = call;
-    // rows that read an operand B together, on average
-    const int64_t rows = g.grouping == Grouping::kRows ? up(g.m, g.groups) : g.m;
-    const bool by_k = g.grouping == Grouping::kContraction;
-    Plan p = plan_of(g.grouping == Grouping::kRows && rows > 64 ? g.m : by_k ? std::max<int64_t>(rows, 65) : rows, g.n, g.k, by_k ? g.groups : 1, num_cu);
-    if (g.grouping != Grouping::kNone) {
-        // groups of fewer rows than a tall tile leave most of it empty
-        if (!by_k && rows < 192 && (p.route == Route::kBig || p.route == Route::kTall)) p.route = Route::kTiles128;
-        p.parts = 1;
-        if (p.route == Route::kFew) p.waves = up(g.k, 512) <= 4 ? 4 : up(g.k, 512) <= 8 ? 8 : 16;
-    }
+    const bool by_rows = g.grouping == Grouping::kRows, by_k = g.grouping == Grouping::kContraction;
+    const ScaledPlan p = scaled_plan((g.wide ? 2 : 0) + (g.e8m0 ? 0 : 1), g.m, g.n, g.k, g.groups, by_rows, by_k, num_cu);
     if (p.parts > 1) {
         g.parts = p.parts;
         g.c = planes;
@@ -271,16 +235,16 @@ void launch_scaled_gemm(hipStream_t st, const ScaledGemm& call, int num_cu, floa
         g.accumulate = 0;
     }
     switch (p.route) {
-        case Route::kFew: launch_scaled_gemm_few(st, g, int(rows), p.waves); break;
-        case Route::kTiles64: launch_tiles<64, 64, 32, 32, 4>(st, g); break;
-        case Route::kTiles128: launch_tiles<128, 128, 64, 64, 2>(st, g); break;
-        default:
-            if (g.wide) launch_tiles<128, 128, 64, 64, 2>(st, g);
-            else launch_scaled_gemm_big(st, g, p.route == Route::kBig);
+        case ScaledRoute::kFew: launch_scaled_gemm_few(st, g, by_rows ? int(div_up(g.m, g.groups)) : g.m, p.waves); break;
+        case ScaledRoute::kTiles64: launch_tiles<64, 64, 32, 32, 2>(st, g); break;
+        case ScaledRoute::kTiles64Deep: launch_tiles<64, 64, 32, 32, 4>(st, g); break;
+        case ScaledRoute::kTiles128: launch_tiles<128, 128, 64, 64, 2>(st, g); break;
+        case ScaledRoute::kTall: launch_scaled_gemm_big(st, g, false); break;
+        case ScaledRoute::kBig: launch_scaled_gemm_big(st, g, true); break;
     }
     if (p.parts > 1) {
-        const int quads = int(up(g.n, 4));
-        hipLaunchKernelGGL(add_planes_kernel, dim3(unsigned(up(int64_t(g.m) * quads, 256))), dim3(256), 0, st, call, planes, p.parts, quads);
+        const int quads = int(div_up(g.n, 4));
+        hipLaunchKernelGGL(add_planes_kernel, dim3(unsigned(div_up(int64_t(g.m) * quads, 256))), dim3(256), 0, st, call, planes, p.parts, quads);
     }
 }
 

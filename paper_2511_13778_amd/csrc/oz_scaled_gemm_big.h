@@ -43,16 +43,8 @@ __global__ __launch_bounds__(256, 1) void scaled_gemm_big_kernel(ScaledGemm g, i
     using P = Big<NB, SC>;
     constexpr bool kVector = SC != Scales::kE8M0;                         // sums are the vector ALU's
     extern __shared__ __align__(16) uint8_t lds[];
-    // Workgroups are dealt to the XCDs in turn: an XCD gets a contiguous run of tiles, in blocks of 8 rows of tiles
-    int id = int(blockIdx.x);
-    {
-        const int total = tiles_m * tiles_n, per = total / 8, extra = total % 8, xcd = id & 7, slot = id >> 3;
-        id = xcd * per + min(xcd, extra) + slot;
-    }
-    constexpr int kBand = 8;
-    const int band = id / (kBand * tiles_n), in_band = id - band * kBand * tiles_n;
-    const int high = min(kBand, tiles_m - band * kBand);
-    const GemmTile t = locate<kTM, P::kTN>(g, band * kBand + in_band % high, in_band / high, int(blockIdx.y));
+    const TilePlace place = tile_place(tiles_m, tiles_n);
+    const GemmTile t = locate<kTM, P::kTN>(g, place.m, place.n, int(blockIdx.y));
     if (t.none) return;
     if (t.k == 0) {
         store_nothing(g, t);

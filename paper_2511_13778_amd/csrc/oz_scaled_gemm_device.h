@@ -94,6 +94,17 @@ struct GemmTile {
     bool none;
 };
 
+// Which tile a workgroup takes.  Workgroups are dealt to the XCDs in turn: an XCD gets a contiguous run of tiles, in bands of eight rows of
+// tiles, so that those it has at a time share their operands in its L2.
+struct TilePlace { int m, n; };
+__device__ __forceinline__ TilePlace tile_place(int tiles_m, int tiles_n) {
+    constexpr int kBand = 8;
+    const int total = tiles_m * tiles_n, per = total / 8, extra = total % 8, xcd = int(blockIdx.x) & 7;
+    const int id = xcd * per + min(xcd, extra) + (int(blockIdx.x) >> 3);
+    const int band = id / (kBand * tiles_n), in_band = id - band * kBand * tiles_n, high = min(kBand, tiles_m - band * kBand);
+    return TilePlace{band * kBand + in_band % high, in_band / high};
+}
+
 // Rows `row` on of group `group`; TM rows, TN columns of C per tile.
 template <int TM, int TN>
 __device__ __forceinline__ GemmTile locate(const ScaledGemm& g, int tile_m, int tile_n, int group) {
