@@ -48,7 +48,7 @@ struct QuantizeCall {
 };
 
 void launch_scaled_gemm(hipStream_t st, const ScaledGemm& g, int num_cu, float* planes);
-void launch_scaled_gemm_big(hipStream_t st, const ScaledGemm& g, bool wide);       // wide: tiles of 256 x 256, else 256 x 128
+void launch_scaled_gemm_big(hipStream_t st, const ScaledGemm& g, bool square);     // tiles of 256 x 256, else 256 x 128
 void launch_scaled_gemm_big_f32(hipStream_t st, const ScaledGemm& g);
 bool prepare_scaled_gemm_f32();
 void launch_scaled_gemm_few(hipStream_t st, const ScaledGemm& g, int rows, int waves);

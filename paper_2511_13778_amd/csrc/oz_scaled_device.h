@@ -19,6 +19,18 @@ struct GroupPiece {
 
 __device__ __forceinline__ int clamp_offset(const int32_t* offsets, int g, int rows) { return min(max(offsets[g], 0), rows); }
 
+// How many pieces there are.
+template <int SIZE>
+__device__ __forceinline__ int count_pieces(const int32_t* __restrict__ offsets, int groups, int rows) {
+    int sum = 0;
+    for (int g = threadIdx.x & 63; g <= groups; g += 64) {
+        const int lo = clamp_offset(offsets, g, rows), hi = g < groups ? max(lo, clamp_offset(offsets, g + 1, rows)) : rows;
+        sum += (hi - lo + SIZE - 1) / SIZE;
+    }
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    return __builtin_amdgcn_readfirstlane(sum);
+}
+
 template <int SIZE>
 __device__ __forceinline__ GroupPiece find_piece(const int32_t* __restrict__ offsets, int groups, int rows, int t) {
     const int lane = threadIdx.x & 63;

@@ -21,7 +21,8 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
     constexpr int MT = WM / 16, NT = WN / 16;
     __shared__ __align__(16) uint8_t lds[STAGES * STAGE_BYTES + 2 * SCALE_BYTES];
 
-    const TilePlace place = tile_place(tiles_m, tiles_n);
+    const TilePlace place = tile_place<BM>(g, tiles_m, tiles_n);
+    if (place.n < 0) return;
     const GemmTile t = locate<BM, BN>(g, place.m, place.n, int(blockIdx.y));
     if (t.none) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
                         for (int j = 0; j < NT; ++j)
 #pragma unroll
                             for (int i = 0; i < MT; ++i)
-                                acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j].part[w], wa[i].part[w], acc[j][i], 0, 0, 0);
+                                acc[j][i] = mfma_bf16(wb[j].part[w], wa[i].part[w], acc[j][i]);
                 } else {
 #pragma unroll
                     for (int j = 0; j < NT; ++j)
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
                         for (int w = 0; w < 4; ++w)
 #pragma unroll
                             for (int i = 0; i < MT; ++i)
-                                p[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j].part[w], wa[i].part[w], w == 0 ? v4f{0, 0, 0, 0} : p[i], 0, 0, 0);
+                                p[i] = mfma_bf16(wb[j].part[w], wa[i].part[w], w == 0 ? v4f{0, 0, 0, 0} : p[i]);
                     } else {
 #pragma unroll
                         for (int i = 0; i < MT; ++i) p[i] = mfma_plain<A_E5M2>(fb[j], fa[i]);

@@ -5,9 +5,9 @@ namespace oz {
 
 bool prepare_scaled_gemm() { return prepare<4, Scales::kE8M0>() && prepare<2, Scales::kE8M0>() && prepare_scaled_gemm_f32(); }
 
-void launch_scaled_gemm_big(hipStream_t st, const ScaledGemm& g, bool wide) {
+void launch_scaled_gemm_big(hipStream_t st, const ScaledGemm& g, bool square) {
     if (!g.e8m0) launch_scaled_gemm_big_f32(st, g);
-    else if (wide) launch<4, Scales::kE8M0>(st, g);
+    else if (square) launch<4, Scales::kE8M0>(st, g);
     else launch<2, Scales::kE8M0>(st, g);
 }
 

@@ -50,33 +50,39 @@ __device__ __forceinline__ v4f mfma_plain(v8i32 b, v8i32 a) {
 // whose sums keep 32 bits (8e-9 on the same data) at half the rate.  A fragment's 32 bytes per lane make four operands.
 typedef bf16_t v8bf __attribute__((ext_vector_type(8)));
 typedef bf16_t v2bf __attribute__((ext_vector_type(2)));
+// four bytes: two pairs
 template <bool E5M2>
-__device__ __forceinline__ v8bf widen(uint32_t lo, uint32_t hi, float scale) {
-    union { v8bf v; v2bf p[4]; } u;
+__device__ __forceinline__ void widen4(uint32_t x, float scale, int& lo, int& hi) {
+    v2bf p, q;
     if constexpr (E5M2) {
-        u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, false);
-        u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, true);
-        u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, false);
-        u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, true);
+        p = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(x, scale, false);
+        q = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(x, scale, true);
     } else {
-        u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
-        u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-        u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
-        u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+        p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false);
+        q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true);
     }
-    return u.v;
+    lo = __builtin_bit_cast(int, p);
+    hi = __builtin_bit_cast(int, q);
 }
-struct Wide { v8bf part[4]; };
+struct Wide { v4i32 part[4]; };         // pairs of bfloat16
 template <bool E5M2>
 __device__ __forceinline__ Wide widen(const v8i32& f, float scale) {
     Wide w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w.part[i] = widen<E5M2>(uint32_t(f[2 * i]), uint32_t(f[2 * i + 1]), scale);
+    for (int i = 0; i < 8; ++i) {
+        int lo, hi;
+        widen4<E5M2>(uint32_t(f[i]), scale, lo, hi);
+        w.part[i >> 1][2 * (i & 1)] = lo;
+        w.part[i >> 1][2 * (i & 1) + 1] = hi;
+    }
     return w;
+}
+__device__ __forceinline__ v4f mfma_bf16(const v4i32& b, const v4i32& a, v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, b), __builtin_bit_cast(v8bf, a), c, 0, 0, 0);
 }
 __device__ __forceinline__ v4f mfma_wide(const Wide& b, const Wide& a, v4f c) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.part[i], a.part[i], c, 0, 0, 0);
+    for (int i = 0; i < 4; ++i) c = mfma_bf16(b.part[i], a.part[i], c);
     return c;
 }
 // An E8M0 scale as the conversion takes it: a float of that exponent.
@@ -95,12 +101,16 @@ struct GemmTile {
 };
 
 // Which tile a workgroup takes.  Workgroups are dealt to the XCDs in turn: an XCD gets a contiguous run of tiles, in bands of eight rows of
-// tiles, so that those it has at a time share their operands in its L2.
-struct TilePlace { int m, n; };
-__device__ __forceinline__ TilePlace tile_place(int tiles_m, int tiles_n) {
+// tiles, so that those it has at a time share their operands in its L2.  Rows in groups: of the tiles that there are, fewer than the
+// launch has workgroups for (8192 rows in 8 groups, the runs counted by the launch 68 us, by the tiles 54: the last XCDs were idle).
+struct TilePlace { int m, n; };      // n < 0: none
+template <int TM>
+__device__ __forceinline__ TilePlace tile_place(const ScaledGemm& g, int tiles_m, int tiles_n) {
     constexpr int kBand = 8;
-    const int total = tiles_m * tiles_n, per = total / 8, extra = total % 8, xcd = int(blockIdx.x) & 7;
-    const int id = xcd * per + min(xcd, extra) + (int(blockIdx.x) >> 3);
+    if (g.grouping == Grouping::kRows) tiles_m = count_pieces<TM>(g.offsets, g.groups, g.m);
+    const int total = tiles_m * tiles_n, per = total / 8, extra = total % 8, xcd = int(blockIdx.x) & 7, slot = int(blockIdx.x) >> 3;
+    if (slot >= per + (xcd < extra ? 1 : 0)) return TilePlace{0, -1};
+    const int id = xcd * per + min(xcd, extra) + slot;
     const int band = id / (kBand * tiles_n), in_band = id - band * kBand * tiles_n, high = min(kBand, tiles_m - band * kBand);
     return TilePlace{band * kBand + in_band % high, in_band / high};
 }

@@ -1,8 +1,8 @@
 // Which kernel computes a product of 8-bit block-scaled matrices, by sizes and types alone; host code.
 //
-// Time of a route, in us:  3 + steps * max(alone, per * c) + each * c,  c = tiles / compute units, rounded up: a step of 128 of k takes
-// `per` for each of a CU's tiles (its matrix unit and LDS are shared), but no less than a lone tile takes, and a tile's first loads and its
-// results cost `each`.  The constants are fits to times measured over 19 sizes from 256 x 1000 x 1000 to 8192^3 (within 10 % where a
+// Time of a route, in us:  3 + steps * (rounds of a full CU, and what is left) + each * c,  c = tiles / compute units, rounded up: a step of
+// 128 of k takes `per` for each of the tiles that a CU has at a time (its matrix unit and LDS are shared), but no less than a lone
+// tile takes, and a tile's first loads and its results cost `each`.  The constants are fits to times measured over 19 sizes from 256 x 1000 x 1000 to 8192^3 (within 10 % where a
 // route is the best one).  Tiles of 256 x 256 need the fewest bytes per operation and win on large outputs (8192^3 402 us, 256 x 128 462,
 // 128 x 128 556), those of 128 x 128 and 64 x 64, several to a CU, overlap one's results with another's products and win on
 // short k and where larger ones leave CUs idle (8192 x 8192 x 512 56 us, 256 x 256 62; 1024^3 6.2 us in 64 x 64, 9.6 in 128 x 128).
@@ -39,10 +39,13 @@ inline double route_time(int kind, int route, int64_t m, int64_t n, int64_t bloc
     static const int rows[5] = {64, 64, 128, 256, 256}, cols[5] = {64, 64, 128, 128, 256};
     const RouteCost& c = kRouteCost[kind][route];
     if (c.per == 0) return 1e30;
-    // groups end inside a tile: half a tile each, on average
-    const double tiles_m = groups > 1 ? std::min(double(m) / rows[route] + 0.5 * double(groups), double(m)) : double(div_up(m, rows[route]));
+    // groups end inside a tile, and are not equally large: a tile more for each (16384 rows in 16 uneven groups, float32 scales: 256 x 128 tiles
+    // 231 us and 234 by this count, 128 x 128 220 and 221)
+    const double tiles_m = groups > 1 ? std::min(double(m) / rows[route] + double(groups), double(m)) : double(div_up(m, rows[route]));
     const double per_cu = double(div_up(int64_t(tiles_m * double(div_up(n, cols[route])) * double(repeats) + 0.5), num_cu));
-    return 3.0 + double(blocks) * std::max(c.alone, c.per * per_cu) + c.each * per_cu;
+    static const int together[5] = {4, 2, 2, 1, 1};
+    const double full = double(int64_t(per_cu) / together[route] * together[route]), left = per_cu - full;
+    return 3.0 + double(blocks) * (full * c.per + (left > 0 ? std::max(c.alone, left * c.per) : 0.0)) + c.each * per_cu;
 }
 
 // Rows of A that share a read of B, on average, up to which that read is what counts.
