@@ -14,6 +14,7 @@ from __future__ import annotations
 import torch
 
 from . import ozdgemm as g
+from . import scaled
 from .scaled import check_ints, check_matrix, float_type, stream_of
 
 
@@ -97,3 +98,57 @@ def combine_backward(h: g.Handle, dy, xs, routing: Routing, weights):
            xs.data_ptr(), ldx, xs.shape[0], routing.order.data_ptr(), routing.place.data_ptr(), _weights(weights, routing), dxs.data_ptr(),
            max(dxs.shape[1], 1), dw.data_ptr())
     return dxs, dw
+
+
+class ExpertLayer:
+    """Experts of two linear layers with silu between them, y = sum_j w_j W2_e silu(W1_e x) over a token's choices e: an example of the calls
+    above as a training step and a serving step make them.
+
+    w1 (experts x inner x width) and w2 (experts x width x inner) are the caller's, in any float type; prepare_weights() makes their 8-bit
+    copies, for the forward products and, transposed, for the input gradients, and is called again when they have changed.  Only silu
+    and its derivative are torch's."""
+
+    def __init__(self, h: g.Handle, w1, w2, scale_dtype=torch.uint8):
+        if w1.dim() != 3 or w2.shape != (w1.shape[0], w1.shape[2], w1.shape[1]):
+            raise ValueError("w1 experts x inner x width and w2 experts x width x inner, not %s and %s" % (tuple(w1.shape), tuple(w2.shape)))
+        self.h, self.w1, self.w2, self.scale_dtype, self.experts = h, w1, w2, scale_dtype, w1.shape[0]
+        self.prepare_weights()
+
+    def prepare_weights(self):
+        self.q1, self.q1t = scaled.quantize(self.h, self.w1, scale_dtype=self.scale_dtype, block_rows=128, which="both")
+        self.q2, self.q2t = scaled.quantize(self.h, self.w2, scale_dtype=self.scale_dtype, block_rows=128, which="both")
+
+    def serve(self, x, ids, weights):
+        """y for tokens x (tokens x width) without anything kept for gradients."""
+        h = self.h
+        routing = sort_tokens(h, ids, self.experts)
+        a = scaled.quantize(h, x, scale_dtype=self.scale_dtype, routing=routing)
+        inner = torch.nn.functional.silu(scaled.gemm_grouped(h, a, self.q1, routing.offsets, dtype=x.dtype))
+        out = scaled.gemm_grouped(h, scaled.quantize(h, inner, scale_dtype=self.scale_dtype), self.q2, routing.offsets, dtype=x.dtype)
+        return combine(h, out, routing, weights)
+
+    def forward(self, x, ids, weights):
+        """(y, what backward needs)."""
+        h, sc = self.h, self.scale_dtype
+        routing = sort_tokens(h, ids, self.experts)
+        xs = gather(h, x, routing)
+        a, at = scaled.quantize(h, xs, scale_dtype=sc, which="both", offsets=routing.offsets)
+        pre = scaled.gemm_grouped(h, a, self.q1, routing.offsets, dtype=x.dtype)
+        b, bt = scaled.quantize(h, torch.nn.functional.silu(pre), scale_dtype=sc, which="both", offsets=routing.offsets)
+        out = scaled.gemm_grouped(h, b, self.q2, routing.offsets, dtype=x.dtype)
+        return combine(h, out, routing, weights), (routing, weights, at, pre, bt, out)
+
+    def backward(self, dy, kept, dw1=None, dw2=None):
+        """(dx, dweights, dw1, dw2) of forward; the weights' gradients in float32, added to dw1 and dw2 where they are given."""
+        h, sc = self.h, self.scale_dtype
+        routing, weights, at, pre, bt, out = kept
+        offsets = routing.offsets
+        dout, dweights = combine_backward(h, dy, out, routing, weights)
+        d, dt = scaled.quantize(h, dout, dtype=torch.float8_e5m2, scale_dtype=sc, which="both", offsets=offsets)
+        dw2 = scaled.gemm_grouped_k(h, dt, bt, offsets, out=dw2, accumulate=dw2 is not None)
+        dinner = scaled.gemm_grouped(h, d, self.q2t, offsets, dtype=dy.dtype)
+        dpre = torch.ops.aten.silu_backward(dinner, pre)
+        d, dt = scaled.quantize(h, dpre, dtype=torch.float8_e5m2, scale_dtype=sc, which="both", offsets=offsets)
+        dw1 = scaled.gemm_grouped_k(h, dt, at, offsets, out=dw1, accumulate=dw1 is not None)
+        dx = combine(h, scaled.gemm_grouped(h, d, self.q1t, offsets, dtype=dy.dtype), routing)
+        return dx, dweights, dw1, dw2
