@@ -47,7 +47,9 @@ def sort_tokens(h: g.Handle, ids, experts: int) -> Routing:
     base = all_.data_ptr()
     h.call("oz_sort_tokens", stream_of(ids), tokens, topk, experts, ids.data_ptr(), ids.element_size(), base, base + 4 * at[1], base + 4 * at[2],
            base + 4 * ws_at if need else None, need)
-    return Routing(all_[:experts + 1], all_[at[1]:at[2]], all_[at[2]:at[2] + n].view(tokens, topk), topk)
+    r = Routing.__new__(Routing)            # right by construction
+    r.offsets, r.order, r.place, r.topk, r.tokens = all_[:experts + 1], all_[at[1]:at[2]], all_[at[2]:at[2] + n].view(tokens, topk), topk, tokens
+    return r
 
 
 def gather(h: g.Handle, x, routing: Routing, out=None):
