@@ -74,7 +74,7 @@ struct RowArgs {
     ScaledOperand out;
     const int32_t* order;
     int order_div, x_rows, rows, cols, nblk;
-    bool e8m0, vec;
+    bool e8m0;
 };
 
 // A block of 128 per 16 lanes, 8 values a lane: maximum by shuffles, no LDS.  grid (blocks of the matrix / 16, batch)
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(RowArgs p) {
     const int64_t src = source_row(p.order, p.order_div, p.x_rows, r);
     float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (src >= 0)
-        load_row<8>(static_cast<const T*>(p.x) + int64_t(blockIdx.y) * p.stride_x + src * p.ldx + col, p.cols - col, p.vec, x);
+        load_row<8>(static_cast<const T*>(p.x) + int64_t(blockIdx.y) * p.stride_x + src * p.ldx + col, p.cols - col, x);
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
@@ -112,7 +112,7 @@ struct TileArgs {
     int order_div, x_rows, rows, cols;
     const int32_t* offsets;
     int groups;
-    bool rows_e8m0, cols_e8m0, vec;
+    bool rows_e8m0, cols_e8m0;
 };
 
 // A tile of 128 x 128: rows, columns or the whole share a scale; written as it is and transposed from one read.
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
     for (int i = 0; i < 8; ++i) {
         const int r = row0 + g * 8 + i;
         const int64_t src = r < end ? source_row(p.order, p.order_div, p.x_rows, r) : -1;
-        if (src >= 0) load_row<8>(x0 + src * p.ldx + col, p.cols - col, p.vec, x[i]);
+        if (src >= 0) load_row<8>(x0 + src * p.ldx + col, p.cols - col, x[i]);
         else
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[i][j] = 0.0f;
@@ -252,16 +252,15 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
 template <typename T>
 void quantize_typed(hipStream_t st, const QuantizeCall& q) {
     const int nblk = (q.cols + kScaleBlock - 1) / kScaleBlock;
-    const bool vec = reinterpret_cast<uintptr_t>(q.x) % 16 == 0 && q.ldx * int64_t(sizeof(T)) % 16 == 0 && q.stride_x * int64_t(sizeof(T)) % 16 == 0;
     if (!q.tiles && !q.out_cols.data) {
-        const RowArgs p{q.x, q.ldx, q.stride_x, q.out_rows, q.order, q.order_div, q.x_rows, q.rows, q.cols, nblk, q.rows_e8m0, vec};
+        const RowArgs p{q.x, q.ldx, q.stride_x, q.out_rows, q.order, q.order_div, q.x_rows, q.rows, q.cols, nblk, q.rows_e8m0};
         const dim3 grid(unsigned((int64_t(q.rows) * nblk + 15) / 16), unsigned(q.batch));
         if (q.rows_e5m2) hipLaunchKernelGGL((quantize_rows_kernel<T, true>), grid, dim3(256), 0, st, p);
         else hipLaunchKernelGGL((quantize_rows_kernel<T, false>), grid, dim3(256), 0, st, p);
         return;
     }
     const TileArgs p{q.x, q.ldx, q.stride_x, q.out_rows, q.out_cols, q.order, q.order_div, q.x_rows, q.rows, q.cols, q.offsets, q.groups,
-                     q.rows_e8m0, q.cols_e8m0, vec};
+                     q.rows_e8m0, q.cols_e8m0};
     const int64_t tiles = q.offsets ? group_pieces(q.rows, q.groups, kScaleBlock) : (q.rows + kScaleBlock - 1) / kScaleBlock;
     const dim3 grid{unsigned(tiles), unsigned(nblk), unsigned(q.batch)};
     const int kind = (q.tiles ? 4 : 0) + (q.rows_e5m2 ? 2 : 0) + (q.cols_e5m2 ? 1 : 0);

@@ -204,7 +204,8 @@ struct GatherArgs {
 
 // A wave per 4 KB of a token's row, which it reads once and writes for each choice: from the slots' side every choice would read it again,
 // long after it has left L2 (65536 slots of 4 KB 76 us that way, 61 this).  Few tokens have a wave per choice (33 tokens with 8
-// choices 2.7 us, 5 with one wave for all).  grid.y: choices / per.  T: the widest type that every row's address and length is a multiple of.
+// choices 2.7 us, 5 with one wave for all).  grid.y: choices / per.  T: 16 bytes, at any element's address, or an element where a row is shorter; a row's last 16 bytes may
+// overlap those before them, which carry the same there.
 template <typename T>
 __global__ __launch_bounds__(256) void gather_rows_kernel(GatherArgs p) {
     const uint32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -215,24 +216,26 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(GatherArgs p) {
     constexpr int kStep = 64 * int(sizeof(T));
     for (int at = from + lane * int(sizeof(T)); at < to; at += kStep * kUnitVecs) {
         T v[kUnitVecs];
+        int pos[kUnitVecs];
 #pragma unroll
         for (int u = 0; u < kUnitVecs; ++u) {
+            pos[u] = min(at + u * kStep, p.row_bytes - int(sizeof(T)));
             v[u] = T{};
-            if (at + u * kStep < to) v[u] = *reinterpret_cast<const T*>(x + at + u * kStep);
+            if (at + u * kStep < to) v[u] = *reinterpret_cast<const T*>(x + pos[u]);
         }
         for (int j = int(blockIdx.y) * p.per; j < min((int(blockIdx.y) + 1) * p.per, p.topk); ++j) {
             const int c = t * p.topk + j, s = p.place[c];
             if (s >= 0 && s < slots) {
-                uint8_t* y = p.y + int64_t(s) * p.ldy + at;
+                uint8_t* y = p.y + int64_t(s) * p.ldy;
 #pragma unroll
                 for (int u = 0; u < kUnitVecs; ++u)
-                    if (at + u * kStep < to) __builtin_nontemporal_store(v[u], reinterpret_cast<T*>(y + u * kStep));
+                    if (at + u * kStep < to) __builtin_nontemporal_store(v[u], reinterpret_cast<T*>(y + pos[u]));
             }
             if (p.order[c] < 0) {         // slot c belongs to no choice
-                uint8_t* y = p.y + int64_t(c) * p.ldy + at;
+                uint8_t* y = p.y + int64_t(c) * p.ldy;
 #pragma unroll
                 for (int u = 0; u < kUnitVecs; ++u)
-                    if (at + u * kStep < to) *reinterpret_cast<T*>(y + u * kStep) = T{};
+                    if (at + u * kStep < to) *reinterpret_cast<T*>(y + pos[u]) = T{};
             }
         }
     }
@@ -246,9 +249,7 @@ struct CombineArgs {
     const float* weights;
     float* dweights;
     int tokens, topk, cols, slots, pieces;
-    bool vec;
 };
-
 
 // A wave per 512 columns of a token; the choices' rows four at a time.
 template <typename T>
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs p) {
             const int s = j0 + u < p.topk ? p.place[c] : -1;
             live[u] = s >= 0 && s < p.slots;
             w[u] = live[u] && p.weights ? p.weights[c] : 1.0f;
-            if (live[u]) load_row<8, true>(x + int64_t(s) * p.ldx + col, have, p.vec, v[u]);
+            if (live[u]) load_row<8, true>(x + int64_t(s) * p.ldx + col, have, v[u]);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -276,7 +277,7 @@ __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs p) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[u], v[u][i], sum[i]);
     }
-    store_row<8>(static_cast<T*>(p.y) + int64_t(t) * p.ldy + col, have, p.vec, sum);
+    store_row<8>(static_cast<T*>(p.y) + int64_t(t) * p.ldy + col, have, sum);
 }
 
 // A wave per choice: the choices of a token lie in one workgroup and find its dY in the cache.
@@ -299,8 +300,8 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs p) {
             for (int u = 0; u < 2; ++u) {
                 const int at = col + u * 512;
                 if (at < p.cols) {
-                    load_row<8>(dy + at, p.cols - at, p.vec, g[u]);
-                    if (p.dweights) load_row<8, true>(x + at, p.cols - at, p.vec, v[u]);
+                    load_row<8>(dy + at, p.cols - at, g[u]);
+                    if (p.dweights) load_row<8, true>(x + at, p.cols - at, v[u]);
                 }
             }
 #pragma unroll
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs p) {
                         if (p.dweights) dot = fmaf(g[u][i], v[u][i], dot);
                         out[i] = w * g[u][i];
                     }
-                    store_row<8, true>(dx + at, p.cols - at, p.vec, out);
+                    store_row<8, true>(dx + at, p.cols - at, out);
                 }
             }
         }
@@ -323,18 +324,12 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs p) {
     if (p.order[c] < 0) {                 // slot c belongs to no choice
         const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         T* row = static_cast<T*>(p.dx) + int64_t(c) * p.lddx;
-        for (int col = lane * 8; col < p.cols; col += 512) store_row<8>(row + col, p.cols - col, p.vec, none);
+        for (int col = lane * 8; col < p.cols; col += 512) store_row<8>(row + col, p.cols - col, none);
     }
 }
 
 template <typename T>
-bool aligned16(const void* p, int64_t ld) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * int64_t(sizeof(T)) % 16 == 0;
-}
-
-template <typename T>
 void combine_typed(hipStream_t st, CombineArgs p) {
-    p.vec = aligned16<T>(p.x, p.ldx) && aligned16<T>(p.y, p.ldy);
     p.pieces = (p.cols + 511) / 512;
     const int64_t waves = int64_t(p.tokens) * p.pieces;
     hipLaunchKernelGGL(combine_rows_kernel<T>, dim3(unsigned((waves + 3) / 4)), dim3(256), 0, st, p);
@@ -342,7 +337,6 @@ void combine_typed(hipStream_t st, CombineArgs p) {
 
 template <typename T>
 void combine_grad_typed(hipStream_t st, CombineArgs p) {
-    p.vec = aligned16<T>(p.dy, p.lddy) && aligned16<T>(p.dx, p.lddx) && (!p.dweights || aligned16<T>(p.x, p.ldx));
     hipLaunchKernelGGL(combine_grad_kernel<T>, dim3(unsigned((int64_t(p.slots) + 3) / 4)), dim3(256), 0, st, p);
 }
 
@@ -371,10 +365,8 @@ void launch_gather_rows(hipStream_t st, int tokens, int topk, int cols, int elem
                  cols * elem_bytes, 0, topk};
     p.pieces = (p.row_bytes + 4095) / 4096;
     if (int64_t(tokens) * p.pieces < 4096) p.per = 1;
-    const uintptr_t all = reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y) | uintptr_t(p.ldx) | uintptr_t(p.ldy) | uintptr_t(p.row_bytes);
     const dim3 grid(unsigned((int64_t(tokens) * p.pieces + 3) / 4), unsigned(topk / p.per));
-    if (all % 16 == 0) hipLaunchKernelGGL(gather_rows_kernel<v4i32>, grid, dim3(256), 0, st, p);
-    else if (all % 4 == 0) hipLaunchKernelGGL(gather_rows_kernel<uint32_t>, grid, dim3(256), 0, st, p);
+    if (p.row_bytes >= 16) hipLaunchKernelGGL(gather_rows_kernel<v4i32_any>, grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL(gather_rows_kernel<uint16_t>, grid, dim3(256), 0, st, p);
 }
 

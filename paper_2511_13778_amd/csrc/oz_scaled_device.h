@@ -88,35 +88,44 @@ __device__ __forceinline__ float to_float(T x) { return static_cast<float>(x); }
 template <typename T>
 __device__ __forceinline__ void put(T* p, float x) { *p = static_cast<T>(x); }
 
-// N consecutive elements as floats: one to N/4 16-byte loads where `vec` says that p is aligned for them and all are there, else one by one
-// with zeros from `have` on.  STREAM: read (written) once, past the caches.
+// 16 bytes of a row that starts at any element: global loads and stores need no more than the element's own alignment.
+typedef v4i32 __attribute__((aligned(2), may_alias)) v4i32_any;
+
+// N consecutive elements as floats: one to N/4 16-byte loads where all are there, else one by one with zeros from `have` on (all on their
+// way together: what is not there reads the last that is).  STREAM: read (written) once, past the caches.
 template <int N, bool STREAM = false, typename T>
-__device__ __forceinline__ void load_row(const T* __restrict__ p, int have, bool vec, float (&x)[N]) {
-    if (vec && have >= N) {
+__device__ __forceinline__ void load_row(const T* __restrict__ p, int have, float (&x)[N]) {
+    if (have >= N) {
         constexpr int kVec = N * int(sizeof(T)) / 16;
         static_assert(kVec * 16 == N * int(sizeof(T)), "whole 16-byte loads");
         union { v4i32 v[kVec]; T e[N]; } u;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) u.v[i] = STREAM ? __builtin_nontemporal_load(reinterpret_cast<const v4i32*>(p) + i) : reinterpret_cast<const v4i32*>(p)[i];
+        for (int i = 0; i < kVec; ++i) u.v[i] = STREAM ? __builtin_nontemporal_load(reinterpret_cast<const v4i32_any*>(p) + i) : reinterpret_cast<const v4i32_any*>(p)[i];
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = to_float(u.e[i]);
+    } else if (have > 0) {
+        T e[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) e[i] = p[min(i, have - 1)];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = i < have ? to_float(e[i]) : 0.0f;
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = i < have ? to_float(p[i]) : 0.0f;
+        for (int i = 0; i < N; ++i) x[i] = 0.0f;
     }
 }
 
 template <int N, bool STREAM = false, typename T>
-__device__ __forceinline__ void store_row(T* __restrict__ p, int have, bool vec, const float (&x)[N]) {
-    if (vec && have >= N) {
+__device__ __forceinline__ void store_row(T* __restrict__ p, int have, const float (&x)[N]) {
+    if (have >= N) {
         constexpr int kVec = N * int(sizeof(T)) / 16;
         union { v4i32 v[kVec]; T e[N]; } u;
 #pragma unroll
         for (int i = 0; i < N; ++i) put(&u.e[i], x[i]);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            if constexpr (STREAM) __builtin_nontemporal_store(u.v[i], reinterpret_cast<v4i32*>(p) + i);
-            else reinterpret_cast<v4i32*>(p)[i] = u.v[i];
+            if constexpr (STREAM) __builtin_nontemporal_store(u.v[i], reinterpret_cast<v4i32_any*>(p) + i);
+            else reinterpret_cast<v4i32_any*>(p)[i] = u.v[i];
         }
     } else {
 #pragma unroll

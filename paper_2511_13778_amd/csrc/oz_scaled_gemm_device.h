@@ -174,14 +174,15 @@ __device__ __forceinline__ v4f unpack4(uint2 w) {
 // Four consecutive results of one row of C.
 template <typename T>
 __device__ __forceinline__ void put4(T* p, int have, bool add, v4f s) {
-    typedef T quad __attribute__((ext_vector_type(4)));
-    if (have >= 4 && reinterpret_cast<uintptr_t>(p) % sizeof(quad) == 0) {
+    typedef T aligned_quad __attribute__((ext_vector_type(4)));
+    typedef aligned_quad __attribute__((aligned(2), may_alias)) quad;
+    if (have >= 4) {
         quad* at = reinterpret_cast<quad*>(p);
         if (add) {
-            const quad old = *at;
+            const aligned_quad old = *at;
             s += v4f{float(old[0]), float(old[1]), float(old[2]), float(old[3])};
         }
-        *at = quad{T(s[0]), T(s[1]), T(s[2]), T(s[3])};
+        *at = aligned_quad{T(s[0]), T(s[1]), T(s[2]), T(s[3])};
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -217,8 +218,7 @@ __device__ __forceinline__ void store_typed(const ScaledGemm& g, v4f (&acc)[NT][
     const int lane = threadIdx.x & 63, q = lane >> 4, x16 = lane & 15;
     uint8_t* const out = static_cast<uint8_t*>(g.c) + c * ES;
     const int64_t ld = g.ldc * ES;
-    const bool vec = ((uintptr_t(out) | uintptr_t(ld)) & 15) == 0;
-    const bool whole = vec && rows >= MT * 16 && cols >= NT * 16;
+    const bool whole = rows >= MT * 16 && cols >= NT * 16;
     // piece x of the part, in the order of LDS: row, column, how many of its elements there are
     auto each = [&](int part, auto&& f) {
 #pragma unroll 1
@@ -241,7 +241,7 @@ __device__ __forceinline__ void store_typed(const ScaledGemm& g, v4f (&acc)[NT][
             each(part, [&](v4i32* piece, const T* p, int have) {
                 union { v4i32 v; T e[kPer]; } u;
                 u.v = v4i32{0, 0, 0, 0};
-                if (vec && have >= kPer) u.v = *reinterpret_cast<const v4i32*>(p);
+                if (have >= kPer) u.v = *reinterpret_cast<const v4i32_any*>(p);
                 else
 #pragma unroll
                     for (int i = 0; i < kPer; ++i)
@@ -278,7 +278,7 @@ __device__ __forceinline__ void store_typed(const ScaledGemm& g, v4f (&acc)[NT][
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
                     const int r = (x + u) * kStepRows + r0;
-                    *reinterpret_cast<v4i32*>(out + (part * kPartRows + r) * ld + (((lane % kPieces) ^ (r & kMask)) << 4)) = v[u];
+                    *reinterpret_cast<v4i32_any*>(out + (part * kPartRows + r) * ld + (((lane % kPieces) ^ (r & kMask)) << 4)) = v[u];
                 }
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -286,7 +286,7 @@ __device__ __forceinline__ void store_typed(const ScaledGemm& g, v4f (&acc)[NT][
             each(part, [&](const v4i32* piece, T* p, int have) {
                 union { v4i32 v; T e[kPer]; } u;
                 u.v = *piece;
-                if (vec && have >= kPer) *reinterpret_cast<v4i32*>(p) = u.v;
+                if (have >= kPer) *reinterpret_cast<v4i32_any*>(p) = u.v;
                 else
 #pragma unroll
                     for (int i = 0; i < kPer; ++i)
