@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(RowArgs p) {
     const int64_t src = source_row(p.order, p.order_div, p.x_rows, r);
     float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (src >= 0)
-        load_row<8>(static_cast<const T*>(p.x) + int64_t(blockIdx.y) * p.stride_x + src * p.ldx + col, p.cols - col, x);
+        load_row<8>(static_cast<const T*>(p.x) + int64_t(blockIdx.y) * p.stride_x + src * p.ldx + col, p.cols - col, p.cols, x);
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
@@ -140,16 +140,21 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
     }
     const int col = int(blockIdx.y) * kScaleBlock + l * 8;
     const T* x0 = static_cast<const T*>(p.x) + int64_t(blockIdx.z) * p.stride_x;
-    float x[8][8];
+    // the rows' places first, then all rows on their way together, then their values
+    int from[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) from[i] = p.order ? p.order[min(row0 + g * 8 + i, p.rows - 1)] : row0 + g * 8 + i;
+    RowPiece<8, T> piece[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int r = row0 + g * 8 + i;
-        const int64_t src = r < end ? source_row(p.order, p.order_div, p.x_rows, r) : -1;
-        if (src >= 0) load_row<8>(x0 + src * p.ldx + col, p.cols - col, x[i]);
-        else
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[i][j] = 0.0f;
+        int src = from[i];
+        if (p.order) src = src < 0 || src / p.order_div >= p.x_rows ? -1 : src / p.order_div;
+        if (row0 + g * 8 + i >= end) src = -1;
+        fetch_row<8>(x0 + int64_t(max(src, 0)) * p.ldx + col, src < 0 ? 0 : p.cols - col, p.cols, piece[i]);
     }
+    float x[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) as_floats(piece[i], p.cols - col, p.cols, x[i]);
     auto mag = [](float v) -> uint32_t { return __float_as_uint(v) & 0x7FFFFFFFu; };
     const int64_t rsize = p.rows_e8m0 ? 1 : 4, csize = p.cols_e8m0 ? 1 : 4;
     uint8_t* rscale = p.by_rows.scale + int64_t(blockIdx.z) * p.by_rows.scale_stride * rsize;

@@ -261,7 +261,8 @@ __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs p) {
     const T* x = static_cast<const T*>(p.x);
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int j0 = 0; j0 < p.topk; j0 += 4) {
-        float v[4][8], w[4];
+        RowPiece<8, T> v[4];
+        float w[4];
         bool live[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -269,13 +270,16 @@ __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs p) {
             const int s = j0 + u < p.topk ? p.place[c] : -1;
             live[u] = s >= 0 && s < p.slots;
             w[u] = live[u] && p.weights ? p.weights[c] : 1.0f;
-            if (live[u]) load_row<8, true>(x + int64_t(s) * p.ldx + col, have, v[u]);
+            fetch_row<8, true>(x + int64_t(live[u] ? s : 0) * p.ldx + col, live[u] ? have : 0, p.cols, v[u]);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (live[u])
+            if (live[u]) {
+                float e[8];
+                as_floats(v[u], have, p.cols, e);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[u], v[u][i], sum[i]);
+                for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[u], e[i], sum[i]);
+            }
     }
     store_row<8>(static_cast<T*>(p.y) + int64_t(t) * p.ldy + col, have, sum);
 }
@@ -295,25 +299,27 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs p) {
     float dot = 0.0f;
     if (live) {
         for (int col = lane * 8; col < p.cols; col += 1024) {
-            float g[2][8], v[2][8];
+            RowPiece<8, T> gp[2], vp[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int at = col + u * 512;
-                if (at < p.cols) {
-                    load_row<8>(dy + at, p.cols - at, g[u]);
-                    if (p.dweights) load_row<8, true>(x + at, p.cols - at, v[u]);
-                }
+                fetch_row<8>(dy + at, p.cols - at, p.cols, gp[u]);
+                if (p.dweights) fetch_row<8, true>(x + at, p.cols - at, p.cols, vp[u]);
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int at = col + u * 512;
                 if (at < p.cols) {
-                    float out[8];
+                    float g[8], out[8];
+                    as_floats(gp[u], p.cols - at, p.cols, g);
+                    if (p.dweights) {
+                        float v[8];
+                        as_floats(vp[u], p.cols - at, p.cols, v);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (p.dweights) dot = fmaf(g[u][i], v[u][i], dot);
-                        out[i] = w * g[u][i];
+                        for (int i = 0; i < 8; ++i) dot = fmaf(g[i], v[i], dot);
                     }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) out[i] = w * g[i];
                     store_row<8, true>(dx + at, p.cols - at, out);
                 }
             }

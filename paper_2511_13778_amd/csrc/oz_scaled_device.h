@@ -91,30 +91,56 @@ __device__ __forceinline__ void put(T* p, float x) { *p = static_cast<T>(x); }
 // 16 bytes of a row that starts at any element: global loads and stores need no more than the element's own alignment.
 typedef v4i32 __attribute__((aligned(2), may_alias)) v4i32_any;
 
-// N consecutive elements as floats: one to N/4 16-byte loads where all are there, else one by one with zeros from `have` on (all on their
-// way together: what is not there reads the last that is).  STREAM: read (written) once, past the caches.
+// N consecutive elements of a row, from p on, of which `have` are there before its end (any number, also none or less); `cols` is the row's length.
+// fetch_row sends for them, as_floats waits for them and puts zeros from `have` on: several rows are on their way together when all are
+// fetched first.  16-byte loads throughout; a row's last piece is read from N before its end and moved down (rows shorter than N: element
+// by element).  STREAM: read once, past the caches.
+template <int N, typename T>
+struct RowPiece {
+    static constexpr int kVec = N * int(sizeof(T)) / 16;
+    static_assert(kVec * 16 == N * int(sizeof(T)), "whole 16-byte loads");
+    union { v4i32 v[kVec]; uint32_t w[4 * kVec]; T e[N]; };
+};
 template <int N, bool STREAM = false, typename T>
-__device__ __forceinline__ void load_row(const T* __restrict__ p, int have, float (&x)[N]) {
-    if (have >= N) {
-        constexpr int kVec = N * int(sizeof(T)) / 16;
-        static_assert(kVec * 16 == N * int(sizeof(T)), "whole 16-byte loads");
-        union { v4i32 v[kVec]; T e[N]; } u;
+__device__ __forceinline__ void fetch_row(const T* __restrict__ p, int have, int cols, RowPiece<N, T>& r) {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) u.v[i] = STREAM ? __builtin_nontemporal_load(reinterpret_cast<const v4i32_any*>(p) + i) : reinterpret_cast<const v4i32_any*>(p)[i];
+    for (int i = 0; i < r.kVec; ++i) r.v[i] = v4i32{0, 0, 0, 0};
+    if (have <= 0) return;
+    if (cols >= N) {
+        const v4i32_any* at = reinterpret_cast<const v4i32_any*>(p - max(N - have, 0));
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = to_float(u.e[i]);
-    } else if (have > 0) {
-        T e[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) e[i] = p[min(i, have - 1)];
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = i < have ? to_float(e[i]) : 0.0f;
+        for (int i = 0; i < r.kVec; ++i) r.v[i] = STREAM ? __builtin_nontemporal_load(at + i) : at[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = 0.0f;
+        for (int i = 0; i < N; ++i)
+            if (i < have) r.e[i] = p[i];
     }
 }
+template <int N, typename T>
+__device__ __forceinline__ void as_floats(RowPiece<N, T> r, int have, int cols, float (&x)[N]) {
+    constexpr int kWords = 4 * r.kVec, kPer = 4 / int(sizeof(T));
+    if (have > 0 && have < N && cols >= N) {
+        const int down = (N - have) / kPer;
+#pragma unroll
+        for (int step = kWords / 2; step > 0; step /= 2)
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) r.w[i] = (down & step) ? (i + step < kWords ? r.w[i + step] : 0u) : r.w[i];
+        if (kPer == 2 && (have & 1)) {                    // N is even
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) r.w[i] = (r.w[i] >> 16) | (i + 1 < kWords ? r.w[i + 1] << 16 : 0u);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = to_float(r.e[i]);
+}
+template <int N, bool STREAM = false, typename T>
+__device__ __forceinline__ void load_row(const T* __restrict__ p, int have, int cols, float (&x)[N]) {
+    RowPiece<N, T> r;
+    fetch_row<N, STREAM>(p, have, cols, r);
+    as_floats(r, have, cols, x);
+}
 
+// N floats to consecutive elements of a row, `have` of them.
 template <int N, bool STREAM = false, typename T>
 __device__ __forceinline__ void store_row(T* __restrict__ p, int have, const float (&x)[N]) {
     if (have >= N) {
