@@ -13,20 +13,61 @@ namespace oz {
 
 namespace {
 
-// e of a block whose largest |x| has the bits `top` (an infinity or NaN: any value, the caller looks)
-template <bool E5M2>
-__device__ __forceinline__ int block_exponent(uint32_t top) {
-    if (top == 0) return 0;
-    const int e = int(top >> 23) - 127 - (E5M2 ? 15 : 8) + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-    return max(e, -126);
+// ---- magnitudes: an element without its sign, one of 32 bits or two of 16 in a word, whose order is that of the values; an infinity or NaN
+// is above all others
+typedef uint16_t v2u16 __attribute__((ext_vector_type(2)));
+template <typename T>
+__device__ __forceinline__ uint32_t magnitudes(uint32_t w) { return w & (sizeof(T) == 2 ? 0x7FFF7FFFu : 0x7FFFFFFFu); }
+template <typename T>
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    if constexpr (sizeof(T) == 4) return max(a, b);
+    else return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2u16, a), __builtin_bit_cast(v2u16, b)));
+}
+// the largest of a word, as the bits of a float32
+template <typename T>
+__device__ __forceinline__ uint32_t float_bits(uint32_t w) {
+    if constexpr (sizeof(T) == 4) return w;
+    else return __float_as_uint(to_float(__builtin_bit_cast(T, uint16_t(max(w & 0xFFFFu, w >> 16)))));
+}
+// over the 16 lanes of a group: each lane meets the one 8, 4, 2 and 1 further round
+template <int R>
+__device__ __forceinline__ uint32_t turned_by(uint32_t w) { return uint32_t(__builtin_amdgcn_mov_dpp(int(w), 0x120 + R, 0xF, 0xF, false)); }
+template <typename T>
+__device__ __forceinline__ uint32_t largest_of_16(uint32_t w) {
+    w = larger<T>(w, turned_by<8>(w));
+    w = larger<T>(w, turned_by<4>(w));
+    w = larger<T>(w, turned_by<2>(w));
+    return larger<T>(w, turned_by<1>(w));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t largest_of_piece(const RowPiece<8, T>& r) {
+    uint32_t top = magnitudes<T>(r.w[0]);
+#pragma unroll
+    for (int i = 1; i < r.kWords; ++i) top = larger<T>(top, magnitudes<T>(r.w[i]));
+    return top;
 }
 
+// ---- scales, from the bits `top` of a block's largest |x| -----------------------------------------
+// e + 127: the sum carries into the exponent where the fraction is above 0.75
+template <bool E5M2>
+__device__ __forceinline__ uint32_t biased_exponent(uint32_t top) { return uint32_t(max(int((top + 0x1FFFFFu) >> 23) - (E5M2 ? 15 : 8), 1)); }
 __device__ __forceinline__ bool is_wild(uint32_t top) { return top >= 0x7F800000u; }
+// 2^-e, or NaN (0 only meets zeros)
+template <bool E5M2>
+__device__ __forceinline__ float multiplier(uint32_t top) {
+    return __uint_as_float(is_wild(top) ? 0x7FC00000u : (254u - biased_exponent<E5M2>(top)) << 23);
+}
+template <bool E5M2>
+__device__ __forceinline__ void put_scale(uint8_t* base, int64_t at, bool e8m0, uint32_t top) {
+    const uint32_t b = top == 0 ? 127u : biased_exponent<E5M2>(top);
+    if (e8m0) base[at] = is_wild(top) ? uint8_t(255) : uint8_t(b);
+    else reinterpret_cast<uint32_t*>(base)[at] = is_wild(top) ? 0x7FC00000u : b << 23;
+}
 
 // four values in one word; `mul` scales exactly (a power of two, or NaN for a block that has none)
 template <bool E5M2>
 __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
-    int w = 0;
+    int w = __float_as_int(a);             // both halves are written
     if constexpr (E5M2) {
         w = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, w, false);
         w = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, w, true);
@@ -37,34 +78,10 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
     return uint32_t(w);
 }
 
-struct Scale {
-    float mul;        // 2^-e, or NaN
-    uint8_t e8m0;
-    float value;
-};
-template <bool E5M2>
-__device__ __forceinline__ Scale scale_of(uint32_t top) {
-    Scale s;
-    const int e = block_exponent<E5M2>(top);      // -126 .. 120
-    s.mul = __uint_as_float(uint32_t(127 - e) << 23);
-    s.e8m0 = uint8_t(e + 127);
-    s.value = __uint_as_float(uint32_t(e + 127) << 23);
-    if (is_wild(top)) {
-        s.mul = s.value = __uint_as_float(0x7FC00000u);
-        s.e8m0 = 255;
-    }
-    return s;
-}
-
-__device__ __forceinline__ void put_scale(uint8_t* base, int64_t at, bool e8m0, const Scale& s) {
-    if (e8m0) base[at] = s.e8m0;
-    else reinterpret_cast<float*>(base)[at] = s.value;
-}
-
-__device__ __forceinline__ int64_t source_row(const int32_t* __restrict__ order, int div, int x_rows, int r) {
+__device__ __forceinline__ int source_row(const int32_t* __restrict__ order, int div, int x_rows, int r) {
     if (!order) return r;
     const int o = order[r];
-    const int s = o < 0 ? -1 : o / div;
+    const int s = o < 0 ? -1 : int(uint32_t(o) / uint32_t(div));
     return s < x_rows ? s : -1;
 }
 
@@ -77,31 +94,26 @@ struct RowArgs {
     bool e8m0;
 };
 
-// A block of 128 per 16 lanes, 8 values a lane: maximum by shuffles, no LDS.  grid (blocks of the matrix / 16, batch)
+// A block of 128 per 16 lanes, 8 values a lane: maximum by lane rotations, no LDS.  grid (blocks of the matrix / 16, batch)
 template <typename T, bool E5M2>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(RowArgs p) {
     const uint32_t id = blockIdx.x * 16 + (threadIdx.x >> 4);        // less than 2^31: the caller bounds rows * nblk
     const int r = int(id / uint32_t(p.nblk)), blk = int(id - uint32_t(r) * uint32_t(p.nblk)), l = threadIdx.x & 15;
     if (r >= p.rows) return;               // whole groups of 16 lanes
-    const int col = blk * kScaleBlock + l * 8;
-    const int64_t src = source_row(p.order, p.order_div, p.x_rows, r);
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (src >= 0)
-        load_row<8>(static_cast<const T*>(p.x) + int64_t(blockIdx.y) * p.stride_x + src * p.ldx + col, p.cols - col, p.cols, x);
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) top = max(top, uint32_t(__shfl_xor(int(top), d)));
-    const Scale s = scale_of<E5M2>(top);
+    const int col = blk * kScaleBlock + l * 8, src = source_row(p.order, p.order_div, p.x_rows, r), have = src < 0 ? 0 : p.cols - col;
+    RowPiece<8, T> x;
+    fetch_row<8>(static_cast<const T*>(p.x) + int64_t(blockIdx.y) * p.stride_x + int64_t(max(src, 0)) * p.ldx + col, have, p.cols, x);
+    settle_row(x, have, p.cols);
+    const uint32_t top = float_bits<T>(largest_of_16<T>(largest_of_piece(x)));
+    const float mul = multiplier<E5M2>(top);
     uint32_t w[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-        w[i] = pack4<E5M2>(x[4 * i] * s.mul, x[4 * i + 1] * s.mul, x[4 * i + 2] * s.mul, x[4 * i + 3] * s.mul);
+        w[i] = pack4<E5M2>(to_float(x.e[4 * i]) * mul, to_float(x.e[4 * i + 1]) * mul, to_float(x.e[4 * i + 2]) * mul, to_float(x.e[4 * i + 3]) * mul);
     uint8_t* out = p.out.data + int64_t(blockIdx.y) * p.out.stride + int64_t(r) * p.out.ld;
     if (col < ((p.cols + 15) & ~15)) *reinterpret_cast<uint2*>(out + col) = make_uint2(w[0], w[1]);
     const int64_t esize = p.e8m0 ? 1 : 4;
-    if (l == 0) put_scale(p.out.scale + int64_t(blockIdx.y) * p.out.scale_stride * esize, int64_t(r) * p.out.scale_ld + blk, p.e8m0, s);
+    if (l == 0) put_scale<E5M2>(p.out.scale + int64_t(blockIdx.y) * p.out.scale_stride * esize, int64_t(r) * p.out.scale_ld + blk, p.e8m0, top);
 }
 
 struct TileArgs {
@@ -119,9 +131,13 @@ struct TileArgs {
 // Thread (g, l): rows 8g .. 8g+7, columns 8l .. 8l+7, in registers throughout; the transposed bytes change places through LDS.
 // grid (row tiles, column tiles, batch)
 // There the eight bytes of thread (g, l) lie at place g ^ l of their row: the 16 rows that lanes write at a time meet different banks.
+// A call of few tiles takes as long as its instructions take to come from memory: maxima are of the elements' own bits, two of 16
+// in a word, and what ragged ends need is behind one branch.
 template <typename T, bool ROWS_E5M2, bool COLS_E5M2, bool SHARED>
 __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
-    __shared__ __align__(16) uint32_t col_top[16][kScaleBlock];
+    constexpr int kWords = RowPiece<8, T>::kWords;
+    __shared__ __align__(16) uint32_t col_words[16][16 * kWords];       // thread (g, l)'s column maxima
+    __shared__ __align__(16) uint32_t col_top[kScaleBlock];
     __shared__ __align__(16) uint8_t turned[kScaleBlock * kScaleBlock];
     const int g = threadIdx.x >> 4, l = threadIdx.x & 15;
     int row0 = int(blockIdx.x) * kScaleBlock, end = p.rows, out_col = row0;
@@ -138,105 +154,98 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
         cols_too = cols_too && out_col + kScaleBlock <= p.by_cols.ld;
         if (!cols_too && !p.by_rows.data) return;
     }
-    const int col = int(blockIdx.y) * kScaleBlock + l * 8;
-    const T* x0 = static_cast<const T*>(p.x) + int64_t(blockIdx.z) * p.stride_x;
-    // the rows' places first, then all rows on their way together, then their values
-    int from[8];
+    const int col = int(blockIdx.y) * kScaleBlock + l * 8, have = p.cols - col;
+    const T* x0 = static_cast<const T*>(p.x) + int64_t(blockIdx.z) * p.stride_x + col;
+    // a wave's lanes find the sources of its 32 rows; then all rows are on their way together
+    const int found = source_row(p.order, p.order_div, p.x_rows, min(row0 + int(threadIdx.x >> 6) * 32 + int(threadIdx.x & 31), p.rows - 1));
+    RowPiece<8, T> x[8];
+    auto fetch = [&](auto&& load) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) from[i] = p.order ? p.order[min(row0 + g * 8 + i, p.rows - 1)] : row0 + g * 8 + i;
-    RowPiece<8, T> piece[8];
+        for (int i = 0; i < 8; ++i) {
+            const int src = row0 + g * 8 + i < end ? __shfl(found, (g & 3) * 8 + i) : -1;
+            load(x0 + int64_t(max(src, 0)) * p.ldx, src < 0 ? 0 : have, x[i]);
+        }
+    };
+    if (p.cols >= 8) {
+        fetch([](const T* at, int n, RowPiece<8, T>& r) { fetch_long_row<8>(at, n, r); });
+        if (have > 0 && have < 8)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        int src = from[i];
-        if (p.order) src = src < 0 || src / p.order_div >= p.x_rows ? -1 : src / p.order_div;
-        if (row0 + g * 8 + i >= end) src = -1;
-        fetch_row<8>(x0 + int64_t(max(src, 0)) * p.ldx + col, src < 0 ? 0 : p.cols - col, p.cols, piece[i]);
+            for (int i = 0; i < 8; ++i) move_down(x[i], have);
+    } else {
+        fetch([](const T* at, int n, RowPiece<8, T>& r) { fetch_short_row(at, n, r); });
     }
-    float x[8][8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) as_floats(piece[i], p.cols - col, p.cols, x[i]);
-    auto mag = [](float v) -> uint32_t { return __float_as_uint(v) & 0x7FFFFFFFu; };
     const int64_t rsize = p.rows_e8m0 ? 1 : 4, csize = p.cols_e8m0 ? 1 : 4;
     uint8_t* rscale = p.by_rows.scale + int64_t(blockIdx.z) * p.by_rows.scale_stride * rsize;
     uint8_t* cscale = p.by_cols.scale + int64_t(blockIdx.z) * p.by_cols.scale_stride * csize;
     uint32_t shared_top = 0;
     if constexpr (SHARED) {
+        uint32_t top = largest_of_piece(x[0]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) shared_top = max(shared_top, mag(x[i][j]));
-        for (int d = 1; d < 64; d <<= 1) shared_top = max(shared_top, uint32_t(__shfl_xor(int(shared_top), d)));
-        if ((threadIdx.x & 63) == 0) col_top[0][threadIdx.x >> 6] = shared_top;
+        for (int i = 1; i < 8; ++i) top = larger<T>(top, largest_of_piece(x[i]));
+        top = largest_of_16<T>(top);
+        top = larger<T>(top, uint32_t(__shfl_xor(int(top), 16)));
+        top = larger<T>(top, uint32_t(__shfl_xor(int(top), 32)));
+        if ((threadIdx.x & 63) == 0) col_top[threadIdx.x >> 6] = top;
         __syncthreads();
-        shared_top = max(max(col_top[0][0], col_top[0][1]), max(col_top[0][2], col_top[0][3]));
+        shared_top = float_bits<T>(larger<T>(larger<T>(col_top[0], col_top[1]), larger<T>(col_top[2], col_top[3])));
         if (threadIdx.x == 0) {
-            if (p.by_rows.data)
-                put_scale(rscale, int64_t(blockIdx.x) * p.by_rows.scale_ld + blockIdx.y, p.rows_e8m0, scale_of<ROWS_E5M2>(shared_top));
-            if (cols_too)
-                put_scale(cscale, int64_t(blockIdx.y) * p.by_cols.scale_ld + blockIdx.x, p.cols_e8m0, scale_of<COLS_E5M2>(shared_top));
+            if (p.by_rows.data) put_scale<ROWS_E5M2>(rscale, int64_t(blockIdx.x) * p.by_rows.scale_ld + blockIdx.y, p.rows_e8m0, shared_top);
+            if (cols_too) put_scale<COLS_E5M2>(cscale, int64_t(blockIdx.y) * p.by_cols.scale_ld + blockIdx.x, p.cols_e8m0, shared_top);
         }
     }
     if (p.by_rows.data) {
-        uint8_t* out = p.by_rows.data + int64_t(blockIdx.z) * p.by_rows.stride;
+        const int r0 = row0 + g * 8;
+        uint8_t* out = p.by_rows.data + int64_t(blockIdx.z) * p.by_rows.stride + int64_t(r0) * p.by_rows.ld + col;
+        const int last = col < ((p.cols + 15) & ~15) ? end - r0 : 0;
+        uint32_t mine = 0;                       // lane l < 8: row l's
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int r = row0 + g * 8 + i;
-            uint32_t top = shared_top;
-            if constexpr (!SHARED) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) top = max(top, mag(x[i][j]));
-#pragma unroll
-                for (int d = 1; d < 16; d <<= 1) top = max(top, uint32_t(__shfl_xor(int(top), d)));
-            }
-            const Scale s = scale_of<ROWS_E5M2>(top);
-            if (r < end && col < ((p.cols + 15) & ~15)) {
-                uint32_t w[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    w[j] = pack4<ROWS_E5M2>(x[i][4 * j] * s.mul, x[i][4 * j + 1] * s.mul, x[i][4 * j + 2] * s.mul, x[i][4 * j + 3] * s.mul);
-                *reinterpret_cast<uint2*>(out + int64_t(r) * p.by_rows.ld + col) = make_uint2(w[0], w[1]);
-            }
-            if constexpr (!SHARED)
-                if (l == 0 && r < end) put_scale(rscale, int64_t(r) * p.by_rows.scale_ld + blockIdx.y, p.rows_e8m0, s);
+            const uint32_t top = SHARED ? shared_top : float_bits<T>(largest_of_16<T>(largest_of_piece(x[i])));
+            if (l == i) mine = top;
+            const float mul = multiplier<ROWS_E5M2>(top);
+            auto at = [&](int j) { return to_float(x[i].e[j]) * mul; };
+            const uint2 w = make_uint2(pack4<ROWS_E5M2>(at(0), at(1), at(2), at(3)), pack4<ROWS_E5M2>(at(4), at(5), at(6), at(7)));
+            if (i < last) *reinterpret_cast<uint2*>(out + int64_t(i) * p.by_rows.ld) = w;
         }
+        if (!SHARED && l < 8 && r0 + l < end) put_scale<ROWS_E5M2>(rscale, int64_t(r0 + l) * p.by_rows.scale_ld + blockIdx.y, p.rows_e8m0, mine);
     }
     if (!cols_too) return;                       // the same for all of a workgroup
     if constexpr (!SHARED) {
-        uint32_t tops[8];
+        uint32_t tops[kWords];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            tops[j] = 0;
+        for (int j = 0; j < kWords; ++j) {
+            tops[j] = magnitudes<T>(x[0].w[j]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) tops[j] = max(tops[j], mag(x[i][j]));
+            for (int i = 1; i < 8; ++i) tops[j] = larger<T>(tops[j], magnitudes<T>(x[i].w[j]));
         }
 #pragma unroll
-        for (int j = 0; j < 8; j += 4) *reinterpret_cast<uint4*>(&col_top[g][l * 8 + j]) = make_uint4(tops[j], tops[j + 1], tops[j + 2], tops[j + 3]);
+        for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4*>(&col_words[g][l * kWords + j]) = make_uint4(tops[j], tops[j + 1], tops[j + 2], tops[j + 3]);
         __syncthreads();
         if (threadIdx.x < kScaleBlock) {
+            constexpr int kPer = 4 / int(sizeof(T));
             uint32_t top = 0;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = max(top, col_top[i][threadIdx.x]);
-            col_top[0][threadIdx.x] = top;       // this thread alone reads its column
+            for (int i = 0; i < 16; ++i) top = larger<T>(top, col_words[i][threadIdx.x / kPer]);
+            if (kPer == 2) top = (threadIdx.x & 1) ? top >> 16 : top & 0xFFFFu;
+            top = float_bits<T>(top);
+            col_top[threadIdx.x] = top;
             const int c = int(blockIdx.y) * kScaleBlock + threadIdx.x;
-            if (c < p.cols)
-                put_scale(cscale, int64_t(c) * p.by_cols.scale_ld + out_col / kScaleBlock, p.cols_e8m0, scale_of<COLS_E5M2>(top));
+            if (c < p.cols) put_scale<COLS_E5M2>(cscale, int64_t(c) * p.by_cols.scale_ld + out_col / kScaleBlock, p.cols_e8m0, top);
         }
         __syncthreads();
     }
     uint32_t tops[8];
 #pragma unroll
     for (int j = 0; j < 8; j += 4) {
-        const uint4 v = SHARED ? make_uint4(shared_top, shared_top, shared_top, shared_top) : *reinterpret_cast<const uint4*>(&col_top[0][l * 8 + j]);
+        const uint4 v = SHARED ? make_uint4(shared_top, shared_top, shared_top, shared_top) : *reinterpret_cast<const uint4*>(&col_top[l * 8 + j]);
         tops[j] = v.x; tops[j + 1] = v.y; tops[j + 2] = v.z; tops[j + 3] = v.w;
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const Scale s = scale_of<COLS_E5M2>(tops[j]);
-        uint32_t w[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            w[i] = pack4<COLS_E5M2>(x[4 * i][j] * s.mul, x[4 * i + 1][j] * s.mul, x[4 * i + 2][j] * s.mul, x[4 * i + 3][j] * s.mul);
-        *reinterpret_cast<uint2*>(turned + (l * 8 + j) * kScaleBlock + (g ^ l) * 8) = make_uint2(w[0], w[1]);
+        const float mul = multiplier<COLS_E5M2>(tops[j]);
+        auto at = [&](int i) { return to_float(x[i].e[j]) * mul; };
+        *reinterpret_cast<uint2*>(turned + (l * 8 + j) * kScaleBlock + (g ^ l) * 8) =
+            make_uint2(pack4<COLS_E5M2>(at(0), at(1), at(2), at(3)), pack4<COLS_E5M2>(at(4), at(5), at(6), at(7)));
     }
     __syncthreads();
     // columns to write: all 128 of a group's block, else what is there, up to a multiple of 16

@@ -92,44 +92,59 @@ __device__ __forceinline__ void put(T* p, float x) { *p = static_cast<T>(x); }
 typedef v4i32 __attribute__((aligned(2), may_alias)) v4i32_any;
 
 // N consecutive elements of a row, from p on, of which `have` are there before its end (any number, also none or less); `cols` is the row's length.
-// fetch_row sends for them, as_floats waits for them and puts zeros from `have` on: several rows are on their way together when all are
+// fetch_row sends for them, settle_row waits for them and puts zeros from `have` on: several rows are on their way together when all are
 // fetched first.  16-byte loads throughout; a row's last piece is read from N before its end and moved down (rows shorter than N: element
 // by element).  STREAM: read once, past the caches.
 template <int N, typename T>
 struct RowPiece {
-    static constexpr int kVec = N * int(sizeof(T)) / 16;
+    static constexpr int kVec = N * int(sizeof(T)) / 16, kWords = 4 * kVec;
     static_assert(kVec * 16 == N * int(sizeof(T)), "whole 16-byte loads");
-    union { v4i32 v[kVec]; uint32_t w[4 * kVec]; T e[N]; };
+    union { v4i32 v[kVec]; uint32_t w[kWords]; T e[N]; };
 };
+// cols >= N
 template <int N, bool STREAM = false, typename T>
-__device__ __forceinline__ void fetch_row(const T* __restrict__ p, int have, int cols, RowPiece<N, T>& r) {
+__device__ __forceinline__ void fetch_long_row(const T* __restrict__ p, int have, RowPiece<N, T>& r) {
 #pragma unroll
     for (int i = 0; i < r.kVec; ++i) r.v[i] = v4i32{0, 0, 0, 0};
     if (have <= 0) return;
-    if (cols >= N) {
-        const v4i32_any* at = reinterpret_cast<const v4i32_any*>(p - max(N - have, 0));
+    const v4i32_any* at = reinterpret_cast<const v4i32_any*>(p - max(N - have, 0));
 #pragma unroll
-        for (int i = 0; i < r.kVec; ++i) r.v[i] = STREAM ? __builtin_nontemporal_load(at + i) : at[i];
-    } else {
+    for (int i = 0; i < r.kVec; ++i) r.v[i] = STREAM ? __builtin_nontemporal_load(at + i) : at[i];
+}
+template <int N, typename T>
+__device__ __forceinline__ void fetch_short_row(const T* __restrict__ p, int have, RowPiece<N, T>& r) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (i < have) r.e[i] = p[i];
+    for (int i = 0; i < r.kVec; ++i) r.v[i] = v4i32{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < have) r.e[i] = p[i];
+}
+template <int N, bool STREAM = false, typename T>
+__device__ __forceinline__ void fetch_row(const T* __restrict__ p, int have, int cols, RowPiece<N, T>& r) {
+    if (cols >= N) fetch_long_row<N, STREAM>(p, have, r);
+    else fetch_short_row(p, have, r);
+}
+// 0 < have < N <= cols
+template <int N, typename T>
+__device__ __forceinline__ void move_down(RowPiece<N, T>& r, int have) {
+    constexpr int kPer = 4 / int(sizeof(T));
+    const int down = (N - have) / kPer;
+#pragma unroll
+    for (int step = r.kWords / 2; step > 0; step /= 2)
+#pragma unroll
+        for (int i = 0; i < r.kWords; ++i) r.w[i] = (down & step) ? (i + step < r.kWords ? r.w[i + step] : 0u) : r.w[i];
+    if (kPer == 2 && (have & 1)) {                        // N is even
+#pragma unroll
+        for (int i = 0; i < r.kWords; ++i) r.w[i] = (r.w[i] >> 16) | (i + 1 < r.kWords ? r.w[i + 1] << 16 : 0u);
     }
 }
 template <int N, typename T>
+__device__ __forceinline__ void settle_row(RowPiece<N, T>& r, int have, int cols) {
+    if (have > 0 && have < N && cols >= N) move_down(r, have);
+}
+template <int N, typename T>
 __device__ __forceinline__ void as_floats(RowPiece<N, T> r, int have, int cols, float (&x)[N]) {
-    constexpr int kWords = 4 * r.kVec, kPer = 4 / int(sizeof(T));
-    if (have > 0 && have < N && cols >= N) {
-        const int down = (N - have) / kPer;
-#pragma unroll
-        for (int step = kWords / 2; step > 0; step /= 2)
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) r.w[i] = (down & step) ? (i + step < kWords ? r.w[i + step] : 0u) : r.w[i];
-        if (kPer == 2 && (have & 1)) {                    // N is even
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) r.w[i] = (r.w[i] >> 16) | (i + 1 < kWords ? r.w[i + 1] << 16 : 0u);
-        }
-    }
+    settle_row(r, have, cols);
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = to_float(r.e[i]);
 }
