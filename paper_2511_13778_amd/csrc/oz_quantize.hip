@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
     int row0 = int(blockIdx.x) * kScaleBlock, end = p.rows, out_col = row0;
     bool cols_too = p.by_cols.data != nullptr;
     if (p.offsets) {
-        const GroupPiece piece = find_piece<kScaleBlock>(p.offsets, p.groups, p.rows, int(blockIdx.x));
+        const GroupPiece piece = GroupPieces<kScaleBlock>(p.offsets, p.groups, p.rows).template find<true>(int(blockIdx.x));
         if (piece.group < 0) return;
         row0 = piece.row;
         end = piece.end;

@@ -146,11 +146,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs p) {
     for (int e0 = 0; e0 < p.experts; e0 += kSortThreads) {
         const int e = e0 + threadIdx.x;
         const int mine = e < p.experts ? total[e] : 0;
-        int sum = mine;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(sum, d);
-            if (lane >= d) sum += o;
-        }
+        const int sum = sum_up_to(mine);
         if (lane == 63) wave_total[wave] = sum;
         __syncthreads();
         int base = carry;

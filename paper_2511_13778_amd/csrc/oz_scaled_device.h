@@ -9,74 +9,88 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef int v4i32 __attribute__((ext_vector_type(4)));
 typedef int v8i32 __attribute__((ext_vector_type(8)));
 
-// A piece of the rows: piece `t` of the groups cut into pieces of SIZE rows, each group for itself; group `groups` holds the rows
-// behind the last one.  blocks_before: 128-row blocks of the groups before.  Called by whole waves; offsets that are not ascending
-// or pass `rows` give wrong pieces, none outside 0 .. rows.
+// Sums over the lanes up to each, by a whole wave: within rows of 16 lanes, then rows 0 and 2 into the next, then the lower half into the upper.
+// Six additions; shuffles go through LDS and take its latency each (groups' offsets loaded and scanned twice, by shuffles: experts' products
+// of 2296 rows, 2345 x 334, 13.6 us, once and so 11.2).
+__device__ __forceinline__ int sum_up_to(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+
+__device__ __forceinline__ int clamp_offset(const int32_t* offsets, int g, int rows) { return min(max(offsets[g], 0), rows); }
+
+// A piece of the rows: the groups are cut into pieces of SIZE rows, each group for itself; group `groups` holds the rows behind the last
+// one.  blocks_before: 128-row blocks of the groups before.
 struct GroupPiece {
     int group, row, end;      // rows row .. min(row + SIZE, end) - 1; group < 0: no such piece
     int blocks_before;
 };
 
-__device__ __forceinline__ int clamp_offset(const int32_t* offsets, int g, int rows) { return min(max(offsets[g], 0), rows); }
-
-// How many pieces there are.
+// The pieces of a call, by whole waves: a lane has a group (of the first 64; more are read again).  Offsets that are not ascending
+// or pass `rows` give wrong pieces, none outside 0 .. rows.
 template <int SIZE>
-__device__ __forceinline__ int count_pieces(const int32_t* __restrict__ offsets, int groups, int rows) {
-    int sum = 0;
-    for (int g = threadIdx.x & 63; g <= groups; g += 64) {
-        const int lo = clamp_offset(offsets, g, rows), hi = g < groups ? max(lo, clamp_offset(offsets, g + 1, rows)) : rows;
-        sum += (hi - lo + SIZE - 1) / SIZE;
-    }
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    return __builtin_amdgcn_readfirstlane(sum);
-}
+struct GroupPieces {
+    const int32_t* offsets;
+    int groups, rows;
+    int lo, hi, upto;         // a lane's group: its rows, and the pieces of the groups up to it
+    int count;                // of all
 
-template <int SIZE>
-__device__ __forceinline__ GroupPiece find_piece(const int32_t* __restrict__ offsets, int groups, int rows, int t) {
-    const int lane = threadIdx.x & 63;
-    int pieces = 0, blocks = 0;               // of the groups before this round's
-    for (int g0 = 0; g0 <= groups; g0 += 64) {
-        const int g = g0 + lane;
-        int lo = 0, hi = 0;
-        if (g <= groups) {
-            lo = clamp_offset(offsets, g, rows);
-            hi = g < groups ? max(lo, clamp_offset(offsets, g + 1, rows)) : rows;
-        }
-        const int mine = (hi - lo + SIZE - 1) / SIZE, blk = (hi - lo + kScaleBlock - 1) / kScaleBlock;
-        int sum = mine, bsum = blk;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(sum, d), ob = __shfl_up(bsum, d);
-            if (lane >= d) { sum += o; bsum += ob; }
-        }
-        const unsigned long long has = __ballot(pieces + sum > t);
-        if (has) {
-            const int src = __ffsll(has) - 1;
-            const int first = pieces + __shfl(sum, src) - __shfl(mine, src);
-            GroupPiece p;
-            p.group = __builtin_amdgcn_readfirstlane(g0 + src);
-            p.row = __builtin_amdgcn_readfirstlane(__shfl(lo, src) + (t - first) * SIZE);
-            p.end = __builtin_amdgcn_readfirstlane(__shfl(hi, src));
-            p.blocks_before = __builtin_amdgcn_readfirstlane(blocks + __shfl(bsum, src) - __shfl(blk, src));
-            return p;
-        }
-        pieces += __shfl(sum, 63);
-        blocks += __shfl(bsum, 63);
+    __device__ __forceinline__ void load(int g0, int before) {
+        const int g = g0 + int(threadIdx.x & 63);
+        lo = clamp_offset(offsets, min(g, groups), rows);
+        hi = g < groups ? max(lo, clamp_offset(offsets, min(g + 1, groups), rows)) : rows;
+        if (g > groups) lo = hi = 0;
+        upto = before + sum_up_to((hi - lo + SIZE - 1) / SIZE);
     }
-    return GroupPiece{-1, 0, 0, 0};
-}
+    __device__ __forceinline__ int last() const { return __builtin_amdgcn_readlane(upto, 63); }
+    __device__ __forceinline__ GroupPieces(const int32_t* o, int n, int r) : offsets(o), groups(n), rows(r) {
+        load(0, 0);
+        count = last();
+        if (groups >= 64) {
+            for (int g0 = 64; g0 <= groups; g0 += 64) {
+                load(g0, count);
+                count = last();
+            }
+            load(0, 0);
+        }
+    }
+    template <bool BLOCKS>
+    __device__ __forceinline__ GroupPiece find(int t) {
+        int blocks = 0;
+        for (int g0 = 0;;) {
+            const unsigned long long has = __ballot(upto > t);
+            const int blk = (hi - lo + kScaleBlock - 1) / kScaleBlock, blk_upto = BLOCKS ? sum_up_to(blk) : 0;
+            if (has) {
+                const int src = __builtin_ctzll(has), in = __builtin_amdgcn_readlane(lo, src), out = __builtin_amdgcn_readlane(hi, src);
+                const int first = __builtin_amdgcn_readlane(upto, src) - (out - in + SIZE - 1) / SIZE;
+                return GroupPiece{g0 + src, in + (t - first) * SIZE, out,
+                                  BLOCKS ? blocks + __builtin_amdgcn_readlane(blk_upto, src) - (out - in + kScaleBlock - 1) / kScaleBlock : 0};
+            }
+            if (BLOCKS) blocks += __builtin_amdgcn_readlane(blk_upto, 63);
+            g0 += 64;
+            if (g0 > groups) return GroupPiece{-1, 0, 0, 0};
+            load(g0, last());
+        }
+    }
+};
 
 // Rows of group g, and the 128-row blocks of the groups before it.
 struct GroupSpan { int count, blocks_before; };
 __device__ __forceinline__ GroupSpan group_span(const int32_t* __restrict__ offsets, int g, int rows) {
     const int lane = threadIdx.x & 63;
-    int blocks = 0;
-    for (int q = lane; q < g; q += 64) {
-        const int lo = clamp_offset(offsets, q, rows), hi = max(lo, clamp_offset(offsets, q + 1, rows));
-        blocks += (hi - lo + kScaleBlock - 1) / kScaleBlock;
+    int blocks = 0, rows_of = 0;
+    for (int q0 = 0; q0 <= g; q0 += 64) {
+        const int q = q0 + lane;
+        const int lo = clamp_offset(offsets, min(q, g), rows), hi = max(lo, clamp_offset(offsets, min(q, g) + 1, rows));
+        if (q < g) blocks += (hi - lo + kScaleBlock - 1) / kScaleBlock;
+        if (q == g) rows_of = hi - lo;
     }
-    for (int d = 1; d < 64; d <<= 1) blocks += __shfl_xor(blocks, d);
-    const int lo = clamp_offset(offsets, g, rows), hi = max(lo, clamp_offset(offsets, g + 1, rows));
-    return GroupSpan{__builtin_amdgcn_readfirstlane(hi - lo), __builtin_amdgcn_readfirstlane(blocks)};
+    return GroupSpan{__builtin_amdgcn_readlane(sum_up_to(rows_of), 63), __builtin_amdgcn_readlane(sum_up_to(blocks), 63)};
 }
 
 // ---- elements of 32 and 16 bits; a conversion to fewer bits rounds to nearest even ----------------

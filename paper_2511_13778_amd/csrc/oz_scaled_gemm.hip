@@ -21,9 +21,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
     constexpr int MT = WM / 16, NT = WN / 16;
     __shared__ __align__(16) uint8_t lds[STAGES * STAGE_BYTES + 2 * SCALE_BYTES];
 
-    const TilePlace place = tile_place<BM>(g, tiles_m, tiles_n);
-    if (place.n < 0) return;
-    const GemmTile t = locate<BM, BN>(g, place.m, place.n, int(blockIdx.y));
+    const GemmTile t = locate<BM, BN, true>(g, tiles_m, tiles_n);
     if (t.none) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % (BM / WM) * WM, wn = wave / (BM / WM) * WN;

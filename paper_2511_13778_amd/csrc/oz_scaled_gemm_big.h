@@ -43,9 +43,7 @@ __global__ __launch_bounds__(256, 1) void scaled_gemm_big_kernel(ScaledGemm g, i
     using P = Big<NB, SC>;
     constexpr bool kVector = SC != Scales::kE8M0;                         // sums are the vector ALU's
     extern __shared__ __align__(16) uint8_t lds[];
-    const TilePlace place = tile_place<kTM>(g, tiles_m, tiles_n);
-    if (place.n < 0) return;
-    const GemmTile t = locate<kTM, P::kTN>(g, place.m, place.n, int(blockIdx.y));
+    const GemmTile t = locate<kTM, P::kTN, true>(g, tiles_m, tiles_n);
     if (t.none) return;
     if (t.k == 0) {
         store_nothing(g, t);

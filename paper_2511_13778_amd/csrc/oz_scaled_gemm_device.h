@@ -104,10 +104,8 @@ struct GemmTile {
 // tiles, so that those it has at a time share their operands in its L2.  Rows in groups: of the tiles that there are, fewer than the
 // launch has workgroups for (8192 rows in 8 groups, the runs counted by the launch 68 us, by the tiles 54: the last XCDs were idle).
 struct TilePlace { int m, n; };      // n < 0: none
-template <int TM>
-__device__ __forceinline__ TilePlace tile_place(const ScaledGemm& g, int tiles_m, int tiles_n) {
+__device__ __forceinline__ TilePlace tile_place(int tiles_m, int tiles_n) {
     constexpr int kBand = 8;
-    if (g.grouping == Grouping::kRows) tiles_m = count_pieces<TM>(g.offsets, g.groups, g.m);
     const int total = tiles_m * tiles_n, per = total / 8, extra = total % 8, xcd = int(blockIdx.x) & 7, slot = int(blockIdx.x) >> 3;
     if (slot >= per + (xcd < extra ? 1 : 0)) return TilePlace{0, -1};
     const int id = xcd * per + min(xcd, extra) + slot;
@@ -115,9 +113,9 @@ __device__ __forceinline__ TilePlace tile_place(const ScaledGemm& g, int tiles_m
     return TilePlace{band * kBand + in_band % high, in_band / high};
 }
 
-// Rows `row` on of group `group`; TM rows, TN columns of C per tile.
+// The tile at (tile_m, tile_n), TM rows and TN columns of C, of product or part `group`; p: where it is if rows come in groups.
 template <int TM, int TN>
-__device__ __forceinline__ GemmTile locate(const ScaledGemm& g, int tile_m, int tile_n, int group) {
+__device__ __forceinline__ GemmTile tile_at(const ScaledGemm& g, int tile_m, int tile_n, int group, const GroupPiece& p) {
     GemmTile t;
     t.none = false;
     t.row = tile_m * TM;
@@ -128,7 +126,6 @@ __device__ __forceinline__ GemmTile locate(const ScaledGemm& g, int tile_m, int 
     t.c = 0;
     int row_end = g.m, weights = 0;
     if (g.grouping == Grouping::kRows) {
-        const GroupPiece p = find_piece<TM>(g.offsets, g.groups, g.m, tile_m);
         if (p.group < 0) { t.none = true; return t; }
         t.row = p.row;
         row_end = p.end;
@@ -153,6 +150,22 @@ __device__ __forceinline__ GemmTile locate(const ScaledGemm& g, int tile_m, int 
     const int64_t esize = g.e8m0 ? 1 : 4;
     t.sa = g.a.scale;
     t.sb = g.b.scale + int64_t(weights) * g.b.scale_stride * esize;
+    return t;
+}
+// A workgroup's tile.  DEALT: over the XCDs as above, of tiles_m rows of tiles (with groups: of those that there are), else row by row.
+template <int TM, int TN, bool DEALT>
+__device__ __forceinline__ GemmTile locate(const ScaledGemm& g, int tiles_m, int tiles_n) {
+    TilePlace place{int(blockIdx.x) / tiles_n, int(blockIdx.x) % tiles_n};
+    GroupPiece p = {};
+    if (g.grouping == Grouping::kRows) {
+        GroupPieces<TM> pieces(g.offsets, g.groups, g.m);
+        if (DEALT) place = tile_place(pieces.count, tiles_n);
+        if (place.n >= 0) p = pieces.template find<false>(place.m);
+    } else if (DEALT) {
+        place = tile_place(tiles_m, tiles_n);
+    }
+    GemmTile t = tile_at<TM, TN>(g, place.m, max(place.n, 0), int(blockIdx.y), p);
+    if (place.n < 0) t.none = true;
     return t;
 }
 

@@ -20,7 +20,7 @@ __global__ __launch_bounds__(MT == 1 ? 1024 : 512) void scaled_gemm_few_kernel(S
     extern __shared__ __align__(16) float sums[];                 // [wave][row][16]
     constexpr int kB = kFew<MT>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = int(blockDim.x) >> 6;
-    const GemmTile t = locate<MT * 16, 16>(g, int(blockIdx.x) / strips, int(blockIdx.x) % strips, int(blockIdx.y));
+    const GemmTile t = locate<MT * 16, 16, false>(g, 0, strips);
     if (t.none) return;
     const int q = lane >> 4, x16 = lane & 15;
     const int blocks = (t.k + kScaleBlock - 1) / kScaleBlock, tail = t.k & (kScaleBlock - 1);
