@@ -128,15 +128,17 @@ struct TileArgs {
 };
 
 // A tile of 128 x 128: rows, columns or the whole share a scale; written as it is and transposed from one read.
-// Thread (g, l): rows 8g .. 8g+7, columns 8l .. 8l+7, in registers throughout; the transposed bytes change places through LDS.
+// Thread (g, l): rows R g .. R g + R-1, columns 8l .. 8l+7, in registers throughout; the transposed bytes change places through LDS.
 // grid (row tiles, column tiles, batch)
-// There the eight bytes of thread (g, l) lie at place g ^ l of their row: the 16 rows that lanes write at a time meet different banks.
+// There eight bytes' place is turned by l: the 16 rows that lanes write at a time meet different banks.
+// R: 8, or 4 for calls of up to 1024 tiles, where a thread's own chain of loads and instructions is what takes the time (rows and columns of
+// 128 x 128 bfloat16 6.0 -> 4.8 us, 4096 x 1024 7.4 -> 6.4, but 5155 x 3470 20.0 -> 20.4, 4100 x 8192 of float32 38 -> 41).
 // A call of few tiles takes as long as its instructions take to come from memory: maxima are of the elements' own bits, two of 16
 // in a word, and what ragged ends need is behind one branch.
-template <typename T, bool ROWS_E5M2, bool COLS_E5M2, bool SHARED>
-__global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
-    constexpr int kWords = RowPiece<8, T>::kWords;
-    __shared__ __align__(16) uint32_t col_words[16][16 * kWords];       // thread (g, l)'s column maxima
+template <int R, typename T, bool ROWS_E5M2, bool COLS_E5M2, bool SHARED>
+__global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
+    constexpr int kWords = RowPiece<8, T>::kWords, kThreads = 2048 / R;
+    __shared__ __align__(16) uint32_t col_words[kScaleBlock / R][16 * kWords];       // thread (g, l)'s column maxima
     __shared__ __align__(16) uint32_t col_top[kScaleBlock];
     __shared__ __align__(16) uint8_t turned[kScaleBlock * kScaleBlock];
     const int g = threadIdx.x >> 4, l = threadIdx.x & 15;
@@ -156,13 +158,13 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
     }
     const int col = int(blockIdx.y) * kScaleBlock + l * 8, have = p.cols - col;
     const T* x0 = static_cast<const T*>(p.x) + int64_t(blockIdx.z) * p.stride_x + col;
-    // a wave's lanes find the sources of its 32 rows; then all rows are on their way together
-    const int found = source_row(p.order, p.order_div, p.x_rows, min(row0 + int(threadIdx.x >> 6) * 32 + int(threadIdx.x & 31), p.rows - 1));
-    RowPiece<8, T> x[8];
+    // a wave's lanes find the sources of its 4 R rows; then all rows are on their way together
+    const int found = source_row(p.order, p.order_div, p.x_rows, min(row0 + int(threadIdx.x >> 6) * (4 * R) + int(threadIdx.x & (4 * R - 1)), p.rows - 1));
+    RowPiece<8, T> x[R];
     auto fetch = [&](auto&& load) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int src = row0 + g * 8 + i < end ? __shfl(found, (g & 3) * 8 + i) : -1;
+        for (int i = 0; i < R; ++i) {
+            const int src = row0 + g * R + i < end ? __shfl(found, (g & 3) * R + i) : -1;
             load(x0 + int64_t(max(src, 0)) * p.ldx, src < 0 ? 0 : have, x[i]);
         }
     };
@@ -170,7 +172,7 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
         fetch([](const T* at, int n, RowPiece<8, T>& r) { fetch_long_row<8>(at, n, r); });
         if (have > 0 && have < 8)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) move_down(x[i], have);
+            for (int i = 0; i < R; ++i) move_down(x[i], have);
     } else {
         fetch([](const T* at, int n, RowPiece<8, T>& r) { fetch_short_row(at, n, r); });
     }
@@ -181,25 +183,28 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
     if constexpr (SHARED) {
         uint32_t top = largest_of_piece(x[0]);
 #pragma unroll
-        for (int i = 1; i < 8; ++i) top = larger<T>(top, largest_of_piece(x[i]));
+        for (int i = 1; i < R; ++i) top = larger<T>(top, largest_of_piece(x[i]));
         top = largest_of_16<T>(top);
         top = larger<T>(top, uint32_t(__shfl_xor(int(top), 16)));
         top = larger<T>(top, uint32_t(__shfl_xor(int(top), 32)));
         if ((threadIdx.x & 63) == 0) col_top[threadIdx.x >> 6] = top;
         __syncthreads();
-        shared_top = float_bits<T>(larger<T>(larger<T>(col_top[0], col_top[1]), larger<T>(col_top[2], col_top[3])));
+        top = col_top[0];
+#pragma unroll
+        for (int w = 1; w < kThreads / 64; ++w) top = larger<T>(top, col_top[w]);
+        shared_top = float_bits<T>(top);
         if (threadIdx.x == 0) {
             if (p.by_rows.data) put_scale<ROWS_E5M2>(rscale, int64_t(blockIdx.x) * p.by_rows.scale_ld + blockIdx.y, p.rows_e8m0, shared_top);
             if (cols_too) put_scale<COLS_E5M2>(cscale, int64_t(blockIdx.y) * p.by_cols.scale_ld + blockIdx.x, p.cols_e8m0, shared_top);
         }
     }
     if (p.by_rows.data) {
-        const int r0 = row0 + g * 8;
+        const int r0 = row0 + g * R;
         uint8_t* out = p.by_rows.data + int64_t(blockIdx.z) * p.by_rows.stride + int64_t(r0) * p.by_rows.ld + col;
         const int last = col < ((p.cols + 15) & ~15) ? end - r0 : 0;
-        uint32_t mine = 0;                       // lane l < 8: row l's
+        uint32_t mine = 0;                       // lane l < R: row l's
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < R; ++i) {
             const uint32_t top = SHARED ? shared_top : float_bits<T>(largest_of_16<T>(largest_of_piece(x[i])));
             if (l == i) mine = top;
             const float mul = multiplier<ROWS_E5M2>(top);
@@ -207,7 +212,7 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
             const uint2 w = make_uint2(pack4<ROWS_E5M2>(at(0), at(1), at(2), at(3)), pack4<ROWS_E5M2>(at(4), at(5), at(6), at(7)));
             if (i < last) *reinterpret_cast<uint2*>(out + int64_t(i) * p.by_rows.ld) = w;
         }
-        if (!SHARED && l < 8 && r0 + l < end) put_scale<ROWS_E5M2>(rscale, int64_t(r0 + l) * p.by_rows.scale_ld + blockIdx.y, p.rows_e8m0, mine);
+        if (!SHARED && l < R && r0 + l < end) put_scale<ROWS_E5M2>(rscale, int64_t(r0 + l) * p.by_rows.scale_ld + blockIdx.y, p.rows_e8m0, mine);
     }
     if (!cols_too) return;                       // the same for all of a workgroup
     if constexpr (!SHARED) {
@@ -216,7 +221,7 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
         for (int j = 0; j < kWords; ++j) {
             tops[j] = magnitudes<T>(x[0].w[j]);
 #pragma unroll
-            for (int i = 1; i < 8; ++i) tops[j] = larger<T>(tops[j], magnitudes<T>(x[i].w[j]));
+            for (int i = 1; i < R; ++i) tops[j] = larger<T>(tops[j], magnitudes<T>(x[i].w[j]));
         }
 #pragma unroll
         for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4*>(&col_words[g][l * kWords + j]) = make_uint4(tops[j], tops[j + 1], tops[j + 2], tops[j + 3]);
@@ -225,7 +230,7 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
             constexpr int kPer = 4 / int(sizeof(T));
             uint32_t top = 0;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = larger<T>(top, col_words[i][threadIdx.x / kPer]);
+            for (int i = 0; i < kScaleBlock / R; ++i) top = larger<T>(top, col_words[i][threadIdx.x / kPer]);
             if (kPer == 2) top = (threadIdx.x & 1) ? top >> 16 : top & 0xFFFFu;
             top = float_bits<T>(top);
             col_top[threadIdx.x] = top;
@@ -244,22 +249,41 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(TileArgs p) {
     for (int j = 0; j < 8; ++j) {
         const float mul = multiplier<COLS_E5M2>(tops[j]);
         auto at = [&](int i) { return to_float(x[i].e[j]) * mul; };
-        *reinterpret_cast<uint2*>(turned + (l * 8 + j) * kScaleBlock + (g ^ l) * 8) =
-            make_uint2(pack4<COLS_E5M2>(at(0), at(1), at(2), at(3)), pack4<COLS_E5M2>(at(4), at(5), at(6), at(7)));
+        uint8_t* to = turned + (l * 8 + j) * kScaleBlock;
+        if constexpr (R == 8)
+            *reinterpret_cast<uint2*>(to + (g ^ l) * 8) = make_uint2(pack4<COLS_E5M2>(at(0), at(1), at(2), at(3)), pack4<COLS_E5M2>(at(R - 4), at(R - 3), at(R - 2), at(R - 1)));
+        else
+            *reinterpret_cast<uint32_t*>(to + ((g >> 1) ^ l) * 8 + (g & 1) * 4) = pack4<COLS_E5M2>(at(0), at(1), at(2), at(3));
     }
     __syncthreads();
     // columns to write: all 128 of a group's block, else what is there, up to a multiple of 16
     const int wide = p.offsets ? kScaleBlock : min(kScaleBlock, ((p.rows + 15) & ~15) - row0);
     uint8_t* out = p.by_cols.data + int64_t(blockIdx.z) * p.by_cols.stride;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int q = i * 256 + threadIdx.x, tr = q >> 3, piece = (q & 7) * 16;
+    for (int i = 0; i < 1024 / kThreads; ++i) {
+        const int q = i * kThreads + threadIdx.x, tr = q >> 3, piece = (q & 7) * 16;
         const int c = int(blockIdx.y) * kScaleBlock + tr;
         // eight bytes 2p at place 2p ^ l, 2p+1 beside it: in turned order where l is odd
         const int tl = tr >> 3;
         const v4i32 v = *reinterpret_cast<const v4i32*>(turned + tr * kScaleBlock + (((q & 7) * 2) ^ (tl & 14)) * 8);
         if (c < p.cols && piece < wide)
             *reinterpret_cast<v4i32*>(out + int64_t(c) * p.by_cols.ld + out_col + piece) = (tl & 1) ? v4i32{v[2], v[3], v[0], v[1]} : v;
+    }
+}
+
+template <int R, typename T>
+void launch_tiles(hipStream_t st, const QuantizeCall& q, const TileArgs& p, const dim3& grid) {
+    const dim3 threads(2048 / R);
+    const int kind = (q.tiles ? 4 : 0) + (q.rows_e5m2 ? 2 : 0) + (q.cols_e5m2 ? 1 : 0);
+    switch (kind) {
+        case 0: hipLaunchKernelGGL((quantize_tiles_kernel<R, T, false, false, false>), grid, threads, 0, st, p); break;
+        case 1: hipLaunchKernelGGL((quantize_tiles_kernel<R, T, false, true, false>), grid, threads, 0, st, p); break;
+        case 2: hipLaunchKernelGGL((quantize_tiles_kernel<R, T, true, false, false>), grid, threads, 0, st, p); break;
+        case 3: hipLaunchKernelGGL((quantize_tiles_kernel<R, T, true, true, false>), grid, threads, 0, st, p); break;
+        case 4: hipLaunchKernelGGL((quantize_tiles_kernel<R, T, false, false, true>), grid, threads, 0, st, p); break;
+        case 5: hipLaunchKernelGGL((quantize_tiles_kernel<R, T, false, true, true>), grid, threads, 0, st, p); break;
+        case 6: hipLaunchKernelGGL((quantize_tiles_kernel<R, T, true, false, true>), grid, threads, 0, st, p); break;
+        default: hipLaunchKernelGGL((quantize_tiles_kernel<R, T, true, true, true>), grid, threads, 0, st, p); break;
     }
 }
 
@@ -277,17 +301,8 @@ void quantize_typed(hipStream_t st, const QuantizeCall& q) {
                      q.rows_e8m0, q.cols_e8m0};
     const int64_t tiles = q.offsets ? group_pieces(q.rows, q.groups, kScaleBlock) : (q.rows + kScaleBlock - 1) / kScaleBlock;
     const dim3 grid{unsigned(tiles), unsigned(nblk), unsigned(q.batch)};
-    const int kind = (q.tiles ? 4 : 0) + (q.rows_e5m2 ? 2 : 0) + (q.cols_e5m2 ? 1 : 0);
-    switch (kind) {
-        case 0: hipLaunchKernelGGL((quantize_tiles_kernel<T, false, false, false>), grid, dim3(256), 0, st, p); break;
-        case 1: hipLaunchKernelGGL((quantize_tiles_kernel<T, false, true, false>), grid, dim3(256), 0, st, p); break;
-        case 2: hipLaunchKernelGGL((quantize_tiles_kernel<T, true, false, false>), grid, dim3(256), 0, st, p); break;
-        case 3: hipLaunchKernelGGL((quantize_tiles_kernel<T, true, true, false>), grid, dim3(256), 0, st, p); break;
-        case 4: hipLaunchKernelGGL((quantize_tiles_kernel<T, false, false, true>), grid, dim3(256), 0, st, p); break;
-        case 5: hipLaunchKernelGGL((quantize_tiles_kernel<T, false, true, true>), grid, dim3(256), 0, st, p); break;
-        case 6: hipLaunchKernelGGL((quantize_tiles_kernel<T, true, false, true>), grid, dim3(256), 0, st, p); break;
-        default: hipLaunchKernelGGL((quantize_tiles_kernel<T, true, true, true>), grid, dim3(256), 0, st, p); break;
-    }
+    if (tiles * nblk * q.batch <= 1024) launch_tiles<4, T>(st, q, p, grid);
+    else launch_tiles<8, T>(st, q, p, grid);
 }
 
 }  // namespace

@@ -189,9 +189,10 @@ __global__ __launch_bounds__(256) void add_planes_kernel(ScaledGemm g, const flo
     const int have = min(4, g.n - c);
     const int64_t at = int64_t(r) * g.n + c, plane = int64_t(g.m) * g.n;
     v4f s = {0, 0, 0, 0};
-    if (have == 4 && g.n % 4 == 0) {
+    typedef v4f __attribute__((aligned(4), may_alias)) v4f_any;
+    if (have == 4) {
 #pragma unroll 8
-        for (int p = 0; p < parts; ++p) s += *reinterpret_cast<const v4f*>(planes + p * plane + at);
+        for (int p = 0; p < parts; ++p) s += *reinterpret_cast<const v4f_any*>(planes + p * plane + at);
     } else {
         for (int p = 0; p < parts; ++p)
 #pragma unroll
