@@ -142,10 +142,14 @@ __global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
     __shared__ __align__(16) uint32_t col_top[kScaleBlock];
     __shared__ __align__(16) uint8_t turned[kScaleBlock * kScaleBlock];
     const int g = threadIdx.x >> 4, l = threadIdx.x & 15;
-    int row0 = int(blockIdx.x) * kScaleBlock, end = p.rows, out_col = row0;
+    // dealt to the XCDs in turn: each gets a run of tiles one below the other, so that pieces of transposed rows meet in its L2
+    const uint32_t tiles = gridDim.x * gridDim.y, dealt = blockIdx.y * gridDim.x + blockIdx.x, xcd = dealt & 7;
+    const uint32_t id = xcd * (tiles >> 3) + min(xcd, tiles & 7) + (dealt >> 3);
+    const int tile_c = int(id / gridDim.x), tile_r = int(id - uint32_t(tile_c) * gridDim.x);
+    int row0 = tile_r * kScaleBlock, end = p.rows, out_col = row0;
     bool cols_too = p.by_cols.data != nullptr;
     if (p.offsets) {
-        const GroupPiece piece = GroupPieces<kScaleBlock>(p.offsets, p.groups, p.rows).template find<true>(int(blockIdx.x));
+        const GroupPiece piece = GroupPieces<kScaleBlock>(p.offsets, p.groups, p.rows).template find<true>(tile_r);
         if (piece.group < 0) return;
         row0 = piece.row;
         end = piece.end;
@@ -156,7 +160,7 @@ __global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
         cols_too = cols_too && out_col + kScaleBlock <= p.by_cols.ld;
         if (!cols_too && !p.by_rows.data) return;
     }
-    const int col = int(blockIdx.y) * kScaleBlock + l * 8, have = p.cols - col;
+    const int col = tile_c * kScaleBlock + l * 8, have = p.cols - col;
     const T* x0 = static_cast<const T*>(p.x) + int64_t(blockIdx.z) * p.stride_x + col;
     // a wave's lanes find the sources of its 4 R rows; then all rows are on their way together
     const int found = source_row(p.order, p.order_div, p.x_rows, min(row0 + int(threadIdx.x >> 6) * (4 * R) + int(threadIdx.x & (4 * R - 1)), p.rows - 1));
@@ -194,8 +198,8 @@ __global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
         for (int w = 1; w < kThreads / 64; ++w) top = larger<T>(top, col_top[w]);
         shared_top = float_bits<T>(top);
         if (threadIdx.x == 0) {
-            if (p.by_rows.data) put_scale<ROWS_E5M2>(rscale, int64_t(blockIdx.x) * p.by_rows.scale_ld + blockIdx.y, p.rows_e8m0, shared_top);
-            if (cols_too) put_scale<COLS_E5M2>(cscale, int64_t(blockIdx.y) * p.by_cols.scale_ld + blockIdx.x, p.cols_e8m0, shared_top);
+            if (p.by_rows.data) put_scale<ROWS_E5M2>(rscale, int64_t(tile_r) * p.by_rows.scale_ld + tile_c, p.rows_e8m0, shared_top);
+            if (cols_too) put_scale<COLS_E5M2>(cscale, int64_t(tile_c) * p.by_cols.scale_ld + tile_r, p.cols_e8m0, shared_top);
         }
     }
     if (p.by_rows.data) {
@@ -212,7 +216,7 @@ __global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
             const uint2 w = make_uint2(pack4<ROWS_E5M2>(at(0), at(1), at(2), at(3)), pack4<ROWS_E5M2>(at(4), at(5), at(6), at(7)));
             if (i < last) *reinterpret_cast<uint2*>(out + int64_t(i) * p.by_rows.ld) = w;
         }
-        if (!SHARED && l < R && r0 + l < end) put_scale<ROWS_E5M2>(rscale, int64_t(r0 + l) * p.by_rows.scale_ld + blockIdx.y, p.rows_e8m0, mine);
+        if (!SHARED && l < R && r0 + l < end) put_scale<ROWS_E5M2>(rscale, int64_t(r0 + l) * p.by_rows.scale_ld + tile_c, p.rows_e8m0, mine);
     }
     if (!cols_too) return;                       // the same for all of a workgroup
     if constexpr (!SHARED) {
@@ -234,7 +238,7 @@ __global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
             if (kPer == 2) top = (threadIdx.x & 1) ? top >> 16 : top & 0xFFFFu;
             top = float_bits<T>(top);
             col_top[threadIdx.x] = top;
-            const int c = int(blockIdx.y) * kScaleBlock + threadIdx.x;
+            const int c = tile_c * kScaleBlock + threadIdx.x;
             if (c < p.cols) put_scale<COLS_E5M2>(cscale, int64_t(c) * p.by_cols.scale_ld + out_col / kScaleBlock, p.cols_e8m0, top);
         }
         __syncthreads();
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
 #pragma unroll
     for (int i = 0; i < 1024 / kThreads; ++i) {
         const int q = i * kThreads + threadIdx.x, tr = q >> 3, piece = (q & 7) * 16;
-        const int c = int(blockIdx.y) * kScaleBlock + tr;
+        const int c = tile_c * kScaleBlock + tr;
         // eight bytes 2p at place 2p ^ l, 2p+1 beside it: in turned order where l is odd
         const int tl = tr >> 3;
         const v4i32 v = *reinterpret_cast<const v4i32*>(turned + tr * kScaleBlock + (((q & 7) * 2) ^ (tl & 14)) * 8);
