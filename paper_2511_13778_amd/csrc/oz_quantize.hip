@@ -5,8 +5,10 @@
 //
 // The scale is a power of two because a floating-point value keeps its relative precision under one: x 2^-e is exact, so the
 // conversion to 8 bits is the only rounding, and the matrix unit can apply the scale itself.  e comes from a's exponent field
-// and one comparison of its fraction with 0.75.  What bounds it: memory; each input is read once, also where rows and columns of it
-// are wanted.
+// and whether its fraction is above 0.75.  What bounds it: memory; each input is read once, also where rows and columns of it
+// are wanted.  4100 x 8192 of bfloat16: its rows 18.9 us (5.3 TB/s), both ways 27 us with operands in the last-level cache (5.0 TB/s), 37
+// from memory: 2112 tiles of one load and one store phase each are little more than a round of the chip, which ends unevenly.
+// 16 x 4096: 2.4 us, the launch.
 #include "oz_scaled_device.h"
 
 namespace oz {
@@ -94,7 +96,8 @@ struct RowArgs {
     bool e8m0;
 };
 
-// A block of 128 per 16 lanes, 8 values a lane: maximum by lane rotations, no LDS.  grid (blocks of the matrix / 16, batch)
+// A block of 128 per 16 lanes, 8 values a lane: maximum by lane rotations, no LDS.  Loads are cached: with an order a token's row is read
+// for each of its choices.  grid (blocks of the matrix / 16, batch)
 template <typename T, bool E5M2>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(RowArgs p) {
     const uint32_t id = blockIdx.x * 16 + (threadIdx.x >> 4);        // less than 2^31: the caller bounds rows * nblk
@@ -133,6 +136,7 @@ struct TileArgs {
 // There eight bytes' place is turned by l: the 16 rows that lanes write at a time meet different banks.
 // R: 8, or 4 for calls of up to 1024 tiles, where a thread's own chain of loads and instructions is what takes the time (rows and columns of
 // 128 x 128 bfloat16 6.0 -> 4.8 us, 4096 x 1024 7.4 -> 6.4, but 5155 x 3470 20.0 -> 20.4, 4100 x 8192 of float32 38 -> 41).
+// Loads are cached: streamed ones are 4 % faster from memory (37.1 -> 35.7 us) but lose a quarter where a kernel before left x in the cache.
 // A call of few tiles takes as long as its instructions take to come from memory: maxima are of the elements' own bits, two of 16
 // in a word, and what ragged ends need is behind one branch.
 template <int R, typename T, bool ROWS_E5M2, bool COLS_E5M2, bool SHARED>

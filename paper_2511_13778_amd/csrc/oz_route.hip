@@ -2,8 +2,11 @@
 //
 // Sort: a stable counting sort of the choices by expert.  Within 64 choices the lanes of one expert find each other with one ballot
 // per bit of its number; rank = lanes before, plus what the wave, the waves before and the blocks before counted of that
-// expert.  No atomics: the order is the same in every run.
-// Gather and combine move rows; what bounds them is memory.
+// expert.  The only atomics add whole numbers: the order is the same in every run.  Few choices are bound by a chain of latencies (264:
+// 3.8 us), 65536 take 8.3 in two launches.
+// Gather and combine move rows; what bounds them is memory: 16384 tokens of 2048 bfloat16 with four choices 53 us each (6.3 and 6.1 TB/s),
+// the gradient, which reads dY and the rows and writes rows, 95 (6.4).  Rows that are read or written once are streamed past the
+// caches: at that size all three lose 12 to 22 % without, up to 8192 x 2 choices both ways are level.
 #include <algorithm>
 
 #include "oz_scaled_device.h"
@@ -247,7 +250,7 @@ struct CombineArgs {
     int tokens, topk, cols, slots, pieces;
 };
 
-// A wave per 512 columns of a token; the choices' rows four at a time.
+// A wave per 512 columns of a token; the choices' rows four at a time, all of which are on their way before the first is added.
 template <typename T>
 __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs p) {
     const uint32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -280,7 +283,8 @@ __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs p) {
     store_row<8>(static_cast<T*>(p.y) + int64_t(t) * p.ldy + col, have, sum);
 }
 
-// A wave per choice: the choices of a token lie in one workgroup and find its dY in the cache.
+// A wave per choice: the choices of a token lie in one workgroup and find its dY in the cache.  The product of dY and the row is the
+// wave's own sum, lane by lane and then over the lanes in one order: no atomics.
 template <typename T>
 __global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs p) {
     const uint32_t c = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
