@@ -172,7 +172,8 @@ __global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
     auto fetch = [&](auto&& load) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int src = row0 + g * R + i < end ? __shfl(found, (g & 3) * R + i) : -1;
+            const int row = __shfl(found, (g & 3) * R + i);        // by all lanes
+            const int src = row0 + g * R + i < end ? row : -1;
             load(x0 + int64_t(max(src, 0)) * p.ldx, src < 0 ? 0 : have, x[i]);
         }
     };
