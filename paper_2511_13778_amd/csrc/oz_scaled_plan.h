@@ -6,6 +6,9 @@
 // route is the best one).  Tiles of 256 x 256 need the fewest bytes per operation and win on large outputs (8192^3 402 us, 256 x 128 462,
 // 128 x 128 556), those of 128 x 128 and 64 x 64, several to a CU, overlap one's results with another's products and win on
 // short k and where larger ones leave CUs idle (8192 x 8192 x 512 56 us, 256 x 256 62; 1024^3 6.2 us in 64 x 64, 9.6 in 128 x 128).
+// 64 x 64 tiles that are alone on their CU take four stages: from memory two wait for each step's loads (200 x 2048 x 2048 15.2 us, with four 9.8,
+// widened 15.4 and 12.3), from the caches two are ahead (9.0, 9.5), and `alone` of two stages is what they take from memory.  The launch
+// gives them to parts of a k that is cut as well.
 #pragma once
 
 #include <algorithm>
@@ -28,8 +31,8 @@ struct RouteCost { double alone, per, each; };
 constexpr RouteCost kRouteCost[4][5] = {
     {{.49, .197, .40}, {.39, .25, .40}, {.785, .54, 1.2}, {.81, .81, 5.5}, {1.42, 1.42, 9.1}},
     {{.52, .226, .45}, {.48, .29, .45}, {.93, .675, 1.3}, {1.09, 1.09, 5.7}, {0, 0, 0}},
-    {{.54, .298, .51}, {.575, .352, .51}, {1.14, .893, 1.8}, {0, 0, 0}, {0, 0, 0}},
-    {{.625, .34, .51}, {.645, .40, .51}, {1.24, 1.09, 1.8}, {0, 0, 0}, {0, 0, 0}},
+    {{.66, .298, .51}, {.575, .352, .51}, {1.14, .893, 1.8}, {0, 0, 0}, {0, 0, 0}},
+    {{.70, .34, .51}, {.645, .40, .51}, {1.24, 1.09, 1.8}, {0, 0, 0}, {0, 0, 0}},
 };
 
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -48,7 +48,8 @@ def sort_tokens(h: g.Handle, ids, experts: int) -> Routing:
     h.call("oz_sort_tokens", stream_of(ids), tokens, topk, experts, ids.data_ptr(), ids.element_size(), base, base + 4 * at[1], base + 4 * at[2],
            base + 4 * ws_at if need else None, need)
     r = Routing.__new__(Routing)            # right by construction
-    r.offsets, r.order, r.place, r.topk, r.tokens = all_[:experts + 1], all_[at[1]:at[2]], all_[at[2]:at[2] + n].view(tokens, topk), topk, tokens
+    r.offsets, r.order, place, _ = torch.split_with_sizes(all_, (experts + 1, n, n, all_.numel() - at[2] - n))
+    r.place, r.topk, r.tokens = place.view(tokens, topk), topk, tokens
     return r
 
 
