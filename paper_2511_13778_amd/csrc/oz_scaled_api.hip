@@ -212,7 +212,7 @@ oz_status_t oz_combine_rows_grad(oz_handle_t h, void* stream, int64_t tokens, in
     if (!h || esize == 0 || topk < 0 || topk > 64 || !rows_ok(tokens, cols, dY, lddy, esize) || !rows_ok(slots, cols, dX, lddx, esize)) return OZ_ERR_ARG;
     if (dweights && !rows_ok(slots, cols, X, ldx, esize)) return OZ_ERR_ARG;
     if (tokens * topk >= kMaxChoices || slots != tokens * topk || (slots > 0 && (!place || !order))) return OZ_ERR_ARG;
-    if (slots == 0 || cols == 0) return OZ_OK;
+    if (slots == 0 || (cols == 0 && !dweights)) return OZ_OK;       // rows without columns have products all the same: zeros
     if (slots > 4 * kMaxGrid) return OZ_ERR_ARG;
     if (!handle_on_device(h)) return OZ_ERR_DEVICE;
     launch_combine_grad(static_cast<hipStream_t>(stream), int(tokens), int(topk), int(cols), type, dY, lddy, X, ldx, int(slots), order, place,
