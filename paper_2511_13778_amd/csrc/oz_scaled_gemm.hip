@@ -12,6 +12,8 @@
 #include "oz_scaled_gemm_device.h"
 #include "oz_scaled_plan.h"
 
+#include <type_traits>
+
 namespace oz {
 
 namespace {
@@ -26,6 +28,8 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
     constexpr int SCALE_COPIES = ROWS / 64 * (E8M0 ? 1 : 4);
     constexpr int MT = WM / 16, NT = WN / 16;
     __shared__ __align__(16) uint8_t lds[STAGES * STAGE_BYTES + 2 * SCALE_BYTES];
+    constexpr bool kE8M0Wide = E8M0 && WIDE;
+    __shared__ int wild_waves[kE8M0Wide ? WAVES : 1];
 
     const GemmTile t = locate<BM, BN, true>(g, tiles_m, tiles_n);
     if (t.none) return;
@@ -35,10 +39,13 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
     const int tail = t.k & (kScaleBlock - 1);                     // bytes of the last step if it is not whole
 
     v4f acc[NT][MT];
+    auto clear = [&]() {
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int i = 0; i < MT; ++i) acc[j][i] = v4f{0, 0, 0, 0};
+            for (int i = 0; i < MT; ++i) acc[j][i] = v4f{0, 0, 0, 0};
+    };
+    clear();
 
     if (steps > 0) {
         const uint32_t lds0 = lds_address(lds);
@@ -77,106 +84,154 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void scaled_gemm_kernel
             if (s == 0 || ((t.block0 + s) & 3) == 0) copy_scales(s);
             copy_step(s);
         };
-#pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) copy(s);
-
         const uint32_t sw = uint32_t(lane & 7);
         const int q = lane >> 4, x16 = lane & 15;
         // this lane's pieces 2q and 2q+1 of row x16 of a fragment
         const uint32_t p0 = uint32_t(x16) * kScaleBlock + ((uint32_t(2 * q) ^ sw) * 16), p1 = uint32_t(x16) * kScaleBlock + ((uint32_t(2 * q + 1) ^ sw) * 16);
-        for (int s = 0; s < steps; ++s) {
-            if (s + STAGES - 1 <= steps) wait_copies<COPIES * (STAGES - 2)>();
-            else wait_copies<0>();
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            copy(s + STAGES - 1);
-            const uint8_t* st = lds + (s % STAGES) * STAGE_BYTES;
-            auto fragment = [&](int row0) -> v8i32 {
-                union { v8i32 f; v4i32 h[2]; } u;
-                u.h[0] = *reinterpret_cast<const v4i32*>(st + row0 * kScaleBlock + p0);
-                u.h[1] = *reinterpret_cast<const v4i32*>(st + row0 * kScaleBlock + p1);
-                return u.f;
-            };
-            v8i32 fa[MT], fb[NT];
+        // The walk over k.  Widened operands with E8M0 scales: the first walk folds these into the operands and notes the least and the largest
+        // (as float32's exponent field); if a wave met one that does not allow it, the tile is computed once more, APART: scales applied to the
+        // sums.  A branch in the step instead costs every call 5 to 13 % (8192^3 886 -> 980 us, so 905).
+        uint32_t least = 0x7F800000u, most = 0;
+        auto walk = [&](auto APART) {
+            constexpr bool apart = decltype(APART)::value;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) fa[i] = fragment(wm + i * 16);
+            for (int s = 0; s < STAGES - 1; ++s) copy(s);
+            for (int s = 0; s < steps; ++s) {
+                if (s + STAGES - 1 <= steps) wait_copies<COPIES * (STAGES - 2)>();
+                else wait_copies<0>();
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                copy(s + STAGES - 1);
+                const int blk = t.block0 + s;
+                const uint8_t* sc = lds + STAGES * STAGE_BYTES + ((blk >> 2) & 1) * SCALE_BYTES;
+                const uint8_t* st = lds + (s % STAGES) * STAGE_BYTES;
+                auto fragment = [&](int row0) -> v8i32 {
+                    union { v8i32 f; v4i32 h[2]; } u;
+                    u.h[0] = *reinterpret_cast<const v4i32*>(st + row0 * kScaleBlock + p0);
+                    u.h[1] = *reinterpret_cast<const v4i32*>(st + row0 * kScaleBlock + p1);
+                    return u.f;
+                };
+                v8i32 fa[MT], fb[NT];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) fb[j] = fragment(BM + wn + j * 16);
-            if (tail && s == steps - 1) {
+                for (int i = 0; i < MT; ++i) fa[i] = fragment(wm + i * 16);
 #pragma unroll
-                for (int w = 0; w < 8; ++w) {
-                    const int have = min(max(tail - (q * 32 + w * 4), 0), 4);
-                    const int keep = have == 4 ? -1 : (1 << (8 * have)) - 1;
+                for (int j = 0; j < NT; ++j) fb[j] = fragment(BM + wn + j * 16);
+                if (tail && s == steps - 1) {
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) fa[i][w] &= keep;
+                    for (int w = 0; w < 8; ++w) {
+                        const int have = min(max(tail - (q * 32 + w * 4), 0), 4);
+                        const int keep = have == 4 ? -1 : (1 << (8 * have)) - 1;
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) fb[j][w] &= keep;
+                        for (int i = 0; i < MT; ++i) fa[i][w] &= keep;
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) fb[j][w] &= keep;
+                    }
                 }
-            }
-            const int blk = t.block0 + s;
-            const uint8_t* sc = lds + STAGES * STAGE_BYTES + ((blk >> 2) & 1) * SCALE_BYTES;
-            if constexpr (E8M0) {
-                uint32_t sa[MT], sb[NT];
-                const int shift = (blk & 3) * 8;
+                if constexpr (E8M0) {
+                    uint32_t sa[MT], sb[NT];
+                    const int shift = (blk & 3) * 8;
 #pragma unroll
-                for (int i = 0; i < MT; ++i) sa[i] = *reinterpret_cast<const uint32_t*>(sc + (wm + i * 16 + x16) * 4) >> shift;
+                    for (int i = 0; i < MT; ++i) sa[i] = *reinterpret_cast<const uint32_t*>(sc + (wm + i * 16 + x16) * 4) >> shift;
 #pragma unroll
-                for (int j = 0; j < NT; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(sc + (BM + wn + j * 16 + x16) * 4) >> shift;
-                if constexpr (WIDE) {
-                    Wide wa[MT], wb[NT];
+                    for (int j = 0; j < NT; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(sc + (BM + wn + j * 16 + x16) * 4) >> shift;
+                    if constexpr (apart) {
+                        // one product after the other, widened anew for each, in no more registers than the usual step has: they decide how
+                        // many workgroups a CU holds
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) wa[i] = widen<A_E5M2>(fa[i], scale_float(sa[i]));
+                        for (int j = 0; j < NT; ++j) {
+                            const uint4 four = *reinterpret_cast<const uint4*>(sc + (BM + wn + j * 16 + q * 4) * 4);      // of this lane's results
+                            const uint32_t each[4] = {four.x >> shift, four.y >> shift, four.z >> shift, four.w >> shift};
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) wb[j] = widen<false>(fb[j], scale_float(sb[j]));
-                    // a tile's four instructions apart from each other: each waits for the one before it
+                            for (int i = 0; i < MT; ++i) {
+                                float one = 1.0f;
+                                asm volatile("" : "+v"(one));
+                                const v4f p = mfma_wide(widen<false>(fb[j], one), widen<A_E5M2>(fa[i], one), v4f{0, 0, 0, 0});
 #pragma unroll
-                    for (int w = 0; w < 4; ++w)
+                                for (int r = 0; r < 4; ++r) acc[j][i][r] = add_scaled(acc[j][i][r], p[r], sa[i], each[r]);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                    } else if constexpr (WIDE) {
+                        Wide wa[MT], wb[NT];
 #pragma unroll
-                        for (int j = 0; j < NT; ++j)
+                        for (int i = 0; i < MT; ++i) {
+                            const float scale = scale_float(sa[i]);
+                            least = min(least, __float_as_uint(scale));
+                            most = max(most, __float_as_uint(scale));
+                            wa[i] = widen<A_E5M2>(fa[i], scale);
+                        }
 #pragma unroll
-                            for (int i = 0; i < MT; ++i)
-                                acc[j][i] = mfma_bf16(wb[j].part[w], wa[i].part[w], acc[j][i]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < NT; ++j)
-#pragma unroll
-                        for (int i = 0; i < MT; ++i) acc[j][i] = mfma_e8m0<A_E5M2>(fb[j], fa[i], acc[j][i], sb[j], sa[i]);
-                }
-            } else {
-                const float* fs = reinterpret_cast<const float*>(sc) + (blk & 3) * ROWS;
-                float sa[MT];
-                v4f sb[NT];
-#pragma unroll
-                for (int i = 0; i < MT; ++i) sa[i] = fs[wm + i * 16 + x16];
-#pragma unroll
-                for (int j = 0; j < NT; ++j) sb[j] = *reinterpret_cast<const v4f*>(fs + BM + wn + j * 16 + q * 4);
-                Wide wa[MT], wb[NT];
-                if constexpr (WIDE) {
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) wa[i] = widen<A_E5M2>(fa[i], 1.0f);
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) wb[j] = widen<false>(fb[j], 1.0f);
-                }
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    v4f p[MT];
-                    if constexpr (WIDE) {
+                        for (int j = 0; j < NT; ++j) {
+                            const float scale = scale_float(sb[j]);
+                            least = min(least, __float_as_uint(scale));
+                            most = max(most, __float_as_uint(scale));
+                            wb[j] = widen<false>(fb[j], scale);
+                        }
+                        // a tile's four instructions apart from each other: each waits for the one before it
 #pragma unroll
                         for (int w = 0; w < 4; ++w)
 #pragma unroll
-                            for (int i = 0; i < MT; ++i)
-                                p[i] = mfma_bf16(wb[j].part[w], wa[i].part[w], w == 0 ? v4f{0, 0, 0, 0} : p[i]);
+                            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                                for (int i = 0; i < MT; ++i)
+                                    acc[j][i] = mfma_bf16(wb[j].part[w], wa[i].part[w], acc[j][i]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) p[i] = mfma_plain<A_E5M2>(fb[j], fa[i]);
+                        for (int j = 0; j < NT; ++j)
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) acc[j][i] = mfma_e8m0<A_E5M2>(fb[j], fa[i], acc[j][i], sb[j], sa[i]);
+                    }
+                } else {
+                    const float* fs = reinterpret_cast<const float*>(sc) + (blk & 3) * ROWS;
+                    float sa[MT];
+                    v4f sb[NT];
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) sa[i] = fs[wm + i * 16 + x16];
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) sb[j] = *reinterpret_cast<const v4f*>(fs + BM + wn + j * 16 + q * 4);
+                    Wide wa[MT], wb[NT];
+                    if constexpr (WIDE) {
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) wa[i] = widen<A_E5M2>(fa[i], 1.0f);
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) wb[j] = widen<false>(fb[j], 1.0f);
                     }
 #pragma unroll
-                    for (int i = 0; i < MT; ++i)
+                    for (int j = 0; j < NT; ++j) {
+                        v4f p[MT];
+                        if constexpr (WIDE) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[j][i][r] = fmaf(p[i][r] * sb[j][r], sa[i], acc[j][i][r]);
+                            for (int w = 0; w < 4; ++w)
+#pragma unroll
+                                for (int i = 0; i < MT; ++i)
+                                    p[i] = mfma_bf16(wb[j].part[w], wa[i].part[w], w == 0 ? v4f{0, 0, 0, 0} : p[i]);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) p[i] = mfma_plain<A_E5M2>(fb[j], fa[i]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < MT; ++i)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[j][i][r] = fmaf(p[i][r] * sb[j][r], sa[i], acc[j][i][r]);
+                    }
                 }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
+        };
+        walk(std::false_type{});
+        if constexpr (kE8M0Wide) {
+            const bool wild = __ballot(least < kWidenLeast << 23 || most > kWidenMost << 23) != 0;
+            if (lane == 0) wild_waves[wave] = wild;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            int any = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) any |= wild_waves[w];
+            if (__builtin_amdgcn_readfirstlane(any)) {                  // all of the workgroup: they bring the tiles together
+                clear();
+                walk(std::true_type{});
+            }
         }
     }
 

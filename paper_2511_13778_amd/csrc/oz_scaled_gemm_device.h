@@ -87,6 +87,29 @@ __device__ __forceinline__ v4f mfma_wide(const Wide& b, const Wide& a, v4f c) {
 }
 // An E8M0 scale as the conversion takes it: a float of that exponent.
 __device__ __forceinline__ float scale_float(uint32_t byte) { return __uint_as_float((byte & 0xFFu) << 23); }
+// Widening with a scale is exact while no element leaves bfloat16's normal numbers: elements lie in 2^-16 .. 1.75 2^15 (e5m2; e4m3's are
+// within), so exponents from -110 to 112 do.  Where another one turns up, or a NaN, operands are widened without scales and both are applied
+// to the sums (add_scaled): a sum's factor is a power of two, so that costs no precision, only time.
+constexpr uint32_t kWidenLeast = 127 - 110, kWidenMost = 127 + 112;
+// x, y: words of four scales, of which the lowest `blocks` count; by a whole wave.
+template <int M, int N>
+__device__ __forceinline__ bool widens_exactly(const uint32_t (&x)[M], const uint32_t (&y)[N], int blocks) {
+    static_assert(kWidenMost == 0xEF, "above are the bytes whose upper four bits are set");
+    uint32_t wild = 0;
+    // the top bit of a byte: below the least (of a word's first such byte), above the most
+    auto look = [&](uint32_t w) { wild |= ((w - kWidenLeast * 0x01010101u) & ~w) | (w & (w << 1) & (w << 2) & (w << 3)); };
+    const uint32_t there = blocks >= 4 ? 0xFFFFFFFFu : (1u << (8 * blocks)) - 1;
+#pragma unroll
+    for (int i = 0; i < M; ++i) look((x[i] & there) | (0x7F7F7F7Fu & ~there));
+#pragma unroll
+    for (int i = 0; i < N; ++i) look((y[i] & there) | (0x7F7F7F7Fu & ~there));
+    return __ballot((wild & 0x80808080u) != 0) == 0;
+}
+// c + p 2^(ea + eb): the product's exponent is applied at once, whatever the two are.
+__device__ __forceinline__ float add_scaled(float c, float p, uint32_t ea, uint32_t eb) {
+    const uint32_t a = ea & 0xFFu, b = eb & 0xFFu;
+    return c + (max(a, b) == 255 ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_ldexpf(p, int(a + b) - 254));
+}
 
 // The part of a call that a workgroup works on.  Offsets in bytes / elements are 64-bit, what is left inside a tile 32-bit.
 struct GemmTile {

@@ -69,6 +69,11 @@ __global__ __launch_bounds__(MT == 1 ? 1024 : 512) void scaled_gemm_few_kernel(S
                 for (int i = 0; i < MT; ++i) sa[u][i] = reinterpret_cast<const float*>(row_sa[i])[blk];
             }
         }
+        bool ordinary = true;                     // E8M0, widened
+        if constexpr (E8M0 && WIDE) {
+            const uint32_t of_b[1] = {eb};
+            ordinary = widens_exactly(ea, of_b, min(blocks - b0, kB));
+        }
 #pragma unroll
         for (int u = 0; u < kB; ++u) {
             if (b0 + u >= blocks) break;
@@ -86,9 +91,24 @@ __global__ __launch_bounds__(MT == 1 ? 1024 : 512) void scaled_gemm_few_kernel(S
 #pragma unroll
                 for (int i = 0; i < MT; ++i) acc[i] = mfma_e8m0<A_E5M2>(fb[u].f, fa[u][i].f, acc[i], eb >> (8 * u), ea[i] >> (8 * u));
             } else if constexpr (E8M0) {
-                const Wide wb = widen<false>(fb[u].f, scale_float(eb >> (8 * u)));
+                if (__builtin_expect(ordinary, 1)) {
+                    const Wide wb = widen<false>(fb[u].f, scale_float(eb >> (8 * u)));
 #pragma unroll
-                for (int i = 0; i < MT; ++i) acc[i] = mfma_wide(wb, widen<A_E5M2>(fa[u][i].f, scale_float(ea[i] >> (8 * u))), acc[i]);
+                    for (int i = 0; i < MT; ++i) acc[i] = mfma_wide(wb, widen<A_E5M2>(fa[u][i].f, scale_float(ea[i] >> (8 * u))), acc[i]);
+                } else {
+                    uint32_t each[4];             // B's scales of this lane's four results
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) each[r] = uint32_t(__shfl(int(eb >> (8 * u)), q * 4 + r));
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        float one = 1.0f;
+                        asm volatile("" : "+v"(one));
+                        const v4f p = mfma_wide(widen<false>(fb[u].f, one), widen<A_E5M2>(fa[u][i].f, one), v4f{0, 0, 0, 0});
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[i][r] = add_scaled(acc[i][r], p[r], ea[i] >> (8 * u), each[r]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
             } else {
                 v4f each;                     // B's scales of this lane's four results
 #pragma unroll

@@ -1,8 +1,11 @@
-"""Ends of the ranges of sizes and values: rows without columns, through the public calls."""
+"""Ends of the ranges of sizes and values: rows without columns, scales near the least and the largest, through the public calls."""
 import pytest
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
+
+import scaled_reference as ref  # noqa: E402
+from test_gpu_scaled import E4M3, E5M2, close, dense, gen  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -30,3 +33,92 @@ def test_weights_gradient_of_rows_without_columns(h, dtype):
     dxs, dw = ex.combine_backward(h, dy, xs, routing, w)
     assert dxs.shape == (6, 0) and torch.equal(dw, torch.zeros_like(dw))
     assert ex.combine(h, xs, routing, w).shape == (3, 0) and ex.gather(h, dy, routing).shape == (6, 0)
+
+
+# exponents of A's and of B's scales in one block of k: each at or near an end of what a byte holds, their products ordinary
+PAIRS = [(-127, 127), (127, -127), (0, 0), (-127, 112), (114, -126), (-112, 111), (119, -118), (-3, 2)]
+
+
+def far_apart(seed, m, n, k, a_type, down=0):
+    """A (m x k) and B (n x k) whose E8M0 scales differ a little from row to row and lie far out in most blocks; down: taken off the products."""
+    from paper_2511_13778_amd import scaled
+    r = gen(seed)
+    nb = -(-k // 128)
+    parts = []
+    for rows, dtype, side in ((m, a_type, 0), (n, E4M3, 1)):
+        x = torch.zeros((rows, -(-k // 16) * 16), device="cuda")
+        x[:, :k] = torch.randn((rows, k), generator=r, device="cuda") * (ref.TOP[dtype] / 8)
+        e = torch.tensor([PAIRS[(b + seed) % len(PAIRS)][side] for b in range(nb)], device="cuda")
+        e = (e + torch.randint(-1, 2, (rows, nb), generator=r, device="cuda") - (down if side else 0)).clamp(-127, 127)
+        s = torch.full((rows, -(-nb // 4) * 4), 255, dtype=torch.uint8, device="cuda")
+        s[:, :nb] = (e + 127).to(torch.uint8)
+        parts.append(scaled.Scaled(x.clamp(-ref.TOP[dtype], ref.TOP[dtype]).to(dtype), s, k))
+    return parts
+
+
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("a_type", [E4M3, E5M2])
+@pytest.mark.parametrize("m,n,k", [(1, 40, 1100), (20, 70, 1060), (60, 33, 260), (70, 150, 1100), (75, 121, 2432), (1143, 2782, 640), (1094, 3794, 1410), (3867, 3169, 652)])
+def test_scales_at_the_ends_of_a_byte(h, m, n, k, a_type, out):
+    # each kernel, whatever the result's type: a product whose two scales make an ordinary factor is an ordinary product
+    from paper_2511_13778_amd import scaled
+    a, b = far_apart(m + k, m, n, k, a_type)
+    da, db = dense(a), dense(b)
+    exact, size = da @ db.t(), da.abs() @ db.abs().t()
+    got = scaled.gemm(h, a, b, dtype=out)
+    close(got, exact, size, k)
+    c = torch.ones_like(got)
+    scaled.gemm(h, a, b, out=c, accumulate=True)
+    close(c, exact + 1, size + 1, k)
+
+
+def test_scales_at_the_ends_of_a_byte_in_float16(h):
+    from paper_2511_13778_amd import scaled
+    for m, n, k in ((5, 70, 1100), (130, 257, 1000)):
+        a, b = far_apart(m, m, n, k, E4M3, 14)
+        a.scale[:, :-(-k // 128)].clamp_(max=113)               # B's are held at -127: within float16's range
+        da, db = dense(a), dense(b)
+        close(scaled.gemm(h, a, b, dtype=torch.float16), da @ db.t(), da.abs() @ db.abs().t(), k)
+
+
+def test_one_element_and_its_scales(h):
+    # 16 2^125 times 1 2^-125 is 16, in every type; NaN scales stay NaN and zeros stay zero
+    from paper_2511_13778_amd import scaled
+    for rows in (1, 40, 90):
+        for ea, eb, x, want in ((125, -125, 16.0, 16.0), (-125, 125, 16.0, 16.0), (-127, 127, 2.0 ** -9, 2.0 ** -9), (127, -127, 448.0, 448.0), (127, 127, 0.0, 0.0),
+                                (-127, -127, 1.0, 0.0), (128, -100, 1.0, float("nan")), (127, -126, 64.0, 128.0)):
+            a, b = torch.zeros((rows, 128), device="cuda"), torch.zeros((rows, 128), device="cuda")
+            a[:, 77], b[:, 77] = x, 1.0
+            sa, sb = (torch.full((rows, 4), e + 127, dtype=torch.uint8, device="cuda") for e in (ea, eb))
+            for out in (torch.float32, torch.bfloat16, torch.float16):
+                got = scaled.gemm(h, scaled.Scaled(a.to(E4M3), sa), scaled.Scaled(b.to(E4M3), sb), dtype=out)
+                assert torch.equal(got.float().nan_to_num(nan=-1.0), torch.full((rows, rows), want, device="cuda").nan_to_num(nan=-1.0)), (rows, ea, eb, out)
+
+
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+def test_scales_at_the_ends_of_a_byte_in_groups(h, out):
+    from paper_2511_13778_amd import scaled
+    counts, n, k = [3, 0, 200, 40, 1], 150, 700
+    rows = sum(counts)
+    offsets = torch.tensor([sum(counts[:i]) for i in range(len(counts) + 1)], dtype=torch.int32, device="cuda")
+    a, b = far_apart(2, rows, n * len(counts), k, E4M3)
+    da, db = dense(a), dense(b).view(len(counts), n, k)
+    got = scaled.gemm_grouped(h, a, scaled.Scaled(b.data.view(len(counts), n, -1), b.scale.view(len(counts), n, -1), k), offsets, dtype=out)
+    for e, c in enumerate(counts):
+        s = slice(int(offsets[e]), int(offsets[e]) + c)
+        if c:
+            close(got[s], da[s] @ db[e].t(), da[s].abs() @ db[e].abs().t(), k)
+    # contraction in groups: the quantised transposes' scales are set to what is wanted
+    y, x = torch.randn((rows, 140), generator=gen(3), device="cuda"), torch.randn((rows, 260), generator=gen(4), device="cuda")
+    a, b = (scaled.quantize(h, v, which="columns", offsets=offsets) for v in (y, x))
+    for b_ in range(a.scale.shape[1]):
+        a.scale[:, b_], b.scale[:, b_] = PAIRS[b_ % len(PAIRS)][0] + 127, PAIRS[b_ % len(PAIRS)][1] + 127
+    da, db = dense(a), dense(b)
+    got = scaled.gemm_grouped_k(h, a, b, offsets, dtype=out)
+    at = 0
+    for e, c in enumerate(counts):
+        wide = -(-c // 128) * 128
+        pa, pb = da[:, at:at + c], db[:, at:at + c]
+        if c:
+            close(got[e], pa @ pb.t(), pa.abs() @ pb.abs().t(), c)
+        at += wide
