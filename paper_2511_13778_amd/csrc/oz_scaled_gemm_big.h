@@ -15,8 +15,8 @@
 // What bounds it: at 8192^3 (E8M0, 256 x 256) 367 to 407 us, 2.7 to 3.0 PFLOP/s, 1.03 to 1.15 of the library's product with one scale
 // for all, the power limit: the matrix unit is busy 72 % of the cycles at 2.1 GHz.  A tile's first loads and its results cost 9 us of about
 // 95, and nothing hides them: a workgroup that went on to its next tile's loads while it stored took 389 where this took 390 (float32
-// scales 645 against 620): its registers for two tiles' places slow the walk over k by as much.  float32 scales 607 to 633 us with one per
-// 128 rows of B, 732 to 774 with one per row: the vector ALU's multiply-adds.
+// scales 645 against 620): its registers for two tiles' places slow the walk over k by as much.  float32 scales 609 us with one per
+// 128 rows of B (587 with both scales multiplied first, which loses range), 684 to 774 with one per row.
 #pragma once
 
 #include "oz_scaled_gemm_device.h"
@@ -143,12 +143,13 @@ __global__ __launch_bounds__(256, 1) void scaled_gemm_big_kernel(ScaledGemm g, i
     };
 
     // ---- scales of the halves.  E8M0: four blocks' bytes, this step's in the low one.  float32: a row's, per fragment of A; of B
-    // one for all (kBlocks: already in A's factors), or a lane's four rows' per fragment.
+    // one for all (kBlocks: in A's factors and in the matrix instruction), or a lane's four rows' per fragment.
     typedef uint32_t v4u __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) const v4u* lds4_t;
     typedef __attribute__((address_space(3))) const uint32_t* lds1_t;
     typedef __attribute__((address_space(3))) const uint64_t* lds2_t;
-    v4u ea[2], eb[2], ea_new, eb_new;                          // E8M0; float32: A's (with kBlocks times B's), bit patterns
+    v4u ea[2], eb[2], ea_new, eb_new;                          // E8M0; float32: A's (with kBlocks times B's fraction), bit patterns
+    uint32_t eb_all[2] = {127, 127};                           // kBlocks: B's exponent, as a byte
     v4f sb[2][NB], sb_new[NB];                                 // kRows
     uint32_t b_new = 0;                                        // kBlocks
     uint32_t sc_at = 0;                                        // this step's part of LDS
@@ -183,8 +184,14 @@ __global__ __launch_bounds__(256, 1) void scaled_gemm_big_kernel(ScaledGemm g, i
             ea[ha] = ea_new >> sc_shift;
             eb[hb] = eb_new >> sc_shift;
         } else if constexpr (SC == Scales::kBlocks) {
+            // The product of the two scales may leave float32's range where the result does not: B's power of two goes into the matrix instruction,
+            // its fraction, below 1, to A's scale.
+            const float b = __uint_as_float(b_new);
+            const int e = min(max(__builtin_amdgcn_frexp_expf(b), -126), 127);
+            const float fraction = __builtin_amdgcn_ldexpf(b, -e);
+            eb_all[ha] = uint32_t(e + 127);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ea[ha][i] = live ? __float_as_uint(__uint_as_float(ea_new[i]) * __uint_as_float(b_new)) : 0;
+            for (int i = 0; i < 4; ++i) ea[ha][i] = live ? __float_as_uint(__uint_as_float(ea_new[i]) * fraction) : 0;
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) ea[ha][i] = live ? ea_new[i] : 0;
@@ -234,7 +241,8 @@ __global__ __launch_bounds__(256, 1) void scaled_gemm_big_kernel(ScaledGemm g, i
                 // before the first of a step lies the step that started with the other half
                 const int pb0 = px < 0 && h == 0 ? b1 : b0, phb = (ph == 0) == pfirst ? pb0 : 1 - pb0;
                 finish(ph, fi(pnew, py % kQ), phb, jf(pnew, py % kQ), made[(x - kLag) & 3]);
-                made[x & 3] = mfma_plain<A_E5M2>(fb[hb][j].f, fa[ha][i].f);
+                if constexpr (SC == Scales::kBlocks) made[x & 3] = mfma_e8m0<A_E5M2>(fb[hb][j].f, fa[ha][i].f, v4f{0, 0, 0, 0}, eb_all[ha], 127);
+                else made[x & 3] = mfma_plain<A_E5M2>(fb[hb][j].f, fa[ha][i].f);
                 asm volatile("" : "+v"(made[x & 3]));
             }
             __builtin_amdgcn_sched_barrier(0);

@@ -122,3 +122,48 @@ def test_scales_at_the_ends_of_a_byte_in_groups(h, out):
         if c:
             close(got[e], pa @ pb.t(), pa.abs() @ pb.abs().t(), c)
         at += wide
+
+
+def plain_scales(seed, rows, k, dtype, block_rows, exponents):
+    """A matrix with float32 scales of either sign: block b's are near 2^exponents[b]."""
+    from paper_2511_13778_amd import scaled
+    r = gen(seed)
+    x = torch.zeros((rows, -(-k // 16) * 16), device="cuda")
+    x[:, :k] = torch.randn((rows, k), generator=r, device="cuda") * (ref.TOP[dtype] / 8)
+    high = -(-rows // block_rows)
+    s = torch.rand((high, len(exponents)), generator=r, device="cuda") + 1
+    s *= torch.where(torch.rand(s.shape, generator=r, device="cuda") < 0.5, -1.0, 1.0)
+    s = (s.double() * ref.power(torch.tensor(exponents, device="cuda"))).float()
+    return scaled.Scaled(x.clamp(-ref.TOP[dtype], ref.TOP[dtype]).to(dtype), s, k, block_rows)
+
+
+@pytest.mark.parametrize("rows_b", [1, 128])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("m,n,k", [(5, 70, 300), (70, 150, 300), (75, 121, 2432), (1143, 2782, 640), (2183, 1893, 1425), (899, 4368, 1543)])
+def test_float32_scales_whose_product_leaves_the_range(h, m, n, k, out, rows_b):
+    # each kernel: scales that together are no float32, and results that are one
+    from paper_2511_13778_amd import scaled
+    unit, loss = {torch.bfloat16: (2.0 ** -8, 2.0 ** -14), torch.float32: (2.0 ** -23, (k + 128) * 2.0 ** -24)}[out]
+    nb = -(-k // 128)
+    # 2^-146 times sums of about 2^19: as precise as any
+    low = [-73] * nb
+    a, b = plain_scales(m, m, k, E4M3, 1, low), plain_scales(n, n, k, E4M3, rows_b, low)
+    da, db = dense(a), dense(b)
+    exact, size = da @ db.t(), da.abs() @ db.abs().t()
+    got = scaled.gemm(h, a, b, dtype=out)
+    assert ((got.double() - exact).abs() <= unit * exact.abs() + loss * size + 2.0 ** -133).all()
+    # 2^140 times zeros, and in one place times 2^-18; blocks beside them with ordinary scales
+    high = [70 if i % 3 == 1 else -4 for i in range(nb)]
+    a, b = plain_scales(m + 1, m, k, E5M2, 1, high), plain_scales(n + 1, n, k, E4M3, rows_b, high)
+    for x in (a, b):
+        for i in range(1, nb, 3):
+            x.data[:, i * 128:(i + 1) * 128] = torch.zeros((), device="cuda").to(x.data.dtype)
+    got = scaled.gemm(h, a, b, dtype=out)
+    da, db = dense(a), dense(b)
+    exact, size = da @ db.t(), da.abs() @ db.abs().t()
+    assert ((got.double() - exact).abs() <= unit * exact.abs() + loss * size).all()
+    a.data[m - 1, 130], b.data[n - 1, 130] = 2.0 ** -9, 2.0 ** -9
+    da, db = dense(a), dense(b)
+    got = scaled.gemm(h, a, b, dtype=out)[m - 1, n - 1].item()
+    exact = (da[m - 1] * db[n - 1]).sum().item()
+    assert 2.0 ** 120 < abs(exact) < 2.0 ** 125 and abs(got - exact) <= (unit + loss) * abs(exact)
