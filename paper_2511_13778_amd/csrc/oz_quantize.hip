@@ -80,6 +80,12 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
     return uint32_t(w);
 }
 
+// The lowest `have` bytes of word w of a run: what lies behind a row's end is zero also where the multiplier is NaN.
+__device__ __forceinline__ uint32_t bytes_there(int have, int w) {
+    const int n = min(max(have - 4 * w, 0), 4);
+    return n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1;
+}
+
 __device__ __forceinline__ int source_row(const int32_t* __restrict__ order, int div, int x_rows, int r) {
     if (!order) return r;
     const int o = order[r];
@@ -113,6 +119,10 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(RowArgs p) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
         w[i] = pack4<E5M2>(to_float(x.e[4 * i]) * mul, to_float(x.e[4 * i + 1]) * mul, to_float(x.e[4 * i + 2]) * mul, to_float(x.e[4 * i + 3]) * mul);
+    if (is_wild(top)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) w[i] &= bytes_there(have, i);
+    }
     uint8_t* out = p.out.data + int64_t(blockIdx.y) * p.out.stride + int64_t(r) * p.out.ld;
     if (col < ((p.cols + 15) & ~15)) *reinterpret_cast<uint2*>(out + col) = make_uint2(w[0], w[1]);
     const int64_t esize = p.e8m0 ? 1 : 4;
@@ -211,6 +221,7 @@ __global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
         const int r0 = row0 + g * R;
         uint8_t* out = p.by_rows.data + int64_t(blockIdx.z) * p.by_rows.stride + int64_t(r0) * p.by_rows.ld + col;
         const int last = col < ((p.cols + 15) & ~15) ? end - r0 : 0;
+        const uint32_t keep[2] = {bytes_there(have, 0), bytes_there(have, 1)};
         uint32_t mine = 0;                       // lane l < R: row l's
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -218,7 +229,7 @@ __global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
             if (l == i) mine = top;
             const float mul = multiplier<ROWS_E5M2>(top);
             auto at = [&](int j) { return to_float(x[i].e[j]) * mul; };
-            const uint2 w = make_uint2(pack4<ROWS_E5M2>(at(0), at(1), at(2), at(3)), pack4<ROWS_E5M2>(at(4), at(5), at(6), at(7)));
+            const uint2 w = make_uint2(pack4<ROWS_E5M2>(at(0), at(1), at(2), at(3)) & keep[0], pack4<ROWS_E5M2>(at(4), at(5), at(6), at(7)) & keep[1]);
             if (i < last) *reinterpret_cast<uint2*>(out + int64_t(i) * p.by_rows.ld) = w;
         }
         if (!SHARED && l < R && r0 + l < end) put_scale<ROWS_E5M2>(rscale, int64_t(r0 + l) * p.by_rows.scale_ld + tile_c, p.rows_e8m0, mine);
@@ -254,15 +265,17 @@ __global__ __launch_bounds__(2048 / R) void quantize_tiles_kernel(TileArgs p) {
         const uint4 v = SHARED ? make_uint4(shared_top, shared_top, shared_top, shared_top) : *reinterpret_cast<const uint4*>(&col_top[l * 8 + j]);
         tops[j] = v.x; tops[j + 1] = v.y; tops[j + 2] = v.z; tops[j + 3] = v.w;
     }
+    const int there = end - (row0 + g * R);
+    const uint32_t keep[2] = {bytes_there(there, 0), bytes_there(there, 1)};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const float mul = multiplier<COLS_E5M2>(tops[j]);
         auto at = [&](int i) { return to_float(x[i].e[j]) * mul; };
         uint8_t* to = turned + (l * 8 + j) * kScaleBlock;
         if constexpr (R == 8)
-            *reinterpret_cast<uint2*>(to + (g ^ l) * 8) = make_uint2(pack4<COLS_E5M2>(at(0), at(1), at(2), at(3)), pack4<COLS_E5M2>(at(R - 4), at(R - 3), at(R - 2), at(R - 1)));
+            *reinterpret_cast<uint2*>(to + (g ^ l) * 8) = make_uint2(pack4<COLS_E5M2>(at(0), at(1), at(2), at(3)) & keep[0], pack4<COLS_E5M2>(at(R - 4), at(R - 3), at(R - 2), at(R - 1)) & keep[1]);
         else
-            *reinterpret_cast<uint32_t*>(to + ((g >> 1) ^ l) * 8 + (g & 1) * 4) = pack4<COLS_E5M2>(at(0), at(1), at(2), at(3));
+            *reinterpret_cast<uint32_t*>(to + ((g >> 1) ^ l) * 8 + (g & 1) * 4) = pack4<COLS_E5M2>(at(0), at(1), at(2), at(3)) & keep[0];
     }
     __syncthreads();
     // columns to write: all 128 of a group's block, else what is there, up to a multiple of 16

@@ -167,3 +167,27 @@ def test_float32_scales_whose_product_leaves_the_range(h, m, n, k, out, rows_b):
     got = scaled.gemm(h, a, b, dtype=out)[m - 1, n - 1].item()
     exact = (da[m - 1] * db[n - 1]).sum().item()
     assert 2.0 ** 120 < abs(exact) < 2.0 ** 125 and abs(got - exact) <= (unit + loss) * abs(exact)
+
+
+@pytest.mark.parametrize("scale", [torch.uint8, torch.float32])
+@pytest.mark.parametrize("x_type", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(200, 300), (3, 5), (129, 131), (1, 250), (1300, 1301)])
+def test_padding_of_blocks_without_a_scale(h, rows, cols, x_type, scale):
+    # up to the next multiple of 16, and of 128 behind a group, bytes are zero also where an infinity or NaN makes the block NaN
+    from paper_2511_13778_amd import scaled
+    x = torch.randn((rows, cols), generator=gen(rows), device="cuda").to(x_type)
+    x[rows - 1, cols - 1] = float("inf")
+    x[0, cols - 1] = float("nan")
+    for dtype in (E4M3, E5M2):
+        for block_rows in (1, 128):
+            a, t = scaled.quantize(h, x, dtype, scale, block_rows, which="both")
+            for m in (a, t, scaled.quantize(h, x, dtype, scale, block_rows), scaled.quantize(h, x, dtype, scale, block_rows, which="columns")):
+                assert m.values().float().isnan().any()
+                assert not m.data[:, m.cols:].view(torch.uint8).any()
+    ends = torch.tensor([0, rows // 3, rows], dtype=torch.int32, device="cuda")
+    t = scaled.quantize(h, x, scale_dtype=scale, which="columns", offsets=ends)
+    data, at = t.data.view(torch.uint8), 0
+    for n in (rows // 3, rows - rows // 3):
+        wide = -(-n // 128) * 128
+        assert not data[:, at + n:at + wide].any() and (not n or (data[cols - 1, at:at + n] & 0x7F == 0x7F).any())
+        at += wide
