@@ -57,16 +57,20 @@ def check_ints(t, what, n=None):
 
 class Scaled:
     """An 8-bit matrix (rows x ld, or groups x rows x ld; the first `cols` columns count) and its scales ((rows / block_rows) x at
-    least ceil(cols / 128), for each group).  Rows start at multiples of 16 bytes; E8M0 scales' rows at multiples of 4."""
+    least ceil(cols / 128), for each group).  Rows start at multiples of 16 bytes; E8M0 scales' rows at multiples of 4.
+    data, scale, cols and block_rows may be set to others, which are checked as here."""
 
-    __slots__ = ("data", "scale", "cols", "block_rows", "desc")
+    # desc: what the C ABI takes, addresses and strides of the two tensors; made anew with them
+    __slots__ = ("_data", "_scale", "_cols", "_block_rows", "desc")
 
     def __init__(self, data, scale, cols=None, block_rows=1):
+        self._set(data, scale, data.shape[-1] if cols is None else cols, block_rows)
+
+    def _set(self, data, scale, cols, block_rows):
         if data.dtype not in _EIGHT or scale.dtype not in _SCALE:
             raise ValueError("8-bit floats with uint8, float8_e8m0fnu or float32 scales, not %s with %s" % (data.dtype, scale.dtype))
         if data.dim() not in (2, 3) or scale.dim() != data.dim() or not data.is_cuda or scale.device != data.device:
             raise ValueError("matrix and scales: two or three dimensions each, on one GPU")
-        cols = data.shape[-1] if cols is None else cols
         rows = data.shape[-2]
         if not 0 <= cols <= data.shape[-1] or block_rows not in (1, BLOCK):
             raise ValueError("cols %s of %d, block_rows %s" % (cols, data.shape[-1], block_rows))
@@ -74,7 +78,7 @@ class Scaled:
             raise ValueError("scales %s do not cover %d x %d" % (tuple(scale.shape), rows, cols))
         if (data.shape[-1] > 1 and data.stride(-1) != 1) or (scale.shape[-1] > 1 and scale.stride(-1) != 1):
             raise ValueError("rows of the matrix and of its scales are contiguous")
-        self.data, self.scale, self.cols, self.block_rows = data, scale, cols, block_rows
+        self._data, self._scale, self._cols, self._block_rows = data, scale, cols, block_rows
         groups = data.dim() == 3
         # a single row has no distance to the next one: what the ABI asks of it is taken
         ld = data.stride(-2) if rows > 1 else -(-data.shape[-1] // 16) * 16
@@ -82,37 +86,42 @@ class Scaled:
         self.desc = g.oz_scaled_t(data.data_ptr(), scale.data_ptr(), ld, sld, data.stride(0) if groups else 0,
                                   scale.stride(0) if groups else 0, _EIGHT[data.dtype], _SCALE[scale.dtype], block_rows, 0)
 
+    data = property(lambda self: self._data, lambda self, v: self._set(v, self._scale, self._cols, self._block_rows))
+    scale = property(lambda self: self._scale, lambda self, v: self._set(self._data, v, self._cols, self._block_rows))
+    cols = property(lambda self: self._cols, lambda self, v: self._set(self._data, self._scale, v, self._block_rows))
+    block_rows = property(lambda self: self._block_rows, lambda self, v: self._set(self._data, self._scale, self._cols, v))
+
     @property
     def rows(self):
-        return self.data.shape[-2]
+        return self._data.shape[-2]
 
     @property
     def groups(self):
-        return self.data.shape[0] if self.data.dim() == 3 else 1
+        return self._data.shape[0] if self._data.dim() == 3 else 1
 
     def values(self):
         """The 8-bit numbers, without padding."""
-        return self.data if self.data.shape[-1] == self.cols else self.data[..., :self.cols]
+        return self._data if self._data.shape[-1] == self._cols else self._data[..., :self._cols]
 
     def scales(self):
         """The scales, without padding."""
-        blocks = -(-self.cols // BLOCK)
-        return self.scale if self.scale.shape[-1] == blocks else self.scale[..., :blocks]
+        blocks = -(-self._cols // BLOCK)
+        return self._scale if self._scale.shape[-1] == blocks else self._scale[..., :blocks]
 
 
 def empty(rows, cols, block_rows=1, dtype=torch.float8_e4m3fn, scale_dtype=torch.uint8, groups=None, device="cuda") -> Scaled:
     """An uninitialised matrix in the layout that the calls here want."""
     ld, blocks, high = max(-(-cols // 16) * 16, 16), max(-(-cols // (4 * BLOCK)) * 4, 4), -(-rows // block_rows)
     m = Scaled.__new__(Scaled)          # sizes and types are right by construction
-    m.cols, m.block_rows = cols, block_rows
+    m._cols, m._block_rows = cols, block_rows
     if groups is None:
-        m.data = torch.empty((rows, ld), dtype=dtype, device=device)
-        m.scale = torch.empty((high, blocks), dtype=scale_dtype, device=device)
-        m.desc = g.oz_scaled_t(m.data.data_ptr(), m.scale.data_ptr(), ld, blocks, 0, 0, _EIGHT[dtype], _SCALE[scale_dtype], block_rows, 0)
+        m._data = torch.empty((rows, ld), dtype=dtype, device=device)
+        m._scale = torch.empty((high, blocks), dtype=scale_dtype, device=device)
+        m.desc = g.oz_scaled_t(m._data.data_ptr(), m._scale.data_ptr(), ld, blocks, 0, 0, _EIGHT[dtype], _SCALE[scale_dtype], block_rows, 0)
     else:
-        m.data = torch.empty((groups, rows, ld), dtype=dtype, device=device)
-        m.scale = torch.empty((groups, high, blocks), dtype=scale_dtype, device=device)
-        m.desc = g.oz_scaled_t(m.data.data_ptr(), m.scale.data_ptr(), ld, blocks, rows * ld, high * blocks, _EIGHT[dtype], _SCALE[scale_dtype],
+        m._data = torch.empty((groups, rows, ld), dtype=dtype, device=device)
+        m._scale = torch.empty((groups, high, blocks), dtype=scale_dtype, device=device)
+        m.desc = g.oz_scaled_t(m._data.data_ptr(), m._scale.data_ptr(), ld, blocks, rows * ld, high * blocks, _EIGHT[dtype], _SCALE[scale_dtype],
                                block_rows, 0)
     return m
 

@@ -191,3 +191,34 @@ def test_padding_of_blocks_without_a_scale(h, rows, cols, x_type, scale):
         wide = -(-n // 128) * 128
         assert not data[:, at + n:at + wide].any() and (not n or (data[cols - 1, at:at + n] & 0x7F == 0x7F).any())
         at += wide
+
+
+def test_attributes_of_a_matrix_are_what_products_read(h):
+    from paper_2511_13778_amd import scaled
+    r = gen(1)
+    x, y, w = (torch.randn(s, generator=r, device="cuda") for s in ((20, 300), (30, 300), (40, 300)))
+    for scale in (torch.uint8, torch.float32):
+        a, other, b = (scaled.quantize(h, t, scale_dtype=scale) for t in (x, y, w))
+        first, second = scaled.gemm(h, a, b, dtype=torch.float32), scaled.gemm(h, other, b, dtype=torch.float32)
+        old = a.scale
+        a.scale = old + 1 if scale == torch.uint8 else old * 2
+        assert torch.equal(scaled.gemm(h, a, b, dtype=torch.float32), 2 * first)
+        old.fill_(0)                                             # the tensor that was there before is no longer read
+        assert torch.equal(scaled.gemm(h, a, b, dtype=torch.float32), 2 * first)
+        for bad in (dict(data=a.data.float()), dict(scale=a.scale[:3]), dict(scale=a.scale.cpu()), dict(data=a.data.t()), dict(cols=1000), dict(block_rows=64)):
+            with pytest.raises(ValueError):
+                setattr(a, *next(iter(bad.items())))
+        assert torch.equal(scaled.gemm(h, a, b, dtype=torch.float32), 2 * first)      # a refusal changes nothing
+        a.scale = torch.cat((a.scale, a.scale))                  # more rows than there are, then the matrix that has them
+        a.data, a.scale = other.data, other.scale
+        assert torch.equal(scaled.gemm(h, a, b, dtype=torch.float32), second)
+        # a view with other strides, and fewer columns: what follows in a row is not read
+        a.data = torch.cat((other.data, other.data), 1)
+        assert torch.equal(scaled.gemm(h, a, b, dtype=torch.float32), second)
+        a.cols = b.cols = 128
+        part = [scaled.quantize(h, t[:, :128].contiguous(), scale_dtype=scale) for t in (y, w)]
+        assert torch.equal(scaled.gemm(h, a, b, dtype=torch.float32), scaled.gemm(h, *part, dtype=torch.float32))
+        made = scaled.empty(5, 128, scale_dtype=scale)
+        made.data, made.scale = a.data[:5], a.scale[:5]
+        made.cols = 128
+        assert torch.equal(scaled.gemm(h, made, b, dtype=torch.float32), scaled.gemm(h, *part, dtype=torch.float32)[:5])
