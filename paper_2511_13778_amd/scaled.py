@@ -147,6 +147,8 @@ def quantize(h: g.Handle, x, dtype=torch.float8_e4m3fn, scale_dtype=torch.uint8,
         groups, stride = None, 0
         ldx = check_matrix(x, "x")
         x_rows, cols = x.shape
+    if routing is not None and routing.tokens != x_rows:
+        raise ValueError("x has %d rows, the routing %d tokens" % (x_rows, routing.tokens))
     order, topk, rows = (None, 1, x_rows) if routing is None else (routing.order.data_ptr(), routing.topk, routing.order.numel())
     ends, sections = (None, 0) if offsets is None else (check_ints(offsets, "offsets").data_ptr(), offsets.numel() - 1)
     device = x.device

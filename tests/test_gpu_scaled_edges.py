@@ -222,3 +222,14 @@ def test_attributes_of_a_matrix_are_what_products_read(h):
         made.data, made.scale = a.data[:5], a.scale[:5]
         made.cols = 128
         assert torch.equal(scaled.gemm(h, made, b, dtype=torch.float32), scaled.gemm(h, *part, dtype=torch.float32)[:5])
+
+
+def test_routing_of_another_number_of_tokens(h):
+    from paper_2511_13778_amd import experts as ex, scaled
+    routing = ex.sort_tokens(h, torch.tensor([[0, 1], [1, 0], [2, 1]], device="cuda"), 3)
+    x = torch.randn((4, 130), device="cuda")
+    for rows in (2, 4, 0):
+        for which in ("rows", "columns", "both"):
+            with pytest.raises(ValueError):
+                scaled.quantize(h, x[:rows], which=which, routing=routing)
+    assert scaled.quantize(h, x[:3], routing=routing).rows == 6
