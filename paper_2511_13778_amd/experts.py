@@ -7,7 +7,7 @@ A layer whose tokens go to their chosen experts:
     ys = scaled.gemm_grouped(h, a, w, routing.offsets)
     y = combine(h, ys, routing, weights)
 
-Everything is enqueued on the current stream; nothing is read back, so no call waits for the GPU.
+Everything is enqueued on the current stream of the handle's GPU, where all tensors are; nothing is read back, so no call waits for the GPU.
 """
 from __future__ import annotations
 
@@ -15,7 +15,7 @@ import torch
 
 from . import ozdgemm as g
 from . import scaled
-from .scaled import check_ints, check_matrix, float_type, stream_of
+from .scaled import check_device, check_ints, check_matrix, float_type, stream_of
 
 
 class Routing:
@@ -28,6 +28,8 @@ class Routing:
         check_ints(offsets, "offsets")
         check_ints(order, "order")
         check_ints(place, "place", order.numel())
+        if offsets.device != order.device or place.device != order.device:
+            raise ValueError("offsets, order and place on one GPU, not %s, %s and %s" % (offsets.device, order.device, place.device))
         if topk < 1 or order.numel() % topk:
             raise ValueError("%d choices are not %s per token" % (order.numel(), topk))
         self.offsets, self.order, self.place, self.topk, self.tokens = offsets, order, place, topk, order.numel() // topk
@@ -37,6 +39,7 @@ def sort_tokens(h: g.Handle, ids, experts: int) -> Routing:
     """Sorts the choices ids (tokens x topk, int64 or int32) by expert, each expert's in their own order."""
     if not ids.is_cuda or ids.dim() != 2 or ids.shape[1] < 1 or ids.dtype not in (torch.int64, torch.int32) or not ids.is_contiguous():
         raise ValueError("ids: contiguous tokens x topk, int64 or int32, on the GPU")
+    check_device(h, ids)
     tokens, topk = ids.shape
     n = tokens * topk
     need = h.sort_tokens_workspace_bytes(tokens, topk, experts)
@@ -56,6 +59,7 @@ def sort_tokens(h: g.Handle, ids, experts: int) -> Routing:
 def gather(h: g.Handle, x, routing: Routing, out=None):
     """Each choice's row of x (tokens x cols), sorted by expert; zeros behind the last."""
     ldx = check_matrix(x, "x")
+    check_device(h, x, routing.order, out)
     if x.shape[0] != routing.tokens:
         raise ValueError("x has %d rows, the routing %d tokens" % (x.shape[0], routing.tokens))
     slots = routing.order.numel()
@@ -79,6 +83,7 @@ def _weights(weights, routing):
 def combine(h: g.Handle, xs, routing: Routing, weights=None, out=None):
     """Sum over each token's choices of weight * the choice's row of xs, in 32 bits, rounded once.  Without weights: the gradient of gather."""
     ldx = check_matrix(xs, "xs")
+    check_device(h, xs, routing.order, weights, out)
     if xs.shape[0] != routing.order.numel():
         raise ValueError("xs has %d rows, the routing %d slots" % (xs.shape[0], routing.order.numel()))
     y = torch.empty((routing.tokens, xs.shape[1]), dtype=xs.dtype, device=xs.device) if out is None else out
@@ -93,6 +98,7 @@ def combine(h: g.Handle, xs, routing: Routing, weights=None, out=None):
 def combine_backward(h: g.Handle, dy, xs, routing: Routing, weights):
     """Gradients of combine for dy (tokens x cols): (of xs, of the weights)."""
     lddy, ldx = check_matrix(dy, "dy"), check_matrix(xs, "xs")
+    check_device(h, dy, xs, routing.order, weights)
     if xs.shape != (routing.order.numel(), dy.shape[1]) or dy.shape[0] != routing.tokens or dy.dtype != xs.dtype:
         raise ValueError("dy %s %s and xs %s %s do not belong to this routing" % (tuple(dy.shape), dy.dtype, tuple(xs.shape), xs.dtype))
     dxs = torch.empty(xs.shape, dtype=xs.dtype, device=xs.device)

@@ -184,6 +184,7 @@ class Handle:
     def __init__(self, device: int = 0):
         self.lib = load_library()
         self._h = C.c_void_p()
+        self.device = device
         _check(self.lib.oz_create(C.byref(self._h), device), "oz_create")
 
     def close(self):

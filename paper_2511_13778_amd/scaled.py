@@ -11,7 +11,7 @@ C = A B^T, so a linear layer is
     d, dt = quantize(h, dy, dtype=torch.float8_e5m2, which="both")
     dx, dw = gemm(h, d, wt), gemm(h, dt, xt, dtype=torch.float32)
 
-Everything is enqueued on the current stream of the tensors' device; argument checks of the C ABI (include/ozdgemm.h) raise OzError, those
+Everything is enqueued on the current stream of the tensors' device, which is the handle's and the current one; argument checks of the C ABI (include/ozdgemm.h) raise OzError, those
 made here ValueError.  Calls marshal arguments and allocate outputs; the arithmetic is in the HIP kernels.
 """
 from __future__ import annotations
@@ -34,8 +34,16 @@ def float_type(dtype) -> int:
     return _FLOAT[dtype]
 
 
+def check_device(h, *tensors):
+    """All tensors (None: left out) are on the handle's GPU: kernels run there and may not reach another one's memory.  That it is the
+    current device as well is checked by the C ABI."""
+    for t in tensors:
+        if t is not None and t.get_device() != h.device:
+            raise ValueError("a tensor on %s, but the handle is of cuda:%d" % (t.device, h.device))
+
+
 def stream_of(t) -> int:
-    """The current stream of the tensor's device, which has to be the current device."""
+    """The current stream of the tensor's device."""
     return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
@@ -139,6 +147,7 @@ def quantize(h: g.Handle, x, dtype=torch.float8_e4m3fn, scale_dtype=torch.uint8,
         raise ValueError("which: rows, columns or both, not %r" % (which,))
     if dtype not in _EIGHT or scale_dtype not in _SCALE:
         raise ValueError("8-bit floats with uint8, float8_e8m0fnu or float32 scales, not %s with %s" % (dtype, scale_dtype))
+    check_device(h, x, offsets, *(() if routing is None else (routing.order,)))
     if x.dim() == 3:
         groups, stride = x.shape[0], x.stride(0)
         ldx = check_matrix(x[0], "x") if groups else x.shape[2]
@@ -185,6 +194,7 @@ def _check_product(a, b, groups):
 def gemm(h: g.Handle, a: Scaled, b: Scaled, dtype=torch.bfloat16, out=None, accumulate=False):
     """A B^T in `dtype` (or out's), summed in 32 bits; accumulate: added to `out`."""
     _check_product(a, b, 1)
+    check_device(h, a.data, out)
     m, n, k = a.data.shape[0], b.data.shape[-2], a.cols
     c = _output(a, (m, n), dtype, out, accumulate)
     need = h.scaled_gemm_workspace_bytes(m, n, k)
@@ -198,6 +208,7 @@ def gemm_grouped(h: g.Handle, a: Scaled, b: Scaled, offsets, dtype=torch.bfloat1
     """Rows offsets[g] .. offsets[g+1] of A times B_g^T, for every group; zeros behind the last."""
     groups = check_ints(offsets, "offsets").numel() - 1
     _check_product(a, b, groups)
+    check_device(h, a.data, offsets, out)
     c = _output(a, (a.rows, b.rows), dtype, out, False)
     h.call("oz_scaled_gemm_grouped", stream_of(c), groups, offsets.data_ptr(), a.rows, b.rows, a.cols, a.desc, b.desc, c.data_ptr(), _ld(c),
            float_type(c.dtype))
@@ -208,6 +219,7 @@ def gemm_grouped_k(h: g.Handle, a: Scaled, b: Scaled, offsets, dtype=torch.float
     """A_g B_g^T for every group (groups x rows of A x rows of B), A_g and B_g the group's columns as quantize(offsets=...) lays them out."""
     groups = check_ints(offsets, "offsets").numel() - 1
     _check_product(a, b, 1)
+    check_device(h, a.data, offsets, out)
     c = _output(a, (groups, a.rows, b.rows), dtype, out, accumulate)
     h.call("oz_scaled_gemm_grouped_k", stream_of(c), groups, offsets.data_ptr(), a.rows, b.rows, a.cols, a.desc, b.desc, c.data_ptr(),
            _ld(c), c.stride(0) if groups > 1 else a.rows * _ld(c), float_type(c.dtype), int(accumulate))
