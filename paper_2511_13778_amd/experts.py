@@ -95,17 +95,17 @@ def combine(h: g.Handle, xs, routing: Routing, weights=None, out=None):
     return y
 
 
-def combine_backward(h: g.Handle, dy, xs, routing: Routing, weights):
-    """Gradients of combine for dy (tokens x cols): (of xs, of the weights)."""
+def combine_backward(h: g.Handle, dy, xs, routing: Routing, weights=None):
+    """Gradients of combine for dy (tokens x cols): (of xs, of the weights or None where there are none)."""
     lddy, ldx = check_matrix(dy, "dy"), check_matrix(xs, "xs")
     check_device(h, dy, xs, routing.order, weights)
     if xs.shape != (routing.order.numel(), dy.shape[1]) or dy.shape[0] != routing.tokens or dy.dtype != xs.dtype:
         raise ValueError("dy %s %s and xs %s %s do not belong to this routing" % (tuple(dy.shape), dy.dtype, tuple(xs.shape), xs.dtype))
     dxs = torch.empty(xs.shape, dtype=xs.dtype, device=xs.device)
-    dw = torch.empty(weights.shape, dtype=torch.float32, device=xs.device)
+    dw = None if weights is None else torch.empty(weights.shape, dtype=torch.float32, device=xs.device)
     h.call("oz_combine_rows_grad", stream_of(dy), routing.tokens, routing.topk, dy.shape[1], float_type(dy.dtype), dy.data_ptr(), lddy,
            xs.data_ptr(), ldx, xs.shape[0], routing.order.data_ptr(), routing.place.data_ptr(), _weights(weights, routing), dxs.data_ptr(),
-           max(dxs.shape[1], 1), dw.data_ptr())
+           max(dxs.shape[1], 1), None if dw is None else dw.data_ptr())
     return dxs, dw
 
 

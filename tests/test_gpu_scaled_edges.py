@@ -233,3 +233,15 @@ def test_routing_of_another_number_of_tokens(h):
             with pytest.raises(ValueError):
                 scaled.quantize(h, x[:rows], which=which, routing=routing)
     assert scaled.quantize(h, x[:3], routing=routing).rows == 6
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_of_combine_without_weights(h, dtype):
+    # the rows' gradient as with weights of one, and none of weights that there are not
+    from paper_2511_13778_amd import experts as ex
+    ids = torch.randint(-1, 4, (33, 3), generator=gen(2), device="cuda")
+    routing = ex.sort_tokens(h, ids, 4)
+    dy, xs = torch.randn((33, 70), generator=gen(3), device="cuda").to(dtype), torch.randn((99, 70), generator=gen(4), device="cuda").to(dtype)
+    want, _ = ex.combine_backward(h, dy, xs, routing, torch.ones((33, 3), device="cuda"))
+    for got, dw in (ex.combine_backward(h, dy, xs, routing), ex.combine_backward(h, dy, xs, routing, None)):
+        assert torch.equal(got, want) and dw is None
