@@ -7,6 +7,7 @@ A layer whose tokens go to their chosen experts:
     ys = scaled.gemm_grouped(h, a, w, routing.offsets)
     y = combine(h, ys, routing, weights)
 
+Gradients are calls too (combine without weights is gather's, combine_backward is combine's): results carry no history for torch's autograd.
 Everything is enqueued on the current stream of the handle's GPU, where all tensors are; nothing is read back, so no call waits for the GPU.
 """
 from __future__ import annotations
@@ -124,8 +125,8 @@ class ExpertLayer:
         self.prepare_weights()
 
     def prepare_weights(self):
-        self.q1, self.q1t = scaled.quantize(self.h, self.w1, scale_dtype=self.scale_dtype, block_rows=128, which="both")
-        self.q2, self.q2t = scaled.quantize(self.h, self.w2, scale_dtype=self.scale_dtype, block_rows=128, which="both")
+        self.q1, self.q1t = scaled.quantize(self.h, self.w1.detach(), scale_dtype=self.scale_dtype, block_rows=128, which="both")
+        self.q2, self.q2t = scaled.quantize(self.h, self.w2.detach(), scale_dtype=self.scale_dtype, block_rows=128, which="both")
 
     def serve(self, x, ids, weights):
         """y for tokens x (tokens x width) without anything kept for gradients."""

@@ -12,11 +12,13 @@ C = A B^T, so a linear layer is
     dx, dw = gemm(h, d, wt), gemm(h, dt, xt, dtype=torch.float32)
 
 Everything is enqueued on the current stream of the tensors' device, which is the handle's and the current one; argument checks of the C ABI (include/ozdgemm.h) raise OzError, those
-made here ValueError.  Calls marshal arguments and allocate outputs; the arithmetic is in the HIP kernels.
+made here ValueError.  Results carry no history for torch's autograd: a gradient is a call of its own, as above, and an argument that requires
+one draws a warning.  Calls marshal arguments and allocate outputs; the arithmetic is in the HIP kernels.
 """
 from __future__ import annotations
 
 import ctypes as C
+import warnings
 
 import torch
 
@@ -36,10 +38,14 @@ def float_type(dtype) -> int:
 
 def check_device(h, *tensors):
     """All tensors (None: left out) are on the handle's GPU: kernels run there and may not reach another one's memory.  That it is the
-    current device as well is checked by the C ABI."""
+    current device as well is checked by the C ABI.  Warns of gradients that would be lost."""
     for t in tensors:
-        if t is not None and t.get_device() != h.device:
-            raise ValueError("a tensor on %s, but the handle is of cuda:%d" % (t.device, h.device))
+        if t is not None:
+            if t.get_device() != h.device:
+                raise ValueError("a tensor on %s, but the handle is of cuda:%d" % (t.device, h.device))
+            if t.requires_grad and torch.is_grad_enabled():
+                warnings.warn("an argument requires gradients, but the result carries no history: call the operator's gradient yourself, "
+                              "and this under torch.no_grad() or on detach()", stacklevel=3)
 
 
 def stream_of(t) -> int:

@@ -245,3 +245,21 @@ def test_gradients_of_combine_without_weights(h, dtype):
     want, _ = ex.combine_backward(h, dy, xs, routing, torch.ones((33, 3), device="cuda"))
     for got, dw in (ex.combine_backward(h, dy, xs, routing), ex.combine_backward(h, dy, xs, routing, None)):
         assert torch.equal(got, want) and dw is None
+
+
+def test_layer_of_parameters_gives_its_gradients_by_itself(h):
+    import warnings
+    from paper_2511_13778_amd import experts as ex
+    r = gen(6)
+    w1, w2 = torch.randn((3, 40, 30), generator=r, device="cuda"), torch.randn((3, 30, 40), generator=r, device="cuda")
+    x, dy = (torch.randn((20, 30), generator=r, device="cuda").bfloat16() for _ in range(2))
+    ids, p = torch.randint(0, 3, (20, 2), generator=r, device="cuda"), torch.rand((20, 2), generator=r, device="cuda")
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        plain, held = ex.ExpertLayer(h, w1, w2), ex.ExpertLayer(h, torch.nn.Parameter(w1), torch.nn.Parameter(w2))
+        results = []
+        for layer in (plain, held):
+            y, kept = layer.forward(x, ids, p)
+            results.append((y, *layer.backward(dy, kept)))
+    for a, b in zip(*results):
+        assert torch.equal(a, b) and not b.requires_grad

@@ -67,3 +67,29 @@ def test_tensors_on_another_gpu(monkeypatch):
             d = ["cuda:1" if i == odd else "cuda:0" for i in range(3)]
             with pytest.raises(ValueError):
                 ex.Routing(made(i32, d[0], 4), made(i32, d[1], 6), made(i32, d[2], 3, 2), 2)
+
+
+@pytest.mark.filterwarnings("ignore:Accessing the data pointer")
+def test_lost_gradients_are_told(monkeypatch):
+    # every floating-point argument that a gradient would flow to; not where none is recorded anyway
+    import warnings
+    from paper_2511_13778_amd import experts as ex, scaled
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    h, f32, d = Nowhere(), torch.float32, "cuda:0"
+    with FakeTensorMode():
+        r = routing_on(d)
+        xs, x, w = made(f32, d, 6, 8), made(f32, d, 3, 8), made(f32, d, 3, 2)
+        calls = [(lambda x: scaled.quantize(h, x), x), (lambda x: scaled.quantize(h, x, which="both", routing=r), x), (lambda x: ex.gather(h, x, r), x),
+                 (lambda xs, w: ex.combine(h, xs, r, w), xs, w), (lambda dy, xs, w: ex.combine_backward(h, dy, xs, r, w), x, xs, w)]
+        for call, *args in calls:
+            for asked in range(len(args)):
+                given = [a.detach().requires_grad_(i == asked) for i, a in enumerate(args)]
+                with pytest.warns(UserWarning, match="requires gradients") as seen, pytest.raises(AssertionError, match="enqueued"):
+                    call(*given)
+                assert all(s.filename == __file__ for s in seen if "requires gradients" in str(s.message))
+                with warnings.catch_warnings():
+                    warnings.filterwarnings("error", message=".*requires gradients")
+                    with torch.no_grad(), pytest.raises(AssertionError, match="enqueued"):
+                        call(*given)
+                    with pytest.raises(AssertionError, match="enqueued"):
+                        call(*args)
