@@ -274,13 +274,16 @@ oz_status_t oz_native_dgemm(oz_handle_t handle, void* stream, char transa, char 
  * 128 along the contraction, as language models are trained and served with.  Conventions of this part:
  *   - Matrices are row-major with the contraction contiguous: a product is C = A * B^T with A m x k, B n x k, C m x n.
  *   - Device pointers owned by the caller, work enqueued on `stream`, nothing allocated, nothing synchronised, as above.
- *   - Sizes of zero are no errors.  Limits: rows and columns <= 2^24, bytes per row < 2^23, groups <= 1024, choices < 2^30.
+ *   - Sizes of zero are no errors.  Limits, beyond which calls return OZ_ERR_ARG: rows and columns <= 2^24; of 8-bit matrices bytes per row
+ *     < 2^23 and scales per row < 2^17; leading dimensions of the others <= 2^32 elements; groups <= 1024, choices < 2^30.  Some
+ *     calls name more.
  *   - offsets: device int32[groups + 1], ascending from 0 to at most the number of rows: rows offsets[g] .. offsets[g+1] - 1
  *     are group g's.  Groups may be empty. */
 typedef enum { OZ_F32 = 0, OZ_BF16 = 1, OZ_F16 = 2, OZ_E4M3 = 3, OZ_E5M2 = 4, OZ_E8M0 = 5 } oz_type_t;
 
 /* A matrix of 8-bit floats with its scales: element (r, c) stands for data * scale of block (r / block_rows, c / 128).
- * OZ_E8M0 scales are bytes b for 2^(b-127), 255 for NaN: the matrix unit applies them itself.  OZ_F32 scales may have any value. */
+ * OZ_E8M0 scales are bytes b for 2^(b-127), 255 for NaN: the matrix unit applies them itself.  OZ_F32 scales may have any value; a block's
+ * sum is multiplied by B's, then by A's, in 32 bits. */
 typedef struct {
     void* data;           /* (r, c) at r*ld + c; 16-byte aligned */
     void* scale;          /* (i, b) at i*scale_ld + b; 4-byte aligned */
@@ -303,13 +306,19 @@ typedef struct {
  *     or the row is not there.
  *   offsets (may be NULL; batch 1, block_rows 1): the columns of by_columns are cut into groups: group g's rows of X become columns from
  *     128 * sum_{g' < g} ceil(count_g' / 128) on, zeros up to the next multiple of 128; rows behind the last group are left out.
- *     by_columns needs ld >= 128 * w and scale_ld >= w with w = floor((rows + 127 * min(groups, rows)) / 128). */
+ *     by_columns needs ld >= 128 * w and scale_ld >= w with w = floor((rows + 127 * min(groups, rows)) / 128).
+ * Limits: cols < 2^22, rows * ceil(cols / 128) <= 2^27, batch <= 65535. */
 oz_status_t oz_quantize(oz_handle_t handle, void* stream, int64_t rows, int64_t cols, const void* X, int64_t ldx, int32_t x_type,
                         int64_t batch, int64_t stride_x, const int32_t* order, int64_t order_div, int64_t x_rows,
                         const int32_t* offsets, int64_t groups, const oz_scaled_t* by_rows, const oz_scaled_t* by_columns);
 
 /* C = A B^T (+ C if accumulate), C row-major m x n in OZ_F32, OZ_BF16 or OZ_F16, ldc in elements.  A in OZ_E4M3 or OZ_E5M2, B in OZ_E4M3;
- * both with scales of one type.  Sums are held in 32 bits and rounded once.  k == 0: C = 0, or C as it is.
+ * both with scales of one type.  k == 0: C = 0, or C as it is.
+ * Sums are held in 32 bits and rounded once to C's type.  For OZ_F32 that is all; for OZ_BF16 and OZ_F16 the 8-bit matrix instruction first adds
+ * products by eights (k = 8i .. 8i + 7) and cuts each off, towards zero, at 2^-13 of the largest of the eight.  On data of one order of
+ * magnitude that is 1.4e-5 of the result, far below its rounding; where large products cancel within an eight, ask for OZ_F32.
+ * Limits: ceil(m / 64) * ceil(n / 64) < 2^24, with up to 64 rows (per group on average) ceil(m / 16) * ceil(n / 16) < 2^22; with groups of
+ * rows, groups + 1 more in the first factor.
  * workspace: 256-byte aligned, oz_scaled_gemm_workspace_bytes(...) bytes (0: may be NULL): parts of a k that is cut where the output alone
  * leaves the GPU idle, added in their order. */
 size_t oz_scaled_gemm_workspace_bytes(oz_handle_t handle, int64_t m, int64_t n, int64_t k);
@@ -338,17 +347,18 @@ oz_status_t oz_sort_tokens(oz_handle_t handle, void* stream, int64_t tokens, int
                            int32_t id_bytes, int32_t* offsets, int32_t* order, int32_t* place, void* workspace, size_t workspace_bytes);
 
 /* Y[place[t * topk + j]] = X[t] for every choice that has a place: rows of `cols` values sorted by expert; rows s of Y (tokens * topk of
- * them) with order[s] negative become zero.  type of X and Y: OZ_F32, OZ_BF16 or OZ_F16.  topk <= 64. */
+ * them) with order[s] negative become zero.  type of X and Y: OZ_F32, OZ_BF16 or OZ_F16.  topk <= 64.
+ * Limits: tokens * ceil(cols * bytes / 4096) <= 2^26 - 4. */
 oz_status_t oz_gather_rows(oz_handle_t handle, void* stream, int64_t tokens, int64_t topk, int64_t cols, int32_t type, const void* X,
                            int64_t ldx, const int32_t* order, const int32_t* place, void* Y, int64_t ldy);
 
 /* Y[t] = sum_j weights[t * topk + j] * X[place[t * topk + j]], j ascending, in 32 bits, rounded once; choices without a row in X (slots rows)
- * are left out.  weights NULL: all 1 (the gradient of oz_gather_rows).  topk <= 64. */
+ * are left out.  weights NULL: all 1 (the gradient of oz_gather_rows).  topk <= 64.  Limits: tokens * ceil(cols / 512) <= 2^26 - 4. */
 oz_status_t oz_combine_rows(oz_handle_t handle, void* stream, int64_t tokens, int64_t topk, int64_t cols, int32_t type, const void* X,
                             int64_t ldx, int64_t slots, const int32_t* place, const float* weights, void* Y, int64_t ldy);
 
 /* Gradients of oz_combine_rows: dX[place] = weight * dY[t], rows of slots that no choice has (order[s] negative) zero; dweights = <dY[t],
- * X[place]>, 0 for dropped choices.  dweights NULL, or weights NULL: not computed, or 1. */
+ * X[place]>, 0 for dropped choices.  dweights NULL, or weights NULL: not computed, or 1.  Limits: slots <= 2^26 - 4. */
 oz_status_t oz_combine_rows_grad(oz_handle_t handle, void* stream, int64_t tokens, int64_t topk, int64_t cols, int32_t type, const void* dY,
                                  int64_t lddy, const void* X, int64_t ldx, int64_t slots, const int32_t* order, const int32_t* place,
                                  const float* weights, void* dX, int64_t lddx, float* dweights);

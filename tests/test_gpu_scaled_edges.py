@@ -263,3 +263,32 @@ def test_layer_of_parameters_gives_its_gradients_by_itself(h):
             results.append((y, *layer.backward(dy, kept)))
     for a, b in zip(*results):
         assert torch.equal(a, b) and not b.requires_grad
+
+
+def test_limits_that_the_header_names(h):
+    # one step past each; refused on the host, before any address is used
+    from paper_2511_13778_amd import ozdgemm as g
+    big, some = 1 << 24, torch.zeros(64, dtype=torch.int32, device="cuda")
+    at = some.data_ptr()
+
+    def m(ld, scale_ld=4, scale=g.OZ_E8M0):
+        return g.oz_scaled_t(at, at, ld, scale_ld, 0, 0, g.OZ_E4M3, scale, 1, 0)
+
+    def quantize(rows, cols, batch=1, ldx=None, groups=None):
+        return ("oz_quantize", 0, rows, cols, at, cols if ldx is None else ldx, g.OZ_BF16, batch, 0, None, 1, 1, None if groups is None else at, groups or 0,
+                m(-(-cols // 16) * 16, -(-cols // 512) * 4), None)
+
+    def gemm(rows, cols, k=128, ldc=None, a=None):
+        return ("oz_scaled_gemm", 0, rows, cols, k, a or m(128), m(128), at, cols if ldc is None else ldc, g.OZ_BF16, 0, None, 0)
+    calls = [quantize(1, 1 << 22), quantize(big, 9 * 128), quantize(1, 16, 65536), quantize(1, 16, ldx=(1 << 32) + 1), quantize(1, 16, groups=1025),
+             quantize(big + 1, 16), gemm(big, 4096), gemm(64, big), gemm(big + 1, 1), gemm(1, 1, ldc=(1 << 32) + 1), gemm(1, 1, a=m(1 << 23)),
+             gemm(1, 1, a=m(128, 1 << 17)),
+             ("oz_scaled_gemm_grouped", 0, 1025, at, 1, 1, 1, m(16), m(16), at, 1, g.OZ_BF16),
+             ("oz_gather_rows", 0, 1 << 26, 1, 8, g.OZ_BF16, at, 8, at, at, at, 8), ("oz_combine_rows", 0, 1 << 26, 1, 8, g.OZ_BF16, at, 8, 1 << 26, at, None, at, 8),
+             ("oz_combine_rows_grad", 0, 1 << 26, 1, 8, g.OZ_BF16, at, 8, at, 8, 1 << 26, at, at, None, at, 8, None),
+             ("oz_sort_tokens", 0, 1 << 29, 2, 4, at, 4, at, at, at, None, 0)]
+    for name, *args in calls:
+        with pytest.raises(g.OzError) as e:
+            h.call(name, *args)
+        assert e.value.status == 1, (name, args)
+    torch.cuda.synchronize()
