@@ -2,8 +2,8 @@
 //
 // Time of a route, in us:  3 + steps * (rounds of a full CU, and what is left) + each * c,  c = tiles / compute units, rounded up: a step of
 // 128 of k takes `per` for each of the tiles that a CU has at a time (its matrix unit and LDS are shared), but no less than a lone
-// tile takes, and a tile's first loads and its results cost `each`.  The constants are fits to times measured over 19 sizes from 256 x 1000 x 1000 to 8192^3 (within 10 % where a
-// route is the best one).  Tiles of 256 x 256 need the fewest bytes per operation and win on large outputs (8192^3 402 us, 256 x 128 462,
+// tile takes, and a tile's first loads and its results cost `each`.  The constants are fits to times measured at twelve sizes from 256 x 1000 x 1000 to 8192^3: where a route
+// is the best one within 13 % from 17 us on, up to 28 % too long for calls under 10 us, where the choice loses 3 %.  Tiles of 256 x 256 need the fewest bytes per operation and win on large outputs (8192^3 402 us, 256 x 128 462,
 // 128 x 128 556), those of 128 x 128 and 64 x 64, several to a CU, overlap one's results with another's products and win on
 // short k and where larger ones leave CUs idle (8192 x 8192 x 512 56 us, 256 x 256 62; 1024^3 6.2 us in 64 x 64, 9.6 in 128 x 128).
 // 64 x 64 tiles that are alone on their CU take four stages: from memory two wait for each step's loads (200 x 2048 x 2048 15.2 us, with four 9.8,
@@ -52,6 +52,7 @@ inline double route_time(int kind, int route, int64_t m, int64_t n, int64_t bloc
 }
 
 // Rows of A that share a read of B, on average, up to which that read is what counts.
+// (With groups the average decides: a group with many more rows reads its B once per 16, 32 or 64 of them.)
 constexpr int kFewRows = 64;
 
 // A product without groups may be cut along k: into how many parts is decided by its sizes alone, because the workspace is.

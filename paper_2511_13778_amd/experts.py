@@ -116,7 +116,11 @@ class ExpertLayer:
 
     w1 (experts x inner x width) and w2 (experts x width x inner) are the caller's, in any float type; prepare_weights() makes their 8-bit
     copies, for the forward products and, transposed, for the input gradients, and is called again when they have changed.  Only silu
-    and its derivative are torch's."""
+    and its derivative are torch's.
+
+    The experts' rows between the second product and combine have x's type, as the activations between the products have before they are
+    quantised: half the bytes of float32 at the price of one more rounding of each (with bfloat16 2^-9, against the 2^-4 of an element in
+    8 bits).  The products alone can be asked for float32 rows, which combine then adds as they are."""
 
     def __init__(self, h: g.Handle, w1, w2, scale_dtype=torch.uint8):
         if w1.dim() != 3 or w2.shape != (w1.shape[0], w1.shape[2], w1.shape[1]):
