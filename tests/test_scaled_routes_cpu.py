@@ -64,3 +64,18 @@ def test_large_tiles_see_odd_and_even_steps_and_ragged_ends():
         assert {b for b, _ in blocks} == {0, 1} and {w for _, w in blocks} == {True, False}, label
         steps = {-(-c // 128) for counts, *_ in sr.CONTRACTION[label] for c in counts}
         assert {0, 1} <= steps and any(s > 2 and s % 2 for s in steps)
+
+
+def test_registers_leave_room_for_the_workgroups_that_a_cu_holds(tmp_path):
+    # a SIMD has 512: two workgroups of 128 x 128 tiles, four of 64 x 64 in two stages, sixteen waves of one few-row workgroup; nothing in memory
+    from test_streaming_isa import resources
+    most = {"scaled_gemm_kernelILi128E": 256, "scaled_gemm_kernelILi64ELi64ELi32ELi32ELi2E": 128, "scaled_gemm_kernelILi64ELi64ELi32ELi32ELi4E": 256,
+            "scaled_gemm_few_kernelILi1E": 128, "scaled_gemm_few_kernelILi2E": 256, "scaled_gemm_few_kernelILi4E": 256}
+    seen = set()
+    for source in ("oz_scaled_gemm", "oz_scaled_gemm_few"):
+        for name, (registers, scratch) in resources(source, tmp_path).items():
+            for part, limit in most.items():
+                if part in name:
+                    seen.add(part)
+                    assert registers <= limit and scratch == 0, (name, registers, scratch)
+    assert seen == set(most)
