@@ -6,7 +6,7 @@
 // The scale is a power of two because a floating-point value keeps its relative precision under one: x 2^-e is exact, so the
 // conversion to 8 bits is the only rounding, and the matrix unit can apply the scale itself.  e comes from a's exponent field
 // and whether its fraction is above 0.75.  What bounds it: memory; each input is read once, also where rows and columns of it
-// are wanted.  4100 x 8192 of bfloat16: its rows 18.9 us (5.3 TB/s), both ways 27 us with operands in the last-level cache (5.0 TB/s), 37
+// are wanted.  4100 x 8192 of bfloat16: its rows 18.9 us (5.3 TB/s), both ways 28 us with operands in the last-level cache (4.9 TB/s), 38
 // from memory: 2112 tiles of one load and one store phase each are little more than a round of the chip, which ends unevenly.
 // 16 x 4096: 2.4 us, the launch.
 #include "oz_scaled_device.h"

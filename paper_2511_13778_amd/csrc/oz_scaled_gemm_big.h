@@ -13,10 +13,10 @@
 // share a scale (one factor per row of A then), eight where each has its own.
 //
 // What bounds it: at 8192^3 (E8M0, 256 x 256) 367 to 407 us, 2.7 to 3.0 PFLOP/s, 1.03 to 1.15 of the library's product with one scale
-// for all, the power limit: the matrix unit is busy 72 % of the cycles at 2.1 GHz.  A tile's first loads and its results cost 9 us of about
+// for all, the power limit: the matrix unit is busy 72 % of the cycles at 2.0 to 2.1 GHz.  A tile's first loads and its results cost 9 us of about
 // 95, and nothing hides them: a workgroup that went on to its next tile's loads while it stored took 389 where this took 390 (float32
-// scales 645 against 620): its registers for two tiles' places slow the walk over k by as much.  float32 scales 609 us with one per
-// 128 rows of B (587 with both scales multiplied first, which loses range), 684 to 774 with one per row.  There the matrix unit is busy 39 and
+// scales 645 against 620): its registers for two tiles' places slow the walk over k by as much.  float32 scales 609 to 651 us with one
+// per 128 rows of B (3 to 4 % less with both scales multiplied first, which loses range), 684 to 774 with one per row.  There the matrix unit is busy 39 and
 // 34 % of the cycles, vector instructions (matrix ones among them) are issued in 34 and 46 %, and waves wait in 23 and 21 %: with one wave
 // per SIMD these add up, which of the waits could go is not known.  LDS is active 40 % (E8M0) and 30 to 32 %.
 #pragma once
