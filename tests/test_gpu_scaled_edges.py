@@ -1,4 +1,5 @@
-"""Ends of the ranges of sizes and values: rows without columns, scales near the least and the largest, through the public calls."""
+"""Ends of the ranges of sizes and values (rows without columns, scales near the least and the largest, padding of blocks without a scale, limits), what
+calls do with the matrices, routings and weights that they are given, and captured calls, through the public calls."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -292,3 +293,39 @@ def test_limits_that_the_header_names(h):
             h.call(name, *args)
         assert e.value.status == 1, (name, args)
     torch.cuda.synchronize()
+
+
+def test_captured_calls_replay_like_eager_ones(h):
+    # a layer served, a cut k with its planes, a sort in two launches and its gradients: replayed with other inputs, eager work in between
+    from paper_2511_13778_amd import experts as ex, scaled
+    r = gen(9)
+    layer = ex.ExpertLayer(h, torch.randn((6, 90, 70), generator=r, device="cuda"), torch.randn((6, 70, 90), generator=r, device="cuda"))
+    w = scaled.quantize(h, torch.randn((300, 9000), generator=r, device="cuda"), block_rows=128)
+
+    def fresh():
+        return (torch.randn((2500, 70), generator=r, device="cuda").bfloat16(), torch.randint(-1, 6, (2500, 2), generator=r, device="cuda"),
+                torch.rand((2500, 2), generator=r, device="cuda"), torch.randn((100, 9000), generator=r, device="cuda").bfloat16())
+
+    def work(x, ids, p, long):
+        routing = ex.sort_tokens(h, ids, 6)
+        xs = ex.gather(h, x, routing)
+        dxs, dp = ex.combine_backward(h, x, xs, routing, p)
+        return (layer.serve(x, ids, p), xs, dxs, dp, scaled.gemm(h, scaled.quantize(h, long), w), scaled.gemm(h, scaled.quantize(h, long), w, dtype=torch.float32))
+    held = fresh()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        work(*held)
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = work(*held)
+    for _ in range(5):
+        now = fresh()
+        want = work(*now)
+        for to, new in zip(held, now):
+            to.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
