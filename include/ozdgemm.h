@@ -363,6 +363,83 @@ oz_status_t oz_combine_rows_grad(oz_handle_t handle, void* stream, int64_t token
                                  int64_t lddy, const void* X, int64_t ldx, int64_t slots, const int32_t* order, const int32_t* place,
                                  const float* weights, void* dX, int64_t lddx, float* dweights);
 
+/* ---- the router's choice, weights in 4 bits, orthogonal updates --------------------------------------
+ * Conventions as in the part above. */
+
+/* A router's choice: each token's topk experts by falling score (ties: the lowest expert), and their weights.  With p = softmax(scores of the token):
+ *   ids     int32[tokens * topk]   the token's j-th expert; -1 where it has none
+ *   weights float[tokens * topk]   p of that expert (normalize 0), or its share of the chosen ones' sum (1); 0 where there is none
+ * and, unless all four are NULL, of the whole batch:
+ *   counts  int32[experts]         how often each was chosen
+ *   counted int32[1]               tokens that have an expert
+ *   shares  float[experts]         P_e, the mean of p_e over those tokens
+ *   loss    float[1]               experts * sum_e f_e P_e, f_e = counts_e / sum of counts: 1 where choices are even, up to experts where they are not
+ * scores: tokens x experts, rows ld elements apart, OZ_F32, OZ_BF16 or OZ_F16; a score of -infinity is an expert that is not to be had.
+ * live: uint8[tokens] or NULL; tokens with 0, and those that no expert is to be had for, are padding: they have no ids, weights of 0, and do not
+ * count; what stands in the scores of a token that is not live may be anything.  A NaN is above every other score, and makes its token's
+ * probabilities NaN, as +infinity does (and with them P and the loss).
+ * experts <= 1024, topk <= 64 and <= experts.  Sums are in a fixed order: two runs give the same bits.
+ * workspace (only with counts): 256-byte aligned, oz_choose_experts_workspace_bytes(...) bytes. */
+size_t oz_choose_experts_workspace_bytes(oz_handle_t handle, int64_t tokens, int64_t experts);
+oz_status_t oz_choose_experts(oz_handle_t handle, void* stream, int64_t tokens, int64_t experts, int64_t topk, const void* scores, int64_t ld,
+                              int32_t type, const uint8_t* live, int32_t normalize, int32_t* ids, float* weights, int32_t* counts, int32_t* counted,
+                              float* shares, float* loss, void* workspace, size_t workspace_bytes);
+
+/* The scores' gradient from that of the weights (dweights, tokens x topk, or NULL: none) and, unless counts and counted are NULL, from factor * *dloss
+ * (dloss a device pointer; NULL: 1) for the loss.  ids, weights, counts, counted: as oz_choose_experts left them with the same scores, live and
+ * normalize; counts may have been added up over several GPUs since: f_e then is theirs.  dscores: type and columns of scores; zero for padding
+ * and for experts that are not to be had.  Which experts are chosen has no gradient, so f_e is a constant here. */
+oz_status_t oz_choose_experts_grad(oz_handle_t handle, void* stream, int64_t tokens, int64_t experts, int64_t topk, const void* scores, int64_t ld,
+                                   int32_t type, const uint8_t* live, int32_t normalize, const int32_t* ids, const float* weights,
+                                   const float* dweights, const int32_t* counts, const int32_t* counted, const float* dloss, float factor,
+                                   void* dscores, int64_t ldd);
+
+/* A matrix in 4 bits: element (r, c) stands for scale * (code - zero), with the scale and the zero point of row r and group c / group. */
+typedef struct {
+    void* data;           /* codes 0 .. 15 of columns 2i (low half) and 2i + 1 of row r at r*ld + i; 16-byte aligned */
+    void* scale;          /* (g, r) at g*scale_ld + r */
+    void* zero;           /* as scale, of its type, any value; NULL: 8 */
+    int64_t ld;           /* bytes per row, multiple of 16, >= 16 * ceil(columns / 32) */
+    int64_t scale_ld;     /* elements per group, >= rows */
+    int64_t stride;       /* bytes from one matrix of a batch, or one group's, to the next; multiple of 16 */
+    int64_t scale_stride; /* the same for scale and zero, in elements */
+    int32_t scale_type;   /* OZ_F32, OZ_BF16 or OZ_F16 */
+    int32_t group;        /* columns that share a scale: 32, 64 or 128 */
+    int32_t reserved_;    /* 0 */
+} oz_packed_t;
+
+/* X (rows x cols, batch matrices stride_x elements apart) in 4 bits.  Without W->zero: scale = max|x| / 7 of the group, rounded to its type,
+ * code = min(max(rint(x / scale), -8), 7) + 8.  With: scale = (max(x, 0) - min(x, 0)) / 15, zero = rint(-min(x, 0) / scale),
+ * code = min(max(rint(x / scale) + zero, 0), 15).  Quotients are float32, rint is to nearest even.  A group of zeros has scale 0; one with an
+ * infinity or a NaN, or whose scale is beyond its type's range, has scale NaN.  Codes up to the next multiple of 32 columns are written, as 0.
+ * Limits: rows * ceil(cols / 512) <= 2^26 - 4, batch <= 65535. */
+oz_status_t oz_pack4(oz_handle_t handle, void* stream, int64_t rows, int64_t cols, const void* X, int64_t ldx, int32_t x_type, int64_t batch,
+                     int64_t stride_x, const oz_packed_t* W);
+
+/* The other way: X = the values that W stands for, rounded once to x_type. */
+oz_status_t oz_unpack4(oz_handle_t handle, void* stream, int64_t rows, int64_t cols, void* X, int64_t ldx, int32_t x_type, int64_t batch,
+                       int64_t stride_x, const oz_packed_t* W);
+
+/* Y = X W^T, X m x k in OZ_F32, OZ_BF16 or OZ_F16, W n x k in 4 bits, Y m x n.  Made for few rows (a token, a few in flight): W is read once for every 64
+ * rows of X.  offsets NULL, groups 0: one matrix.  Otherwise rows offsets[g] .. of Y = the same rows of X times W_g^T, and rows of Y behind the last
+ * group are set to zero.  Sums are held in 32 bits, each group's of code - 8 before it is scaled; the one rounding to fewer bits is the result's.
+ * k == 0: Y = 0.  Limits: (ceil(m / 16) + groups + 1) * ceil(n / 16) < 2^22. */
+oz_status_t oz_packed_gemm(oz_handle_t handle, void* stream, int64_t groups, const int32_t* offsets, int64_t m, int64_t n, int64_t k, const void* X,
+                           int64_t ldx, int32_t x_type, const oz_packed_t* W, void* Y, int64_t ldy, int32_t y_type);
+
+/* Y = X made orthogonal, batch matrices of rows x cols, by `steps` Newton-Schulz steps Z <- a Z + (b A + c A^2) Z, A = Z Z^T, from Z = X / (|X| + eps) with
+ * |X| the square root of the sum of squares (Z is taken transposed where rows > cols).  With a = 3.4445, b = -4.775, c = 2.0315 five steps bring singular
+ * values above 0.003 |X| into 0.68 .. 1.13 or so: the direction of a weight update that keeps X's singular vectors.
+ * Coefficients have to keep singular values below 4 on the way, |b| + |c| times their square's square below 15 (these do: 1.3).  X in OZ_BF16: operands of
+ * the products have 11 bits, an error of about 0.001 of the result; OZ_F32, OZ_F16: 22 bits, about 10^-6.  Everything else is in 32 bits,
+ * |X| in 64.  A matrix of zeros stays one if eps > 0; an infinity or a NaN makes NaN of its matrix.
+ * Y may be X, with the same strides.  Sums are in a fixed order.  Limits: rows, cols <= 32768, batch <= 65535, 1 <= steps <= 64.
+ * workspace: 256-byte aligned, oz_orthogonalize_workspace_bytes(...) bytes (up to 24 per element of a few matrices, of which more are done in turn). */
+size_t oz_orthogonalize_workspace_bytes(oz_handle_t handle, int64_t batch, int64_t rows, int64_t cols, int32_t type);
+oz_status_t oz_orthogonalize(oz_handle_t handle, void* stream, int64_t batch, int64_t rows, int64_t cols, int32_t type, const void* X, int64_t ldx,
+                             int64_t stride_x, void* Y, int64_t ldy, int64_t stride_y, int32_t steps, float a, float b, float c, float eps,
+                             void* workspace, size_t workspace_bytes);
+
 const char* oz_status_string(oz_status_t status);
 
 #ifdef __cplusplus

@@ -9,7 +9,7 @@
 #include <vector>
 
 #include "oz_f64_direct.h"
-#include "oz_scaled.h"
+#include "oz_layer.h"
 
 // Workspace of oz_dgemm_static: device memory owned by the library, one copy per GPU that loads
 // it, held until the process ends.  In host code this name is only a handle for
@@ -259,7 +259,7 @@ oz_status_t oz_create(oz_handle_t* handle, int device) {
         h->static_ws = nullptr;
         bool ok = hipGetDevice(&prev) == hipSuccess && hipSetDevice(device) == hipSuccess &&
                   hipGetSymbolAddress(&h->static_ws, HIP_SYMBOL(scratch)) == hipSuccess && h->static_ws != nullptr &&
-                  prepare_gemm_i8() && prepare_scaled_gemm();
+                  prepare_gemm_i8() && prepare_scaled_gemm() && prepare_ortho();
         if (prev >= 0 && prev != device) ok = (hipSetDevice(prev) == hipSuccess) && ok;
         if (!ok) {
             delete h;

@@ -1,13 +1,15 @@
-"""Rows sorted by expert and back, on torch tensors: what stands before and behind the experts' products (scaled.gemm_grouped).
+"""The router's choice, rows sorted by expert and back, on torch tensors: what stands before and behind the experts' products
+(scaled.gemm_grouped, packed.gemm_grouped).
 
 A layer whose tokens go to their chosen experts:
 
-    routing = sort_tokens(h, ids, experts)                    # ids: tokens x topk, -1 where a choice is dropped
+    choice = choose(h, scores, topk)                          # scores: tokens x experts; its balance loss is choice.loss
+    routing = sort_tokens(h, choice.ids, experts)             # ids: tokens x topk, -1 where a choice is dropped
     a = scaled.quantize(h, x, routing=routing)                # each choice's row, sorted by expert, in 8-bit floats
     ys = scaled.gemm_grouped(h, a, w, routing.offsets)
-    y = combine(h, ys, routing, weights)
+    y = combine(h, ys, routing, choice.weights)
 
-Gradients are calls too (combine without weights is gather's, combine_backward is combine's): results carry no history for torch's autograd.
+Gradients are calls too (combine without weights is gather's, combine_backward is combine's, choose_backward is choose's): results carry no history for torch's autograd.
 Everything is enqueued on the current stream of the handle's GPU, where all tensors are; nothing is read back, so no call waits for the GPU.
 """
 from __future__ import annotations
@@ -108,6 +110,87 @@ def combine_backward(h: g.Handle, dy, xs, routing: Routing, weights=None):
            xs.data_ptr(), ldx, xs.shape[0], routing.order.data_ptr(), routing.place.data_ptr(), _weights(weights, routing), dxs.data_ptr(),
            max(dxs.shape[1], 1), None if dw is None else dw.data_ptr())
     return dxs, dw
+
+
+class Choice:
+    """What choose found: ids (tokens x topk, int32, -1 where there is none), weights (float32), and, if asked for, counts (how often each
+    expert was chosen, int32), counted (one int32: tokens that have an expert), shares (their mean probability of each expert, float32) and
+    loss (float32, one value).  counts may be added up over several GPUs before choose_backward."""
+
+    __slots__ = ("ids", "weights", "counts", "counted", "shares", "loss", "live", "normalize")
+
+    def __init__(self, ids, weights, counts=None, counted=None, shares=None, loss=None, live=None, normalize=True):
+        self.ids, self.weights, self.counts, self.counted, self.shares, self.loss = ids, weights, counts, counted, shares, loss
+        self.live, self.normalize = live, normalize
+
+
+def _live(live, tokens):
+    if live is None:
+        return None
+    if not live.is_cuda or live.dtype not in (torch.bool, torch.uint8) or not live.is_contiguous() or live.numel() != tokens:
+        raise ValueError("live: contiguous bool, one per token, on the GPU")
+    return live.data_ptr()
+
+
+def choose(h: g.Handle, scores, topk: int, live=None, normalize=True, balance=True) -> Choice:
+    """Each token's topk experts by falling score (ties: the lowest), scores tokens x experts (-inf: not to be had), with their weights: the softmax
+    over all experts, of which the chosen ones' share of their sum is taken if normalize.  Tokens where live is False are padding.
+    balance: also counts, shares and the loss experts * sum_e f_e P_e (f_e an expert's share of the choices, P_e its mean probability)."""
+    ld = check_matrix(scores, "scores")
+    check_device(h, scores, live)
+    tokens, experts = scores.shape
+    if not 1 <= topk <= min(experts, 64):
+        raise ValueError("topk 1 .. 64 of %d experts, not %s" % (experts, topk))
+    device = scores.device
+    both = torch.empty((2, tokens, topk), dtype=torch.int32, device=device)
+    ids, weights = both.unbind(0)
+    weights = weights.view(torch.float32)
+    c = Choice(ids, weights, live=live, normalize=bool(normalize))
+    at = ids.data_ptr()
+    if balance:
+        need = h.choose_experts_workspace_bytes(tokens, experts)
+        first = -(-(2 * experts + 2) // 64) * 64          # the four results, then the workspace
+        table = torch.empty(first + (need + 3) // 4, dtype=torch.int32, device=device)
+        c.counts, c.counted = table[:experts], table[experts:experts + 1]
+        real = table[experts + 1:2 * experts + 2].view(torch.float32)
+        c.shares, c.loss = real[:experts], real[experts]
+        base = table.data_ptr()
+        more = (base, base + 4 * experts, base + 4 * (experts + 1), base + 4 * (2 * experts + 1), base + 4 * first, need)
+    else:
+        more = (None, None, None, None, None, 0)
+    h.call("oz_choose_experts", stream_of(scores), tokens, experts, topk, scores.data_ptr(), ld, float_type(scores.dtype), _live(live, tokens),
+           int(c.normalize), at, at + 4 * tokens * topk, *more)
+    return c
+
+
+def choose_backward(h: g.Handle, scores, choice: Choice, dweights=None, dloss=None):
+    """The gradient of choose's scores, for dweights (tokens x topk, float32) and dloss (a number, or one float32 on the GPU); either may be None."""
+    ld = check_matrix(scores, "scores")
+    check_device(h, scores, choice.ids, choice.weights, choice.counts, choice.counted, choice.live, dweights, dloss if torch.is_tensor(dloss) else None)
+    tokens, experts = scores.shape
+    ids = choice.ids
+    if ids.dim() != 2 or ids.shape[0] != tokens or choice.weights.shape != ids.shape or choice.weights.dtype != torch.float32 or not choice.weights.is_contiguous():
+        raise ValueError("scores %s do not belong to this choice of %s" % (tuple(scores.shape), tuple(ids.shape)))
+    check_ints(ids, "ids")
+    if dweights is not None and (dweights.dtype != torch.float32 or dweights.shape != ids.shape or not dweights.is_contiguous()):
+        raise ValueError("dweights: contiguous float32 of %s" % (tuple(ids.shape),))
+    counts = counted = scalar = None
+    factor = 1.0
+    if dloss is not None:
+        if choice.counts is None or choice.counted is None:
+            raise ValueError("a gradient of the loss needs the choice's counts: choose(balance=True)")
+        counts, counted = check_ints(choice.counts, "counts", experts).data_ptr(), check_ints(choice.counted, "counted", 1).data_ptr()
+        if torch.is_tensor(dloss):
+            if not dloss.is_cuda or dloss.dtype != torch.float32 or dloss.numel() != 1:
+                raise ValueError("dloss: a number, or one float32 on the GPU")
+            scalar = dloss.data_ptr()
+        else:
+            factor = float(dloss)
+    d = torch.empty((tokens, experts), dtype=scores.dtype, device=scores.device)
+    h.call("oz_choose_experts_grad", stream_of(scores), tokens, experts, ids.shape[1], scores.data_ptr(), ld, float_type(scores.dtype),
+           _live(choice.live, tokens), int(choice.normalize), ids.data_ptr(), choice.weights.data_ptr(), None if dweights is None else dweights.data_ptr(),
+           counts, counted, scalar, factor, d.data_ptr(), max(experts, 1))
+    return d
 
 
 class ExpertLayer:

@@ -56,11 +56,18 @@ class oz_scaled_t(C.Structure):
                 ("block_rows", C.c_int32), ("reserved_", C.c_int32)]
 
 
+class oz_packed_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("zero", C.c_void_p), ("ld", C.c_int64), ("scale_ld", C.c_int64),
+                ("stride", C.c_int64), ("scale_stride", C.c_int64), ("scale_type", C.c_int32), ("group", C.c_int32), ("reserved_", C.c_int32)]
+
+
 EXPORTS = ("oz_create", "oz_destroy", "oz_default_opts", "oz_set_heuristic",
            "oz_dgemm_workspace_bytes", "oz_dgemm", "oz_dgemm_static", "oz_zgemm_workspace_bytes", "oz_zgemm", "oz_dgemm_strided_batched", "oz_dgemm_layout", "oz_profile_enable",
            "oz_profile_read", "oz_native_dgemm", "oz_status_string",
            "oz_quantize", "oz_scaled_gemm_workspace_bytes", "oz_scaled_gemm", "oz_scaled_gemm_grouped", "oz_scaled_gemm_grouped_k",
-           "oz_sort_tokens_workspace_bytes", "oz_sort_tokens", "oz_gather_rows", "oz_combine_rows", "oz_combine_rows_grad")
+           "oz_sort_tokens_workspace_bytes", "oz_sort_tokens", "oz_gather_rows", "oz_combine_rows", "oz_combine_rows_grad",
+           "oz_choose_experts_workspace_bytes", "oz_choose_experts", "oz_choose_experts_grad", "oz_pack4", "oz_unpack4", "oz_packed_gemm",
+           "oz_orthogonalize_workspace_bytes", "oz_orthogonalize")
 
 _lib = None
 
@@ -118,7 +125,7 @@ def load_library() -> C.CDLL:
     lib.oz_profile_read.restype = C.c_int
     lib.oz_status_string.argtypes = [C.c_int]
     lib.oz_status_string.restype = C.c_char_p
-    P, I, L, S = C.c_void_p, C.c_int32, C.c_int64, C.POINTER(oz_scaled_t)
+    P, I, L, F, S, W = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.POINTER(oz_scaled_t), C.POINTER(oz_packed_t)
     for name, args in (("oz_quantize", [L, L, P, L, I, L, L, P, L, L, P, L, S, S]),
                        ("oz_scaled_gemm", [L, L, L, S, S, P, L, I, I, P, C.c_size_t]),
                        ("oz_scaled_gemm_grouped", [L, P, L, L, L, S, S, P, L, I]),
@@ -126,12 +133,21 @@ def load_library() -> C.CDLL:
                        ("oz_sort_tokens", [L, L, L, P, I, P, P, P, P, C.c_size_t]),
                        ("oz_gather_rows", [L, L, L, I, P, L, P, P, P, L]),
                        ("oz_combine_rows", [L, L, L, I, P, L, L, P, P, P, L]),
-                       ("oz_combine_rows_grad", [L, L, L, I, P, L, P, L, L, P, P, P, P, L, P])):
+                       ("oz_combine_rows_grad", [L, L, L, I, P, L, P, L, L, P, P, P, P, L, P]),
+                       ("oz_choose_experts", [L, L, L, P, L, I, P, I, P, P, P, P, P, P, P, C.c_size_t]),
+                       ("oz_choose_experts_grad", [L, L, L, P, L, I, P, I, P, P, P, P, P, P, F, P, L]),
+                       ("oz_pack4", [L, L, P, L, I, L, L, W]), ("oz_unpack4", [L, L, P, L, I, L, L, W]),
+                       ("oz_packed_gemm", [L, P, L, L, L, P, L, I, W, P, L, I]),
+                       ("oz_orthogonalize", [L, L, L, I, P, L, L, P, L, L, I, F, F, F, F, P, C.c_size_t])):
         getattr(lib, name).argtypes = [H, C.c_void_p] + args
         getattr(lib, name).restype = C.c_int
     for name in ("oz_scaled_gemm_workspace_bytes", "oz_sort_tokens_workspace_bytes"):
         getattr(lib, name).argtypes = [H, L, L, L]
         getattr(lib, name).restype = C.c_size_t
+    lib.oz_choose_experts_workspace_bytes.argtypes = [H, L, L]
+    lib.oz_choose_experts_workspace_bytes.restype = C.c_size_t
+    lib.oz_orthogonalize_workspace_bytes.argtypes = [H, L, L, L, I]
+    lib.oz_orthogonalize_workspace_bytes.restype = C.c_size_t
     _lib = lib
     return lib
 
@@ -247,10 +263,10 @@ class Handle:
         _check(self.lib.oz_native_dgemm(self._h, stream_ptr, transa.encode(), transb.encode(), m, n, k,
                                         alpha, A_ptr, lda, B_ptr, ldb, beta, C_ptr, ldc), "oz_native_dgemm")
 
-    # 8-bit block-scaled operands and sorted rows: arguments as in include/ozdgemm.h, matrices as oz_scaled_t or None.  The calls
-    # on tensors are in `scaled` and `experts`.
+    # 8-bit block-scaled operands, sorted rows, and what stands around them: arguments as in include/ozdgemm.h, matrices as oz_scaled_t,
+    # oz_packed_t or None.  The calls on tensors are in `scaled`, `experts`, `packed` and `orthogonal`.
     def call(self, name, stream_ptr, *args):
-        """Enqueues the entry point `name` (oz_quantize .. oz_combine_rows_grad) on a stream; raises OzError on its status."""
+        """Enqueues the entry point `name` (oz_quantize .. oz_orthogonalize) on a stream; raises OzError on its status."""
         status = getattr(self.lib, name)(self._h, stream_ptr, *args)
         if status:
             raise OzError(status, name)
@@ -260,6 +276,12 @@ class Handle:
 
     def sort_tokens_workspace_bytes(self, tokens, topk, experts) -> int:
         return self.lib.oz_sort_tokens_workspace_bytes(self._h, tokens, topk, experts)
+
+    def choose_experts_workspace_bytes(self, tokens, experts) -> int:
+        return self.lib.oz_choose_experts_workspace_bytes(self._h, tokens, experts)
+
+    def orthogonalize_workspace_bytes(self, batch, rows, cols, type_) -> int:
+        return self.lib.oz_orthogonalize_workspace_bytes(self._h, batch, rows, cols, type_)
 
     def profile_enable(self, max_calls: int):
         _check(self.lib.oz_profile_enable(self._h, max_calls), "oz_profile_enable")

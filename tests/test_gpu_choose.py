@@ -1,0 +1,229 @@
+"""The router's choice, its balance loss and their gradient, against loops in 64 bits."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+import layer_reference as ref  # noqa: E402
+
+F = 2.0 ** -24
+# Numbers below 2^-126 are whole multiples of 2^-149, whatever their size: exp and each product after it are off by up to that much there (times
+# what they are multiplied by next, which is below 16 here), which no relative bound covers.
+LEAST = 4 * 2.0 ** -149
+
+
+@pytest.fixture(scope="module")
+def h():
+    from paper_2511_13778_amd import ozdgemm as g
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible: the HIP path cannot run (there is no CPU fallback)")
+    handle = g.Handle(0)
+    yield handle
+    handle.close()
+
+
+def scores_of(seed, tokens, experts, dtype, spread=2.0):
+    r = torch.Generator().manual_seed(seed)
+    return (torch.randn((tokens, experts), generator=r) * spread + torch.randn((experts,), generator=r)).to(dtype)
+
+
+def close(got, exact, bound, what):
+    err = (got.double().cpu() - exact).abs()
+    assert got.shape == exact.shape and (err <= bound).all(), (what, (err - bound).max().item(), err.max().item())
+
+
+def check(h, scores, topk, live=None, normalize=True, dloss=0.7, view=None):
+    """Everything that there is of one batch.  Relative errors: a quotient of exponentials, each of a difference that is off by half a step of the
+    spread, with 2 steps of exp; sums over up to 32 values of a lane and 6 folds."""
+    from paper_2511_13778_amd import experts as ex
+    tokens, experts = scores.shape
+    ids, w, p, counts, counted = ref.choose(scores, topk, live, normalize)
+    finite = scores.double()[scores.double().isfinite()]
+    spread = (finite.max() - finite.min()).item() if finite.numel() else 0.0
+    rel = (2 * spread + 2 * 4 + 40) * F
+    d_live = None if live is None else live.cuda()
+    x = scores.cuda() if view is None else view(scores)
+    c = ex.choose(h, x, topk, live=d_live, normalize=normalize)
+    assert torch.equal(c.ids.cpu().long(), ids)
+    close(c.weights, w, rel * w + LEAST, "weights")
+    assert torch.equal(c.counts.cpu().long(), counts) and c.counted.item() == counted
+    shares, loss, f = ref.balance(p, counts, counted)
+    rel_sum = rel + (tokens / 8192 + 24) * F
+    close(c.shares, shares, rel_sum * shares + LEAST, "shares")
+    close(c.loss, loss, rel_sum * loss + LEAST * experts, "loss")
+    plain = ex.choose(h, x, topk, live=d_live, normalize=normalize, balance=False)
+    assert torch.equal(plain.ids, c.ids) and torch.equal(plain.weights, c.weights) and plain.loss is None
+    r = torch.Generator().manual_seed(1)
+    dw = torch.randn((tokens, topk), generator=r)
+    for weights, dl in ((dw, dloss), (dw, None), (None, dloss)):
+        exact, size = ref.choose_grad(ids, w, p, f, counted, (dw if weights is not None else 0 * dw).double(), dl, normalize)
+        d = ex.choose_backward(h, x, c, None if weights is None else weights.cuda(), dl)
+        assert d.dtype == scores.dtype
+        close(d, exact, (2 * rel + (topk + 16) * F) * size + ref.rounded(exact, scores.dtype) + 16 * LEAST, "dscores")
+    return c
+
+
+# experts around each width of a lane's part and of a token's lanes
+SIZES = [(1, 1, 1), (1, 2, 1), (3, 5, 5), (24, 16, 4), (33, 17, 2), (17, 32, 4), (40, 60, 6), (100, 64, 8), (16, 65, 1), (50, 128, 8), (19, 129, 3), (70, 256, 8), (9, 257, 5),
+         (30, 384, 6), (5, 512, 64), (7, 513, 33), (6, 1000, 64), (4, 1024, 17), (2, 64, 64), (3, 30, 30)]
+
+
+@pytest.mark.parametrize("tokens,experts,topk", SIZES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_sizes(h, tokens, experts, topk, dtype, normalize):
+    check(h, scores_of(tokens * experts + topk, tokens, experts, dtype), topk, normalize=normalize)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_many_tokens(h, dtype):
+    # more tokens than one pass of all workgroups takes
+    check(h, scores_of(7, 20011, 24, dtype), 3)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_ties_go_to_the_lowest(h, dtype):
+    x = torch.zeros((40, 130))
+    x[10:20] = torch.arange(130) // 7 % 3
+    x[20:30, ::2] = -0.0                      # equal to +0
+    x[30:, 64:] = 1.0
+    check(h, x.to(dtype), 8)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_padding_and_experts_that_are_not_there(h, dtype, normalize):
+    x = scores_of(3, 60, 40, dtype)
+    live = torch.rand(60, generator=torch.Generator().manual_seed(2)) < 0.6
+    live[4:20] = True
+    x[5] = float("-inf")                      # nobody
+    x[6, 1:] = float("-inf")                  # one
+    x[7, 3:] = float("-inf")                  # fewer than are asked for
+    x[8, ::2] = float("-inf")
+    c = check(h, x, 4, live, normalize)
+    assert (c.ids[5] == -1).all() and c.ids[7].tolist()[3] == -1
+    dead = (~live).nonzero()[:, 0]
+    x[dead] = float("nan")
+    x[dead[::2]] = float("inf")
+    got = check(h, x, 4, live, normalize)
+    assert torch.equal(got.ids, c.ids) and torch.equal(got.weights, c.weights) and torch.equal(got.loss, c.loss)
+    check(h, x, 4, torch.zeros(60, dtype=torch.bool), normalize)          # nobody at all
+    check(h, x[:0], 4, None, normalize)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_not_a_number(h, dtype):
+    from paper_2511_13778_amd import experts as ex
+    x = scores_of(4, 8, 20, dtype)
+    x[2, 7] = x[2, 11] = float("nan")
+    x[5, 3] = float("inf")
+    x[6, 4] = -float("nan")
+    c = ex.choose(h, x.cuda(), 3)
+    ids = ref.choose(x, 3)[0]
+    assert torch.equal(c.ids.cpu().long(), ids) and ids[2].tolist()[:2] == [7, 11] and ids[6, 0] == 4 and ids[5, 0] == 3
+    bad = c.weights.isnan().any(1).cpu()
+    assert bad.tolist() == [False, False, True, False, False, True, True, False]
+    assert c.loss.isnan() and c.shares.isnan().all()
+    d = ex.choose_backward(h, x.cuda(), c, torch.ones((8, 3), device="cuda")).cpu()
+    assert d.isnan().any(1).tolist() == bad.tolist()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_far_scores(h, dtype):
+    # softmax without overflow, and experts whose probability is nothing
+    x = scores_of(5, 30, 48, dtype, spread=60.0)
+    check(h, x, 4)
+    check(h, x, 4, normalize=False)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_strides_and_alignment(h, dtype):
+    x = scores_of(6, 37, 45, dtype)
+
+    def inside(ld, start):
+        def view(s):
+            big = torch.full((s.shape[0] * ld + start + 64,), float("nan"), dtype=dtype, device="cuda")
+            v = big[start:start + s.shape[0] * ld].view(s.shape[0], ld)[:, :s.shape[1]]
+            v.copy_(s)
+            return v
+        return view
+    for ld, start in ((45, 1), (46, 3), (47, 0), (64, 5)):
+        check(h, x, 5, view=inside(ld, start))
+
+
+def test_gradient_by_differences(h):
+    from paper_2511_13778_amd import experts as ex
+    x = scores_of(8, 6, 10, torch.float32).double()
+    dw = torch.randn((6, 3), generator=torch.Generator().manual_seed(9)).double()
+    for normalize in (True, False):
+        def value(s):
+            ids, w, p, counts, counted = ref.choose(s, 3, None, normalize)
+            return ids, (w * dw).sum() + 0.5 * ref.balance(p, counts, counted)[1]
+        ids, _ = value(x)
+        c = ex.choose(h, x.float().cuda(), 3, normalize=normalize)
+        d = ex.choose_backward(h, x.float().cuda(), c, dw.float().cuda(), 0.5).cpu()
+        step = 1e-5
+        for t in range(6):
+            for e in range(10):
+                up, down = x.clone(), x.clone()
+                up[t, e] += step
+                down[t, e] -= step
+                (i, a), (j, b) = value(up), value(down)
+                assert torch.equal(i, ids) and torch.equal(j, ids)
+                # third derivatives are below 10: the difference is off by 10 step^2, the inputs by their rounding to 32 bits
+                assert abs((a - b).item() / (2 * step) - d[t, e].item()) < 1e-5
+
+
+def test_loss_gradient_on_the_gpu_and_counts_of_several(h):
+    from paper_2511_13778_amd import experts as ex
+    x = scores_of(10, 300, 16, torch.float32)
+    c = ex.choose(h, x.cuda(), 2)
+    scalar = torch.tensor(0.25, device="cuda")
+    assert torch.equal(ex.choose_backward(h, x.cuda(), c, None, scalar), ex.choose_backward(h, x.cuda(), c, None, 0.25))
+    # another GPU's choices added in: its f_e, this one's mean
+    ids, w, p, counts, counted = ref.choose(x, 2)
+    other = torch.arange(16) * 40
+    c.counts = (c.counts.cpu() + other).to(torch.int32).cuda()
+    f = (counts + other).double() / (counts + other).sum()
+    exact, size = ref.choose_grad(ids, w, p, f, counted, torch.zeros((300, 2)).double(), 0.25, True)
+    close(ex.choose_backward(h, x.cuda(), c, None, 0.25), exact, 200 * F * size + ref.rounded(exact, torch.float32), "dscores")
+
+
+def test_same_bits_again_and_on_another_stream(h):
+    from paper_2511_13778_amd import experts as ex
+    x = scores_of(11, 30000, 60, torch.bfloat16).cuda()
+    dw = torch.randn((30000, 6), device="cuda")
+    a = ex.choose(h, x, 6)
+    da = ex.choose_backward(h, x, a, dw, 0.1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b = ex.choose(h, x, 6)
+        db = ex.choose_backward(h, x, b, dw, 0.1)
+    torch.cuda.synchronize()
+    for m, n in ((a.ids, b.ids), (a.weights, b.weights), (a.counts, b.counts), (a.shares, b.shares), (a.loss, b.loss), (da, db)):
+        assert torch.equal(m, n)
+
+
+def test_captured_and_replayed_with_other_inputs(h):
+    from paper_2511_13778_amd import experts as ex
+    x = scores_of(12, 500, 64, torch.float32).cuda()
+    dw = torch.randn((500, 4), device="cuda")
+
+    def step():
+        c = ex.choose(h, x, 4)
+        return c.ids, c.weights, c.counts, c.shares, c.loss, ex.choose_backward(h, x, c, dw, 0.3)
+    step()
+    torch.cuda.synchronize()
+    graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    with torch.cuda.graph(other):
+        got2 = step()
+    for seed in range(4):
+        x.copy_(scores_of(20 + seed, 500, 64, torch.float32))
+        graph.replay()
+        other.replay()
+        torch.cuda.synchronize()
+        for a, b, c in zip(step(), got, got2):
+            assert torch.equal(a, b) and torch.equal(a, c)

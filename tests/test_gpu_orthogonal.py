@@ -1,0 +1,142 @@
+"""Orthogonal updates against 64-bit steps: one step entry by entry, five by the method's own loss."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+import layer_reference as ref  # noqa: E402
+
+FLOATS = [torch.float32, torch.bfloat16, torch.float16]
+QUINTIC, CUBIC = (3.4445, -4.7750, 2.0315), (1.5, -0.5, 0.0)
+EPS = 1e-7
+
+
+@pytest.fixture(scope="module")
+def h():
+    from paper_2511_13778_amd import ozdgemm as g
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible: the HIP path cannot run (there is no CPU fallback)")
+    handle = g.Handle(0)
+    yield handle
+    handle.close()
+
+
+def parts_of(dtype):
+    return 1 if dtype == torch.bfloat16 else 2
+
+
+def gradient(r, *shape):
+    u = torch.randn(shape[:-1] + (4,), generator=r, device="cuda") @ torch.randn(shape[:-2] + (4, shape[-1]), generator=r, device="cuda")
+    return u + 0.3 * torch.randn(shape, generator=r, device="cuda")
+
+
+SIZES = [(1, 1), (1, 7), (7, 1), (5, 5), (16, 16), (33, 64), (64, 33), (64, 64), (65, 65), (100, 300), (300, 100), (128, 129), (257, 260), (260, 400), (513, 300)]
+
+
+@pytest.mark.parametrize("rows,cols", SIZES)
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("coefficients", [QUINTIC, CUBIC])
+def test_one_step(h, rows, cols, dtype, coefficients):
+    from paper_2511_13778_amd import orthogonal
+    r = torch.Generator(device="cuda").manual_seed(rows + 1000 * cols)
+    x = gradient(r, rows, cols).to(dtype)
+    got = orthogonal.orthogonalize(h, x, steps=1, coefficients=coefficients, eps=EPS)
+    exact, bound = ref.orthogonalize_bound(x, coefficients, EPS, parts_of(dtype))
+    err = (got.double() - exact).abs()
+    bound = bound + ref.rounded(exact, dtype)
+    assert got.dtype == dtype and got.shape == x.shape and (err <= bound).all(), (err / bound).max().item()
+
+
+def off(a, b):
+    return ((a - b).norm() / b.norm()).item()
+
+
+def check_five(got, x, eps=EPS):
+    """Off by what the method loses on this very matrix (operands in 16-bit parts, computed in 64 bits), half as much again for sums of another order, and the
+    result's own rounding.  32-bit sums that the 64-bit form does not have: each of a step's three is off by at most (inner length) 2^-24 of what is added, in a
+    random walk its square root, and five steps make 3.4^4 of the first."""
+    exact = ref.orthogonalize(x, 5, QUINTIC, eps)
+    own = off(ref.orthogonalize_in_parts(x, 5, QUINTIC, eps, parts_of(x.dtype)), exact)
+    sums = 3 * max(x.shape) ** 0.5 * 2.0 ** -24 * 3.4445 ** 2
+    assert off(got.double(), exact) <= 1.5 * own + sums + ref.MANTISSA[x.dtype], (off(got.double(), exact), own, sums)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 9), (48, 48), (64, 200), (200, 64), (150, 150), (300, 513), (640, 256)])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_five_steps(h, rows, cols, dtype):
+    from paper_2511_13778_amd import orthogonal
+    r = torch.Generator(device="cuda").manual_seed(rows * 7 + cols)
+    for x in (gradient(r, rows, cols), torch.randn((rows, cols), generator=r, device="cuda")):
+        x = (x * 1e-3).to(dtype)
+        got = orthogonal.orthogonalize(h, x)
+        check_five(got, x)
+        s = torch.linalg.svdvals(got.double().cpu())
+        big = torch.linalg.svdvals(x.double().cpu()) > 0.02 * x.double().norm().item()
+        assert s.max() < 1.3 and (s[big] > 0.6).all()
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_batches_strides_and_in_place(h, dtype):
+    from paper_2511_13778_amd import orthogonal
+    r = torch.Generator(device="cuda").manual_seed(3)
+    big = gradient(r, 5, 90, 200).to(dtype)
+    x = big[:, 3:80, 7:150]
+    one = [orthogonal.orthogonalize(h, m.contiguous()) for m in x]
+    got = orthogonal.orthogonalize(h, x)
+    assert all(torch.equal(a, b) for a, b in zip(got, one))
+    room = torch.full((5, 90, 200), 7.0, device="cuda", dtype=dtype)
+    orthogonal.orthogonalize(h, x, out=room[:, 3:80, 7:150])
+    assert torch.equal(room[:, 3:80, 7:150], got)
+    room[:, 3:80, 7:150] = 7.0
+    assert (room == 7.0).all()
+    before = big.clone()
+    orthogonal.orthogonalize(h, x, out=x)
+    assert torch.equal(x, got)
+    x.copy_(before[:, 3:80, 7:150])
+    assert torch.equal(big, before)
+    turned = orthogonal.orthogonalize(h, x.transpose(1, 2).contiguous())
+    assert torch.equal(turned.transpose(1, 2), got)
+
+
+def test_more_matrices_than_are_done_at_a_time(h):
+    from paper_2511_13778_amd import orthogonal
+    r = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn((5000, 20, 12), generator=r, device="cuda").bfloat16()
+    got = orthogonal.orthogonalize(h, x)
+    for i in (0, 1, 4095, 4096, 4097, 4999):
+        assert torch.equal(got[i], orthogonal.orthogonalize(h, x[i]))
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_zeros_sizes_of_gradients_and_not_numbers(h, dtype):
+    from paper_2511_13778_amd import orthogonal
+    r = torch.Generator(device="cuda").manual_seed(5)
+    x = gradient(r, 6, 40, 70).to(dtype)
+    x[1] = 0
+    x[2, 3, 4] = float("nan")
+    x[3, 5, 6] = float("inf")
+    x[4, 20:] = 0                             # rank 20
+    got = orthogonal.orthogonalize(h, x)
+    assert not got[1].any() and got[2].isnan().all() and got[3].isnan().all() and not got[4, 20:].any()
+    for i in (0, 4, 5):
+        check_five(got[i], x[i])
+    if dtype != torch.float16:
+        for size in (1e-35, 1e-22, 1e25, 1e36):
+            y = (gradient(r, 40, 70) * size).to(dtype)
+            check_five(orthogonal.orthogonalize(h, y, eps=0.0), y, eps=0.0)
+
+
+def test_captured_and_replayed_with_other_inputs(h):
+    from paper_2511_13778_amd import orthogonal
+    r = torch.Generator(device="cuda").manual_seed(6)
+    x = gradient(r, 3, 130, 200).bfloat16()
+    orthogonal.orthogonalize(h, x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = orthogonal.orthogonalize(h, x)
+    for _ in range(4):
+        x.copy_(gradient(r, 3, 130, 200))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(orthogonal.orthogonalize(h, x), got)
