@@ -123,10 +123,11 @@ __device__ __forceinline__ void multiply(uint8_t* lds, const f16_t* l, const f16
     const int steps = k / kStep, total = steps * (PARTS == 2 ? 3 : 1);
     // eight rows a transfer; the four waves take them in turn
     auto copy = [&](int s) {
-        const int pass = PARTS == 2 ? s / steps : 0;              // hi hi, hi lo, lo hi
-        const uint32_t at = uint32_t(s - pass * steps) * 128, to = lds0 + uint32_t(s & 1) * S::kStage;
-        const v4i32 src_l = tile_buffer(reinterpret_cast<const uint8_t*>(l + (pass == 2 ? l_part : 0)), uint32_t(T) * ld);
-        const v4i32 src_r = tile_buffer(reinterpret_cast<const uint8_t*>(r + (pass == 1 ? r_part : 0)), uint32_t(T) * ld);
+        // hi lo, lo hi, hi hi: the small sums first, so that only a third of the additions are rounded at the size of the result
+        const int pass = PARTS == 2 ? s / steps : 2;
+        const uint32_t at = uint32_t(PARTS == 2 ? s - pass * steps : s) * 128, to = lds0 + uint32_t(s & 1) * S::kStage;
+        const v4i32 src_l = tile_buffer(reinterpret_cast<const uint8_t*>(l + (pass == 1 ? l_part : 0)), uint32_t(T) * ld);
+        const v4i32 src_r = tile_buffer(reinterpret_cast<const uint8_t*>(r + (pass == 0 ? r_part : 0)), uint32_t(T) * ld);
 #pragma unroll
         for (int x = 0; x < T / 32; ++x) {
             const uint32_t row = uint32_t(x * 4 + wave) * 8;
