@@ -15,7 +15,8 @@ PROBE_SOURCES = ["oz_probe.hip"]
 SOURCES = ["oz_api.hip", "oz_scan.hip", "oz_esc.hip", "oz_slice.hip", "oz_esc_slice.hip", "oz_gemm_i8.hip", "oz_gemm_few.hip", "oz_gemm_small.hip", "oz_gemm_mid.hip",
            "oz_recompose.hip", "oz_dgemm_f64.hip", "oz_dgemm_f64_direct.hip", "oz_complex.hip",
            "oz_scaled_api.hip", "oz_quantize.hip", "oz_scaled_gemm.hip", "oz_scaled_gemm_big.hip", "oz_scaled_gemm_big_f32.hip", "oz_scaled_gemm_few.hip", "oz_route.hip",
-           "oz_layer_api.hip", "oz_choose.hip", "oz_packed.hip", "oz_ortho.hip"]
+           "oz_layer_api.hip", "oz_choose.hip", "oz_packed.hip", "oz_packed_gemm_f32.hip", "oz_packed_gemm_bf16.hip",
+           "oz_packed_gemm_f16.hip", "oz_ortho.hip"]
 # packed FP32 instructions are switched off for all device code (known-bad on the test machines)
 # -ffp-contract=off: the FP64 epilogues round every product and sum separately, as the header specifies;
 # hipcc's default would fuse a*b + c into one rounding.

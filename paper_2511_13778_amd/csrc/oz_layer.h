@@ -62,6 +62,9 @@ struct PackedGemm {
 void launch_pack(hipStream_t st, const PackCall& c);
 void launch_unpack(hipStream_t st, const PackCall& c);         // x is written
 void launch_packed_gemm(hipStream_t st, const PackedGemm& g, int num_cu);
+void launch_packed_gemm_f32(hipStream_t st, const PackedGemm& g, int num_cu);
+void launch_packed_gemm_bf16(hipStream_t st, const PackedGemm& g, int num_cu);
+void launch_packed_gemm_f16(hipStream_t st, const PackedGemm& g, int num_cu);
 
 // ---- orthogonal updates
 struct OrthoCall {

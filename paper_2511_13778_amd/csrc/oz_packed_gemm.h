@@ -1,0 +1,438 @@
+// Product with weights in 4 bits for few rows of x: what bounds it is the read of the weights.
+//
+// A workgroup has 16 R rows of W and up to 64 rows of x; its waves share k, in runs of blocks of 128, and add up their sums through LDS in the waves'
+// order.  code - 8 is exact in x's 16-bit type, and goes with x into v_mfma_f32_16x16x32 (float32 x as three bfloat16 parts, exactly); scales
+// are applied to each group's sum, in 32 bits, so a result of 16 bits has one rounding, the last.  The sums of x that zero points need are one
+// more matrix instruction, with a matrix of ones.
+#pragma once
+
+#include <algorithm>
+#include <type_traits>
+
+#include "oz_layer.h"
+#include "oz_scaled_device.h"
+
+namespace oz {
+
+namespace {
+
+typedef uint32_t v4u32 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kBlock = 128;              // of k that a wave takes at a time
+
+// Eight codes as the matrix instruction takes them, in the order 0 4 1 5 2 6 3 7 (x's elements in the same): float16 and EXACT: code - 8;
+// bfloat16 else: 128 + code, a third of the instructions, and what is too much comes off the sums.
+template <typename W, bool EXACT>
+__device__ __forceinline__ void widen_codes(uint32_t codes, uint32_t (&w)[4]) {
+    if constexpr (std::is_same_v<W, f16_t>) {
+        // 1024 + code, whose last bits are the code's
+        const f16x2 less = {f16_t(1032.0f), f16_t(1032.0f)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, ((codes >> (4 * i)) & 0x000F000Fu) | 0x64006400u) - less);
+    } else if constexpr (EXACT) {
+        const uint32_t even = codes & 0x0F0F0F0Fu, odd = (codes >> 4) & 0x0F0F0F0Fu;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t of = i % 2 ? odd : even;
+            const float a = float((of >> (i / 2 * 8)) & 0xFFu) - 8.0f, b = float((of >> (i / 2 * 8 + 16)) & 0xFFu) - 8.0f;
+            w[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);       // whole numbers: the upper halves hold all of them
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = ((codes >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
+    }
+}
+
+__device__ __forceinline__ v4f mfma16(const uint32_t (&a)[4], const uint32_t (&b)[4], v4f c, f16_t) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mfma16(const uint32_t (&a)[4], const uint32_t (&b)[4], v4f c, bf16_t) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Eight consecutive elements of a row of x, and as the matrix instruction takes them, in the codes' order: one part, three of float32.
+template <typename X>
+struct Eight {
+    static constexpr int kParts = sizeof(X) == 4 ? 3 : 1, kWords = 2 * int(sizeof(X));
+    using W = std::conditional_t<sizeof(X) == 4, bf16_t, X>;
+    uint32_t e[kWords];
+    __device__ __forceinline__ void load(const X* p) { __builtin_memcpy(e, p, sizeof(e)); }
+    // What load(row + from) brought, moved down by `down` elements, zeros behind it.
+    __device__ __forceinline__ void move_down(int down) {
+        constexpr int kPer = 4 / int(sizeof(X));
+#pragma unroll
+        for (int step = kWords / 2; step > 0; step /= 2)
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+                const uint32_t now = e[i], far = i + step < kWords ? e[i + step] : 0u;
+                e[i] = (down & (step * kPer)) ? far : now;
+            }
+        if (kPer == 2) {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+                const uint32_t now = e[i], odd = (now >> 16) | (i + 1 < kWords ? e[i + 1] << 16 : 0u);
+                e[i] = (down & 1) ? odd : now;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) e[i] = down >= 8 ? 0u : e[i];
+    }
+    __device__ __forceinline__ void parts(uint32_t (&w)[kParts][4]) const {
+        if constexpr (kParts == 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[0][i] = __builtin_amdgcn_perm(e[i / 2 + 2], e[i / 2], i % 2 ? 0x07060302u : 0x05040100u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t bits[2][3];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    // cut off, not rounded: what is left is exact, and no part is larger than the whole
+                    float x = __uint_as_float(e[i + 4 * j]);
+                    const bool fine = (e[i + 4 * j] & 0x7F800000u) != 0x7F800000u;
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) {
+                        bits[j][p] = __float_as_uint(x) & 0xFFFF0000u;
+                        if (p == 0 && x != x) bits[j][0] = 0x7FC00000u;
+                        x = fine ? x - __uint_as_float(bits[j][p]) : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int p = 0; p < 3; ++p) w[p][i] = __builtin_amdgcn_perm(bits[1][p], bits[0][p], 0x07060302u);
+            }
+        }
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, int have, v4f v) {
+    T t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put(t + i, v[i]);
+    if (have >= 4) {
+        __builtin_memcpy(p, t, sizeof(t));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) p[i] = t[i];
+    }
+}
+__device__ __forceinline__ void store_results(const PackedGemm& g, int64_t at, int have, v4f v) {
+    if (g.y_type == OZ_F32) store4(static_cast<float*>(g.y) + at, have, v);
+    else if (g.y_type == OZ_BF16) store4(static_cast<bf16_t*>(g.y) + at, have, v);
+    else store4(static_cast<f16_t*>(g.y) + at, have, v);
+}
+
+// A scale or zero point of any of the three types, without a branch that would wait for what else is on its way: two halves of a float32, or the same 16
+// bits twice.
+struct ScaleLoad {
+    const uint8_t* p;
+    int shift, second;
+    bool wide, bf16;
+    __device__ __forceinline__ ScaleLoad(const void* q, int type)
+        : p(static_cast<const uint8_t*>(q)), shift(type == OZ_F32 ? 2 : 1), second(type == OZ_F32 ? 2 : 0), wide(type == OZ_F32), bf16(type == OZ_BF16) {}
+    struct Halves { uint16_t lo, hi; };
+    __device__ __forceinline__ Halves fetch(int64_t at) const {
+        const uint8_t* from = p + (at << shift);
+        return Halves{*reinterpret_cast<const uint16_t*>(from), *reinterpret_cast<const uint16_t*>(from + second)};
+    }
+    __device__ __forceinline__ float value(Halves h) const {
+        const float half = to_float(__builtin_bit_cast(f16_t, h.lo));
+        return wide ? __uint_as_float(uint32_t(h.lo) | uint32_t(h.hi) << 16) : bf16 ? __uint_as_float(uint32_t(h.lo) << 16) : half;
+    }
+};
+
+// MT: 16s of rows of x.  R: 16s of rows of W.  SMALL: groups of 32 or 64 columns, else of 128.  EXACT: bfloat16 codes with nothing to come off the sums.
+// That 128 + code is multiplied instead of code - 8 makes the sums 136 / 4.6 times as large and their 32-bit roundings with them: 4e-6 of a result, or
+// 4e-5 where all of x has one sign, beside a rounding to bfloat16 of 2e-3.
+template <typename X, int MT, int R, bool SMALL, bool ZEROS, bool EXACT>
+struct Shape {
+    static constexpr int kAhead = MT == 1 ? 2 : 4;                     // blocks whose weights are on their way together
+    static constexpr int kX = MT == 1 && sizeof(X) == 2 ? kAhead : 1; // of them, those whose x is too
+    static constexpr int kPer = SMALL ? 4 : 1;                        // sums of a block that are scaled apart
+    static constexpr int kLoads = (kAhead * kPer * 16 * R + 63) / 64, kScales = kLoads * 64;      // of a wave, in LDS
+    static constexpr int kThreads = MT == 1 && R < 4 ? 1024 : 512;
+    static constexpr int kWaveBytes = std::max(MT * 16 * 16 * R, kScales * (ZEROS ? 2 : 1)) * 4;      // scales, and in the end the sums
+};
+
+template <typename X, int MT, int R, bool SMALL, bool ZEROS, bool EXACT>
+__global__ __launch_bounds__((Shape<X, MT, R, SMALL, ZEROS, EXACT>::kThreads)) void packed_gemm_kernel(PackedGemm g, int strips) {
+    using E = Eight<X>;
+    using W = typename E::W;
+    using S = Shape<X, MT, R, SMALL, ZEROS, EXACT>;
+    constexpr int kPer = S::kPer, kEach = 4 / kPer, kAhead = S::kAhead, kX = S::kX;
+    constexpr bool kSums = ZEROS || !EXACT;                           // sums of x are needed
+    extern __shared__ __align__(16) float lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = int(blockDim.x) >> 6;
+    const int q = lane >> 4, x16 = lane & 15;
+    const int strip = int(blockIdx.x % unsigned(strips)), piece = int(blockIdx.x / unsigned(strips)), col0 = strip * 16 * R, cols = min(g.n - col0, 16 * R);
+    int row0 = piece * MT * 16, rows = min(g.m - row0, MT * 16), of = 0;
+    if (g.offsets) {
+        GroupPieces<MT * 16> pieces(g.offsets, g.groups, g.m);
+        const GroupPiece p = pieces.template find<false>(piece);
+        if (p.group < 0) return;
+        of = p.group;
+        row0 = p.row;
+        rows = min(p.end - p.row, MT * 16);
+    }
+    const bool none = g.offsets && of >= g.groups;                    // rows behind the last group: zeros
+    float* mine = lds + wave * (S::kWaveBytes / 4);
+    v4f acc[MT][R];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int s = 0; s < R; ++s) acc[i][s] = v4f{0, 0, 0, 0};
+    if (!none) {
+        const int bytes = (g.k + 31) / 32 * 16;
+        const uint8_t* w_row[R];
+#pragma unroll
+        for (int s = 0; s < R; ++s) w_row[s] = g.w.data + of * g.w.stride + int64_t(col0 + min(s * 16 + x16, cols - 1)) * g.w.ld;
+        const X* x_row[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) x_row[i] = static_cast<const X*>(g.x) + int64_t(row0 + min(i * 16 + x16, rows - 1)) * g.ldx;
+        const int blocks = (g.k + kBlock - 1) / kBlock, per = (blocks + waves - 1) / waves, begin = wave * per, end = min(begin + per, blocks);
+        const ScaleLoad scales(g.w.scale, g.w.type), zeros(g.w.zero, g.w.type);
+        uint32_t ones[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ones[i] = uint32_t(__builtin_bit_cast(uint16_t, static_cast<W>(1.0f))) * 0x10001u;
+        for (int b0 = begin; b0 < end; b0 += kAhead) {
+            // what this chunk reads is sent for without a branch; blocks behind the end are the last one again, and bytes behind a row's end its last ones,
+            // whose columns have zeros in x
+            v4u32 codes[kAhead][R];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int s = 0; s < R; ++s) codes[u][s] = *reinterpret_cast<const v4u32*>(w_row[s] + min(min(b0 + u, end - 1) * 64 + q * 16, bytes - 16));
+            // the blocks' scales, [block, group][row], for this wave alone
+            ScaleLoad::Halves scale_bits[S::kLoads], zero_bits[ZEROS ? S::kLoads : 1];
+#pragma unroll
+            for (int y = 0; y < S::kLoads; ++y) {
+                const int z = y * 64 + lane, row = z % (16 * R), p = z / (16 * R);
+                const int64_t group = min(((b0 * kPer + p) * (kBlock / kPer)) >> g.w.shift, (g.k - 1) >> g.w.shift);
+                const int64_t at = of * g.w.scale_stride + group * g.w.scale_ld + col0 + min(row, cols - 1);
+                scale_bits[y] = scales.fetch(at);
+                if constexpr (ZEROS) zero_bits[y] = zeros.fetch(at);
+            }
+            E x[kX][MT][4];
+            auto fetch = [&](int u, E (&n)[MT][4]) {
+                const int b = min(b0 + u, end - 1);
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        // which of the block's columns lane q's part of instruction v covers: any order that both operands share
+                        n[i][v].load(x_row[i] + min(b * kBlock + (SMALL ? v * 32 + q * 8 : q * 32 + v * 8), g.k - 8));
+            };
+#pragma unroll
+            for (int u = 0; u < kX; ++u) fetch(u, x[u]);
+#pragma unroll
+            for (int y = 0; y < S::kLoads; ++y) {
+                mine[y * 64 + lane] = scales.value(scale_bits[y]);
+                if constexpr (ZEROS) mine[S::kScales + y * 64 + lane] = (EXACT ? 8.0f : -128.0f) - zeros.value(zero_bits[y]);
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int b = b0 + u;
+                if (b >= end) break;
+                E (&now)[MT][4] = x[u % kX];
+                if (u >= kX) fetch(u, now);
+                uint32_t w[4][4];
+                if ((b + 1) * kBlock > g.k) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        if (i > 0 && i * 16 >= rows) break;
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            const int at = b * kBlock + (SMALL ? v * 32 + q * 8 : q * 32 + v * 8);
+                            now[i][v].move_down(max(at - (g.k - 8), 0));
+                        }
+                    }
+                }
+                // sums of x, once for all of W's rows
+                constexpr bool kOnce = kSums && R > 1;
+                v4f all[kOnce ? MT : 1][kOnce ? kPer : 1];
+                if constexpr (kOnce) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        if (i > 0 && i * 16 >= rows) break;
+#pragma unroll
+                        for (int p = 0; p < kPer; ++p) {
+                            all[i][p] = v4f{0, 0, 0, 0};
+#pragma unroll
+                            for (int v = p * kEach; v < (p + 1) * kEach; ++v) {
+                                uint32_t part[E::kParts][4];
+                                now[i][v].parts(part);
+#pragma unroll
+                                for (int y = E::kParts - 1; y >= 0; --y) all[i][p] = mfma16(ones, part[y], all[i][p], W{});
+                            }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < R; ++s) {
+                    uint32_t word[4] = {codes[u][s][0], codes[u][s][1], codes[u][s][2], codes[u][s][3]};
+                    if constexpr (SMALL) {
+                        // instruction v takes 32 consecutive columns: word v of each lane goes to the lanes of the v-th 16 (4 x 4 transposed over q)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const auto two = __builtin_amdgcn_permlane32_swap(word[i], word[i + 2], false, false);
+                            word[i] = two[0];
+                            word[i + 2] = two[1];
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; i += 2) {
+                            const auto two = __builtin_amdgcn_permlane16_swap(word[i], word[i + 1], false, false);
+                            word[i] = two[0];
+                            word[i + 1] = two[1];
+                        }
+                    }
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) widen_codes<W, EXACT>(word[v], w[v]);
+#pragma unroll
+                    for (int p = 0; p < kPer; ++p) {
+                        const float* of_group = mine + (u * kPer + p) * (16 * R) + s * 16 + q * 4;
+                        const v4f scale = *reinterpret_cast<const v4f*>(of_group);
+                        v4f less = {-136.0f, -136.0f, -136.0f, -136.0f};
+                        if constexpr (ZEROS) less = *reinterpret_cast<const v4f*>(of_group + S::kScales);
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) {
+                            if (i > 0 && i * 16 >= rows) break;
+                            v4f sum = {0, 0, 0, 0}, here = {0, 0, 0, 0};
+                            if constexpr (kOnce) here = all[i][p];
+#pragma unroll
+                            for (int v = p * kEach; v < (p + 1) * kEach; ++v) {
+                                uint32_t part[E::kParts][4];
+                                now[i][v].parts(part);
+#pragma unroll
+                                for (int y = E::kParts - 1; y >= 0; --y) {
+                                    sum = mfma16(w[v], part[y], sum, W{});
+                                    if constexpr (kSums && !kOnce) here = mfma16(ones, part[y], here, W{});
+                                }
+                            }
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                float e = sum[r];
+                                if constexpr (kSums) e = fmaf(less[r], here[r], e);
+                                acc[i][s][r] = fmaf(scale[r], e, acc[i][s][r]);
+                            }
+                        }
+                    }
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    // the wave's sums take the place of its scales
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int s = 0; s < R; ++s) *reinterpret_cast<v4f*>(mine + (i * 16 + x16) * (16 * R) + s * 16 + q * 4) = acc[i][s];
+    __syncthreads();
+    for (int x = threadIdx.x; x < MT * 64 * R; x += blockDim.x) {
+        const int r = x / (4 * R), c = (x % (4 * R)) * 4;
+        if (r >= rows || c >= cols) continue;
+        v4f s = {0, 0, 0, 0};
+        for (int w = 0; w < waves; ++w) s += *reinterpret_cast<const v4f*>(lds + w * (S::kWaveBytes / 4) + r * (16 * R) + c);
+        store_results(g, int64_t(row0 + r) * g.ldy + col0 + c, cols - c, s);
+    }
+}
+
+// Rows of less than eight: a thread for each result.
+template <typename X>
+__global__ __launch_bounds__(256) void packed_gemm_short_kernel(PackedGemm g) {
+    const ScaleLoad scales(g.w.scale, g.w.type), zeros(g.w.zero, g.w.type);
+    const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x, row = id / g.n, col = id - row * g.n;
+    if (row >= g.m) return;
+    int of = 0;
+    if (g.offsets) {
+        of = -1;
+        for (int e = 0; e < g.groups; ++e)
+            if (row >= clamp_offset(g.offsets, e, g.m) && row < clamp_offset(g.offsets, e + 1, g.m)) of = e;
+    }
+    float sum = 0.0f;
+    if (of >= 0 && g.k > 0) {
+        const int64_t at = of * g.w.scale_stride + col;
+        const float scale = scales.value(scales.fetch(at)), zero = g.w.zero ? zeros.value(zeros.fetch(at)) : 8.0f;
+        const uint8_t* w = g.w.data + of * g.w.stride + col * g.w.ld;
+        const X* x = static_cast<const X*>(g.x) + row * g.ldx;
+        float all = 0.0f;
+        for (int l = 0; l < g.k; ++l) {
+            const float v = to_float(x[l]);
+            sum = fmaf(float((w[l / 2] >> (4 * (l & 1))) & 15) - 8.0f, v, sum);
+            all += v;
+        }
+        sum = scale * (g.w.zero ? fmaf(8.0f - zero, all, sum) : sum);
+    }
+    store_results(g, row * g.ldy + col, 1, v4f{sum, 0, 0, 0});
+}
+
+template <typename X, int MT, int R>
+void launch_rows(hipStream_t st, const PackedGemm& g, int waves) {
+    const int strips = (g.n + 16 * R - 1) / (16 * R);
+    const int64_t tiles = g.offsets ? group_pieces(g.m, g.groups, MT * 16) : (g.m + MT * 16 - 1) / (MT * 16);
+    const dim3 grid(unsigned(tiles * strips)), block(64 * waves);
+    const std::true_type yes;
+    const std::false_type no;
+    auto launch = [&](auto small, auto zeros, auto exact) {
+        constexpr bool kSmall = decltype(small)::value, kZeros = decltype(zeros)::value, kExact = decltype(exact)::value;
+        const size_t bytes = size_t(waves) * Shape<X, MT, R, kSmall, kZeros, kExact>::kWaveBytes;
+        hipLaunchKernelGGL((packed_gemm_kernel<X, MT, R, kSmall, kZeros, kExact>), grid, block, bytes, st, g, strips);
+    };
+    auto of_shift = [&](auto exact) {
+        if (g.w.shift != 7 && g.w.zero) launch(yes, yes, exact);
+        else if (g.w.shift != 7) launch(yes, no, exact);
+        else if (g.w.zero) launch(no, yes, exact);
+        else launch(no, no, exact);
+    };
+    if constexpr (std::is_same_v<X, bf16_t>) {
+        if (g.y_type != OZ_F32) return of_shift(no);
+    }
+    of_shift(yes);
+}
+
+template <typename X>
+void launch_typed(hipStream_t st, const PackedGemm& g, int num_cu) {
+    if (g.k < 8) {
+        hipLaunchKernelGGL(packed_gemm_short_kernel<X>, dim3(unsigned((int64_t(g.m) * g.n + 255) / 256)), dim3(256), 0, st, g);
+        return;
+    }
+    const int64_t avg = g.offsets ? (int64_t(g.m) + g.groups - 1) / g.groups : g.m;      // rows of a group on average
+    const int blocks = std::max((g.k + kBlock - 1) / kBlock, 1);
+    const int mt = avg <= 16 ? 1 : avg <= 32 ? 2 : 4;
+    const int64_t tiles = g.offsets ? group_pieces(g.m, g.groups, mt * 16) : (g.m + mt * 16 - 1) / (mt * 16);
+    const int64_t strips = tiles * ((g.n + 15) / 16);
+    // 16s of rows of W to a workgroup, and waves that share k: what fills the chip with 16 waves to a CU that have two blocks each, with as much of W to a
+    // wave as that leaves, since all of it shares the wave's x.
+    auto waves_of = [&](int rows, int most) {
+        int w = 1;
+        while (w < most && w < blocks && strips / rows * w < 16 * num_cu) w *= 2;
+        return w;
+    };
+    int r = 1, waves = waves_of(1, mt == 1 ? 16 : 8);
+    for (int more = 2; more <= (mt == 1 ? 4 : mt == 2 && sizeof(X) == 2 ? 2 : 1); more *= 2) {
+        const int w = waves_of(more, mt == 1 && more < 4 ? 16 : 8);
+        if (strips / more * w < 16 * num_cu) break;
+        r = more;
+        waves = w;
+    }
+    if (mt == 1) {
+        if (r == 4) launch_rows<X, 1, 4>(st, g, waves);
+        else if (r == 2) launch_rows<X, 1, 2>(st, g, waves);
+        else launch_rows<X, 1, 1>(st, g, waves);
+    } else if (mt == 2) {
+        if constexpr (sizeof(X) == 2) {
+            if (r == 2) return launch_rows<X, 2, 2>(st, g, waves);
+        }
+        launch_rows<X, 2, 1>(st, g, waves);
+    } else {
+        launch_rows<X, 4, 1>(st, g, waves);
+    }
+}
+
+}  // namespace
+
+}  // namespace oz

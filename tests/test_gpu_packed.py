@@ -96,6 +96,11 @@ def check_product(got, x, codes, scale, zero, group, what):
     k = x.shape[1]
     # every addition of 32 bits off by a step of what is added, scales and zero points four more
     bound = (k + 8) * 2.0 ** -23 * size + ref.rounded(exact, got.dtype)
+    if x.dtype == got.dtype == torch.bfloat16:
+        # 128 + code is summed, at most 143 in the place of code - 8, and 136 (or 128 + zero point) times the sum of x comes off: additions of a
+        # group's up to 128 products in 4 instructions and one fused subtraction, each off by a step of sums of 143 |x|
+        at = torch.arange(k, device=x.device) // group
+        bound = bound + 10 * 2.0 ** -24 * 143 * (x.double().abs() @ scale.double().abs().T[:, at].T)
     err = (got.double() - exact).abs()
     assert got.shape == exact.shape and (err <= bound).all(), (what, (err / bound).max().item())
 
