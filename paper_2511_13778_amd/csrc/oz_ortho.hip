@@ -21,27 +21,27 @@ namespace oz {
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 // Scales of the operands: singular values stay below 1.3 (coefficients up to these: include/ozdgemm.h), so entries of X are below 1.3, of O below 0.9,
 // off-diagonals of P below a; small ones reach down to 2^-24 below.
 constexpr float kScaleX = 4096.0f, kScaleO = 16384.0f, kScaleP = 4096.0f;
 constexpr int kStep = 64;                 // of k: 128 bytes of a row
-constexpr int kNormParts = 64;
+constexpr int kNormParts = 256;
 
-// What a matrix of the batch has in the workspace; everything is padded to tiles.
+// What a matrix of the batch has in the workspace.  Rows and columns are there up to whole tiles of each product, with zeros behind m and n as far as
+// another product reads them: sums run to the next multiple of 64.
 struct Ortho {
     const void* g;
     void* y;
     int64_t ldg, stride_g, ldy, stride_y;
-    int rows, cols, m, n, mp, np, batch, tiles_m, tiles_n;
-    bool tall, last;
+    int rows, cols, m, n, ldm, ldn, batch;
+    bool tall;
     float a, b, c, eps;
     double* norm;                         // [batch][parts]
-    float* x;                             // [batch][mp][np]
-    float* gram;                          // [batch][mp][mp], at and below the diagonal
-    float *diag, *scale;                  // [batch][mp]: of A; of P
-    f16_t *xh, *xt, *xt_new, *o, *p;      // [batch][parts] of [mp][np], [np][mp], [np][mp], [mp][mp], [mp][mp]
+    float* x;                             // [batch][ldm][ldn], times kScaleX: with operands of two parts
+    f16_t* x_rest;                        // [batch][ldm][ldn], times kScaleX: what xh leaves of X, with operands of one
+    float *diag, *scale;                  // [batch][ldm]: of A; of P
+    f16_t *xh, *xt, *xt_new, *o, *p;      // [batch][parts] of [ldm][ldn], [ldn][ldm], [ldn][ldm], [ldm][ldm], [ldm][ldm]
 };
 
 __device__ __forceinline__ void split(float v, f16_t& hi, f16_t& lo) {
@@ -78,8 +78,11 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(Ortho o) {
     const int b = blockIdx.z, i0 = int(blockIdx.y) * 64, j0 = int(blockIdx.x) * 64;
     const T* g = static_cast<const T*>(o.g) + b * o.stride_g;
     const int x = threadIdx.x & 63, y0 = threadIdx.x >> 6;
+    // the parts in one order, by every wave for itself
     double sum = 0.0;
-    for (int p = 0; p < kNormParts; ++p) sum += o.norm[b * kNormParts + p];
+#pragma unroll
+    for (int p = 0; p < kNormParts / 64; ++p) sum += o.norm[b * kNormParts + p * 64 + (threadIdx.x & 63)];
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     const double inverse = 1.0 / (sqrt(sum) + double(o.eps));
     for (int y = y0; y < 64; y += 4) {
         // (y, x) along G's own rows
@@ -89,265 +92,595 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(Ortho o) {
         else tile[y][x] = v;
     }
     __syncthreads();
-    const int64_t size = int64_t(o.mp) * o.np;
+    const int64_t size = int64_t(o.ldm) * o.ldn;
     for (int y = y0; y < 64; y += 4) {
-        const float v = tile[y][x], w = tile[x][y];
-        const int64_t at = int64_t(i0 + y) * o.np + j0 + x, turned = int64_t(j0 + y) * o.mp + i0 + x;
-        o.x[b * size + at] = v;
+        const float v = tile[y][x] * kScaleX, w = tile[x][y] * kScaleX;
+        const int64_t at = int64_t(i0 + y) * o.ldn + j0 + x, turned = int64_t(j0 + y) * o.ldm + i0 + x;
         f16_t hi, lo;
-        split(v * kScaleX, hi, lo);
+        split(v, hi, lo);
         o.xh[b * PARTS * size + at] = hi;
-        if (PARTS == 2) o.xh[(b * PARTS + 1) * size + at] = lo;
-        split(w * kScaleX, hi, lo);
+        if (PARTS == 2) {
+            o.x[b * size + at] = v;
+            o.xh[(b * PARTS + 1) * size + at] = lo;
+        } else {
+            o.x_rest[b * size + at] = lo;
+        }
+        split(w, hi, lo);
         o.xt[b * PARTS * size + turned] = hi;
         if (PARTS == 2) o.xt[(b * PARTS + 1) * size + turned] = lo;
     }
 }
 
-enum class Product { kGram, kSquare, kApply };
+enum class Product { kGram, kSquare, kApply, kLast };        // kLast: the last step's kApply, which leaves the result
 
-// One tile of a product L R^T, L and R in rows of `k`: T x T by four waves.  acc[j][i][r]: row 16 i + lane % 16 of L, row 16 j + 4 (lane / 16) + r of R,
-// from the wave's corner on.  Two LDS stages: the transfers of a step lie beside the products of the one before.
-template <int T>
+// One tile of a product L R^T, L and R in rows of `k`: T = 32 F rows of each by four waves, (T/2) x (T/2) each.  acc[j][i][r]: row 16 i + lane % 16 of L, row
+// 16 j + 4 (lane / 16) + r of R, from the wave's corner on.  Two LDS stages of 64 of k, whose pieces of 16 bytes are turned by the row so that reads
+// of 16 rows lie in different banks.
+template <int F>
 struct Tile {
-    static constexpr int kWave = T / 2, kF = kWave / 16;          // rows of a wave, fragments of 16
-    static constexpr int kStage = 2 * T * 128, kLds = 2 * kStage;
+    static constexpr int kT = 32 * F, kWave = 16 * F, kH = F / 2;      // rows; of a wave; fragments of half of them
+    static constexpr int kStage = 2 * kT * 128, kLds = 2 * kStage;
 };
+typedef __attribute__((address_space(3))) const v4i32* lds16_t;
 
-template <int T, int PARTS>
-__device__ __forceinline__ void multiply(uint8_t* lds, const f16_t* l, const f16_t* r, int64_t l_part, int64_t r_part, int k, v4f (&acc)[Tile<T>::kF][Tile<T>::kF]) {
-    using S = Tile<T>;
+template <int N>
+struct Int { static constexpr int v = N; };
+
+__device__ __forceinline__ v4f multiply_add(const v4i32& r, const v4i32& l, v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, r), __builtin_bit_cast(f16x8, l), c, 0, 0, 0);
+}
+
+// Small tiles: a ring of stages, of which all but one are on their way.  Two parts: hi lo and lo hi are summed apart from hi hi and added last.
+template <int F, int PARTS>
+struct Ring {
+    static constexpr int kPlane = Tile<F>::kT * 128, kStage = 2 * PARTS * kPlane, kStages = PARTS == 1 ? 4 : 3, kLds = kStages * kStage;
+    static constexpr int kCopies = 2 * PARTS * Tile<F>::kT / 32;          // a wave's, of a stage
+};
+template <int F, int PARTS>
+__device__ __forceinline__ void multiply_small(uint8_t* lds, const f16_t* l, const f16_t* r, int64_t l_part, int64_t r_part, int k, int64_t l_ld, int64_t r_ld, v4f (&acc)[F][F]) {
+    using S = Tile<F>;
+    using G = Ring<F, PARTS>;
+    constexpr int T = S::kT;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t lds0 = lds_address(lds), ld = uint32_t(k) * 2;
-    const uint32_t piece = uint32_t((lane & 7) ^ (lane >> 4)) * 16, off[2] = {uint32_t(lane >> 3) * ld + piece, uint32_t(lane >> 3) * ld + (piece ^ 64)};
-    const int steps = k / kStep, total = steps * (PARTS == 2 ? 3 : 1);
-    // eight rows a transfer; the four waves take them in turn
-    auto copy = [&](int s) {
-        // hi lo, lo hi, hi hi: the small sums first, so that only a third of the additions are rounded at the size of the result
-        const int pass = PARTS == 2 ? s / steps : 2;
-        const uint32_t at = uint32_t(PARTS == 2 ? s - pass * steps : s) * 128, to = lds0 + uint32_t(s & 1) * S::kStage;
-        const v4i32 src_l = tile_buffer(reinterpret_cast<const uint8_t*>(l + (pass == 1 ? l_part : 0)), uint32_t(T) * ld);
-        const v4i32 src_r = tile_buffer(reinterpret_cast<const uint8_t*>(r + (pass == 0 ? r_part : 0)), uint32_t(T) * ld);
+    const uint32_t lds0 = lds_address(lds), ld_l = uint32_t(l_ld) * 2, ld_r = uint32_t(r_ld) * 2;
+    const uint32_t piece = (uint32_t((lane & 7) ^ (lane >> 4)) * 16) ^ ((wave & 1) ? 64u : 0u);
+    const uint32_t off_l = uint32_t(lane >> 3) * ld_l + piece, off_r = uint32_t(lane >> 3) * ld_r + piece;
+    const int steps = k / kStep;
+    v4i32 src_l[PARTS], src_r[PARTS];
 #pragma unroll
-        for (int x = 0; x < T / 32; ++x) {
-            const uint32_t row = uint32_t(x * 4 + wave) * 8;
-            copy16_to_lds(src_l, off[wave & 1], row * ld + at, to + row * 128);
-            copy16_to_lds(src_r, off[wave & 1], row * ld + at, to + (T + row) * 128);
+    for (int p = 0; p < PARTS; ++p) {
+        src_l[p] = tile_buffer(reinterpret_cast<const uint8_t*>(l + p * l_part), uint32_t(T - 1) * ld_l + uint32_t(k) * 2);
+        src_r[p] = tile_buffer(reinterpret_cast<const uint8_t*>(r + p * r_part), uint32_t(T - 1) * ld_r + uint32_t(k) * 2);
+    }
+    // eight rows a transfer; the four waves take them in turn.  Behind the last step its transfers once more, into a stage that nobody reads: so
+    // that as many are always on their way
+    auto copy = [&](int s, int stage) {
+        const uint32_t at = uint32_t(min(s, steps - 1)) * 128, to = lds0 + uint32_t(stage) * G::kStage;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int x = 0; x < T / 32; ++x) {
+                const uint32_t row = uint32_t(x * 4 + wave) * 8;
+                copy16_to_lds(src_l[p], off_l, row * ld_l + at, to + uint32_t(2 * p) * G::kPlane + row * 128);
+                copy16_to_lds(src_r[p], off_r, row * ld_r + at, to + uint32_t(2 * p + 1) * G::kPlane + row * 128);
+            }
+    };
+    const int q = lane >> 4, x16 = lane & 15;
+    const uint32_t sw = uint32_t(x16 >> 1) & 7;
+    uint32_t at[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) at[u] = uint32_t(x16) * 128 + ((uint32_t(2 * q + u) ^ sw) * 16);
+    const uint32_t wl = uint32_t(wave & 1) * S::kWave * 128, wr = uint32_t(G::kPlane + (wave >> 1) * S::kWave * 128);
+    v4f few[F][F];
+#pragma unroll
+    for (int j = 0; j < F; ++j)
+#pragma unroll
+        for (int i = 0; i < F; ++i) acc[j][i] = few[j][i] = v4f{0, 0, 0, 0};
+#pragma unroll
+    for (int s = 0; s < G::kStages - 1; ++s) copy(s, s);
+    int stage = 0;
+    for (int s = 0; s < steps; ++s) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"((G::kStages - 2) * G::kCopies) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        copy(s + G::kStages - 1, stage == 0 ? G::kStages - 1 : stage - 1);
+        const uint32_t from = lds0 + uint32_t(stage) * G::kStage;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            v4i32 fl[PARTS][F], fr[PARTS][F];
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                for (int i = 0; i < F; ++i) {
+                    fl[p][i] = *reinterpret_cast<lds16_t>(from + uint32_t(2 * p) * G::kPlane + wl + uint32_t(i * 16) * 128 + at[u]);
+                    fr[p][i] = *reinterpret_cast<lds16_t>(from + uint32_t(2 * p) * G::kPlane + wr + uint32_t(i * 16) * 128 + at[u]);
+                }
+#pragma unroll
+            for (int j = 0; j < F; ++j)
+#pragma unroll
+                for (int i = 0; i < F; ++i) {
+                    acc[j][i] = multiply_add(fr[0][j], fl[0][i], acc[j][i]);
+                    if (PARTS == 2) {
+                        few[j][i] = multiply_add(fr[PARTS - 1][j], fl[0][i], few[j][i]);
+                        few[j][i] = multiply_add(fr[0][j], fl[PARTS - 1][i], few[j][i]);
+                    }
+                }
+        }
+        stage = stage + 1 == G::kStages ? 0 : stage + 1;
+    }
+    if (PARTS == 2) {
+#pragma unroll
+        for (int j = 0; j < F; ++j)
+#pragma unroll
+            for (int i = 0; i < F; ++i) acc[j][i] += few[j][i];
+    }
+    // what is still on its way lands in stages that nobody reads; the workgroup's LDS is not given back before
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+}
+
+// Large tiles, one wave per SIMD: nothing hides an instruction that delays the next matrix instruction, so reads and transfers lie between them at fixed
+// places.  A step goes in four quarters, (L0,R0) (L0,R1) (L1,R1) (L1,R0), of which each needs one new half of an operand, read before it; the next step
+// starts with the half of R that this one ended with, hence two forms of a step that take turns, one per LDS stage.  A stage's halves are
+// given up as they have been read: X, what a step's first quarter needs, when that step begins, Y, the rest, in its middle.  At both points the waves
+// meet, and the transfers of the same half two steps on start: they have one and a half steps to arrive.
+template <int F, int PARTS>
+__device__ __forceinline__ void multiply_large(uint8_t* lds, const f16_t* l, const f16_t* r, int64_t l_part, int64_t r_part, int k, int64_t l_ld, int64_t r_ld, v4f (&acc)[F][F]) {
+    using S = Tile<F>;
+    constexpr int T = S::kT, H = S::kH, kPlaces = 2 * H * H, kQuarter = H * H, kReads = 4 * H, kCopies = F;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lds0 = lds_address(lds), ld_l = uint32_t(l_ld) * 2, ld_r = uint32_t(r_ld) * 2;
+    const uint32_t bytes_l = uint32_t(T - 1) * ld_l + uint32_t(k) * 2, bytes_r = uint32_t(T - 1) * ld_r + uint32_t(k) * 2;
+    const int per = k / kStep, steps = per * (PARTS == 2 ? 3 : 1);
+    const v4i32 src_l[2] = {tile_buffer(reinterpret_cast<const uint8_t*>(l), bytes_l),
+                            tile_buffer(reinterpret_cast<const uint8_t*>(l + (PARTS == 2 ? l_part : 0)), bytes_l)};
+    const v4i32 src_r[2] = {tile_buffer(reinterpret_cast<const uint8_t*>(r), bytes_r),
+                            tile_buffer(reinterpret_cast<const uint8_t*>(r + (PARTS == 2 ? r_part : 0)), bytes_r)};
+    // a wave's transfers: T/8 rows of half of L and of half of R, eight at a time.  Lane: row lane / 8, piece (lane % 8) turned by the row, which differs by four
+    // pieces between even and odd eights.
+    const uint32_t mine = uint32_t((wave & 1) * (T / 2) + (wave >> 1) * (T / 8)), odd = (mine >> 3) & 1;
+    const uint32_t piece = uint32_t((lane & 7) ^ (lane >> 4)) * 16;
+    const uint32_t even_piece = odd ? piece ^ 64 : piece, row8 = uint32_t(lane >> 3);
+    const uint32_t off_l[2] = {row8 * ld_l + even_piece, row8 * ld_l + (even_piece ^ 64)}, off_r[2] = {row8 * ld_r + even_piece, row8 * ld_r + (even_piece ^ 64)};
+    // transfer x of half hl of L (x < H) or hr of R, of step s, into stage ST
+    auto copy1 = [&](auto ST, int s, int hl, int hr, int x) {
+        const int pass = PARTS == 2 ? (s >= per) + (s >= 2 * per) : 0;        // hi lo, lo hi, hi hi: the small sums first
+        const uint32_t at = uint32_t(s - pass * per) * 128, to = lds0 + decltype(ST)::v * S::kStage;
+        if (x < H) {
+            const uint32_t row = mine + uint32_t(hl * (T / 4) + x * 8);
+            copy16_to_lds(PARTS == 2 && pass == 1 ? src_l[1] : src_l[0], off_l[x & 1], row * ld_l + at, to + row * 128);
+        } else {
+            const uint32_t row = mine + uint32_t(hr * (T / 4) + (x - H) * 8);
+            copy16_to_lds(PARTS == 2 && pass == 0 ? src_r[1] : src_r[0], off_r[(x - H) & 1], row * ld_r + at, to + (T + row) * 128);
         }
     };
     const int q = lane >> 4, x16 = lane & 15;
     const uint32_t sw = uint32_t(x16 >> 1) & 7;
-    typedef __attribute__((address_space(3))) const v4i32* lds16_t;
-    uint32_t at[2];
+    uint32_t rd_l[2][2], rd_r[2][2];          // [stage][half of the fragment's 64 of k]
 #pragma unroll
-    for (int u = 0; u < 2; ++u) at[u] = uint32_t(x16) * 128 + ((uint32_t(u * 4 + q) ^ sw) * 16);
-    const uint32_t wl = uint32_t(wave & 1) * S::kWave * 128, wr = uint32_t(T + (wave >> 1) * S::kWave) * 128;
-    copy(0);
-    for (int s = 0; s < total; ++s) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (s + 1 < total) copy(s + 1);
-        const uint32_t from = lds0 + uint32_t(s & 1) * S::kStage;
+    for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            f16x8 fl[S::kF], fr[S::kF];
-#pragma unroll
-            for (int i = 0; i < S::kF; ++i) {
-                fl[i] = __builtin_bit_cast(f16x8, *reinterpret_cast<lds16_t>(from + wl + uint32_t(i * 16) * 128 + at[u]));
-                fr[i] = __builtin_bit_cast(f16x8, *reinterpret_cast<lds16_t>(from + wr + uint32_t(i * 16) * 128 + at[u]));
-            }
-#pragma unroll
-            for (int j = 0; j < S::kF; ++j)
-#pragma unroll
-                for (int i = 0; i < S::kF; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fr[j], fl[i], acc[j][i], 0, 0, 0);
+            const uint32_t at = lds0 + uint32_t(st) * S::kStage + uint32_t(x16) * 128 + ((uint32_t(2 * q + u) ^ sw) * 16);
+            rd_l[st][u] = at + uint32_t(wave & 1) * S::kWave * 128;
+            rd_r[st][u] = at + uint32_t(T + (wave >> 1) * S::kWave) * 128;
         }
+    v4i32 fl[2][H][2], fr[2][H][2];
+    auto read_l = [&](auto ST, int half, int x) {
+        fl[half][x >> 1][x & 1] = *reinterpret_cast<lds16_t>(rd_l[decltype(ST)::v][x & 1] + uint32_t(half * (T / 4) + (x >> 1) * 16) * 128);
+    };
+    auto read_r = [&](auto ST, int half, int x) {
+        fr[half][x >> 1][x & 1] = *reinterpret_cast<lds16_t>(rd_r[decltype(ST)::v][x & 1] + uint32_t(half * (T / 4) + (x >> 1) * 16) * 128);
+    };
+    // where the matrix instructions of place y of a quarter lie; after a new half of L its fragments one after the other
+    auto jf = [](bool new_l, int y) constexpr -> int { return new_l ? ((y / H) & 1 ? H - 1 - y % H : y % H) : y / H; };
+    auto fi = [](bool new_l, int y) constexpr -> int { return new_l ? y / H : ((y / H) & 1 ? H - 1 - y % H : y % H); };
+    auto half_step = [&](auto HH, auto BB, auto&& read, auto&& copy) {
+        constexpr int h = decltype(HH)::v, b0 = decltype(BB)::v, b1 = 1 - b0;
+#pragma unroll
+        for (int x = 0; x < kPlaces; ++x) {
+            const int y = x % kQuarter;
+            const bool first = x < kQuarter, new_l = h == 1 && first;
+            const int hr = (h == 0) == first ? b0 : b1, j = jf(new_l, y), i = fi(new_l, y);
+            v4f& s = acc[hr * H + j][h * H + i];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                s = multiply_add(fr[hr][j][u], fl[h][i][u], s);
+                // holds the instruction here and its sums in the accumulation registers
+                asm volatile("" : "+a"(s));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            // first half: the other half of R, then L1; second: L0, then, its registers being free, the half of R that is next
+#pragma unroll
+            for (int z = 0; z < kReads; ++z)
+                if ((h == 0 ? z * (kPlaces - kPlaces / 8) / kReads : z < 2 * H ? z * kQuarter / (2 * H) : kQuarter + (z - 2 * H) * (kQuarter * 3 / 4) / (2 * H)) == x) read(z);
+#pragma unroll
+            for (int c = 0; c < kCopies; ++c)
+                if ((2 * c + 1) * kPlaces / (2 * kCopies) == x) copy(c);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto meet = [&]() {
+        // two halves may still be on their way
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(2 * kCopies) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // FIRST: the step's LDS stage, and the half of R that it starts with
+    auto step = [&](auto FIRST, int s) {
+        constexpr int b0 = decltype(FIRST)::v, b1 = 1 - b0;
+        // behind the last step its transfers once more, into a stage that nobody reads: no branches
+        const int ahead = min(s + 2, steps - 1);
+        meet();
+        half_step(Int<0>{}, Int<b0>{}, [&](int z) { if (z < 2 * H) read_r(Int<b0>{}, b1, z); else read_l(Int<b0>{}, 1, z - 2 * H); },
+                  [&](int c) { copy1(Int<b0>{}, ahead, 0, b0, c); });
+        meet();
+        half_step(Int<1>{}, Int<b0>{}, [&](int z) { if (z < 2 * H) read_l(Int<b1>{}, 0, z); else read_r(Int<b1>{}, b1, z - 2 * H); },
+                  [&](int c) { copy1(Int<b0>{}, ahead, 1, b1, c); });
+    };
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int x = 0; x < kCopies; ++x) copy1(Int<0>{}, 0, half, half, x);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int x = 0; x < kCopies; ++x) copy1(Int<1>{}, min(1, steps - 1), half, 1 - half, x);
+    // Cleared while the first tiles are on their way, by matrix instructions with zero operands: what the vector ALU writes the register allocator keeps in
+    // ordinary registers, and moves over and back in every step.
+    const v4i32 zero = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < F; ++j)
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            acc[j][i] = multiply_add(zero, zero, v4f{0, 0, 0, 0});
+            asm volatile("" : "+a"(acc[j][i]));
+        }
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(3 * kCopies) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int x = 0; x < 2 * H; ++x) read_l(Int<0>{}, 0, x);
+#pragma unroll
+    for (int x = 0; x < 2 * H; ++x) read_r(Int<0>{}, 0, x);
+    for (int s = 0;;) {
+        step(Int<0>{}, s);
+        if (++s == steps) break;
+        step(Int<1>{}, s);
+        if (++s == steps) break;
     }
+    // what is still on its way lands in stages that nobody reads; the workgroup's LDS is not given back before
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 }
 
-// four consecutive elements of an operand, whole and what is left of them
-template <int PARTS>
-__device__ __forceinline__ void put_operand(f16_t* to, int64_t part, const float (&v)[4]) {
-    f16x4 hi, lo;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        f16_t h, l;
-        split(v[r], h, l);
-        hi[r] = h;
-        lo[r] = l;
-    }
-    *reinterpret_cast<f16x4*>(to) = hi;
-    if (PARTS == 2) *reinterpret_cast<f16x4*>(to + part) = lo;
+typedef uint32_t v2u32 __attribute__((ext_vector_type(2)));
+typedef uint32_t v4u32 __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+template <int CTRL>
+__device__ __forceinline__ uint32_t from_lane(uint32_t x) { return uint32_t(__builtin_amdgcn_update_dpp(0, int(x), CTRL, 0xF, 0xF, false)); }
+
+// Four 16-bit values of consecutive columns c .. c + 3, as two words, and those of the three other lanes of its four, which have the rows beside: lane
+// k gets column c + k of the four rows.
+__device__ __forceinline__ v2u32 turn(v2u32 w) {
+    const uint32_t lane = threadIdx.x, pick = (lane & 1) ? 0x03020706u : 0x05040100u;
+    const uint32_t low = __builtin_amdgcn_perm(from_lane<0xB1>(w[0]), w[0], pick), high = __builtin_amdgcn_perm(from_lane<0xB1>(w[1]), w[1], pick);
+    const uint32_t other = from_lane<0x4E>((lane & 2) ? low : high);
+    return (lane & 2) ? v2u32{other, high} : v2u32{low, other};
 }
-template <int PARTS>
-__device__ __forceinline__ void put_turned(f16_t* to, int64_t part, int64_t ld, const float (&v)[4]) {
+template <typename H>
+__device__ __forceinline__ v2u32 words(const H (&h)[4]) {
+    return v2u32{uint32_t(__builtin_bit_cast(uint16_t, h[0])) | uint32_t(__builtin_bit_cast(uint16_t, h[1])) << 16,
+                 uint32_t(__builtin_bit_cast(uint16_t, h[2])) | uint32_t(__builtin_bit_cast(uint16_t, h[3])) << 16};
+}
+
+// A tile of a matrix that a kernel reads or writes: one offset per lane, one for the wave, no vector arithmetic in between.
+struct Region {
+    __amdgpu_buffer_rsrc_t buffer;
+    uint32_t lane;                        // bytes
+    __device__ __forceinline__ Region(void* base, int64_t rows, int64_t ld, int64_t cols, int bytes, uint32_t lane_row, uint32_t lane_col)
+        : buffer(__builtin_amdgcn_make_buffer_rsrc(base, 0, int(uint32_t(((rows - 1) * ld + cols) * bytes)), 0x00020000)),
+          lane((lane_row * uint32_t(ld) + lane_col) * uint32_t(bytes)) {}
+    __device__ __forceinline__ v4f load4(uint32_t at) const { return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(buffer, lane, at, 0)); }
+    __device__ __forceinline__ v2u32 load2(uint32_t at) const { return __builtin_bit_cast(v2u32, __builtin_amdgcn_raw_buffer_load_b64(buffer, lane, at, 0)); }
+    __device__ __forceinline__ void store4(uint32_t at, const float (&v)[4]) const {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, v4f{v[0], v[1], v[2], v[3]}), buffer, lane, at, 0);
+    }
+    __device__ __forceinline__ void store2(uint32_t at, v2u32 w) const { __builtin_amdgcn_raw_buffer_store_b64(w, buffer, lane, at, 0); }
+};
+
+// Four values as 16-bit numbers in two words, and what is left of them.
+__device__ __forceinline__ v2u32 halves(const float (&v)[4]) {
+    const f16x2 a = __builtin_convertvector((v2f{v[0], v[1]}), f16x2), b = __builtin_convertvector((v2f{v[2], v[3]}), f16x2);
+    return v2u32{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+}
+__device__ __forceinline__ v2u32 rest(const float (&v)[4], v2u32 w) {
+    float left[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        f16_t h, l;
-        split(v[r], h, l);
-        to[r * ld] = h;
-        if (PARTS == 2) to[r * ld + part] = l;
+    for (int r = 0; r < 4; ++r) left[r] = fmaf(to_float(__builtin_bit_cast(f16_t, uint16_t(w[r / 2] >> (16 * (r & 1))))), -1.0f, v[r]);
+    return halves(left);
+}
+
+// An operand's tile, as it is and (`both`) turned, whole and what is left.
+template <int PARTS>
+struct OperandTile {
+    Region whole, turned, whole_rest, turned_rest;
+    uint32_t ld, turned_ld;
+    __device__ __forceinline__ void put(uint32_t row, uint32_t col, const float (&v)[4], bool both) const {
+        const v2u32 h = halves(v);
+        const uint32_t at = (row * ld + col) * 2, back = (col * turned_ld + row) * 2;
+        whole.store2(at, h);
+        if (both) turned.store2(back, turn(h));
+        if (PARTS == 2) {
+            const v2u32 l = rest(v, h);
+            whole_rest.store2(at, l);
+            if (both) turned_rest.store2(back, turn(l));
+        }
+    }
+};
+
+// Four results at (row, col .. col + 3) of the caller's matrix, which may end before them unless the tile is `whole`.
+template <typename Y>
+__device__ __forceinline__ void put_result(const Ortho& o, Y* y, int row, int col, bool whole, const float (&v)[4]) {
+    Y t[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) put(&t[r], v[r]);
+    if (!o.tall) {
+        Y* to = y + row * o.ldy + col;
+        if (whole || (row < o.m && col + 4 <= o.n)) {
+            __builtin_memcpy(to, t, sizeof(t));
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (row < o.m && col + r < o.n) to[r] = t[r];
+        }
+    } else if constexpr (sizeof(Y) == 2) {
+        const v2u32 w = turn(words(t));
+        const int c = col + (threadIdx.x & 3), r0 = row & ~3;
+        Y* to = y + c * o.ldy + r0;
+        if (whole || (c < o.n && r0 + 4 <= o.m)) {
+            __builtin_memcpy(to, &w, 8);
+        } else {
+            __builtin_memcpy(t, &w, 8);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (c < o.n && r0 + r < o.m) to[r] = t[r];
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (whole || (row < o.m && col + r < o.n)) y[(col + r) * o.ldy + row] = t[r];
     }
 }
 
 // Y: the caller's matrix type, where the last step leaves the result
-template <Product WHAT, int T, int PARTS, typename Y>
-__global__ __launch_bounds__(256) void ortho_product_kernel(Ortho o) {
-    using S = Tile<T>;
+template <Product WHAT, int F, int PARTS, typename Y>
+__global__ __launch_bounds__(256, F == 4 ? 2 : 1) void ortho_product_kernel(Ortho o, int tiles_m, int tiles_n) {
+    using S = Tile<F>;
+    constexpr int T = S::kT;
     extern __shared__ __align__(16) uint8_t lds[];
-    const int64_t b = blockIdx.y, mm = int64_t(o.mp) * o.mp, mn = int64_t(o.mp) * o.np;
+    const int64_t mm = int64_t(o.ldm) * o.ldm, mn = int64_t(o.ldm) * o.ldn;
+    // workgroups are dealt to the 8 XCDs in turn: each gets a run of the batch's tiles, which share operands
+    const int xcd = int(blockIdx.x & 7), run = int(gridDim.x >> 3), more = int(gridDim.x & 7);
+    const int id = xcd * run + min(xcd, more) + int(blockIdx.x >> 3);
+    constexpr bool kApplies = WHAT == Product::kApply || WHAT == Product::kLast;
+    const int of = kApplies ? tiles_m * tiles_n : tiles_m * (tiles_m + 1) / 2;
+    const int64_t b = id / of;
+    const int tile = id - int(b) * of;
     int ti, tj;
-    if constexpr (WHAT == Product::kApply) {
-        ti = int(blockIdx.x) % o.tiles_m;
-        tj = int(blockIdx.x) / o.tiles_m;
+    if constexpr (kApplies) {
+        // bands of four rows of tiles
+        const int band = tile / (4 * tiles_n), high = min(tiles_m - band * 4, 4), in = tile - band * 4 * tiles_n;
+        ti = band * 4 + in % high;
+        tj = in / high;
     } else {
         // tiles at and below the diagonal, row by row
-        ti = int((sqrtf(8.0f * float(blockIdx.x) + 1.0f) - 1.0f) * 0.5f);
-        while ((ti + 1) * (ti + 2) / 2 <= int(blockIdx.x)) ++ti;
-        while (ti * (ti + 1) / 2 > int(blockIdx.x)) --ti;
-        tj = int(blockIdx.x) - ti * (ti + 1) / 2;
+        ti = int((sqrtf(8.0f * float(tile) + 1.0f) - 1.0f) * 0.5f);
+        while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
+        while (ti * (ti + 1) / 2 > tile) --ti;
+        tj = tile - ti * (ti + 1) / 2;
     }
-    v4f acc[S::kF][S::kF];
-#pragma unroll
-    for (int j = 0; j < S::kF; ++j)
-#pragma unroll
-        for (int i = 0; i < S::kF; ++i) acc[j][i] = v4f{0, 0, 0, 0};
+    v4f acc[F][F];
+    const f16_t *left, *right;
+    int64_t left_part = mm, right_part = mm, left_ld = o.ldm, right_ld = o.ldm;
+    int k = (o.m + kStep - 1) / kStep * kStep;
     if constexpr (WHAT == Product::kGram) {
-        const f16_t* x = o.xh + b * PARTS * mn;
-        multiply<T, PARTS>(lds, x + int64_t(ti) * T * o.np, x + int64_t(tj) * T * o.np, mn, mn, o.np, acc);
+        k = (o.n + kStep - 1) / kStep * kStep;
+        left = right = o.xh + b * PARTS * mn;
+        left_part = right_part = mn;
+        left_ld = right_ld = o.ldn;
     } else if constexpr (WHAT == Product::kSquare) {
-        const f16_t* x = o.o + b * PARTS * mm;
-        multiply<T, PARTS>(lds, x + int64_t(ti) * T * o.mp, x + int64_t(tj) * T * o.mp, mm, mm, o.mp, acc);
+        left = right = o.o + b * PARTS * mm;
     } else {
-        multiply<T, PARTS>(lds, o.p + b * PARTS * mm + int64_t(ti) * T * o.mp, o.xt + b * PARTS * mn + int64_t(tj) * T * o.mp, mm, mn, o.mp, acc);
+        left = o.p + b * PARTS * mm;
+        right = o.xt + b * PARTS * mn;
+        right_part = mn;
     }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row0 = ti * T + (wave & 1) * S::kWave + (lane & 15), col0 = tj * T + (wave >> 1) * S::kWave + (lane >> 4) * 4;
-    const float* diag = o.diag + b * o.mp;
+    left += int64_t(ti) * T * left_ld;
+    right += int64_t(tj) * T * right_ld;
+    if constexpr (F < 4) multiply_small<F, PARTS>(lds, left, right, left_part, right_part, k, left_ld, right_ld, acc);
+    else multiply_large<F, PARTS>(lds, left, right, left_part, right_part, k, left_ld, right_ld, acc);
+    // ---- what becomes of the sums: fragment (i, j) of a wave has four columns of a row to a lane
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lane_row = uint32_t((wave & 1) * S::kWave + (lane & 15)), lane_col = uint32_t((wave >> 1) * S::kWave + (lane >> 4) * 4);
+    const uint32_t back_row = uint32_t((wave >> 1) * S::kWave + (lane >> 4) * 4 + (lane & 3)), back_col = uint32_t((wave & 1) * S::kWave + (lane & 12));      // turned
+    const int row0 = ti * T + int(lane_row), col0 = tj * T + int(lane_col);
+    // read, a row of fragments ahead: O (times kScaleO) or X (times kScaleX), X of two-part operands in 32 bits, the others in two 16-bit parts
+    constexpr bool kReads = WHAT != Product::kGram, kWide = kApplies && PARTS == 2, kTwo = kReads && !kWide && (kApplies || PARTS == 2);
+    const int64_t ld = kApplies ? o.ldn : o.ldm, corner = int64_t(ti) * T * ld + tj * T, part = kApplies ? mn : mm;
+    f16_t* const to = WHAT == Product::kGram ? o.o + b * PARTS * mm : WHAT == Product::kSquare ? o.p + b * PARTS * mm : o.xh + b * PARTS * mn;
+    f16_t* const back = kApplies ? o.xt_new + b * PARTS * mn : to;
+    const int64_t back_corner = int64_t(tj) * T * o.ldm + ti * T;
+    const OperandTile<PARTS> operand{Region(to + corner, T, ld, T, 2, lane_row, lane_col), Region(back + back_corner, T, o.ldm, T, 2, back_row, back_col),
+                                     Region(to + corner + (PARTS - 1) * part, T, ld, T, 2, lane_row, lane_col),
+                                     Region(back + back_corner + (PARTS - 1) * part, T, o.ldm, T, 2, back_row, back_col), uint32_t(ld), uint32_t(o.ldm)};
+    f16_t* const first = WHAT == Product::kSquare ? o.o + b * PARTS * mm + corner : to + corner;
+    f16_t* const second = kApplies && PARTS == 1 ? o.x_rest + b * mn + corner : first + (PARTS - 1) * part;
+    const Region wide(kWide ? static_cast<void*>(o.x + b * mn + corner) : nullptr, T, ld, T, 4, lane_row, lane_col);
+    const Region high(first, T, ld, T, 2, lane_row, lane_col), low(second, T, ld, T, 2, lane_row, lane_col);
+    struct Old { v4f w; v2u32 h, l; };
+    auto fetch = [&](int i, int j) {
+        Old x{};
+        const uint32_t at = uint32_t(i * 16) * uint32_t(ld) + j * 16;
+        if constexpr (kWide) x.w = wide.load4(at * 4);
+        if constexpr (kReads && !kWide) x.h = high.load2(at * 2);
+        if constexpr (kTwo) x.l = low.load2(at * 2);
+        return x;
+    };
+    // factor * what was there + add
+    auto times_old = [&](const Old& x, int r, float factor, float add) {
+        if constexpr (kWide) return fmaf(factor, x.w[r], add);
+        const float h = to_float(__builtin_bit_cast(f16_t, uint16_t(x.h[r / 2] >> (16 * (r & 1))))), l = to_float(__builtin_bit_cast(f16_t, uint16_t(x.l[r / 2] >> (16 * (r & 1)))));
+        if constexpr (kTwo) add = fmaf(factor, l, add);
+        return fmaf(factor, h, add);
+    };
+    Old old[kReads ? 2 : 1][kReads ? F : 1];
+    v4f of_col[WHAT == Product::kSquare ? F : 1];
+    float of_row[kReads ? F : 1];
+    if constexpr (kReads) {
 #pragma unroll
-    for (int i = 0; i < S::kF; ++i) {
-        const int row = row0 + i * 16;
-        float of_row = 0.0f;
-        if constexpr (WHAT == Product::kSquare) of_row = diag[row];
-        if constexpr (WHAT == Product::kApply) of_row = o.scale[b * o.mp + row];
+        for (int i = 0; i < F; ++i) of_row[i] = (kApplies ? o.scale : o.diag)[b * o.ldm + row0 + i * 16];
 #pragma unroll
-        for (int j = 0; j < S::kF; ++j) {
-            const int col = col0 + j * 16;
+        for (int j = 0; j < F; ++j) {
+            old[0][j] = fetch(0, j);
+            if constexpr (WHAT == Product::kSquare) of_col[j] = *reinterpret_cast<const v4f*>(o.diag + b * o.ldm + col0 + j * 16);
+        }
+    }
+    const bool on_diagonal = !kApplies && ti == tj && (wave & 1) == (wave >> 1);
+    const bool whole = WHAT == Product::kLast && (ti + 1) * T <= o.m && (tj + 1) * T <= o.n;
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+        if constexpr (kReads) {
+            if (i + 1 < F) {
+#pragma unroll
+                for (int j = 0; j < F; ++j) old[(i + 1) & 1][j] = fetch(i + 1, j);
+            }
+        }
+        const float row_part = WHAT == Product::kSquare ? fmaf(o.c, of_row[i], o.b) * (kScaleP / kScaleO) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+            const v4f sum = acc[j][i];
             float v[4];
-            if constexpr (WHAT == Product::kApply) {
-                float* x = o.x + b * mn + int64_t(row) * o.np + col;
-                const v4f old = *reinterpret_cast<const v4f*>(x);
+            if constexpr (kApplies) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = fmaf(of_row, old[r], acc[j][i][r] * (1.0f / (kScaleP * kScaleX)));
-                if (o.last) {
-                    Y* y = static_cast<Y*>(o.y) + b * o.stride_y;
+                for (int r = 0; r < 4; ++r) v[r] = times_old(old[i & 1][j], r, of_row[i], sum[r] * (1.0f / kScaleP));
+                if constexpr (WHAT == Product::kLast) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (row < o.m && col + r < o.n) put(o.tall ? y + (col + r) * o.ldy + row : y + row * o.ldy + col + r, v[r]);
+                    for (int r = 0; r < 4; ++r) v[r] *= 1.0f / kScaleX;
+                    put_result(o, static_cast<Y*>(o.y) + b * o.stride_y, row0 + i * 16, col0 + j * 16, whole, v);
                 } else {
-                    *reinterpret_cast<v4f*>(x) = v4f{v[0], v[1], v[2], v[3]};
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] *= kScaleX;
-                    put_operand<PARTS>(o.xh + b * PARTS * mn + int64_t(row) * o.np + col, mn, v);
-                    put_turned<PARTS>(o.xt_new + b * PARTS * mn + int64_t(col) * o.mp + row, mn, o.mp, v);
+                    const uint32_t at = uint32_t(i * 16) * uint32_t(ld) + j * 16;
+                    if constexpr (kWide) wide.store4(at * 4, v);
+                    else low.store2(at * 2, rest(v, halves(v)));
+                    operand.put(i * 16, j * 16, v, true);
                 }
             } else {
-                float* a = o.gram + b * mm + int64_t(row) * o.mp + col;
-                f16_t* to = (WHAT == Product::kGram ? o.o : o.p) + b * PARTS * mm;
                 if constexpr (WHAT == Product::kGram) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        v[r] = acc[j][i][r] * (1.0f / (kScaleX * kScaleX));
-                        if (row == col + r) o.diag[b * o.mp + row] = v[r];
-                    }
-                    *reinterpret_cast<v4f*>(a) = v4f{v[0], v[1], v[2], v[3]};
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = row == col + r ? 0.0f : v[r] * kScaleO;
+                    for (int r = 0; r < 4; ++r) v[r] = sum[r] * (kScaleO / (kScaleX * kScaleX));
                 } else {
-                    const v4f old = *reinterpret_cast<const v4f*>(a), of_col = *reinterpret_cast<const v4f*>(diag + col);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float square = acc[j][i][r] * (1.0f / (kScaleO * kScaleO));
-                        if (row == col + r) {
-                            o.scale[b * o.mp + row] = fmaf(of_row, fmaf(o.c, of_row, o.b), o.a) + o.c * square;
-                            v[r] = 0.0f;
-                        } else {
-                            v[r] = fmaf(old[r], fmaf(o.c, of_row + of_col[r], o.b), o.c * square) * kScaleP;
-                        }
-                    }
+                    for (int r = 0; r < 4; ++r)
+                        v[r] = times_old(old[i & 1][j], r, fmaf(o.c * (kScaleP / kScaleO), of_col[j][r], row_part), sum[r] * (o.c * (kScaleP / (kScaleO * kScaleO))));
                 }
-                put_operand<PARTS>(to + int64_t(row) * o.mp + col, mm, v);
-                if (ti != tj) put_turned<PARTS>(to + int64_t(col) * o.mp + row, mm, o.mp, v);
+                if (i == j && on_diagonal) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if ((lane & 15) == (lane >> 4) * 4 + r) {
+                            const int64_t d = b * o.ldm + row0 + i * 16;
+                            if constexpr (WHAT == Product::kGram) o.diag[d] = v[r] * (1.0f / kScaleO);
+                            else o.scale[d] = fmaf(of_row[i], fmaf(o.c, of_row[i], o.b), o.a) + o.c * (sum[r] * (1.0f / (kScaleO * kScaleO)));
+                            v[r] = 0.0f;
+                        }
+                }
+                operand.put(i * 16, j * 16, v, ti != tj);          // a tile on the diagonal has both of its sides itself
             }
         }
     }
 }
 
-int tile_of(int64_t, int64_t m, int64_t) { return m <= 256 ? 64 : 128; }
+// Sides of the tiles: of A and A^2, of P X.
+struct Tiles { int square, apply; };
+Tiles tiles_of(int64_t batch, int64_t m, int64_t n, int parts) {
+    const int t = m <= 256 ? 64 : m <= 1024 ? 128 : 256;
+    return Tiles{t, t};
+}
 
 struct Plan {
-    int64_t m, n, mp, np, chunk;
-    int tile, parts;
-    size_t norm, x, gram, vec, xh, o, total;      // bytes of each piece, for a chunk
+    int64_t m, n, ldm, ldn, chunk;
+    Tiles tiles;
+    int parts;
+    size_t norm, x, vec, xh, o, total;      // bytes of each piece, for a chunk
 };
 Plan plan_of(int64_t batch, int64_t rows, int64_t cols, int type) {
     Plan p{};
     p.m = std::min(rows, cols);
     p.n = std::max(rows, cols);
-    p.tile = tile_of(batch, p.m, p.n);
-    p.mp = (p.m + p.tile - 1) / p.tile * p.tile;
-    p.np = (p.n + p.tile - 1) / p.tile * p.tile;
     p.parts = type == OZ_BF16 ? 1 : 2;
+    p.tiles = tiles_of(batch, p.m, p.n, p.parts);
+    auto up = [](int64_t v, int64_t to) { return (v + to - 1) / to * to; };
+    p.ldm = std::max(up(p.m, p.tiles.square), up(p.m, p.tiles.apply));
+    p.ldn = up(p.n, p.tiles.apply);
     // as many matrices at a time as make 4096 tiles: more would only take more memory
-    const int64_t tiles = (p.mp / p.tile) * (p.np / p.tile);
+    const int64_t tiles = up(p.m, p.tiles.apply) / p.tiles.apply * (p.ldn / p.tiles.apply);
     p.chunk = std::min(batch, std::max<int64_t>(1, (4096 + tiles - 1) / tiles));
     auto piece = [&](int64_t elems, int64_t bytes) { return size_t((p.chunk * elems * bytes + 255) / 256 * 256); };
     p.norm = piece(kNormParts, 8);
-    p.x = piece(p.mp * p.np, 4);
-    p.gram = piece(p.mp * p.mp, 4);
-    p.vec = piece(p.mp, 4);
-    p.xh = piece(p.mp * p.np, 2 * p.parts);
-    p.o = piece(p.mp * p.mp, 2 * p.parts);
-    p.total = p.norm + p.x + p.gram + 2 * p.vec + 3 * p.xh + 2 * p.o;
+    p.x = piece(p.ldm * p.ldn, p.parts == 2 ? 4 : 2);
+    p.vec = piece(p.ldm, 4);
+    p.xh = piece(p.ldm * p.ldn, 2 * p.parts);
+    p.o = piece(p.ldm * p.ldm, 2 * p.parts);
+    p.total = p.norm + p.x + 2 * p.vec + 3 * p.xh + 2 * p.o;
     return p;
 }
 
-template <int T, int PARTS, typename Y>
-void products(hipStream_t st, Ortho& o, int steps) {
-    const dim3 half(unsigned(o.tiles_m * (o.tiles_m + 1) / 2), unsigned(o.batch)), all(unsigned(o.tiles_m * o.tiles_n), unsigned(o.batch));
-    constexpr int lds = Tile<T>::kLds;
-    for (int s = 0; s < steps; ++s) {
-        o.last = s == steps - 1;
-        hipLaunchKernelGGL((ortho_product_kernel<Product::kGram, T, PARTS, f16_t>), half, dim3(256), lds, st, o);
-        hipLaunchKernelGGL((ortho_product_kernel<Product::kSquare, T, PARTS, f16_t>), half, dim3(256), lds, st, o);
-        hipLaunchKernelGGL((ortho_product_kernel<Product::kApply, T, PARTS, Y>), all, dim3(256), lds, st, o);
-        std::swap(o.xt, o.xt_new);
-    }
+template <int F, int PARTS>
+constexpr int kLdsOf = F < 4 ? Ring<F, PARTS>::kLds : Tile<F>::kLds;
+
+template <Product WHAT, int F, int PARTS, typename Y>
+void launch_product(hipStream_t st, const Ortho& o) {
+    constexpr int T = Tile<F>::kT;
+    const int tiles_m = (o.m + T - 1) / T, tiles_n = (o.n + T - 1) / T;
+    const bool half = WHAT == Product::kGram || WHAT == Product::kSquare;
+    const unsigned tiles = unsigned((half ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n) * o.batch);
+    constexpr int lds = kLdsOf<F, PARTS>;
+    hipLaunchKernelGGL((ortho_product_kernel<WHAT, F, PARTS, Y>), dim3(tiles), dim3(256), lds, st, o, tiles_m, tiles_n);
+}
+template <Product WHAT, int PARTS, typename Y>
+void product(hipStream_t st, const Ortho& o, int tile) {
+    if (tile == 64) launch_product<WHAT, 2, PARTS, Y>(st, o);
+    else if (tile == 128) launch_product<WHAT, 4, PARTS, Y>(st, o);
+    else if (tile == 192) launch_product<WHAT, 6, PARTS, Y>(st, o);
+    else launch_product<WHAT, 8, PARTS, Y>(st, o);
 }
 
 template <typename Y, int PARTS>
 void run(hipStream_t st, Ortho o, const Plan& p, int steps) {
     hipLaunchKernelGGL(ortho_norm_kernel<Y>, dim3(kNormParts, unsigned(o.batch)), dim3(256), 0, st, o);
-    hipLaunchKernelGGL((ortho_start_kernel<Y, PARTS>), dim3(unsigned(o.np / 64), unsigned(o.mp / 64), unsigned(o.batch)), dim3(256), 0, st, o);
-    if (p.tile == 64) products<64, PARTS, Y>(st, o, steps);
-    else products<128, PARTS, Y>(st, o, steps);
+    hipLaunchKernelGGL((ortho_start_kernel<Y, PARTS>), dim3(unsigned(o.ldn / 64), unsigned(o.ldm / 64), unsigned(o.batch)), dim3(256), 0, st, o);
+    for (int s = 0; s < steps; ++s) {
+        product<Product::kGram, PARTS, f16_t>(st, o, p.tiles.square);
+        product<Product::kSquare, PARTS, f16_t>(st, o, p.tiles.square);
+        if (s + 1 < steps) product<Product::kApply, PARTS, f16_t>(st, o, p.tiles.apply);
+        else product<Product::kLast, PARTS, Y>(st, o, p.tiles.apply);
+        std::swap(o.xt, o.xt_new);
+    }
 }
 
-template <Product WHAT, int T, int PARTS, typename Y>
+template <Product WHAT, int F, int PARTS, typename Y>
 bool allow_lds() {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(ortho_product_kernel<WHAT, T, PARTS, Y>), hipFuncAttributeMaxDynamicSharedMemorySize, Tile<T>::kLds) == hipSuccess;
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(ortho_product_kernel<WHAT, F, PARTS, Y>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               kLdsOf<F, PARTS>) == hipSuccess;
 }
-template <int T, int PARTS>
+template <int F>
 bool allow_tile() {
-    return allow_lds<Product::kGram, T, PARTS, f16_t>() && allow_lds<Product::kSquare, T, PARTS, f16_t>();
+    return allow_lds<Product::kGram, F, 1, f16_t>() && allow_lds<Product::kGram, F, 2, f16_t>() && allow_lds<Product::kSquare, F, 1, f16_t>() &&
+           allow_lds<Product::kSquare, F, 2, f16_t>() && allow_lds<Product::kApply, F, 1, f16_t>() && allow_lds<Product::kApply, F, 2, f16_t>() &&
+           allow_lds<Product::kLast, F, 1, bf16_t>() && allow_lds<Product::kLast, F, 2, f16_t>() && allow_lds<Product::kLast, F, 2, float>();
 }
 
 }  // namespace
 
-bool prepare_ortho() {
-    return allow_tile<128, 1>() && allow_tile<128, 2>() && allow_lds<Product::kApply, 128, 1, bf16_t>() && allow_lds<Product::kApply, 128, 2, f16_t>() &&
-           allow_lds<Product::kApply, 128, 2, float>();
-}
+bool prepare_ortho() { return allow_tile<2>() && allow_tile<4>() && allow_tile<6>() && allow_tile<8>(); }
 
 size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols, int type) {
     return batch > 0 && rows > 0 && cols > 0 ? plan_of(batch, rows, cols, type).total : 0;
@@ -357,15 +690,15 @@ void launch_ortho(hipStream_t st, const OrthoCall& c, int) {
     const Plan p = plan_of(c.batch, c.rows, c.cols, c.type);
     Ortho o{};
     o.ldg = c.ldx; o.stride_g = c.stride_x; o.ldy = c.ldy; o.stride_y = c.stride_y;
-    o.rows = c.rows; o.cols = c.cols; o.m = int(p.m); o.n = int(p.n); o.mp = int(p.mp); o.np = int(p.np);
-    o.tiles_m = o.mp / p.tile; o.tiles_n = o.np / p.tile;
+    o.rows = c.rows; o.cols = c.cols; o.m = int(p.m); o.n = int(p.n); o.ldm = int(p.ldm); o.ldn = int(p.ldn);
     o.tall = c.rows > c.cols;
     o.a = c.a; o.b = c.b; o.c = c.c; o.eps = c.eps;
     uint8_t* at = static_cast<uint8_t*>(c.ws);
     auto take = [&](size_t bytes) { uint8_t* q = at; at += bytes; return q; };
     o.norm = reinterpret_cast<double*>(take(p.norm));
-    o.x = reinterpret_cast<float*>(take(p.x));
-    o.gram = reinterpret_cast<float*>(take(p.gram));
+    uint8_t* const x = take(p.x);
+    o.x = reinterpret_cast<float*>(x);
+    o.x_rest = reinterpret_cast<f16_t*>(x);
     o.diag = reinterpret_cast<float*>(take(p.vec));
     o.scale = reinterpret_cast<float*>(take(p.vec));
     o.xh = reinterpret_cast<f16_t*>(take(p.xh));
