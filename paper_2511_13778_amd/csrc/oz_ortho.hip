@@ -113,9 +113,10 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(Ortho o) {
 
 enum class Product { kGram, kSquare, kApply, kLast };        // kLast: the last step's kApply, which leaves the result
 
-// One tile of a product L R^T, L and R in rows of `k`: T = 32 F rows of each by four waves, (T/2) x (T/2) each.  acc[j][i][r]: row 16 i + lane % 16 of L, row
-// 16 j + 4 (lane / 16) + r of R, from the wave's corner on.  Two LDS stages of 64 of k, whose pieces of 16 bytes are turned by the row so that reads
-// of 16 rows lie in different banks.
+// One tile of a product L R^T, L and R in rows of `k`: T = 32 F rows of each by four waves, (T/2) x (T/2) each, in LDS stages of 64 of k, whose pieces
+// of 16 bytes are turned by the row so that reads of 16 rows lie in different banks.  Rows lie in LDS so that a lane's results of two fragments are
+// neighbours: 32 rows of a wave are two fragments of 16, of which one has the first four of each eight and the other the last four.  With H = F / 2, acc[s H + j][h H + i][r]
+// is row 32 i + 8 (lane % 16 / 4) + 4 h + lane % 4 of L and row 32 j + 8 (lane / 16) + 4 s + r of R, from the wave's corner on.
 template <int F>
 struct Tile {
     static constexpr int kT = 32 * F, kWave = 16 * F, kH = F / 2;      // rows; of a wave; fragments of half of them
@@ -144,8 +145,10 @@ __device__ __forceinline__ void multiply_small(uint8_t* lds, const f16_t* l, con
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lds0 = lds_address(lds), ld_l = uint32_t(l_ld) * 2, ld_r = uint32_t(r_ld) * 2;
     const uint32_t piece = (uint32_t((lane & 7) ^ (lane >> 4)) * 16) ^ ((wave & 1) ? 64u : 0u);
-    const uint32_t off_l = uint32_t(lane >> 3) * ld_l + piece, off_r = uint32_t(lane >> 3) * ld_r + piece;
+    const uint32_t row8 = uint32_t(lane >> 5) * 8 + uint32_t(lane >> 3 & 3);       // of a transfer's eight
+    const uint32_t off_l = row8 * ld_l + piece, off_r = row8 * ld_r + piece;
     const int steps = k / kStep;
+    static_assert(F == 2, "two fragments of a wave");
     v4i32 src_l[PARTS], src_r[PARTS];
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
@@ -160,9 +163,9 @@ __device__ __forceinline__ void multiply_small(uint8_t* lds, const f16_t* l, con
         for (int p = 0; p < PARTS; ++p)
 #pragma unroll
             for (int x = 0; x < T / 32; ++x) {
-                const uint32_t row = uint32_t(x * 4 + wave) * 8;
-                copy16_to_lds(src_l[p], off_l, row * ld_l + at, to + uint32_t(2 * p) * G::kPlane + row * 128);
-                copy16_to_lds(src_r[p], off_r, row * ld_r + at, to + uint32_t(2 * p + 1) * G::kPlane + row * 128);
+                const uint32_t place = uint32_t(x * 4 + wave) * 8, row = uint32_t(x * 32 + (wave & 1) * 16 + (wave >> 1) * 4);
+                copy16_to_lds(src_l[p], off_l, row * ld_l + at, to + uint32_t(2 * p) * G::kPlane + place * 128);
+                copy16_to_lds(src_r[p], off_r, row * ld_r + at, to + uint32_t(2 * p + 1) * G::kPlane + place * 128);
             }
     };
     const int q = lane >> 4, x16 = lane & 15;
@@ -237,20 +240,21 @@ __device__ __forceinline__ void multiply_large(uint8_t* lds, const f16_t* l, con
                             tile_buffer(reinterpret_cast<const uint8_t*>(r + (PARTS == 2 ? r_part : 0)), bytes_r)};
     // a wave's transfers: T/8 rows of half of L and of half of R, eight at a time.  Lane: row lane / 8, piece (lane % 8) turned by the row, which differs by four
     // pieces between even and odd eights.
-    const uint32_t mine = uint32_t((wave & 1) * (T / 2) + (wave >> 1) * (T / 8)), odd = (mine >> 3) & 1;
+    const uint32_t mine = uint32_t((wave & 1) * (T / 2) + (wave >> 1) * (T / 8)), odd = (mine >> 3) & 1;            // in LDS
+    const uint32_t mine_row = uint32_t((wave & 1) * (T / 2) + (wave >> 1) * (T / 4));                             // of the matrix
     const uint32_t piece = uint32_t((lane & 7) ^ (lane >> 4)) * 16;
-    const uint32_t even_piece = odd ? piece ^ 64 : piece, row8 = uint32_t(lane >> 3);
+    const uint32_t even_piece = odd ? piece ^ 64 : piece, row8 = uint32_t(lane >> 5) * 8 + uint32_t(lane >> 3 & 3);
     const uint32_t off_l[2] = {row8 * ld_l + even_piece, row8 * ld_l + (even_piece ^ 64)}, off_r[2] = {row8 * ld_r + even_piece, row8 * ld_r + (even_piece ^ 64)};
     // transfer x of half hl of L (x < H) or hr of R, of step s, into stage ST
     auto copy1 = [&](auto ST, int s, int hl, int hr, int x) {
         const int pass = PARTS == 2 ? (s >= per) + (s >= 2 * per) : 0;        // hi lo, lo hi, hi hi: the small sums first
         const uint32_t at = uint32_t(s - pass * per) * 128, to = lds0 + decltype(ST)::v * S::kStage;
         if (x < H) {
-            const uint32_t row = mine + uint32_t(hl * (T / 4) + x * 8);
-            copy16_to_lds(PARTS == 2 && pass == 1 ? src_l[1] : src_l[0], off_l[x & 1], row * ld_l + at, to + row * 128);
+            const uint32_t place = mine + uint32_t(hl * (T / 4) + x * 8), row = mine_row + uint32_t(x * 16 + hl * 4);
+            copy16_to_lds(PARTS == 2 && pass == 1 ? src_l[1] : src_l[0], off_l[x & 1], row * ld_l + at, to + place * 128);
         } else {
-            const uint32_t row = mine + uint32_t(hr * (T / 4) + (x - H) * 8);
-            copy16_to_lds(PARTS == 2 && pass == 0 ? src_r[1] : src_r[0], off_r[(x - H) & 1], row * ld_r + at, to + (T + row) * 128);
+            const uint32_t place = mine + uint32_t(hr * (T / 4) + (x - H) * 8), row = mine_row + uint32_t((x - H) * 16 + hr * 4);
+            copy16_to_lds(PARTS == 2 && pass == 0 ? src_r[1] : src_r[0], off_r[(x - H) & 1], row * ld_r + at, to + (T + place) * 128);
         }
     };
     const int q = lane >> 4, x16 = lane & 15;
@@ -367,12 +371,6 @@ __device__ __forceinline__ v2u32 turn(v2u32 w) {
     const uint32_t other = from_lane<0x4E>((lane & 2) ? low : high);
     return (lane & 2) ? v2u32{other, high} : v2u32{low, other};
 }
-template <typename H>
-__device__ __forceinline__ v2u32 words(const H (&h)[4]) {
-    return v2u32{uint32_t(__builtin_bit_cast(uint16_t, h[0])) | uint32_t(__builtin_bit_cast(uint16_t, h[1])) << 16,
-                 uint32_t(__builtin_bit_cast(uint16_t, h[2])) | uint32_t(__builtin_bit_cast(uint16_t, h[3])) << 16};
-}
-
 // A tile of a matrix that a kernel reads or writes: one offset per lane, one for the wave, no vector arithmetic in between.
 struct Region {
     __amdgpu_buffer_rsrc_t buffer;
@@ -380,75 +378,67 @@ struct Region {
     __device__ __forceinline__ Region(void* base, int64_t rows, int64_t ld, int64_t cols, int bytes, uint32_t lane_row, uint32_t lane_col)
         : buffer(__builtin_amdgcn_make_buffer_rsrc(base, 0, int(uint32_t(((rows - 1) * ld + cols) * bytes)), 0x00020000)),
           lane((lane_row * uint32_t(ld) + lane_col) * uint32_t(bytes)) {}
-    __device__ __forceinline__ v4f load4(uint32_t at) const { return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(buffer, lane, at, 0)); }
-    __device__ __forceinline__ v2u32 load2(uint32_t at) const { return __builtin_bit_cast(v2u32, __builtin_amdgcn_raw_buffer_load_b64(buffer, lane, at, 0)); }
-    __device__ __forceinline__ void store4(uint32_t at, const float (&v)[4]) const {
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, v4f{v[0], v[1], v[2], v[3]}), buffer, lane, at, 0);
-    }
-    __device__ __forceinline__ void store2(uint32_t at, v2u32 w) const { __builtin_amdgcn_raw_buffer_store_b64(w, buffer, lane, at, 0); }
+    __device__ __forceinline__ v4u32 load(uint32_t at) const { return __builtin_bit_cast(v4u32, __builtin_amdgcn_raw_buffer_load_b128(buffer, lane, at, 0)); }
+    __device__ __forceinline__ void store(uint32_t at, v4u32 w) const { __builtin_amdgcn_raw_buffer_store_b128(w, buffer, lane, at, 0); }
 };
 
-// Four values as 16-bit numbers in two words, and what is left of them.
-__device__ __forceinline__ v2u32 halves(const float (&v)[4]) {
-    const f16x2 a = __builtin_convertvector((v2f{v[0], v[1]}), f16x2), b = __builtin_convertvector((v2f{v[2], v[3]}), f16x2);
-    return v2u32{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
-}
-__device__ __forceinline__ v2u32 rest(const float (&v)[4], v2u32 w) {
-    float left[4];
+// Eight values as 16-bit numbers, two to a word, and what is left of them.
+__device__ __forceinline__ float half_of(v4u32 w, int i) { return to_float(__builtin_bit_cast(f16_t, uint16_t(w[i / 2] >> (16 * (i & 1))))); }
+__device__ __forceinline__ v4u32 halves(const float (&v)[8]) {
+    v4u32 w;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) left[r] = fmaf(to_float(__builtin_bit_cast(f16_t, uint16_t(w[r / 2] >> (16 * (r & 1))))), -1.0f, v[r]);
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{v[2 * i], v[2 * i + 1]}), f16x2));
+    return w;
+}
+__device__ __forceinline__ v4u32 rest(const float (&v)[8], v4u32 w) {
+    float left[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) left[i] = fmaf(half_of(w, i), -1.0f, v[i]);
     return halves(left);
 }
+// Rows 0 and 4 on of a lane's eight columns to eight rows of its own column of the first (s 0) or last four.
+__device__ __forceinline__ v4u32 turn8(const v4u32 (&w)[2], int s) {
+    const v2u32 a = turn(v2u32{w[0][2 * s], w[0][2 * s + 1]}), b = turn(v2u32{w[1][2 * s], w[1][2 * s + 1]});
+    return v4u32{a[0], a[1], b[0], b[1]};
+}
 
-// An operand's tile, as it is and (`both`) turned, whole and what is left.
-template <int PARTS>
-struct OperandTile {
-    Region whole, turned, whole_rest, turned_rest;
-    uint32_t ld, turned_ld;
-    __device__ __forceinline__ void put(uint32_t row, uint32_t col, const float (&v)[4], bool both) const {
-        const v2u32 h = halves(v);
-        const uint32_t at = (row * ld + col) * 2, back = (col * turned_ld + row) * 2;
-        whole.store2(at, h);
-        if (both) turned.store2(back, turn(h));
-        if (PARTS == 2) {
-            const v2u32 l = rest(v, h);
-            whole_rest.store2(at, l);
-            if (both) turned_rest.store2(back, turn(l));
-        }
-    }
-};
-
-// Four results at (row, col .. col + 3) of the caller's matrix, which may end before them unless the tile is `whole`.
+// 2 x 8 results at (row and row + 4, col .. col + 7) of the caller's matrix, which may end before them unless the tile is `whole`.
 template <typename Y>
-__device__ __forceinline__ void put_result(const Ortho& o, Y* y, int row, int col, bool whole, const float (&v)[4]) {
-    Y t[4];
+__device__ __forceinline__ void put_result(const Ortho& o, Y* y, int row, int col, bool whole, const float (&v)[2][8]) {
+    Y t[2][8];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) put(&t[r], v[r]);
-    if (!o.tall) {
-        Y* to = y + row * o.ldy + col;
-        if (whole || (row < o.m && col + 4 <= o.n)) {
-            __builtin_memcpy(to, t, sizeof(t));
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) put(&t[h][i], v[h][i]);
+    auto along = [&](Y* to, const Y (&u)[8], int have) {
+        if (whole || have >= 8) {
+            __builtin_memcpy(to, u, sizeof(u));
         } else {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (row < o.m && col + r < o.n) to[r] = t[r];
+            for (int i = 0; i < 8; ++i)
+                if (i < have) to[i] = u[i];
         }
-    } else if constexpr (sizeof(Y) == 2) {
-        const v2u32 w = turn(words(t));
-        const int c = col + (threadIdx.x & 3), r0 = row & ~3;
-        Y* to = y + c * o.ldy + r0;
-        if (whole || (c < o.n && r0 + 4 <= o.m)) {
-            __builtin_memcpy(to, &w, 8);
-        } else {
-            __builtin_memcpy(t, &w, 8);
+    };
+    if (!o.tall) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (c < o.n && r0 + r < o.m) to[r] = t[r];
+        for (int h = 0; h < 2; ++h) along(y + int64_t(row + 4 * h) * o.ldy + col, t[h], row + 4 * h < o.m ? o.n - col : 0);
+    } else if constexpr (sizeof(Y) == 2) {
+        v4u32 w[2];
+        __builtin_memcpy(w, t, sizeof(w));
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const v4u32 turned = turn8(w, s);
+            const int c = col + 4 * s + (threadIdx.x & 3), r0 = row & ~7;
+            Y u[8];
+            __builtin_memcpy(u, &turned, sizeof(u));
+            along(y + int64_t(c) * o.ldy + r0, u, c < o.n ? o.m - r0 : 0);
         }
     } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (whole || (row < o.m && col + r < o.n)) y[(col + r) * o.ldy + row] = t[r];
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (whole || (row + 4 * h < o.m && col + i < o.n)) y[int64_t(col + i) * o.ldy + row + 4 * h] = t[h][i];
     }
 }
 
@@ -499,100 +489,124 @@ __global__ __launch_bounds__(256, F == 4 ? 2 : 1) void ortho_product_kernel(Orth
     right += int64_t(tj) * T * right_ld;
     if constexpr (F < 4) multiply_small<F, PARTS>(lds, left, right, left_part, right_part, k, left_ld, right_ld, acc);
     else multiply_large<F, PARTS>(lds, left, right, left_part, right_part, k, left_ld, right_ld, acc);
-    // ---- what becomes of the sums: fragment (i, j) of a wave has four columns of a row to a lane
+    // ---- what becomes of the sums: a lane has 2 x 8 of each 32 x 32 of its wave, rows 4 apart and columns beside each other
+    constexpr int H = S::kH;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t lane_row = uint32_t((wave & 1) * S::kWave + (lane & 15)), lane_col = uint32_t((wave >> 1) * S::kWave + (lane >> 4) * 4);
-    const uint32_t back_row = uint32_t((wave >> 1) * S::kWave + (lane >> 4) * 4 + (lane & 3)), back_col = uint32_t((wave & 1) * S::kWave + (lane & 12));      // turned
+    const uint32_t lane_row = uint32_t((wave & 1) * S::kWave + (lane & 12) * 2 + (lane & 3)), lane_col = uint32_t((wave >> 1) * S::kWave + (lane >> 4) * 8);
+    const uint32_t back_row = lane_col + uint32_t(lane & 3), back_col = lane_row & ~7u;                     // turned
     const int row0 = ti * T + int(lane_row), col0 = tj * T + int(lane_col);
-    // read, a row of fragments ahead: O (times kScaleO) or X (times kScaleX), X of two-part operands in 32 bits, the others in two 16-bit parts
+    // read, 32 rows ahead: O (times kScaleO) or X (times kScaleX), X of two-part operands in 32 bits, the others in two 16-bit parts
     constexpr bool kReads = WHAT != Product::kGram, kWide = kApplies && PARTS == 2, kTwo = kReads && !kWide && (kApplies || PARTS == 2);
     const int64_t ld = kApplies ? o.ldn : o.ldm, corner = int64_t(ti) * T * ld + tj * T, part = kApplies ? mn : mm;
     f16_t* const to = WHAT == Product::kGram ? o.o + b * PARTS * mm : WHAT == Product::kSquare ? o.p + b * PARTS * mm : o.xh + b * PARTS * mn;
-    f16_t* const back = kApplies ? o.xt_new + b * PARTS * mn : to;
-    const int64_t back_corner = int64_t(tj) * T * o.ldm + ti * T;
-    const OperandTile<PARTS> operand{Region(to + corner, T, ld, T, 2, lane_row, lane_col), Region(back + back_corner, T, o.ldm, T, 2, back_row, back_col),
-                                     Region(to + corner + (PARTS - 1) * part, T, ld, T, 2, lane_row, lane_col),
-                                     Region(back + back_corner + (PARTS - 1) * part, T, o.ldm, T, 2, back_row, back_col), uint32_t(ld), uint32_t(o.ldm)};
+    f16_t* const back = (kApplies ? o.xt_new + b * PARTS * mn : to) + int64_t(tj) * T * o.ldm + ti * T;
+    const Region whole_to(to + corner, T, ld, T, 2, lane_row, lane_col), rest_to(to + corner + (PARTS - 1) * part, T, ld, T, 2, lane_row, lane_col);
+    const Region whole_back(back, T, o.ldm, T, 2, back_row, back_col), rest_back(back + (PARTS - 1) * part, T, o.ldm, T, 2, back_row, back_col);
     f16_t* const first = WHAT == Product::kSquare ? o.o + b * PARTS * mm + corner : to + corner;
     f16_t* const second = kApplies && PARTS == 1 ? o.x_rest + b * mn + corner : first + (PARTS - 1) * part;
     const Region wide(kWide ? static_cast<void*>(o.x + b * mn + corner) : nullptr, T, ld, T, 4, lane_row, lane_col);
     const Region high(first, T, ld, T, 2, lane_row, lane_col), low(second, T, ld, T, 2, lane_row, lane_col);
-    struct Old { v4f w; v2u32 h, l; };
+    auto place = [&](int i, int h, int j) { return uint32_t(i * 32 + h * 4) * uint32_t(ld) + uint32_t(j * 32); };
+    struct Old { v4u32 a[2], b[2]; };          // of the two rows: high and low parts, or the first and last four in 32 bits
     auto fetch = [&](int i, int j) {
         Old x{};
-        const uint32_t at = uint32_t(i * 16) * uint32_t(ld) + j * 16;
-        if constexpr (kWide) x.w = wide.load4(at * 4);
-        if constexpr (kReads && !kWide) x.h = high.load2(at * 2);
-        if constexpr (kTwo) x.l = low.load2(at * 2);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t at = place(i, h, j);
+            if constexpr (kWide) {
+                x.a[h] = wide.load(at * 4);
+                x.b[h] = wide.load(at * 4 + 16);
+            } else if constexpr (kReads) {
+                x.a[h] = high.load(at * 2);
+                if constexpr (kTwo) x.b[h] = low.load(at * 2);
+            }
+        }
         return x;
     };
     // factor * what was there + add
-    auto times_old = [&](const Old& x, int r, float factor, float add) {
-        if constexpr (kWide) return fmaf(factor, x.w[r], add);
-        const float h = to_float(__builtin_bit_cast(f16_t, uint16_t(x.h[r / 2] >> (16 * (r & 1))))), l = to_float(__builtin_bit_cast(f16_t, uint16_t(x.l[r / 2] >> (16 * (r & 1)))));
-        if constexpr (kTwo) add = fmaf(factor, l, add);
-        return fmaf(factor, h, add);
+    auto times_old = [&](const Old& x, int h, int c, float factor, float add) {
+        if constexpr (kWide) return fmaf(factor, __uint_as_float(c < 4 ? x.a[h][c & 3] : x.b[h][c & 3]), add);
+        if constexpr (kTwo) add = fmaf(factor, half_of(x.b[h], c), add);
+        return fmaf(factor, half_of(x.a[h], c), add);
     };
-    Old old[kReads ? 2 : 1][kReads ? F : 1];
-    v4f of_col[WHAT == Product::kSquare ? F : 1];
-    float of_row[kReads ? F : 1];
+    Old old[kReads ? 2 : 1][kReads ? H : 1];
+    float of_col[WHAT == Product::kSquare ? H : 1][8], of_row[kReads ? H : 1][2];
     if constexpr (kReads) {
 #pragma unroll
-        for (int i = 0; i < F; ++i) of_row[i] = (kApplies ? o.scale : o.diag)[b * o.ldm + row0 + i * 16];
+        for (int i = 0; i < H; ++i)
 #pragma unroll
-        for (int j = 0; j < F; ++j) {
+            for (int h = 0; h < 2; ++h) of_row[i][h] = (kApplies ? o.scale : o.diag)[b * o.ldm + row0 + i * 32 + h * 4];
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
             old[0][j] = fetch(0, j);
-            if constexpr (WHAT == Product::kSquare) of_col[j] = *reinterpret_cast<const v4f*>(o.diag + b * o.ldm + col0 + j * 16);
+            if constexpr (WHAT == Product::kSquare) __builtin_memcpy(of_col[j], o.diag + b * o.ldm + col0 + j * 32, sizeof(of_col[j]));
         }
     }
     const bool on_diagonal = !kApplies && ti == tj && (wave & 1) == (wave >> 1);
     const bool whole = WHAT == Product::kLast && (ti + 1) * T <= o.m && (tj + 1) * T <= o.n;
 #pragma unroll
-    for (int i = 0; i < F; ++i) {
+    for (int i = 0; i < H; ++i) {
         if constexpr (kReads) {
-            if (i + 1 < F) {
+            if (i + 1 < H) {
 #pragma unroll
-                for (int j = 0; j < F; ++j) old[(i + 1) & 1][j] = fetch(i + 1, j);
+                for (int j = 0; j < H; ++j) old[(i + 1) & 1][j] = fetch(i + 1, j);
             }
         }
-        const float row_part = WHAT == Product::kSquare ? fmaf(o.c, of_row[i], o.b) * (kScaleP / kScaleO) : 0.0f;
 #pragma unroll
-        for (int j = 0; j < F; ++j) {
-            const v4f sum = acc[j][i];
-            float v[4];
-            if constexpr (kApplies) {
+        for (int j = 0; j < H; ++j) {
+            float v[2][8];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = times_old(old[i & 1][j], r, of_row[i], sum[r] * (1.0f / kScaleP));
-                if constexpr (WHAT == Product::kLast) {
+            for (int h = 0; h < 2; ++h) {
+                const float row_part = WHAT == Product::kSquare ? fmaf(o.c, of_row[i][h], o.b) * (kScaleP / kScaleO) : 0.0f;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] *= 1.0f / kScaleX;
-                    put_result(o, static_cast<Y*>(o.y) + b * o.stride_y, row0 + i * 16, col0 + j * 16, whole, v);
-                } else {
-                    const uint32_t at = uint32_t(i * 16) * uint32_t(ld) + j * 16;
-                    if constexpr (kWide) wide.store4(at * 4, v);
-                    else low.store2(at * 2, rest(v, halves(v)));
-                    operand.put(i * 16, j * 16, v, true);
+                for (int c = 0; c < 8; ++c) {
+                    const float sum = acc[(c >> 2) * H + j][h * H + i][c & 3];
+                    if constexpr (kApplies) {
+                        v[h][c] = times_old(old[i & 1][j], h, c, of_row[i][h], sum * (1.0f / kScaleP));
+                        if constexpr (WHAT == Product::kLast) v[h][c] *= 1.0f / kScaleX;
+                    } else if constexpr (WHAT == Product::kGram) {
+                        v[h][c] = sum * (kScaleO / (kScaleX * kScaleX));
+                    } else {
+                        v[h][c] = times_old(old[i & 1][j], h, c, fmaf(o.c * (kScaleP / kScaleO), of_col[j][c], row_part), sum * (o.c * (kScaleP / (kScaleO * kScaleO))));
+                    }
                 }
-            } else {
-                if constexpr (WHAT == Product::kGram) {
+            }
+            if constexpr (WHAT == Product::kLast) {
+                put_result(o, static_cast<Y*>(o.y) + b * o.stride_y, row0 + i * 32, col0 + j * 32, whole, v);
+                continue;
+            }
+            if (!kApplies && i == j && on_diagonal) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = sum[r] * (kScaleO / (kScaleX * kScaleX));
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        v[r] = times_old(old[i & 1][j], r, fmaf(o.c * (kScaleP / kScaleO), of_col[j][r], row_part), sum[r] * (o.c * (kScaleP / (kScaleO * kScaleO))));
-                }
-                if (i == j && on_diagonal) {
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if ((lane & 15) == (lane >> 4) * 4 + r) {
-                            const int64_t d = b * o.ldm + row0 + i * 16;
-                            if constexpr (WHAT == Product::kGram) o.diag[d] = v[r] * (1.0f / kScaleO);
-                            else o.scale[d] = fmaf(of_row[i], fmaf(o.c, of_row[i], o.b), o.a) + o.c * (sum[r] * (1.0f / (kScaleO * kScaleO)));
-                            v[r] = 0.0f;
+                            const int64_t d = b * o.ldm + row0 + i * 32 + h * 4;
+                            float& x = v[h][h * 4 + r];
+                            if constexpr (WHAT == Product::kGram) o.diag[d] = x * (1.0f / kScaleO);
+                            if constexpr (WHAT == Product::kSquare)
+                                o.scale[d] = fmaf(of_row[i][h], fmaf(o.c, of_row[i][h], o.b), o.a) + o.c * (acc[h * H + j][h * H + i][r] * (1.0f / (kScaleO * kScaleO)));
+                            x = 0.0f;
                         }
+            }
+            const v4u32 w[2] = {halves(v[0]), halves(v[1])};
+            const v4u32 l[2] = {rest(v[0], w[0]), rest(v[1], w[1])};
+            const bool both = kApplies || ti != tj;                    // a tile on the diagonal has both of its sides itself
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t at = place(i, h, j), at_back = uint32_t(j * 32 + h * 4) * uint32_t(o.ldm) + uint32_t(i * 32);
+                whole_to.store(at * 2, w[h]);
+                if (both) whole_back.store(at_back * 2, turn8(w, h));
+                if constexpr (kWide) {
+                    wide.store(at * 4, v4u32{__float_as_uint(v[h][0]), __float_as_uint(v[h][1]), __float_as_uint(v[h][2]), __float_as_uint(v[h][3])});
+                    wide.store(at * 4 + 16, v4u32{__float_as_uint(v[h][4]), __float_as_uint(v[h][5]), __float_as_uint(v[h][6]), __float_as_uint(v[h][7])});
+                } else if constexpr (kApplies) {
+                    low.store(at * 2, l[h]);
                 }
-                operand.put(i * 16, j * 16, v, ti != tj);          // a tile on the diagonal has both of its sides itself
+                if constexpr (PARTS == 2) {
+                    rest_to.store(at * 2, l[h]);
+                    if (both) rest_back.store(at_back * 2, turn8(l, h));
+                }
             }
         }
     }
