@@ -75,7 +75,7 @@ struct OrthoCall {
     float a, b, c, eps;
     void* ws;
 };
-size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols, int type);
+size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols, int type, int num_cu);
 void launch_ortho(hipStream_t st, const OrthoCall& c, int num_cu);
 bool prepare_ortho();                    // once per process, before the first launch
 

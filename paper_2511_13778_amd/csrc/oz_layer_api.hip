@@ -156,7 +156,7 @@ oz_status_t oz_packed_gemm(oz_handle_t h, void* stream, int64_t groups, const in
 
 size_t oz_orthogonalize_workspace_bytes(oz_handle_t h, int64_t batch, int64_t rows, int64_t cols, int32_t type) {
     if (!h || !ortho_ok(batch, rows, cols, type)) return 0;
-    return ortho_bytes(batch, rows, cols, type);
+    return ortho_bytes(batch, rows, cols, type, handle_compute_units(h));
 }
 
 oz_status_t oz_orthogonalize(oz_handle_t h, void* stream, int64_t batch, int64_t rows, int64_t cols, int32_t type, const void* X, int64_t ldx,
@@ -168,7 +168,7 @@ oz_status_t oz_orthogonalize(oz_handle_t h, void* stream, int64_t batch, int64_t
     if (batch == 0 || rows == 0 || cols == 0) return OZ_OK;
     const uintptr_t esize = uintptr_t(elem_bytes(type));
     if (!there(X, esize) || !there(Y, esize)) return OZ_ERR_ARG;
-    const size_t need = ortho_bytes(batch, rows, cols, type);
+    const size_t need = ortho_bytes(batch, rows, cols, type, handle_compute_units(h));
     if (!workspace || !is_aligned(workspace, kWorkspaceAlign) || workspace_bytes < need) return OZ_ERR_WORKSPACE;
     if (!handle_on_device(h)) return OZ_ERR_DEVICE;
     launch_ortho(static_cast<hipStream_t>(stream),

@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "oz_layer.h"
+#include "oz_ortho_plan.h"
 #include "oz_scaled_gemm_device.h"
 
 namespace oz {
@@ -469,33 +470,13 @@ __global__ __launch_bounds__(256, F == 4 ? 2 : 1) void ortho_product_kernel(Orth
         while (ti * (ti + 1) / 2 > tile) --ti;
         tj = tile - ti * (ti + 1) / 2;
     }
-    v4f acc[F][F];
-    const f16_t *left, *right;
-    int64_t left_part = mm, right_part = mm, left_ld = o.ldm, right_ld = o.ldm;
-    int k = (o.m + kStep - 1) / kStep * kStep;
-    if constexpr (WHAT == Product::kGram) {
-        k = (o.n + kStep - 1) / kStep * kStep;
-        left = right = o.xh + b * PARTS * mn;
-        left_part = right_part = mn;
-        left_ld = right_ld = o.ldn;
-    } else if constexpr (WHAT == Product::kSquare) {
-        left = right = o.o + b * PARTS * mm;
-    } else {
-        left = o.p + b * PARTS * mm;
-        right = o.xt + b * PARTS * mn;
-        right_part = mn;
-    }
-    left += int64_t(ti) * T * left_ld;
-    right += int64_t(tj) * T * right_ld;
-    if constexpr (F < 4) multiply_small<F, PARTS>(lds, left, right, left_part, right_part, k, left_ld, right_ld, acc);
-    else multiply_large<F, PARTS>(lds, left, right, left_part, right_part, k, left_ld, right_ld, acc);
     // ---- what becomes of the sums: a lane has 2 x 8 of each 32 x 32 of its wave, rows 4 apart and columns beside each other
     constexpr int H = S::kH;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lane_row = uint32_t((wave & 1) * S::kWave + (lane & 12) * 2 + (lane & 3)), lane_col = uint32_t((wave >> 1) * S::kWave + (lane >> 4) * 8);
     const uint32_t back_row = lane_col + uint32_t(lane & 3), back_col = lane_row & ~7u;                     // turned
     const int row0 = ti * T + int(lane_row), col0 = tj * T + int(lane_col);
-    // read, 32 rows ahead: O (times kScaleO) or X (times kScaleX), X of two-part operands in 32 bits, the others in two 16-bit parts
+    // read, before the product and then 32 rows ahead: O (times kScaleO) or X (times kScaleX), X of two-part operands in 32 bits, the others in two 16-bit parts
     constexpr bool kReads = WHAT != Product::kGram, kWide = kApplies && PARTS == 2, kTwo = kReads && !kWide && (kApplies || PARTS == 2);
     const int64_t ld = kApplies ? o.ldn : o.ldm, corner = int64_t(ti) * T * ld + tj * T, part = kApplies ? mn : mm;
     f16_t* const to = WHAT == Product::kGram ? o.o + b * PARTS * mm : WHAT == Product::kSquare ? o.p + b * PARTS * mm : o.xh + b * PARTS * mn;
@@ -529,7 +510,35 @@ __global__ __launch_bounds__(256, F == 4 ? 2 : 1) void ortho_product_kernel(Orth
         if constexpr (kTwo) add = fmaf(factor, half_of(x.b[h], c), add);
         return fmaf(factor, half_of(x.a[h], c), add);
     };
-    Old old[kReads ? 2 : 1][kReads ? H : 1];
+    constexpr int kAhead = H < 2 ? 1 : 2, kEarly = F == 8 ? 1 : kAhead;          // beside 256 sums of a lane there is room for fewer
+    Old old[kReads ? H : 1][kReads ? H : 1];
+    if constexpr (kReads) {
+#pragma unroll
+        for (int i = 0; i < kEarly; ++i)
+#pragma unroll
+            for (int j = 0; j < H; ++j) old[i][j] = fetch(i, j);
+    }
+    asm volatile("" ::: "memory");
+    v4f acc[F][F];
+    const f16_t *left, *right;
+    int64_t left_part = mm, right_part = mm, left_ld = o.ldm, right_ld = o.ldm;
+    int k = (o.m + kStep - 1) / kStep * kStep;
+    if constexpr (WHAT == Product::kGram) {
+        k = (o.n + kStep - 1) / kStep * kStep;
+        left = right = o.xh + b * PARTS * mn;
+        left_part = right_part = mn;
+        left_ld = right_ld = o.ldn;
+    } else if constexpr (WHAT == Product::kSquare) {
+        left = right = o.o + b * PARTS * mm;
+    } else {
+        left = o.p + b * PARTS * mm;
+        right = o.xt + b * PARTS * mn;
+        right_part = mn;
+    }
+    left += int64_t(ti) * T * left_ld;
+    right += int64_t(tj) * T * right_ld;
+    if constexpr (F < 4) multiply_small<F, PARTS>(lds, left, right, left_part, right_part, k, left_ld, right_ld, acc);
+    else multiply_large<F, PARTS>(lds, left, right, left_part, right_part, k, left_ld, right_ld, acc);
     float of_col[WHAT == Product::kSquare ? H : 1][8], of_row[kReads ? H : 1][2];
     if constexpr (kReads) {
 #pragma unroll
@@ -538,18 +547,23 @@ __global__ __launch_bounds__(256, F == 4 ? 2 : 1) void ortho_product_kernel(Orth
             for (int h = 0; h < 2; ++h) of_row[i][h] = (kApplies ? o.scale : o.diag)[b * o.ldm + row0 + i * 32 + h * 4];
 #pragma unroll
         for (int j = 0; j < H; ++j) {
-            old[0][j] = fetch(0, j);
             if constexpr (WHAT == Product::kSquare) __builtin_memcpy(of_col[j], o.diag + b * o.ldm + col0 + j * 32, sizeof(of_col[j]));
         }
+    }
+    if constexpr (kReads) {
+#pragma unroll
+        for (int i = kEarly; i < kAhead; ++i)
+#pragma unroll
+            for (int j = 0; j < H; ++j) old[i][j] = fetch(i, j);
     }
     const bool on_diagonal = !kApplies && ti == tj && (wave & 1) == (wave >> 1);
     const bool whole = WHAT == Product::kLast && (ti + 1) * T <= o.m && (tj + 1) * T <= o.n;
 #pragma unroll
     for (int i = 0; i < H; ++i) {
         if constexpr (kReads) {
-            if (i + 1 < H) {
+            if (i + kAhead < H) {
 #pragma unroll
-                for (int j = 0; j < H; ++j) old[(i + 1) & 1][j] = fetch(i + 1, j);
+                for (int j = 0; j < H; ++j) old[i + kAhead][j] = fetch(i + kAhead, j);
             }
         }
 #pragma unroll
@@ -562,12 +576,12 @@ __global__ __launch_bounds__(256, F == 4 ? 2 : 1) void ortho_product_kernel(Orth
                 for (int c = 0; c < 8; ++c) {
                     const float sum = acc[(c >> 2) * H + j][h * H + i][c & 3];
                     if constexpr (kApplies) {
-                        v[h][c] = times_old(old[i & 1][j], h, c, of_row[i][h], sum * (1.0f / kScaleP));
+                        v[h][c] = times_old(old[i][j], h, c, of_row[i][h], sum * (1.0f / kScaleP));
                         if constexpr (WHAT == Product::kLast) v[h][c] *= 1.0f / kScaleX;
                     } else if constexpr (WHAT == Product::kGram) {
                         v[h][c] = sum * (kScaleO / (kScaleX * kScaleX));
                     } else {
-                        v[h][c] = times_old(old[i & 1][j], h, c, fmaf(o.c * (kScaleP / kScaleO), of_col[j][c], row_part), sum * (o.c * (kScaleP / (kScaleO * kScaleO))));
+                        v[h][c] = times_old(old[i][j], h, c, fmaf(o.c * (kScaleP / kScaleO), of_col[j][c], row_part), sum * (o.c * (kScaleP / (kScaleO * kScaleO))));
                     }
                 }
             }
@@ -612,25 +626,18 @@ __global__ __launch_bounds__(256, F == 4 ? 2 : 1) void ortho_product_kernel(Orth
     }
 }
 
-// Sides of the tiles: of A and A^2, of P X.
-struct Tiles { int square, apply; };
-Tiles tiles_of(int64_t batch, int64_t m, int64_t n, int parts) {
-    const int t = m <= 256 ? 64 : m <= 1024 ? 128 : 256;
-    return Tiles{t, t};
-}
-
 struct Plan {
     int64_t m, n, ldm, ldn, chunk;
-    Tiles tiles;
+    OrthoTiles tiles;
     int parts;
     size_t norm, x, vec, xh, o, total;      // bytes of each piece, for a chunk
 };
-Plan plan_of(int64_t batch, int64_t rows, int64_t cols, int type) {
+Plan plan_of(int64_t batch, int64_t rows, int64_t cols, int type, int num_cu) {
     Plan p{};
     p.m = std::min(rows, cols);
     p.n = std::max(rows, cols);
     p.parts = type == OZ_BF16 ? 1 : 2;
-    p.tiles = tiles_of(batch, p.m, p.n, p.parts);
+    p.tiles = ortho_tiles(batch, p.m, p.n, p.parts, num_cu);
     auto up = [](int64_t v, int64_t to) { return (v + to - 1) / to * to; };
     p.ldm = std::max(up(p.m, p.tiles.square), up(p.m, p.tiles.apply));
     p.ldn = up(p.n, p.tiles.apply);
@@ -696,12 +703,12 @@ bool allow_tile() {
 
 bool prepare_ortho() { return allow_tile<2>() && allow_tile<4>() && allow_tile<6>() && allow_tile<8>(); }
 
-size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols, int type) {
-    return batch > 0 && rows > 0 && cols > 0 ? plan_of(batch, rows, cols, type).total : 0;
+size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols, int type, int num_cu) {
+    return batch > 0 && rows > 0 && cols > 0 ? plan_of(batch, rows, cols, type, num_cu).total : 0;
 }
 
-void launch_ortho(hipStream_t st, const OrthoCall& c, int) {
-    const Plan p = plan_of(c.batch, c.rows, c.cols, c.type);
+void launch_ortho(hipStream_t st, const OrthoCall& c, int num_cu) {
+    const Plan p = plan_of(c.batch, c.rows, c.cols, c.type, num_cu);
     Ortho o{};
     o.ldg = c.ldx; o.stride_g = c.stride_x; o.ldy = c.ldy; o.stride_y = c.stride_y;
     o.rows = c.rows; o.cols = c.cols; o.m = int(p.m); o.n = int(p.n); o.ldm = int(p.ldm); o.ldn = int(p.ldn);
