@@ -115,13 +115,32 @@ def combine_backward(h: g.Handle, dy, xs, routing: Routing, weights=None):
 class Choice:
     """What choose found: ids (tokens x topk, int32, -1 where there is none), weights (float32), and, if asked for, counts (how often each
     expert was chosen, int32), counted (one int32: tokens that have an expert), shares (their mean probability of each expert, float32) and
-    loss (float32, one value).  counts may be added up over several GPUs before choose_backward."""
+    loss (float32, one value).  counts may be added up over several GPUs before choose_backward, in place or set to others."""
 
-    __slots__ = ("ids", "weights", "counts", "counted", "shares", "loss", "live", "normalize")
+    __slots__ = ("ids", "weights", "_counts", "_counted", "_shares", "_loss", "_table", "live", "normalize")
 
     def __init__(self, ids, weights, counts=None, counted=None, shares=None, loss=None, live=None, normalize=True):
-        self.ids, self.weights, self.counts, self.counted, self.shares, self.loss = ids, weights, counts, counted, shares, loss
-        self.live, self.normalize = live, normalize
+        self.ids, self.weights, self._counts, self._counted, self._shares, self._loss = ids, weights, counts, counted, shares, loss
+        self._table, self.live, self.normalize = None, live, normalize
+
+    # the four results of the whole batch are parts of one int32 table, looked at when they are asked for
+    def _part(name, at, real):
+        def get(self):
+            have = getattr(self, name)
+            if have is None and self._table is not None:
+                experts = (self._table.shape[0] - 2) // 2
+                lo, hi = at(experts)
+                have = self._table[lo:hi] if hi > lo else self._table[lo]
+                have = have.view(torch.float32) if real else have
+                setattr(self, name, have)
+            return have
+        return property(get, lambda self, v: setattr(self, name, v))
+
+    counts = _part("_counts", lambda n: (0, n), False)
+    counted = _part("_counted", lambda n: (n, n + 1), False)
+    shares = _part("_shares", lambda n: (n + 1, 2 * n + 1), True)
+    loss = _part("_loss", lambda n: (2 * n + 1, 0), True)
+    del _part
 
 
 def _live(live, tokens):
@@ -141,25 +160,24 @@ def choose(h: g.Handle, scores, topk: int, live=None, normalize=True, balance=Tr
     tokens, experts = scores.shape
     if not 1 <= topk <= min(experts, 64):
         raise ValueError("topk 1 .. 64 of %d experts, not %s" % (experts, topk))
-    device = scores.device
-    both = torch.empty((2, tokens, topk), dtype=torch.int32, device=device)
-    ids, weights = both.unbind(0)
-    weights = weights.view(torch.float32)
-    c = Choice(ids, weights, live=live, normalize=bool(normalize))
-    at = ids.data_ptr()
+    # one allocation: ids, weights, the four results of the batch, the workspace
+    n = tokens * topk
+    need = h.choose_experts_workspace_bytes(tokens, experts) if balance else 0
+    head = 2 * n + 2 * experts + 2
+    first = -(-head // 64) * 64
+    all_ = torch.empty(first + (need + 3) // 4 if balance else 2 * n, dtype=torch.int32, device=scores.device)
+    base = all_.data_ptr()
     if balance:
-        need = h.choose_experts_workspace_bytes(tokens, experts)
-        first = -(-(2 * experts + 2) // 64) * 64          # the four results, then the workspace
-        table = torch.empty(first + (need + 3) // 4, dtype=torch.int32, device=device)
-        c.counts, c.counted = table[:experts], table[experts:experts + 1]
-        real = table[experts + 1:2 * experts + 2].view(torch.float32)
-        c.shares, c.loss = real[:experts], real[experts]
-        base = table.data_ptr()
-        more = (base, base + 4 * experts, base + 4 * (experts + 1), base + 4 * (2 * experts + 1), base + 4 * first, need)
+        ids, weights, table, _ = all_.split_with_sizes((n, n, 2 * experts + 2, all_.shape[0] - head))
+        at = base + 8 * n
+        more = (at, at + 4 * experts, at + 4 * experts + 4, at + 8 * experts + 4, base + 4 * first, need)
     else:
-        more = (None, None, None, None, None, 0)
+        ids, weights = all_.split_with_sizes((n, n))
+        table, more = None, (None, None, None, None, None, 0)
+    c = Choice(ids.view(tokens, topk), weights.view(torch.float32).view(tokens, topk), live=live, normalize=bool(normalize))
+    c._table = table
     h.call("oz_choose_experts", stream_of(scores), tokens, experts, topk, scores.data_ptr(), ld, float_type(scores.dtype), _live(live, tokens),
-           int(c.normalize), at, at + 4 * tokens * topk, *more)
+           int(c.normalize), base, base + 4 * n, *more)
     return c
 
 

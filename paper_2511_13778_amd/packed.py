@@ -64,10 +64,17 @@ class Packed:
 
 def empty(rows, cols, group=128, zeros=False, scale_dtype=torch.float16, groups=None, device="cuda") -> Packed:
     """An uninitialised matrix in the layout that the calls here want."""
-    lead = () if groups is None else (groups,)
-    data = torch.empty(lead + (rows, max(-(-cols // 32) * 16, 16)), dtype=torch.uint8, device=device)
-    scale = torch.empty(lead + (-(-cols // group) if group in (32, 64, 128) else 1, rows), dtype=scale_dtype, device=device)
-    return Packed(data, scale, torch.empty_like(scale) if zeros else None, cols=cols, group=group)
+    if group not in (32, 64, 128):
+        raise ValueError("group: 32, 64 or 128, not %s" % (group,))
+    ld, blocks, lead = max(-(-cols // 32) * 16, 16), -(-cols // group), () if groups is None else (groups,)
+    w = Packed.__new__(Packed)              # sizes and types are right by construction
+    w.data = torch.empty(lead + (rows, ld), dtype=torch.uint8, device=device)
+    w.scale = torch.empty(lead + (blocks, rows), dtype=scale_dtype, device=device)
+    w.zero = torch.empty(lead + (blocks, rows), dtype=scale_dtype, device=device) if zeros else None
+    w.cols, w.group = cols, group
+    w.desc = g.oz_packed_t(w.data.data_ptr(), w.scale.data_ptr(), w.zero.data_ptr() if zeros else None, ld, max(rows, 1), 0 if groups is None else rows * ld,
+                           0 if groups is None else blocks * rows, float_type(scale_dtype), group, 0)
+    return w
 
 
 def _matrices(x, what):
