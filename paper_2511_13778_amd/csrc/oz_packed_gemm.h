@@ -145,25 +145,25 @@ struct ScaleLoad {
     }
 };
 
-// MT: 16s of rows of x.  R: 16s of rows of W.  SMALL: groups of 32 or 64 columns, else of 128.  EXACT: bfloat16 codes with nothing to come off the sums.
+// MT: 16s of rows of x.  R: 16s of rows of W.  PER: groups of columns in a block, whose sums are scaled apart.  EXACT: bfloat16 codes with nothing to come off the sums.
 // That 128 + code is multiplied instead of code - 8 makes the sums 136 / 4.6 times as large and their 32-bit roundings with them: 4e-6 of a result, or
 // 4e-5 where all of x has one sign, beside a rounding to bfloat16 of 2e-3.
-template <typename X, int MT, int R, bool SMALL, bool ZEROS, bool EXACT>
+template <typename X, int MT, int R, int PER, bool ZEROS, bool EXACT>
 struct Shape {
-    static constexpr int kAhead = MT == 1 ? 2 : 4;                     // blocks whose weights are on their way together
-    static constexpr int kX = MT == 1 && sizeof(X) == 2 ? kAhead : 1; // of them, those whose x is too
-    static constexpr int kPer = SMALL ? 4 : 1;                        // sums of a block that are scaled apart
-    static constexpr int kLoads = (kAhead * kPer * 16 * R + 63) / 64, kScales = kLoads * 64;      // of a wave, in LDS
-    static constexpr int kThreads = MT == 1 && R < 4 ? 1024 : 512;
+    static constexpr int kAhead = MT == 1 || MT * R == 8 ? 2 : 4;                     // blocks whose weights are on their way together
+    static constexpr int kX = sizeof(X) == 2 ? 2 : 1;                 // of them, those whose x is too
+    static constexpr int kLoads = (kAhead * PER * 16 * R + 63) / 64, kScales = kLoads * 64;      // of a wave, in LDS
+    static constexpr int kThreads = MT == 1 && R * int(sizeof(X)) <= 4 ? 1024 : 512;
     static constexpr int kWaveBytes = std::max(MT * 16 * 16 * R, kScales * (ZEROS ? 2 : 1)) * 4;      // scales, and in the end the sums
 };
 
-template <typename X, int MT, int R, bool SMALL, bool ZEROS, bool EXACT>
-__global__ __launch_bounds__((Shape<X, MT, R, SMALL, ZEROS, EXACT>::kThreads)) void packed_gemm_kernel(PackedGemm g, int strips) {
+template <typename X, int MT, int R, int PER, bool ZEROS, bool EXACT>
+__global__ __launch_bounds__((Shape<X, MT, R, PER, ZEROS, EXACT>::kThreads)) void packed_gemm_kernel(PackedGemm g, int strips) {
     using E = Eight<X>;
     using W = typename E::W;
-    using S = Shape<X, MT, R, SMALL, ZEROS, EXACT>;
-    constexpr int kPer = S::kPer, kEach = 4 / kPer, kAhead = S::kAhead, kX = S::kX;
+    using S = Shape<X, MT, R, PER, ZEROS, EXACT>;
+    constexpr int kPer = PER, kEach = 4 / PER, kAhead = S::kAhead, kX = S::kX;
+    constexpr bool SMALL = PER > 1;
     constexpr bool kSums = ZEROS || !EXACT;                           // sums of x are needed
     extern __shared__ __align__(16) float lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = int(blockDim.x) >> 6;
@@ -199,8 +199,8 @@ __global__ __launch_bounds__((Shape<X, MT, R, SMALL, ZEROS, EXACT>::kThreads)) v
 #pragma unroll
         for (int i = 0; i < 4; ++i) ones[i] = uint32_t(__builtin_bit_cast(uint16_t, static_cast<W>(1.0f))) * 0x10001u;
         for (int b0 = begin; b0 < end; b0 += kAhead) {
-            // what this chunk reads is sent for without a branch; blocks behind the end are the last one again, and bytes behind a row's end its last ones,
-            // whose columns have zeros in x
+            // What this chunk reads is sent for without a branch, which would wait; blocks behind the end are the last one again, and bytes behind a row's end
+            // its last ones, whose columns have zeros in x.  (The next chunk's weights sent for before this one is multiplied: 3 to 14 % slower.)
             v4u32 codes[kAhead][R];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
@@ -377,16 +377,24 @@ void launch_rows(hipStream_t st, const PackedGemm& g, int waves) {
     const dim3 grid(unsigned(tiles * strips)), block(64 * waves);
     const std::true_type yes;
     const std::false_type no;
-    auto launch = [&](auto small, auto zeros, auto exact) {
-        constexpr bool kSmall = decltype(small)::value, kZeros = decltype(zeros)::value, kExact = decltype(exact)::value;
-        const size_t bytes = size_t(waves) * Shape<X, MT, R, kSmall, kZeros, kExact>::kWaveBytes;
-        hipLaunchKernelGGL((packed_gemm_kernel<X, MT, R, kSmall, kZeros, kExact>), grid, block, bytes, st, g, strips);
+    auto launch = [&](auto per, auto zeros, auto exact) {
+        constexpr int kPer = decltype(per)::value;
+        constexpr bool kZeros = decltype(zeros)::value, kExact = decltype(exact)::value;
+        const size_t bytes = size_t(waves) * Shape<X, MT, R, kPer, kZeros, kExact>::kWaveBytes;
+        hipLaunchKernelGGL((packed_gemm_kernel<X, MT, R, kPer, kZeros, kExact>), grid, block, bytes, st, g, strips);
+    };
+    auto of_group = [&](auto zeros, auto exact) {
+        if constexpr (R < 4 && MT * R < 8) {
+            if (g.w.shift == 5) return launch(std::integral_constant<int, 4>{}, zeros, exact);
+        }
+        if constexpr (MT * R < 8) {
+            if (g.w.shift == 6) return launch(std::integral_constant<int, 2>{}, zeros, exact);
+        }
+        launch(std::integral_constant<int, 1>{}, zeros, exact);
     };
     auto of_shift = [&](auto exact) {
-        if (g.w.shift != 7 && g.w.zero) launch(yes, yes, exact);
-        else if (g.w.shift != 7) launch(yes, no, exact);
-        else if (g.w.zero) launch(no, yes, exact);
-        else launch(no, no, exact);
+        if (g.w.zero) of_group(yes, exact);
+        else of_group(no, exact);
     };
     if constexpr (std::is_same_v<X, bf16_t>) {
         if (g.y_type != OZ_F32) return of_shift(no);
@@ -402,9 +410,11 @@ void launch_typed(hipStream_t st, const PackedGemm& g, int num_cu) {
     }
     const int64_t avg = g.offsets ? (int64_t(g.m) + g.groups - 1) / g.groups : g.m;      // rows of a group on average
     const int blocks = std::max((g.k + kBlock - 1) / kBlock, 1);
-    const int mt = avg <= 16 ? 1 : avg <= 32 ? 2 : 4;
-    const int64_t tiles = g.offsets ? group_pieces(g.m, g.groups, mt * 16) : (g.m + mt * 16 - 1) / (mt * 16);
-    const int64_t strips = tiles * ((g.n + 15) / 16);
+    auto strips_of = [&](int mt) { return (g.offsets ? group_pieces(g.m, g.groups, mt * 16) : (g.m + mt * 16 - 1) / (mt * 16)) * ((g.n + 15) / 16); };
+    // 16s of rows of x to a workgroup: as many as there are, up to four, but fewer where that leaves the chip idle
+    int mt = avg <= 16 ? 1 : avg <= 32 ? 2 : 4;
+    while (mt > 1 && strips_of(mt / 2) <= 2 * num_cu) mt /= 2;
+    const int64_t strips = strips_of(mt);
     // 16s of rows of W to a workgroup, and waves that share k: what fills the chip with 16 waves to a CU that have two blocks each, with as much of W to a
     // wave as that leaves, since all of it shares the wave's x.
     auto waves_of = [&](int rows, int most) {
@@ -412,10 +422,13 @@ void launch_typed(hipStream_t st, const PackedGemm& g, int num_cu) {
         while (w < most && w < blocks && strips / rows * w < 16 * num_cu) w *= 2;
         return w;
     };
+    // more rows of W for each x take more registers: groups of 32 with their scales leave room for two strips, small groups and 64 rows of x, and float32
+    // beside more than 16, for one
+    const int most = mt == 1 ? (g.w.shift == 5 ? 2 : 4) : sizeof(X) == 2 && (mt == 2 || g.w.shift == 7) ? 2 : 1;
     int r = 1, waves = waves_of(1, mt == 1 ? 16 : 8);
-    for (int more = 2; more <= (mt == 1 ? 4 : mt == 2 && sizeof(X) == 2 ? 2 : 1); more *= 2) {
-        const int w = waves_of(more, mt == 1 && more < 4 ? 16 : 8);
-        if (strips / more * w < 16 * num_cu) break;
+    for (int more = 2; more <= most; more *= 2) {
+        const int w = waves_of(more, mt == 1 && more * int(sizeof(X)) <= 4 ? 16 : 8);
+        if (strips / more * w < (mt == 4 ? 8 : 16) * num_cu) break;
         r = more;
         waves = w;
     }
@@ -429,6 +442,9 @@ void launch_typed(hipStream_t st, const PackedGemm& g, int num_cu) {
         }
         launch_rows<X, 2, 1>(st, g, waves);
     } else {
+        if constexpr (sizeof(X) == 2) {
+            if (r == 2) return launch_rows<X, 4, 2>(st, g, waves);
+        }
         launch_rows<X, 4, 1>(st, g, waves);
     }
 }
