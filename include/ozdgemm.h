@@ -388,7 +388,8 @@ oz_status_t oz_choose_experts(oz_handle_t handle, void* stream, int64_t tokens, 
 /* The scores' gradient from that of the weights (dweights, tokens x topk, or NULL: none) and, unless counts and counted are NULL, from factor * *dloss
  * (dloss a device pointer; NULL: 1) for the loss.  ids, weights, counts, counted: as oz_choose_experts left them with the same scores, live and
  * normalize; counts may have been added up over several GPUs since: f_e then is theirs.  dscores: type and columns of scores; zero for padding
- * and for experts that are not to be had.  Which experts are chosen has no gradient, so f_e is a constant here. */
+ * and for experts that are not to be had (NaN for all of a token where its probabilities are).  Which experts are chosen has no gradient, so f_e is a
+ * constant here. */
 oz_status_t oz_choose_experts_grad(oz_handle_t handle, void* stream, int64_t tokens, int64_t experts, int64_t topk, const void* scores, int64_t ld,
                                    int32_t type, const uint8_t* live, int32_t normalize, const int32_t* ids, const float* weights,
                                    const float* dweights, const int32_t* counts, const int32_t* counted, const float* dloss, float factor,
@@ -422,7 +423,8 @@ oz_status_t oz_unpack4(oz_handle_t handle, void* stream, int64_t rows, int64_t c
 
 /* Y = X W^T, X m x k in OZ_F32, OZ_BF16 or OZ_F16, W n x k in 4 bits, Y m x n.  Made for few rows (a token, a few in flight): W is read once for every 64
  * rows of X.  offsets NULL, groups 0: one matrix.  Otherwise rows offsets[g] .. of Y = the same rows of X times W_g^T, and rows of Y behind the last
- * group are set to zero.  Sums are held in 32 bits, each group's of code - 8 before it is scaled; the one rounding to fewer bits is the result's.
+ * group are set to zero.  Sums are held in 32 bits, each group's of code - 8 before it is scaled (X and Y in OZ_BF16: of 128 + code, less 136 times the
+ * sum of x, some 10^-5 of the largest terms, which the rounding of Y hides); the one rounding to fewer bits is the result's.
  * k == 0: Y = 0.  Limits: (ceil(m / 16) + groups + 1) * ceil(n / 16) < 2^22. */
 oz_status_t oz_packed_gemm(oz_handle_t handle, void* stream, int64_t groups, const int32_t* offsets, int64_t m, int64_t n, int64_t k, const void* X,
                            int64_t ldx, int32_t x_type, const oz_packed_t* W, void* Y, int64_t ldy, int32_t y_type);
@@ -430,9 +432,10 @@ oz_status_t oz_packed_gemm(oz_handle_t handle, void* stream, int64_t groups, con
 /* Y = X made orthogonal, batch matrices of rows x cols, by `steps` Newton-Schulz steps Z <- a Z + (b A + c A^2) Z, A = Z Z^T, from Z = X / (|X| + eps) with
  * |X| the square root of the sum of squares (Z is taken transposed where rows > cols).  With a = 3.4445, b = -4.775, c = 2.0315 five steps bring singular
  * values above 0.003 |X| into 0.68 .. 1.13 or so: the direction of a weight update that keeps X's singular vectors.
- * Coefficients have to keep singular values below 4 on the way, |b| + |c| times their square's square below 15 (these do: 1.3).  X in OZ_BF16: operands of
- * the products have 11 bits, an error of about 0.001 of the result; OZ_F32, OZ_F16: 22 bits, about 10^-6.  Everything else is in 32 bits,
- * |X| in 64.  A matrix of zeros stays one if eps > 0; an infinity or a NaN makes NaN of its matrix.
+ * Z is held as 4096 Z, elements of A off its diagonal as 16384 A and those of b A + c A^2 as 4096 of them, in 16-bit floating point (up to 65504): the
+ * coefficients have to keep singular values below 2 and the last below 16, or elements become infinite (these do: 1.3 and 4).  X in OZ_BF16: operands
+ * of the products have 11 bits, an error of about 0.002 of the result with its rounding; OZ_F32, OZ_F16: 22 bits, about 10^-6.  Everything else is in 32
+ * bits, |X| in 64.  A matrix of zeros stays one if eps > 0; an infinity or a NaN makes NaN of its matrix.
  * Y may be X, with the same strides.  Sums are in a fixed order.  Limits: rows, cols <= 32768, batch <= 65535, 1 <= steps <= 64.
  * workspace: 256-byte aligned, oz_orthogonalize_workspace_bytes(...) bytes (up to 24 per element of a few matrices, of which more are done in turn). */
 size_t oz_orthogonalize_workspace_bytes(oz_handle_t handle, int64_t batch, int64_t rows, int64_t cols, int32_t type);

@@ -45,73 +45,122 @@ __device__ __forceinline__ float group_largest(float x) {
     return __uint_as_float(fold<L>(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
 }
 template <int L>
+__device__ __forceinline__ int32_t fold_max(int32_t x) {
+    return int32_t(fold<L>(uint32_t(x), [](uint32_t a, uint32_t b) { return uint32_t(max(int32_t(a), int32_t(b))); }));
+}
+template <int L>
 __device__ __forceinline__ uint32_t group_max(uint32_t x) {
     return fold<L>(x, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
 // Scores as whole numbers that rise with them, the expert in the low bits (lower ones above higher ones), so that no two are equal.  16-bit scores
-// are 19 bits of a float32 at most and leave room for the expert in the same word; float32 takes two.  -0 counts as +0, a NaN is above all; what is
-// not above `kNone` is an expert that is not to be had (score -infinity, or no such expert).
+// leave room for the expert in the same word; float32 takes two.  -0 counts as +0, a NaN is above all; what is not above `kNone` is an expert that
+// is not to be had (score -infinity, or no such expert).
 template <typename T>
 struct Key {
     static constexpr bool kNamed = sizeof(T) == 2;
-    using type = std::conditional_t<kNamed, uint32_t, uint64_t>;
-    static constexpr uint32_t kLow = 0x1FFF, kNone = 0x007FFFFF;
-    static __device__ __forceinline__ uint32_t rising(float f) {
-        f = f != f ? __uint_as_float(0x7FFFFFFFu) : f + 0.0f;
-        return __float_as_uint(f) ^ (uint32_t(int32_t(__float_as_uint(f)) >> 31) | 0x80000000u);
-    }
-    static __device__ __forceinline__ type of(float f, int expert) {
-        if constexpr (kNamed) return (rising(f) & ~kLow) | (kLow - uint32_t(expert));
-        else return uint64_t(rising(f)) << 32 | uint32_t(~expert);
-    }
-    static __device__ __forceinline__ uint32_t head(type key) {
-        if constexpr (kNamed) return key;
-        else return uint32_t(key >> 32);
-    }
-    // of a key, or of a float32's upper word
-    static __device__ __forceinline__ float score(uint32_t head) {
-        const uint32_t up = kNamed ? head | kLow : head;
-        const uint32_t u = (head & 0x80000000u) ? (kNamed ? head & ~kLow : head) ^ 0x80000000u : ~up;
-        return __uint_as_float(u);
+    using Head = std::conditional_t<kNamed, int32_t, uint32_t>;          // what is compared first
+    using type = std::conditional_t<kNamed, int32_t, uint64_t>;
+    static constexpr uint32_t kInf = kNamed ? (std::is_same_v<T, f16_t> ? 0x7C00u : 0x7F80u) : 0x7F800000u;
+    static constexpr Head kNone = kNamed ? Head(0xFFFFu - (kInf << 16)) : Head(0x007FFFFFu);
+    static __device__ __forceinline__ Head head(type key) { return kNamed ? Head(key) : Head(uint64_t(key) >> 32); }
+    static __device__ __forceinline__ int expert(type key) { return kNamed ? 0xFFFF - int(uint32_t(key) & 0xFFFFu) : int(~uint32_t(key)); }
+    static __device__ __forceinline__ float score(Head h) {
+        if constexpr (kNamed) {
+            const int up = h >> 16;
+            return to_float(__builtin_bit_cast(T, uint16_t(up < 0 ? 0x8000 - up : up)));
+        } else {
+            return __uint_as_float((h & 0x80000000u) ? h ^ 0x80000000u : ~h);
+        }
     }
 };
 
-// A lane's part of a token's scores, sent for before it is used: V consecutive elements, `have` of which are there, and whether the token counts.
+// A lane's part of a token's scores: V consecutive elements, -infinity behind the last expert.  They are sent for before they are used, without a
+// branch, which would wait for what is on its way: behind the last token its own scores again, behind the last expert the last V, moved into place
+// by `settle`.  There are at least V experts and one token.
 template <int V, typename T>
 struct Scores {
-    T e[V];
-    int have;
-    bool in, on;
+    using K = Key<T>;
+    static constexpr int kWords = V * int(sizeof(T)) / 4;
+    union { T e[V]; uint32_t w[kWords + (V == 1)]; };
+    uint8_t alive;
+    __device__ __forceinline__ Scores() {}
     __device__ __forceinline__ void fetch(const T* scores, int64_t ld, int experts, const uint8_t* live, int64_t t, int64_t tokens, int first) {
-        in = t < tokens;
-        have = in ? experts - first : 0;
-        const T* p = scores + (in ? t : 0) * ld + first;
-        if (have >= V) {
-            __builtin_memcpy(e, p, sizeof(e));
+        t = min(t, tokens - 1);
+        const T* p = scores + t * ld + min(first, experts - V);
+        __builtin_memcpy(e, p, sizeof(e));
+        alive = *(live ? live + t : reinterpret_cast<const uint8_t*>(p));
+    }
+    __device__ __forceinline__ void settle(int experts, int all, int first) {
+        if (experts == all) return;
+        const int d = min(first - min(first, experts - V), V);
+        constexpr uint32_t kLow = sizeof(T) == 4 ? 0xFF800000u : uint32_t(uint16_t(0x8000u | K::kInf)) * 0x10001u;
+        if constexpr (V == 1) {
+            if (d) e[0] = T(-INFINITY);
+        } else {
+            if constexpr (sizeof(T) == 2) {
+                if (experts & 1) {
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) w[i] = d & 1 ? w[i] >> 16 | (i + 1 < kWords ? w[i + 1] : kLow) << 16 : w[i];
+                }
+            }
+#pragma unroll
+            for (int by = 1; by <= kWords; by *= 2) {
+                const bool move = d & (by * 4 / int(sizeof(T)));
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) w[i] = move ? i + by < kWords ? w[i + by] : kLow : w[i];
+            }
+        }
+    }
+    __device__ __forceinline__ void keys(int first, typename K::type (&key)[V]) {
+        if constexpr (K::kNamed && V >= 2) {
+            typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 top = {0, 0};
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[i] & 0x7FFF7FFFu));
+            if (__any(max(top[0], top[1]) > K::kInf)) {
+                // whatever a NaN's sign and other bits are
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if ((__builtin_bit_cast(uint16_t, e[v]) & 0x7FFFu) > K::kInf) e[v] = __builtin_bit_cast(T, uint16_t(0x7FFF));
+            }
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                // magnitude and sign to two's complement, two at a time
+                const i16x2 sign = __builtin_bit_cast(i16x2, w[i]) >> i16x2{15, 15}, size = __builtin_bit_cast(i16x2, w[i] & 0x7FFF7FFFu);
+                const uint32_t up = __builtin_bit_cast(uint32_t, i16x2((size ^ sign) - sign));
+                key[2 * i] = int32_t(up << 16 | uint32_t(0xFFFF - (first + 2 * i)));
+                key[2 * i + 1] = int32_t((up & 0xFFFF0000u) | uint32_t(0xFFFF - (first + 2 * i + 1)));
+            }
         } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) e[v] = v < have ? p[v] : T(0.0f);
+            for (int v = 0; v < V; ++v) {
+                const float f = to_float(e[v]);
+                if constexpr (K::kNamed) {
+                    const uint32_t u = f != f ? 0x7FFFu : uint32_t(__builtin_bit_cast(uint16_t, e[v]));
+                    const int size = int(u & 0x7FFFu), up = (u & 0x8000u) ? -size : size;
+                    key[v] = int32_t(uint32_t(up) << 16 | uint32_t(0xFFFF - (first + v)));
+                } else {
+                    const uint32_t u = f != f ? 0x7FFFFFFFu : __float_as_uint(f + 0.0f);
+                    key[v] = uint64_t(u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u)) << 32 | uint32_t(~(first + v));
+                }
+            }
         }
-        on = in && (!live || live[t]);
-    }
-    // -infinity: not to be had
-    __device__ __forceinline__ void settle(float (&s)[V]) const {
-#pragma unroll
-        for (int v = 0; v < V; ++v) s[v] = on && v < have ? to_float(e[v]) : -INFINITY;
     }
 };
 
-// exp(x), x <= 0: 2^(x log2 e), relatively off by a step of the result and by 2^-24 |x|; zero below 2^-126
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+// exp(s - m) to a step of the result and 2^-23 |s - m|; zero below 2^-126.  (As 2^(s log2 e - m log2 e) it would be an instruction less, and infinite where
+// m log2 e is: bfloat16 and float32 have such m.)
+__device__ __forceinline__ float exp_of(float s, float m) { return __builtin_amdgcn_exp2f((s - m) * 1.44269504f); }
 
-// exp(s - m) and their sum over the group
-template <int L, int V>
-__device__ __forceinline__ float exponentials(const float (&s)[V], float m, float (&ex)[V]) {
+// those of a lane's experts, and their sum over the group
+template <int L, int V, typename T>
+__device__ __forceinline__ float exponentials(const T (&e)[V], float m, float (&ex)[V]) {
     float sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        ex[v] = exp_of(s[v] - m);
+        ex[v] = exp_of(to_float(e[v]), m);
         sum += ex[v];
     }
     return group_sum<L>(sum);
@@ -150,6 +199,44 @@ __device__ __forceinline__ void sort_falling(K (&k)[V]) {
     exchange(k, std::make_integer_sequence<int, Merges<V>().count>{});
 }
 
+// The largest KEEP of V in falling order, the first of `k`; KEEP is V or its half: halves sorted, the larger of the first and the last, the second and
+// the last but one, ..., which rise and fall once, sorted.
+template <int KEEP, int V, typename K>
+__device__ __forceinline__ void sort_first(K (&k)[V]) {
+    if constexpr (KEEP == V) {
+        sort_falling(k);
+    } else {
+        static_assert(2 * KEEP == V, "half of them");
+        K a[KEEP], b[KEEP];
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) {
+            a[i] = k[i];
+            b[i] = k[KEEP + i];
+        }
+        sort_falling(a);
+        sort_falling(b);
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) a[i] = a[i] < b[KEEP - 1 - i] ? b[KEEP - 1 - i] : a[i];
+        auto halve = [&](auto D) {
+            constexpr int d = decltype(D)::value;
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i)
+                if ((i & d) == 0 && i + d < KEEP) {
+                    const K x = a[i], y = a[i + d];
+                    const bool less = x < y;
+                    a[i] = less ? y : x;
+                    a[i + d] = less ? x : y;
+                }
+        };
+        static_assert(KEEP == 8, "steps of 4, 2 and 1");
+        halve(std::integral_constant<int, 4>{});
+        halve(std::integral_constant<int, 2>{});
+        halve(std::integral_constant<int, 1>{});
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) k[i] = a[i];
+    }
+}
+
 struct Partials {                 // in the workspace, for each of `blocks` workgroups
     float* p;                     // [blocks][experts] sums of the probabilities
     int32_t* count;               // [blocks][experts] choices
@@ -178,8 +265,9 @@ Partials partials_of(void* ws, int blocks, int experts) {
     return q;
 }
 
-// A lane sorts its experts; the largest of the lanes' first ones is the next choice, and its lane moves up.
-template <typename T, int L, int V, bool BALANCE>
+// A lane sorts its experts, or the KEEP that can be chosen at all; the largest of the lanes' first ones is the next choice, and its lane moves up.
+// What bounds it is the vector instructions: 65000 tokens of 256 bfloat16 scores, 8 chosen, half a thousand for four tokens.
+template <typename T, int L, int V, int KEEP, bool BALANCE>
 __global__ __launch_bounds__(kThreads) void choose_kernel(ChooseCall c, Partials q) {
     constexpr int kGroups = kThreads / L, kWaves = kThreads / 64;
     using K = Key<T>;
@@ -199,77 +287,85 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(ChooseCall c, Partials
     const int64_t step = int64_t(gridDim.x) * kGroups;
     int64_t t = int64_t(blockIdx.x) * kGroups + group;
     Scores<V, T> next;
-    next.fetch(scores, c.ld, c.experts, c.live, t, c.tokens, first);
+    if (c.tokens > 0) next.fetch(scores, c.ld, c.experts, c.live, t, c.tokens, first);
     // every group of a wave comes along to the end: lanes ask each other
     for (; t - group < c.tokens; t += step) {
-        const bool in = next.in;
-        float s[V];
+        Scores<V, T> now = next;
+        const bool in = t < c.tokens, on = in && (!c.live || now.alive);
+        next.fetch(scores, c.ld, c.experts, c.live, t + step, c.tokens, first);
+        now.settle(c.experts, L * V, first);
         typename K::type key[V];
-        next.settle(s);
-        if (t - group + step < c.tokens) next.fetch(scores, c.ld, c.experts, c.live, t + step, c.tokens, first);
-#pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = K::of(s[v], first + v);
-        sort_falling(key);
-        uint32_t top = group_max<L>(K::head(key[0]));
-        const bool any = top > K::kNone;
+        now.keys(first, key);
+        sort_first<KEEP>(key);
+        auto largest = [&]() {
+            const typename K::Head h = K::head(key[0]);
+            if constexpr (K::kNamed) return fold_max<L>(h);
+            else return group_max<L>(h);
+        };
+        typename K::Head top = largest();
+        const bool any = on && top > K::kNone;
         const float m = any ? K::score(top) : 0.0f;
         float inverse = 0.0f;                        // of the probabilities' sum
         if (BALANCE || !c.normalize) {
             float ex[V];
-            const float sum = exponentials<L>(s, m, ex);
+            const float sum = exponentials<L>(now.e, m, ex);
             inverse = any ? 1.0f / sum : 0.0f;
             if constexpr (BALANCE) {
+                if (any) {
+                    mine += 1;
 #pragma unroll
-                for (int v = 0; v < V; ++v) psum[v] = any ? fmaf(ex[v], inverse, psum[v]) : psum[v];
-                mine += any ? 1 : 0;
+                    for (int v = 0; v < V; ++v) psum[v] = fmaf(ex[v], inverse, psum[v]);
+                }
             }
         }
         int32_t* ids = c.ids + t * c.topk;
         float* weights = c.weights + t * c.topk;
-        float held[64 / L], total = 0.0f;            // lane j % L has the j-th choice
-        int32_t held_id[64 / L];
+        typename K::Head held[64 / L];               // lane j % L has the j-th choice
 #pragma unroll
         for (int j0 = 0; j0 < 64 / L; ++j0) {
-            held[j0] = 0.0f;
-            held_id[j0] = -1;
+            held[j0] = K::kNone;
             if (j0 * L >= c.topk) continue;
             for (int j = j0 * L; j < min(j0 * L + L, c.topk); ++j) {
-                if (j > 0) top = group_max<L>(K::head(key[0]));
-                const bool have = top > K::kNone;
-                bool won = have && K::head(key[0]) == top;
-                if constexpr (K::kNamed) {
-                    if (lane == j - j0 * L && have) held_id[j0] = int32_t(K::kLow - (top & K::kLow));
-                } else {
+                if (j > 0) top = largest();
+                bool won = K::head(key[0]) == top;
+                if (lane == j - j0 * L) held[j0] = top;
+                if constexpr (!K::kNamed) {
                     // of lanes with equal scores the lowest, which has the lower experts
                     uint64_t has = __ballot(won) >> shift;
                     if (L < 64) has &= (uint64_t(1) << (L & 63)) - 1;
                     won = won && (has & ((uint64_t(1) << lane) - 1)) == 0;
-                    if (won) {
-                        const int id = int(~uint32_t(key[0]));
+                    if (won && any && top > K::kNone) {
+                        const int id = K::expert(key[0]);
                         if constexpr (BALANCE) atomicAdd(&count[id], 1);
                         ids[j] = id;
                     }
-                    if (!have && lane == 0 && in) ids[j] = -1;
                 }
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const typename K::type now = key[v], next = v + 1 < V ? key[v + 1] : 0;
+                for (int v = 0; v < KEEP; ++v) {
+                    const typename K::type now = key[v], next = v + 1 < KEEP ? key[v + 1] : typename K::type(K::kNamed ? INT32_MIN : 0);
                     key[v] = won ? next : now;
                 }
-                const float w = have ? exp_of(K::score(top) - m) : 0.0f;
-                total += w;
-                if (lane == j - j0 * L) held[j0] = w;
             }
         }
-        const float scale = c.normalize ? (any ? 1.0f / total : 0.0f) : inverse;
+        float w[64 / L], total = 0.0f;
+#pragma unroll
+        for (int j0 = 0; j0 < 64 / L; ++j0) {
+            w[j0] = any && held[j0] > K::kNone ? exp_of(K::score(held[j0]), m) : 0.0f;
+            total += w[j0];
+        }
+        const float scale = !c.normalize ? inverse : any ? 1.0f / group_sum<L>(total) : 0.0f;
 #pragma unroll
         for (int j0 = 0; j0 < 64 / L; ++j0) {
             const int j = j0 * L + lane;
             if (j < c.topk && in) {
-                weights[j] = held[j0] * scale;
+                const bool have = any && held[j0] > K::kNone;
+                weights[j] = have ? w[j0] * scale : 0.0f;
                 if constexpr (K::kNamed) {
-                    ids[j] = held_id[j0];
-                    if (BALANCE && held_id[j0] >= 0) atomicAdd(&count[held_id[j0]], 1);
+                    const int id = have ? K::expert(held[j0]) : -1;
+                    ids[j] = id;
+                    if (BALANCE && have) atomicAdd(&count[id], 1);
+                } else if (!have) {
+                    ids[j] = -1;
                 }
             }
         }
@@ -376,38 +472,30 @@ __global__ __launch_bounds__(kSumThreads) void balance_kernel(Partials q, int ex
     }
 }
 
-template <typename T, int L, int V>
-__global__ __launch_bounds__(kThreads) void choose_grad_kernel(ChooseGradCall c) {
+enum Parts { kAny, kNormalized, kPlain };
+template <typename T, int L, int V, Parts P>
+__global__ __launch_bounds__(kThreads, 4) void choose_grad_kernel(ChooseGradCall c) {
+    // training has the weights' gradient and the loss's: those without the others' instructions
+    const bool of_weights = P != kAny || c.dweights, normalize = P == kAny ? c.normalize != 0 : P == kNormalized, of_loss = P != kAny || c.counts;
     constexpr int kGroups = kThreads / L;
     // what a token's chosen experts get: a lane's part starts four words further on every 16, so that the lanes' 16 bytes lie in different banks
     constexpr int kPad = V >= 8 ? 4 : 0;
     __shared__ __align__(16) float spread[kGroups][L * (V + kPad)];
     const int lane = threadIdx.x % L, group = threadIdx.x / L, first = lane * V;
     float* part = spread[group] + lane * (V + kPad);
+    auto at = [&](int id) { return &spread[group][id + id / V * kPad]; };
     const T* scores = static_cast<const T*>(c.scores);
-    float f[V], scale = 0.0f;
+    if (of_weights) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) f[v] = 0.0f;
-    if (c.counts) {
-        int n = 0, of[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            of[v] = first + v < c.experts ? c.counts[first + v] : 0;
-            n += of[v];
-        }
-        n = group_count<L>(n);
-        const int tokens = *c.counted;
-        const float inverse = n > 0 ? 1.0f / float(n) : 0.0f;
-        if (tokens > 0) scale = c.factor * (c.dloss ? *c.dloss : 1.0f) * float(c.experts) / float(tokens);
-#pragma unroll
-        for (int v = 0; v < V; ++v) f[v] = float(of[v]) * inverse;
+        for (int v = 0; v < V; ++v) part[v] = 0.0f;
+        __builtin_amdgcn_wave_barrier();
     }
     // a lane's choice of the first L: more are loaded when they are needed
     struct Chosen { int id; float w, dw; };
-    auto chosen = [&](int64_t t, int j, bool in) {
+    auto chosen = [&](int64_t t, int j) {
         Chosen x{-1, 0.0f, 0.0f};
-        if (in && j < c.topk && c.dweights) {
-            const int64_t at = t * c.topk + j;
+        if (of_weights) {
+            const int64_t at = min(t, c.tokens - 1) * c.topk + min(j, c.topk - 1);
             x = Chosen{c.ids[at], c.weights[at], c.dweights[at]};
         }
         return x;
@@ -417,79 +505,101 @@ __global__ __launch_bounds__(kThreads) void choose_grad_kernel(ChooseGradCall c)
     int64_t t = int64_t(blockIdx.x) * kGroups + group;
     Scores<V, T> next;
     next.fetch(scores, c.ld, c.experts, c.live, t, c.tokens, first);
-    Chosen next_chosen = chosen(t, lane, next.in);
-    for (; t - group < c.tokens; t += stride) {
-        const bool in = next.in, on = next.on;
-        const Chosen mine = next_chosen;
-        float s[V], p[V], g[V];
-        next.settle(s);
-        if (t - group + stride < c.tokens) {
-            next.fetch(scores, c.ld, c.experts, c.live, t + stride, c.tokens, first);
-            next_chosen = chosen(t + stride, lane, next.in);
-        }
-        float m = -INFINITY;
+    Chosen next_chosen = chosen(t, lane);
+    float f[V], scale = 0.0f;                 // f_e, times the loss's gradient
+#pragma unroll
+    for (int v = 0; v < V; ++v) f[v] = 0.0f;
+    if (of_loss) {
+        int n = 0, of[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) of[v] = c.counts[min(first + v, c.experts - 1)];
+        const int tokens = *c.counted;
+        const float dloss = c.dloss ? *c.dloss : 1.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            m = fmaxf(m, s[v]);
-            g[v] = scale * f[v];
+            of[v] = first + v < c.experts ? of[v] : 0;
+            n += of[v];
         }
+        n = group_count<L>(n);
+        const float inverse = n > 0 ? 1.0f / float(n) : 0.0f;
+        if (tokens > 0) scale = c.factor * dloss * float(c.experts) / float(tokens);
+#pragma unroll
+        for (int v = 0; v < V; ++v) f[v] = scale * (float(of[v]) * inverse);
+    }
+    for (; t - group < c.tokens; t += stride) {
+        Scores<V, T> now = next;
+        const bool in = t < c.tokens, on = in && (!c.live || now.alive);
+        Chosen mine = next_chosen;
+        if (lane >= c.topk) mine.id = -1;
+        float p[V];
+        next.fetch(scores, c.ld, c.experts, c.live, t + stride, c.tokens, first);
+        next_chosen = chosen(t + stride, lane);
+        now.settle(c.experts, L * V, first);
+        float m = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < V; ++v) m = fmaxf(m, to_float(now.e[v]));
         m = group_largest<L>(m);
-        const bool any = m != -INFINITY;
-        if (c.counts || !c.normalize) {
+        const bool any = on && m != -INFINITY;
+        if (of_loss || !normalize) {
             // a NaN is not seen by the maximum, but in the sum
-            const float sum = exponentials<L>(s, any ? m : 0.0f, p), inverse = any ? 1.0f / sum : 0.0f;
+            const float sum = exponentials<L>(now.e, m, p), inverse = 1.0f / sum;
 #pragma unroll
             for (int v = 0; v < V; ++v) p[v] *= inverse;
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) p[v] = 0.0f;
         }
-        if (c.dweights) {
-            float dot = 0.0f;
+        float s[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) part[v] = 0.0f;
-            if (c.normalize) {
+        for (int v = 0; v < V; ++v) s[v] = 0.0f;
+        if (of_weights) {
+            float dot = 0.0f;
+            if (normalize) {
                 dot = counts(mine, on) ? mine.w * mine.dw : 0.0f;
                 for (int j = lane + L; j < c.topk; j += L) {
-                    const Chosen x = chosen(t, j, in);
+                    const Chosen x = chosen(t, j);
                     if (counts(x, on)) dot += x.w * x.dw;
                 }
                 dot = group_sum<L>(dot);
             }
-            __builtin_amdgcn_wave_barrier();
             // each expert once: the order does not matter
             auto spend = [&](const Chosen& x) {
-                if (counts(x, on)) atomicAdd(&spread[group][x.id + x.id / V * kPad], c.normalize ? x.w * (x.dw - dot) : x.dw);
+                if (counts(x, on)) atomicAdd(at(x.id), normalize ? x.w * (x.dw - dot) : x.dw);
             };
             spend(mine);
-            for (int j = lane + L; j < c.topk; j += L) spend(chosen(t, j, in));
+            for (int j = lane + L; j < c.topk; j += L) spend(chosen(t, j));
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int v = 0; v < V; ++v) s[v] = part[v];
+            __builtin_amdgcn_wave_barrier();
+            // and nothing for the next token
+            if (counts(mine, on)) *at(mine.id) = 0.0f;
+            for (int j = lane + L; j < c.topk; j += L) {
+                const Chosen x = chosen(t, j);
+                if (counts(x, on)) *at(x.id) = 0.0f;
+            }
             __builtin_amdgcn_wave_barrier();
         }
         // through the softmax: of the loss's f, and without normalisation of the weights'
-        if (c.dweights && !c.normalize) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) g[v] += part[v];
-        }
+        const bool through = of_weights && !normalize;
         float dot = 0.0f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) dot = fmaf(g[v], p[v], dot);
+        for (int v = 0; v < V; ++v) dot = fmaf(through ? f[v] + s[v] : f[v], p[v], dot);
         dot = group_sum<L>(dot);
-        T r[V];
+        union { T r[V]; uint32_t w[V * sizeof(T) / 4 + (V == 1)]; } g;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            float d = p[v] * (g[v] - dot);
-            if (c.dweights && c.normalize) d += part[v];
-            put(&r[v], s[v] != -INFINITY ? d : 0.0f);
-        }
-        __builtin_amdgcn_wave_barrier();
+        for (int v = 0; v < V; ++v) put(&g.r[v], through ? p[v] * (f[v] + s[v] - dot) : fmaf(p[v], f[v] - dot, s[v]));
+        // a token that does not count, or has no expert: zero, whatever its scores are
+#pragma unroll
+        for (int i = 0; i < int(V * sizeof(T) + 3) / 4; ++i) g.w[i] = any ? g.w[i] : 0;
         T* out = static_cast<T*>(c.dscores) + t * c.ldd + first;
         const int have = in ? c.experts - first : 0;
         if (have >= V) {
-            __builtin_memcpy(out, r, sizeof(r));
+            __builtin_memcpy(out, g.r, sizeof(g.r));
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                if (v < have) out[v] = r[v];
+                if (v < have) out[v] = g.r[v];
         }
     }
 }
@@ -512,11 +622,14 @@ void choose_typed(hipStream_t st, const ChooseCall& c, int num_cu) {
         constexpr int kL = decltype(L)::value, kV = decltype(V)::value;
         if (c.counts) {
             const Partials q = partials_of(c.ws, choose_blocks(c.tokens, c.experts, num_cu), c.experts);
-            hipLaunchKernelGGL((choose_kernel<T, kL, kV, true>), dim3(unsigned(q.blocks)), dim3(kThreads), 0, st, c, q);
+            if (kV == 16 && c.topk <= 8) hipLaunchKernelGGL((choose_kernel<T, kL, kV, kV == 16 ? 8 : kV, true>), dim3(unsigned(q.blocks)), dim3(kThreads), 0, st, c, q);
+            else hipLaunchKernelGGL((choose_kernel<T, kL, kV, kV, true>), dim3(unsigned(q.blocks)), dim3(kThreads), 0, st, c, q);
             hipLaunchKernelGGL(balance_kernel, dim3(unsigned((c.experts + kPiece - 1) / kPiece)), dim3(kSumThreads), 0, st, q, c.experts, c.counts, c.counted, c.shares, c.loss);
         } else {
             const int64_t blocks = (int64_t(c.tokens) * kL + kThreads - 1) / kThreads;
-            hipLaunchKernelGGL((choose_kernel<T, kL, kV, false>), dim3(unsigned(std::min<int64_t>(blocks, 8 * num_cu))), dim3(kThreads), 0, st, c, Partials{});
+            const dim3 grid(unsigned(std::min<int64_t>(blocks, 8 * num_cu)));
+            if (kV == 16 && c.topk <= 8) hipLaunchKernelGGL((choose_kernel<T, kL, kV, kV == 16 ? 8 : kV, false>), grid, dim3(kThreads), 0, st, c, Partials{});
+            else hipLaunchKernelGGL((choose_kernel<T, kL, kV, kV, false>), grid, dim3(kThreads), 0, st, c, Partials{});
         }
     });
 }
@@ -526,7 +639,11 @@ void choose_grad_typed(hipStream_t st, const ChooseGradCall& c, int num_cu) {
     by_size<T>(c.experts, [&](auto L, auto V) {
         constexpr int kL = decltype(L)::value, kV = decltype(V)::value;
         const int64_t blocks = (int64_t(c.tokens) * kL + kThreads - 1) / kThreads;
-        hipLaunchKernelGGL((choose_grad_kernel<T, kL, kV>), dim3(unsigned(std::min<int64_t>(blocks, 2 * num_cu))), dim3(kThreads), 0, st, c);
+        const dim3 grid(unsigned(std::min<int64_t>(blocks, 2 * num_cu)));
+        auto launch = [&](auto P) { hipLaunchKernelGGL((choose_grad_kernel<T, kL, kV, decltype(P)::value>), grid, dim3(kThreads), 0, st, c); };
+        if (!c.dweights || !c.counts) launch(std::integral_constant<Parts, kAny>{});
+        else if (c.normalize) launch(std::integral_constant<Parts, kNormalized>{});
+        else launch(std::integral_constant<Parts, kPlain>{});
     });
 }
 
