@@ -1,5 +1,5 @@
-"""Experts in 8-bit block-scaled products, trained for a few steps and then served token by token: the calls of `scaled` and
-`experts` together, timed.  Synthetic data; the target is another, random layer.
+"""A router and experts in 8-bit block-scaled products, trained for a few steps and then served token by token, also with weights in 4 bits: the
+calls of `experts`, `scaled`, `packed` and `orthogonal` together, timed.  Synthetic data; the target is another, random layer.
 
     python experiments/expert_layer.py [--tokens 4096] [--width 2048] [--inner 1024] [--experts 16] [--topk 2] [--steps 20]
 """
@@ -25,11 +25,7 @@ def main():
         return [torch.randn(s, generator=r, device="cuda") * scale * s[-1] ** -0.5 for s in ((a.experts, a.inner, a.width), (a.experts, a.width, a.inner))]
 
     layer, target = experts.ExpertLayer(h, *weights(1.0)), experts.ExpertLayer(h, *weights(1.0))
-    router = torch.randn((a.width, a.experts), generator=r, device="cuda") * a.width ** -0.5
-
-    def route(x):
-        top, ids = (x.float() @ router).topk(a.topk, dim=1)
-        return ids, top.softmax(dim=1)
+    router, of_target = (torch.randn((a.width, a.experts), generator=r, device="cuda") * a.width ** -0.5 for _ in range(2))
 
     def ms(f):
         s, e = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
@@ -41,24 +37,30 @@ def main():
 
     for step in range(a.steps):
         x = torch.randn((a.tokens, a.width), generator=r, device="cuda").bfloat16()
-        ids, p = route(x)
-        want = target.serve(x, ids, p)
-        (y, kept), forward = ms(lambda: layer.forward(x, ids, p))
-        dy = (y - want) * (2.0 / a.tokens)
-        (_, _, dw1, dw2), backward = ms(lambda: layer.backward(dy, kept))
-        loss = (y.float() - want.float()).square().sum(1).mean().item() / a.width
-        for w, d in ((layer.w1, dw1), (layer.w2, dw2)):          # a step of 3 % of the weights' size down the gradient
-            w -= d * (0.03 * w.norm() / d.norm())
-        _, prepare = ms(layer.prepare_weights)
+        chosen = experts.choose(h, x.float() @ of_target, a.topk, balance=False)
+        want = target.serve(x, chosen.ids, chosen.weights)
+        scores = x.float() @ router
+        choice, choosing = ms(lambda: experts.choose(h, scores, a.topk))
+        (y, kept), forward = ms(lambda: layer.forward(x, choice.ids, choice.weights))
+        dy = (y - want) * (2.0 / a.tokens / a.width)
+        (_, dp, dw1, dw2), backward = ms(lambda: layer.backward(dy, kept))
+        router -= 0.3 * (x.float().T @ experts.choose_backward(h, scores, choice, dp, 0.01))
+        loss = (y.float() - want.float()).square().mean().item()
+        _, update = ms(lambda: layer.update(dw1, dw2, 0.05))
         if step % 5 == 0 or step == a.steps - 1:
-            print("step %2d  loss %.4f  forward %.3f ms  backward %.3f ms  weights to 8 bits %.3f ms" % (step, loss, forward, backward, prepare), flush=True)
+            print("step %2d  loss %.4f  balance %.3f  choice %.3f ms  forward %.3f ms  backward %.3f ms  update, weights to 8 bits %.3f ms"
+                  % (step, loss, choice.loss.item(), choosing, forward, backward, update), flush=True)
+    layer.pack_weights()
     for tokens in (1, 8, 64):
         x = torch.randn((tokens, a.width), generator=r, device="cuda").bfloat16()
-        ids, w = route(x)
-        for _ in range(3):
-            layer.serve(x, ids, w)
-        _, t = ms(lambda: [layer.serve(x, ids, w) for _ in range(50)])
-        print("serving %2d token(s): %.1f us a step" % (tokens, t * 20))
+        for name, serve in (("8", layer.serve), ("4", layer.serve_packed)):
+            def token():
+                c = experts.choose(h, x.float() @ router, a.topk, balance=False)
+                return serve(x, c.ids, c.weights)
+            for _ in range(3):
+                token()
+            _, t = ms(lambda: [token() for _ in range(50)])
+            print("serving %2d token(s), weights in %s bits: %.1f us a step" % (tokens, name, t * 20))
     h.close()
 
 
