@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "oz_layer.h"
+#include "oz_packed_plan.h"
 #include "oz_scaled_device.h"
 
 namespace oz {
@@ -21,7 +22,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kBlock = 128;              // of k that a wave takes at a time
+constexpr int kBlock = kPackedBlock;     // of k that a wave takes at a time
 
 // Eight codes as the matrix instruction takes them, in the order 0 4 1 5 2 6 3 7 (x's elements in the same): float16 and EXACT: code - 8;
 // bfloat16 else: 128 + code, a third of the instructions, and what is too much comes off the sums.
@@ -373,7 +374,7 @@ __global__ __launch_bounds__(256) void packed_gemm_short_kernel(PackedGemm g) {
 template <typename X, int MT, int R>
 void launch_rows(hipStream_t st, const PackedGemm& g, int waves) {
     const int strips = (g.n + 16 * R - 1) / (16 * R);
-    const int64_t tiles = g.offsets ? group_pieces(g.m, g.groups, MT * 16) : (g.m + MT * 16 - 1) / (MT * 16);
+    const int64_t tiles = packed_tiles(g.m, g.offsets ? g.groups : 0, MT * 16);
     const dim3 grid(unsigned(tiles * strips)), block(64 * waves);
     const std::true_type yes;
     const std::false_type no;
@@ -408,30 +409,8 @@ void launch_typed(hipStream_t st, const PackedGemm& g, int num_cu) {
         hipLaunchKernelGGL(packed_gemm_short_kernel<X>, dim3(unsigned((int64_t(g.m) * g.n + 255) / 256)), dim3(256), 0, st, g);
         return;
     }
-    const int64_t avg = g.offsets ? (int64_t(g.m) + g.groups - 1) / g.groups : g.m;      // rows of a group on average
-    const int blocks = std::max((g.k + kBlock - 1) / kBlock, 1);
-    auto strips_of = [&](int mt) { return (g.offsets ? group_pieces(g.m, g.groups, mt * 16) : (g.m + mt * 16 - 1) / (mt * 16)) * ((g.n + 15) / 16); };
-    // 16s of rows of x to a workgroup: as many as there are, up to four, but fewer where that leaves the chip idle
-    int mt = avg <= 16 ? 1 : avg <= 32 ? 2 : 4;
-    while (mt > 1 && strips_of(mt / 2) <= 2 * num_cu) mt /= 2;
-    const int64_t strips = strips_of(mt);
-    // 16s of rows of W to a workgroup, and waves that share k: what fills the chip with 16 waves to a CU that have two blocks each, with as much of W to a
-    // wave as that leaves, since all of it shares the wave's x.
-    auto waves_of = [&](int rows, int most) {
-        int w = 1;
-        while (w < most && w < blocks && strips / rows * w < 16 * num_cu) w *= 2;
-        return w;
-    };
-    // more rows of W for each x take more registers: groups of 32 with their scales leave room for two strips, small groups and 64 rows of x, and float32
-    // beside more than 16, for one
-    const int most = mt == 1 ? (g.w.shift == 5 ? 2 : 4) : sizeof(X) == 2 && (mt == 2 || g.w.shift == 7) ? 2 : 1;
-    int r = 1, waves = waves_of(1, mt == 1 ? 16 : 8);
-    for (int more = 2; more <= most; more *= 2) {
-        const int w = waves_of(more, mt == 1 && more * int(sizeof(X)) <= 4 ? 16 : 8);
-        if (strips / more * w < (mt == 4 ? 8 : 16) * num_cu) break;
-        r = more;
-        waves = w;
-    }
+    const PackedPlan plan = packed_plan(g.m, g.n, g.k, g.offsets ? g.groups : 0, sizeof(X), g.w.shift, num_cu);
+    const int mt = plan.rows, r = plan.strips, waves = plan.waves;
     if (mt == 1) {
         if (r == 4) launch_rows<X, 1, 4>(st, g, waves);
         else if (r == 2) launch_rows<X, 1, 2>(st, g, waves);

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "oz_scaled_plan.h"
 #include "ozdgemm.h"
 
 namespace oz {
@@ -69,12 +70,6 @@ void launch_combine_grad(hipStream_t st, int tokens, int topk, int cols, int typ
 // Whether the calling thread's current device is the handle's; its compute units.
 bool handle_on_device(oz_handle_t h);
 int handle_compute_units(oz_handle_t h);
-
-// Pieces of `size` that groups of `total` rows can be cut into at most, each group for itself (a group of its own for rows behind the last).
-inline int64_t group_pieces(int64_t total, int64_t groups, int64_t size) {
-    const int64_t g = groups + 1 < total ? groups + 1 : total;
-    return (total + (size - 1) * g) / size;
-}
 
 // Columns, in blocks, that oz_quantize's grouped transpose can take.
 inline int64_t grouped_blocks(int64_t rows, int64_t groups) {

@@ -17,6 +17,12 @@
 
 namespace oz {
 
+// Pieces of `size` that groups of `total` rows can be cut into at most, each group for itself (a group of its own for rows behind the last).
+inline int64_t group_pieces(int64_t total, int64_t groups, int64_t size) {
+    const int64_t g = groups + 1 < total ? groups + 1 : total;
+    return (total + (size - 1) * g) / size;
+}
+
 enum class ScaledRoute { kFew, kTiles64, kTiles64Deep, kTiles128, kTall, kBig };
 
 struct ScaledPlan {

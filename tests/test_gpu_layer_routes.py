@@ -1,0 +1,67 @@
+"""Every way in which products with 4-bit weights and orthogonal updates are cut up, against 64-bit forms."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+import layer_reference as ref  # noqa: E402
+import layer_routes as lr  # noqa: E402
+from test_gpu_orthogonal import EPS, QUINTIC, check_five, gradient, parts_of  # noqa: E402
+from test_gpu_packed import check_product, weights  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def h():
+    from paper_2511_13778_amd import ozdgemm as g
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible: the HIP path cannot run (there is no CPU fallback)")
+    handle = g.Handle(0)
+    yield handle
+    handle.close()
+
+
+@pytest.mark.parametrize("at", sorted(lr.PACKED), ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_packed_products(h, at, dtype):
+    from paper_2511_13778_amd import packed
+    for counts, behind, n, k, group, kinds in lr.PACKED[at]:
+        if dtype.itemsize not in kinds:
+            continue
+        r = torch.Generator(device="cuda").manual_seed(n + k + group)
+        zeros = group != 64
+        w = weights(r, n, k, group, zeros, torch.float16, (len(counts),) if counts else ())
+        m = sum(counts) + behind
+        x = torch.randn((m, k), generator=r, device="cuda").to(dtype)
+        if not counts:
+            check_product(packed.gemm(h, x, w), x, ref.codes_of(w.data, k), w.scale, w.zero, group, (at, n, k))
+            continue
+        offsets = torch.tensor([0] + counts).cumsum(0).to(torch.int32).cuda()
+        y = packed.gemm_grouped(h, x, w, offsets)
+        first = 0
+        for e, c in enumerate(counts):
+            if c:
+                check_product(y[first:first + c], x[first:first + c], ref.codes_of(w.data[e], k), w.scale[e], w.zero[e] if zeros else None, group, (at, n, k, e))
+            first += c
+        assert not y[first:].any()
+
+
+@pytest.mark.parametrize("dtype,at", [(torch.bfloat16, i) for i in range(len(lr.ORTHO[1]))] + [(torch.float32, i) for i in range(len(lr.ORTHO[2]))])
+def test_tiles_of_orthogonal_updates(h, dtype, at):
+    from paper_2511_13778_amd import orthogonal
+    sizes = list(lr.ORTHO[parts_of(dtype)].values())
+    batch, rows, cols = sizes[at]
+    r = torch.Generator(device="cuda").manual_seed(rows + cols)
+    x = gradient(r, batch, rows, cols).to(dtype)
+    got = orthogonal.orthogonalize(h, x, steps=1, eps=EPS)
+    if rows != cols:                          # (square ones are taken as they are: their other product with themselves)
+        turned = orthogonal.orthogonalize(h, x.transpose(1, 2).contiguous(), steps=1, eps=EPS)
+        assert torch.equal(turned.transpose(1, 2), got)
+    for i in range(batch):
+        exact, bound = ref.orthogonalize_bound(x[i], QUINTIC, EPS, parts_of(dtype))
+        err = (got[i].double() - exact).abs()
+        bound = bound + ref.rounded(exact, dtype)
+        assert (err <= bound).all(), (i, (err / bound).max().item())
+    five = orthogonal.orthogonalize(h, x)
+    assert torch.equal(five, orthogonal.orthogonalize(h, x))
+    for i in (0, batch - 1):
+        check_five(five[i], x[i])
