@@ -227,3 +227,38 @@ def test_captured_and_replayed_with_other_inputs(h):
         torch.cuda.synchronize()
         for a, b, c in zip(step(), got, got2):
             assert torch.equal(a, b) and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("tokens,experts,topk", [(20, 200, 9), (11, 256, 40), (13, 250, 8), (37, 131, 8), (9, 255, 64), (300, 9, 9)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_more_of_a_lane_than_half(h, tokens, experts, topk, dtype, normalize):
+    # chosen experts that are neighbours: all of one lane's
+    x = scores_of(11, tokens, experts, dtype)
+    x[::2, experts // 3:experts // 3 + topk] += 20.0
+    check(h, x, topk, normalize=normalize)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("experts", [20, 250, 500])
+def test_the_types_largest_and_zeros_of_both_signs(h, dtype, experts):
+    from paper_2511_13778_amd import experts as ex
+    big = torch.finfo(dtype).max
+    x = torch.zeros((6, experts), dtype=dtype)
+    x[:, 1::2] = -0.0                          # equal: the lowest expert first
+    x[1, 5:9], x[1, 11] = big, -big
+    x[2] = -big                                # above -infinity
+    x[3, 7:] = float("-inf")
+    x[4, 3], x[4, 12] = -big, big
+    x[5] = big
+    for normalize in (True, False):
+        c = ex.choose(h, x.cuda(), 8, normalize=normalize)
+        ids, w, p, counts, counted = ref.choose(x, 8, None, normalize)
+        assert torch.equal(c.ids.cpu().long(), ids) and counted == 6
+        # differences are zero or further than any exponential reaches: shares are quotients of whole numbers
+        close(c.weights, w, 4 * F * w, "weights")
+        dw = torch.randn((6, 8), generator=torch.Generator().manual_seed(1))
+        shares, loss, f = ref.balance(p, counts, counted)
+        exact, size = ref.choose_grad(ids, w, p, f, counted, dw.double(), 0.5, normalize)
+        d = ex.choose_backward(h, x.cuda(), c, dw.cuda(), 0.5)
+        close(d, exact, 64 * F * size + ref.rounded(exact, dtype) + 16 * LEAST, "dscores")
