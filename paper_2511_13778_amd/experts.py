@@ -119,29 +119,28 @@ class Choice:
     expert was chosen, int32), counted (one int32: tokens that have an expert), shares (their mean probability of each expert, float32) and
     loss (float32, one value).  counts may be added up over several GPUs before choose_backward, in place or set to others."""
 
-    __slots__ = ("ids", "weights", "_counts", "_counted", "_shares", "_loss", "_table", "live", "normalize")
+    __slots__ = ("ids", "weights", "live", "normalize", "_parts", "_table")
 
     def __init__(self, ids, weights, counts=None, counted=None, shares=None, loss=None, live=None, normalize=True):
-        self.ids, self.weights, self._counts, self._counted, self._shares, self._loss = ids, weights, counts, counted, shares, loss
-        self._table, self.live, self.normalize = None, live, normalize
+        self.ids, self.weights, self.live, self.normalize = ids, weights, live, normalize
+        self._parts, self._table = [counts, counted, shares, loss], None
 
-    # the four results of the whole batch are parts of one int32 table, looked at when they are asked for
-    def _part(name, at, real):
+    # choose leaves the four results of the whole batch in one table of float32, (2 experts + 2 values): cut out when they are asked for
+    def _part(at, cut):
         def get(self):
-            have = getattr(self, name)
+            have = self._parts[at]
             if have is None and self._table is not None:
-                experts = (self._table.shape[0] - 2) // 2
-                lo, hi = at(experts)
-                have = self._table[lo:hi] if hi > lo else self._table[lo]
-                have = have.view(torch.float32) if real else have
-                setattr(self, name, have)
+                have = self._parts[at] = cut(*self._table)
             return have
-        return property(get, lambda self, v: setattr(self, name, v))
 
-    counts = _part("_counts", lambda n: (0, n), False)
-    counted = _part("_counted", lambda n: (n, n + 1), False)
-    shares = _part("_shares", lambda n: (n + 1, 2 * n + 1), True)
-    loss = _part("_loss", lambda n: (2 * n + 1, 0), True)
+        def put(self, value):
+            self._parts[at] = value
+        return property(get, put)
+
+    counts = _part(0, lambda table, n: table.narrow(0, 0, n).view(torch.int32))
+    counted = _part(1, lambda table, n: table.narrow(0, n, 1).view(torch.int32))
+    shares = _part(2, lambda table, n: table.narrow(0, n + 1, n))
+    loss = _part(3, lambda table, n: table.select(0, 2 * n + 1))
     del _part
 
 
@@ -162,34 +161,28 @@ def choose(h: g.Handle, scores, topk: int, live=None, normalize=True, balance=Tr
     tokens, experts = scores.shape
     if not 1 <= topk <= min(experts, 64):
         raise ValueError("topk 1 .. 64 of %d experts, not %s" % (experts, topk))
-    # one allocation: ids, weights, the four results of the batch, the workspace
-    n = tokens * topk
-    need = h.choose_experts_workspace_bytes(tokens, experts) if balance else 0
-    head = 2 * n + 2 * experts + 2
-    first = -(-head // 64) * 64
-    all_ = torch.empty(first + (need + 3) // 4 if balance else 2 * n, dtype=torch.int32, device=scores.device)
-    base = all_.data_ptr()
+    c = Choice(scores.new_empty((tokens, topk), dtype=torch.int32), scores.new_empty((tokens, topk), dtype=torch.float32), live=live, normalize=bool(normalize))
+    more = (None, None, None, None, None, 0)
     if balance:
-        ids, weights, table, _ = all_.split_with_sizes((n, n, 2 * experts + 2, all_.shape[0] - head))
-        at = base + 8 * n
-        more = (at, at + 4 * experts, at + 4 * experts + 4, at + 8 * experts + 4, base + 4 * first, need)
-    else:
-        ids, weights = all_.split_with_sizes((n, n))
-        table, more = None, (None, None, None, None, None, 0)
-    c = Choice(ids.view(tokens, topk), weights.view(torch.float32).view(tokens, topk), live=live, normalize=bool(normalize))
-    c._table = table
+        # one allocation: the four results of the batch and, behind them, the workspace
+        need = h.choose_experts_workspace_bytes(tokens, experts)
+        first = (2 * experts + 65) // 64 * 64
+        table = scores.new_empty(first + (need + 3) // 4, dtype=torch.float32)
+        c._table = table, experts
+        at = table.data_ptr()
+        more = (at, at + 4 * experts, at + 4 * experts + 4, at + 8 * experts + 4, at + 4 * first, need)
     h.call("oz_choose_experts", stream_of(scores), tokens, experts, topk, scores.data_ptr(), ld, float_type(scores.dtype), _live(live, tokens),
-           int(c.normalize), base, base + 4 * n, *more)
+           int(c.normalize), c.ids.data_ptr(), c.weights.data_ptr(), *more)
     return c
 
 
 def choose_backward(h: g.Handle, scores, choice: Choice, dweights=None, dloss=None):
     """The gradient of choose's scores, for dweights (tokens x topk, float32) and dloss (a number, or one float32 on the GPU); either may be None."""
     ld = check_matrix(scores, "scores")
-    check_device(h, scores, choice.ids, choice.weights, choice.counts, choice.counted, choice.live, dweights, dloss if torch.is_tensor(dloss) else None)
+    ids, weights, live = choice.ids, choice.weights, choice.live
+    check_device(h, scores, ids, weights, live, dweights)
     tokens, experts = scores.shape
-    ids = choice.ids
-    if ids.dim() != 2 or ids.shape[0] != tokens or choice.weights.shape != ids.shape or choice.weights.dtype != torch.float32 or not choice.weights.is_contiguous():
+    if ids.dim() != 2 or ids.shape[0] != tokens or weights.shape != ids.shape or weights.dtype != torch.float32 or not weights.is_contiguous():
         raise ValueError("scores %s do not belong to this choice of %s" % (tuple(scores.shape), tuple(ids.shape)))
     check_ints(ids, "ids")
     if dweights is not None and (dweights.dtype != torch.float32 or dweights.shape != ids.shape or not dweights.is_contiguous()):
@@ -197,18 +190,21 @@ def choose_backward(h: g.Handle, scores, choice: Choice, dweights=None, dloss=No
     counts = counted = scalar = None
     factor = 1.0
     if dloss is not None:
-        if choice.counts is None or choice.counted is None:
+        counts, counted = choice.counts, choice.counted
+        if counts is None or counted is None:
             raise ValueError("a gradient of the loss needs the choice's counts: choose(balance=True)")
-        counts, counted = check_ints(choice.counts, "counts", experts).data_ptr(), check_ints(choice.counted, "counted", 1).data_ptr()
+        check_device(h, counts, counted)
+        counts, counted = check_ints(counts, "counts", experts).data_ptr(), check_ints(counted, "counted", 1).data_ptr()
         if torch.is_tensor(dloss):
+            check_device(h, dloss)
             if not dloss.is_cuda or dloss.dtype != torch.float32 or dloss.numel() != 1:
                 raise ValueError("dloss: a number, or one float32 on the GPU")
             scalar = dloss.data_ptr()
         else:
             factor = float(dloss)
-    d = torch.empty((tokens, experts), dtype=scores.dtype, device=scores.device)
+    d = scores.new_empty((tokens, experts))
     h.call("oz_choose_experts_grad", stream_of(scores), tokens, experts, ids.shape[1], scores.data_ptr(), ld, float_type(scores.dtype),
-           _live(choice.live, tokens), int(choice.normalize), ids.data_ptr(), choice.weights.data_ptr(), None if dweights is None else dweights.data_ptr(),
+           _live(live, tokens), int(choice.normalize), ids.data_ptr(), weights.data_ptr(), None if dweights is None else dweights.data_ptr(),
            counts, counted, scalar, factor, d.data_ptr(), max(experts, 1))
     return d
 

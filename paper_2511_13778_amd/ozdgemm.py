@@ -6,6 +6,7 @@ memory and streams.  There is no CPU fallback: if the compiled library is missin
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 
@@ -202,6 +203,9 @@ class Handle:
         self._h = C.c_void_p()
         self.device = device
         _check(self.lib.oz_create(C.byref(self._h), device), "oz_create")
+        # sizes that every call asks for, functions of their arguments alone
+        self.choose_experts_workspace_bytes = functools.lru_cache(256)(functools.partial(self.lib.oz_choose_experts_workspace_bytes, self._h))
+        self.orthogonalize_workspace_bytes = functools.lru_cache(256)(functools.partial(self.lib.oz_orthogonalize_workspace_bytes, self._h))
 
     def close(self):
         if self._h:
@@ -276,12 +280,6 @@ class Handle:
 
     def sort_tokens_workspace_bytes(self, tokens, topk, experts) -> int:
         return self.lib.oz_sort_tokens_workspace_bytes(self._h, tokens, topk, experts)
-
-    def choose_experts_workspace_bytes(self, tokens, experts) -> int:
-        return self.lib.oz_choose_experts_workspace_bytes(self._h, tokens, experts)
-
-    def orthogonalize_workspace_bytes(self, batch, rows, cols, type_) -> int:
-        return self.lib.oz_orthogonalize_workspace_bytes(self._h, batch, rows, cols, type_)
 
     def profile_enable(self, max_calls: int):
         _check(self.lib.oz_profile_enable(self._h, max_calls), "oz_profile_enable")

@@ -25,8 +25,8 @@ class Packed:
     """A matrix in 4 bits: data uint8 (rows x ld, or groups x rows x ld, ld a multiple of 16 with 2 ld >= cols rounded up to 32), scale and zero
     (ceil(cols / group) x rows, for each group)."""
 
-    # desc: what the C ABI takes, addresses and strides
-    __slots__ = ("data", "scale", "zero", "cols", "group", "desc")
+    # desc: what the C ABI takes, addresses and strides.  What it is made of is not set to others: a matrix with another part is another Packed.
+    __slots__ = ("_data", "_scale", "_zero", "_cols", "_group", "_rows", "_groups", "desc")
 
     def __init__(self, data, scale, zero=None, cols=None, group=128):
         cols = 2 * data.shape[-1] if cols is None else cols
@@ -45,21 +45,25 @@ class Packed:
             raise ValueError("rows of codes and of scales are contiguous")
         if zero is not None and (zero.device != data.device or zero.shape != scale.shape or zero.stride() != scale.stride()):
             raise ValueError("zero points laid out as the scales")
-        self.data, self.scale, self.zero, self.cols, self.group = data, scale, zero, cols, group
-        batched = data.dim() == 3
+        self._keep(data, scale, zero, cols, group)
         # a single row has no distance to the next one: what the ABI asks of it is taken
         ld = data.stride(-2) if rows > 1 else -(-data.shape[-1] // 16) * 16
         sld = scale.stride(-2) if scale.shape[-2] > 1 else max(scale.shape[-1], 1)
+        batched = data.dim() == 3
         self.desc = g.oz_packed_t(data.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr(), ld, sld, data.stride(0) if batched else 0,
                                   scale.stride(0) if batched else 0, float_type(scale.dtype), group, 0)
 
-    @property
-    def rows(self):
-        return self.data.shape[-2]
+    def _keep(self, data, scale, zero, cols, group):
+        self._data, self._scale, self._zero, self._cols, self._group = data, scale, zero, cols, group
+        self._rows, self._groups = data.shape[-2], data.shape[0] if data.dim() == 3 else 1
 
-    @property
-    def groups(self):
-        return self.data.shape[0] if self.data.dim() == 3 else 1
+    data = property(lambda self: self._data)
+    scale = property(lambda self: self._scale)
+    zero = property(lambda self: self._zero)
+    cols = property(lambda self: self._cols)
+    group = property(lambda self: self._group)
+    rows = property(lambda self: self._rows)
+    groups = property(lambda self: self._groups)
 
 
 def empty(rows, cols, group=128, zeros=False, scale_dtype=torch.float16, groups=None, device="cuda") -> Packed:
@@ -68,11 +72,11 @@ def empty(rows, cols, group=128, zeros=False, scale_dtype=torch.float16, groups=
         raise ValueError("group: 32, 64 or 128, not %s" % (group,))
     ld, blocks, lead = max(-(-cols // 32) * 16, 16), -(-cols // group), () if groups is None else (groups,)
     w = Packed.__new__(Packed)              # sizes and types are right by construction
-    w.data = torch.empty(lead + (rows, ld), dtype=torch.uint8, device=device)
-    w.scale = torch.empty(lead + (blocks, rows), dtype=scale_dtype, device=device)
-    w.zero = torch.empty(lead + (blocks, rows), dtype=scale_dtype, device=device) if zeros else None
-    w.cols, w.group = cols, group
-    w.desc = g.oz_packed_t(w.data.data_ptr(), w.scale.data_ptr(), w.zero.data_ptr() if zeros else None, ld, max(rows, 1), 0 if groups is None else rows * ld,
+    data = torch.empty(lead + (rows, ld), dtype=torch.uint8, device=device)
+    scale = data.new_empty(lead + (blocks, rows), dtype=scale_dtype)
+    zero = data.new_empty(lead + (blocks, rows), dtype=scale_dtype) if zeros else None
+    w._keep(data, scale, zero, cols, group)
+    w.desc = g.oz_packed_t(data.data_ptr(), scale.data_ptr(), zero.data_ptr() if zeros else None, ld, max(rows, 1), 0 if groups is None else rows * ld,
                            0 if groups is None else blocks * rows, float_type(scale_dtype), group, 0)
     return w
 
@@ -98,7 +102,7 @@ def quantize(h: g.Handle, x, group=128, zeros=False, scale_dtype=torch.float16) 
 def unpack(h: g.Handle, w: Packed, dtype=torch.float32, out=None):
     """The values of w in `dtype` (or out's)."""
     shape = w.data.shape[:-1] + (w.cols,)
-    y = torch.empty(shape, dtype=dtype, device=w.data.device) if out is None else out
+    y = w.scale.new_empty(shape, dtype=dtype) if out is None else out
     rows, cols, ld, batch, stride = _matrices(y, "out")
     if y.shape != shape:
         raise ValueError("out: %s, not %s" % (tuple(shape), tuple(y.shape)))
@@ -110,16 +114,19 @@ def unpack(h: g.Handle, w: Packed, dtype=torch.float32, out=None):
 
 def _product(h, x, w, groups, offsets, dtype, out):
     ldx = check_matrix(x, "x")
-    check_device(h, x, w.data, w.scale, w.zero, offsets, out)
-    if x.shape[1] != w.cols or w.groups != max(groups, 1):
+    check_device(h, x, w._data, w._scale, w._zero, offsets, out)
+    (m, k), n = x.shape, w._rows
+    if k != w._cols or w._groups != max(groups, 1):
         raise ValueError("x %s and %d matrices of %d x %d do not multiply" % (tuple(x.shape), w.groups, w.rows, w.cols))
-    m, n = x.shape[0], w.rows
-    y = torch.empty((m, n), dtype=x.dtype if dtype is None else dtype, device=x.device) if out is None else out
-    ldy = check_matrix(y, "out")
-    if tuple(y.shape) != (m, n):
-        raise ValueError("out: %d x %d, not %s" % (m, n, tuple(y.shape)))
-    h.call("oz_packed_gemm", stream_of(x), groups, None if offsets is None else offsets.data_ptr(), m, n, w.cols, x.data_ptr(), ldx, float_type(x.dtype),
-           w.desc, y.data_ptr(), ldy, float_type(y.dtype))
+    kind = float_type(x.dtype)
+    if out is None:
+        y, ldy, y_kind = x.new_empty((m, n), dtype=dtype), max(n, 1), kind if dtype is None else float_type(dtype)
+    else:
+        y, ldy, y_kind = out, check_matrix(out, "out"), float_type(out.dtype)
+        if tuple(y.shape) != (m, n):
+            raise ValueError("out: %d x %d, not %s" % (m, n, tuple(y.shape)))
+    h.call("oz_packed_gemm", stream_of(x), groups, None if offsets is None else offsets.data_ptr(), m, n, k, x.data_ptr(), ldx, kind, w.desc, y.data_ptr(),
+           ldy, y_kind)
     return y
 
 

@@ -127,6 +127,9 @@ def test_packed_matrices_that_do_not_fit(mode):
                 (data[:, :24], scale, None, 48, 32), (data, scale, None, -1, 32), (made(U8, d, 6, 64)[:, ::2], scale, None, 64, 32)):
         refused(lambda: packed.Packed(*bad[:3], cols=bad[3], group=bad[4]))
     refused(lambda: packed.empty(4, 64, group=48))
+    for part in ("data", "scale", "zero", "cols", "group"):          # what the C ABI is given was looked at when the matrix was made
+        with pytest.raises(AttributeError):
+            setattr(packed.Packed(data, scale, cols=64, group=32), part, None)
     w, ws, x = packed_on(d, 6, 64), packed_on(d, 6, 64, (2,)), made(F32, d, 3, 64)
     for bad in (made(F32, d, 3, 63), made(torch.float64, d, 3, 64), made(F32, d, 64), made(F32, d, 64, 3).T):
         refused(lambda: packed.gemm(h, bad, w))
