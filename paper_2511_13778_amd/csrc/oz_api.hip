@@ -259,7 +259,8 @@ oz_status_t oz_create(oz_handle_t* handle, int device) {
         h->static_ws = nullptr;
         bool ok = hipGetDevice(&prev) == hipSuccess && hipSetDevice(device) == hipSuccess &&
                   hipGetSymbolAddress(&h->static_ws, HIP_SYMBOL(scratch)) == hipSuccess && h->static_ws != nullptr &&
-                  prepare_gemm_i8() && prepare_scaled_gemm() && prepare_ortho();
+                  prepare_gemm_i8() && prepare_scaled_gemm() && prepare_ortho() && prepare_packed_gemm_f32() &&
+                  prepare_packed_gemm_bf16() && prepare_packed_gemm_f16();
         if (prev >= 0 && prev != device) ok = (hipSetDevice(prev) == hipSuccess) && ok;
         if (!ok) {
             delete h;

@@ -77,6 +77,10 @@ struct OrthoCall {
 };
 size_t ortho_bytes(int64_t batch, int64_t rows, int64_t cols, int type, int num_cu);
 void launch_ortho(hipStream_t st, const OrthoCall& c, int num_cu);
-bool prepare_ortho();                    // once per process, before the first launch
+// once per process, before the first launch
+bool prepare_ortho();
+bool prepare_packed_gemm_f32();
+bool prepare_packed_gemm_bf16();
+bool prepare_packed_gemm_f16();
 
 }  // namespace oz

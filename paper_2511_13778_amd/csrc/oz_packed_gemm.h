@@ -1,6 +1,6 @@
 // Product with weights in 4 bits for few rows of x: what bounds it is the read of the weights.
 //
-// A workgroup has 16 R rows of W and up to 64 rows of x; its waves share k, in runs of blocks of 128, and add up their sums through LDS in the waves'
+// A workgroup has 16 R rows of W and 16 rows of x; its waves share k, in runs of blocks of 128, and add up their sums through LDS in the waves'
 // order.  code - 8 is exact in x's 16-bit type, and goes with x into v_mfma_f32_16x16x32 (float32 x as three bfloat16 parts, exactly); scales
 // are applied to each group's sum, in 32 bits, so a result of 16 bits has one rounding, the last.  The sums of x that zero points need are one
 // more matrix instruction, with a matrix of ones.
@@ -146,23 +146,23 @@ struct ScaleLoad {
     }
 };
 
-// MT: 16s of rows of x.  R: 16s of rows of W.  PER: groups of columns in a block, whose sums are scaled apart.  EXACT: bfloat16 codes with nothing to come off the sums.
+// 16 rows of x; R: 16s of rows of W.  PER: groups of columns in a block, whose sums are scaled apart.  EXACT: bfloat16 codes with nothing to come off the sums.
 // That 128 + code is multiplied instead of code - 8 makes the sums 136 / 4.6 times as large and their 32-bit roundings with them: 4e-6 of a result, or
 // 4e-5 where all of x has one sign, beside a rounding to bfloat16 of 2e-3.
-template <typename X, int MT, int R, int PER, bool ZEROS, bool EXACT>
+template <typename X, int R, int PER, bool ZEROS, bool EXACT>
 struct Shape {
-    static constexpr int kAhead = MT == 1 || MT * R == 8 ? 2 : 4;                     // blocks whose weights are on their way together
+    static constexpr int kAhead = 2;                                               // blocks whose weights are on their way together
     static constexpr int kX = sizeof(X) == 2 ? 2 : 1;                 // of them, those whose x is too
     static constexpr int kLoads = (kAhead * PER * 16 * R + 63) / 64, kScales = kLoads * 64;      // of a wave, in LDS
-    static constexpr int kThreads = MT == 1 && R * int(sizeof(X)) <= 4 ? 1024 : 512;
-    static constexpr int kWaveBytes = std::max(MT * 16 * 16 * R, kScales * (ZEROS ? 2 : 1)) * 4;      // scales, and in the end the sums
+    static constexpr int kThreads = R * int(sizeof(X)) <= 4 ? 1024 : 512;
+    static constexpr int kWaveBytes = std::max(16 * 16 * R, kScales * (ZEROS ? 2 : 1)) * 4;      // scales, and in the end the sums
 };
 
-template <typename X, int MT, int R, int PER, bool ZEROS, bool EXACT>
-__global__ __launch_bounds__((Shape<X, MT, R, PER, ZEROS, EXACT>::kThreads)) void packed_gemm_kernel(PackedGemm g, int strips) {
+template <typename X, int R, int PER, bool ZEROS, bool EXACT>
+__global__ __launch_bounds__((Shape<X, R, PER, ZEROS, EXACT>::kThreads)) void packed_gemm_kernel(PackedGemm g, int strips) {
     using E = Eight<X>;
     using W = typename E::W;
-    using S = Shape<X, MT, R, PER, ZEROS, EXACT>;
+    using S = Shape<X, R, PER, ZEROS, EXACT>;
     constexpr int kPer = PER, kEach = 4 / PER, kAhead = S::kAhead, kX = S::kX;
     constexpr bool SMALL = PER > 1;
     constexpr bool kSums = ZEROS || !EXACT;                           // sums of x are needed
@@ -170,30 +170,26 @@ __global__ __launch_bounds__((Shape<X, MT, R, PER, ZEROS, EXACT>::kThreads)) voi
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = int(blockDim.x) >> 6;
     const int q = lane >> 4, x16 = lane & 15;
     const int strip = int(blockIdx.x % unsigned(strips)), piece = int(blockIdx.x / unsigned(strips)), col0 = strip * 16 * R, cols = min(g.n - col0, 16 * R);
-    int row0 = piece * MT * 16, rows = min(g.m - row0, MT * 16), of = 0;
+    int row0 = piece * 16, rows = min(g.m - row0, 16), of = 0;
     if (g.offsets) {
-        GroupPieces<MT * 16> pieces(g.offsets, g.groups, g.m);
+        GroupPieces<16> pieces(g.offsets, g.groups, g.m);
         const GroupPiece p = pieces.template find<false>(piece);
         if (p.group < 0) return;
         of = p.group;
         row0 = p.row;
-        rows = min(p.end - p.row, MT * 16);
+        rows = min(p.end - p.row, 16);
     }
     const bool none = g.offsets && of >= g.groups;                    // rows behind the last group: zeros
     float* mine = lds + wave * (S::kWaveBytes / 4);
-    v4f acc[MT][R];
+    v4f acc[R];
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int s = 0; s < R; ++s) acc[i][s] = v4f{0, 0, 0, 0};
+    for (int s = 0; s < R; ++s) acc[s] = v4f{0, 0, 0, 0};
     if (!none) {
         const int bytes = (g.k + 31) / 32 * 16;
         const uint8_t* w_row[R];
 #pragma unroll
         for (int s = 0; s < R; ++s) w_row[s] = g.w.data + of * g.w.stride + int64_t(col0 + min(s * 16 + x16, cols - 1)) * g.w.ld;
-        const X* x_row[MT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) x_row[i] = static_cast<const X*>(g.x) + int64_t(row0 + min(i * 16 + x16, rows - 1)) * g.ldx;
+        const X* const x_row = static_cast<const X*>(g.x) + int64_t(row0 + min(x16, rows - 1)) * g.ldx;
         const int blocks = (g.k + kBlock - 1) / kBlock, per = (blocks + waves - 1) / waves, begin = wave * per, end = min(begin + per, blocks);
         const ScaleLoad scales(g.w.scale, g.w.type), zeros(g.w.zero, g.w.type);
         uint32_t ones[4];
@@ -217,15 +213,13 @@ __global__ __launch_bounds__((Shape<X, MT, R, PER, ZEROS, EXACT>::kThreads)) voi
                 scale_bits[y] = scales.fetch(at);
                 if constexpr (ZEROS) zero_bits[y] = zeros.fetch(at);
             }
-            E x[kX][MT][4];
-            auto fetch = [&](int u, E (&n)[MT][4]) {
+            E x[kX][4];
+            auto fetch = [&](int u, E (&n)[4]) {
                 const int b = min(b0 + u, end - 1);
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        // which of the block's columns lane q's part of instruction v covers: any order that both operands share
-                        n[i][v].load(x_row[i] + min(b * kBlock + (SMALL ? v * 32 + q * 8 : q * 32 + v * 8), g.k - 8));
+                for (int v = 0; v < 4; ++v)
+                    // which of the block's columns lane q's part of instruction v covers: any order that both operands share
+                    n[v].load(x_row + min(b * kBlock + (SMALL ? v * 32 + q * 8 : q * 32 + v * 8), g.k - 8));
             };
 #pragma unroll
             for (int u = 0; u < kX; ++u) fetch(u, x[u]);
@@ -239,37 +233,26 @@ __global__ __launch_bounds__((Shape<X, MT, R, PER, ZEROS, EXACT>::kThreads)) voi
             for (int u = 0; u < kAhead; ++u) {
                 const int b = b0 + u;
                 if (b >= end) break;
-                E (&now)[MT][4] = x[u % kX];
+                E (&now)[4] = x[u % kX];
                 if (u >= kX) fetch(u, now);
                 uint32_t w[4][4];
                 if ((b + 1) * kBlock > g.k) {
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        if (i > 0 && i * 16 >= rows) break;
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) {
-                            const int at = b * kBlock + (SMALL ? v * 32 + q * 8 : q * 32 + v * 8);
-                            now[i][v].move_down(max(at - (g.k - 8), 0));
-                        }
-                    }
+                    for (int v = 0; v < 4; ++v) now[v].move_down(max(b * kBlock + (SMALL ? v * 32 + q * 8 : q * 32 + v * 8) - (g.k - 8), 0));
                 }
                 // sums of x, once for all of W's rows
                 constexpr bool kOnce = kSums && R > 1;
-                v4f all[kOnce ? MT : 1][kOnce ? kPer : 1];
+                v4f all[kOnce ? kPer : 1];
                 if constexpr (kOnce) {
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        if (i > 0 && i * 16 >= rows) break;
+                    for (int p = 0; p < kPer; ++p) {
+                        all[p] = v4f{0, 0, 0, 0};
 #pragma unroll
-                        for (int p = 0; p < kPer; ++p) {
-                            all[i][p] = v4f{0, 0, 0, 0};
+                        for (int v = p * kEach; v < (p + 1) * kEach; ++v) {
+                            uint32_t part[E::kParts][4];
+                            now[v].parts(part);
 #pragma unroll
-                            for (int v = p * kEach; v < (p + 1) * kEach; ++v) {
-                                uint32_t part[E::kParts][4];
-                                now[i][v].parts(part);
-#pragma unroll
-                                for (int y = E::kParts - 1; y >= 0; --y) all[i][p] = mfma16(ones, part[y], all[i][p], W{});
-                            }
+                            for (int y = E::kParts - 1; y >= 0; --y) all[p] = mfma16(ones, part[y], all[p], W{});
                         }
                     }
                 }
@@ -299,27 +282,23 @@ __global__ __launch_bounds__((Shape<X, MT, R, PER, ZEROS, EXACT>::kThreads)) voi
                         const v4f scale = *reinterpret_cast<const v4f*>(of_group);
                         v4f less = {-136.0f, -136.0f, -136.0f, -136.0f};
                         if constexpr (ZEROS) less = *reinterpret_cast<const v4f*>(of_group + S::kScales);
+                        v4f sum = {0, 0, 0, 0}, here = {0, 0, 0, 0};
+                        if constexpr (kOnce) here = all[p];
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) {
-                            if (i > 0 && i * 16 >= rows) break;
-                            v4f sum = {0, 0, 0, 0}, here = {0, 0, 0, 0};
-                            if constexpr (kOnce) here = all[i][p];
+                        for (int v = p * kEach; v < (p + 1) * kEach; ++v) {
+                            uint32_t part[E::kParts][4];
+                            now[v].parts(part);
 #pragma unroll
-                            for (int v = p * kEach; v < (p + 1) * kEach; ++v) {
-                                uint32_t part[E::kParts][4];
-                                now[i][v].parts(part);
-#pragma unroll
-                                for (int y = E::kParts - 1; y >= 0; --y) {
-                                    sum = mfma16(w[v], part[y], sum, W{});
-                                    if constexpr (kSums && !kOnce) here = mfma16(ones, part[y], here, W{});
-                                }
+                            for (int y = E::kParts - 1; y >= 0; --y) {
+                                sum = mfma16(w[v], part[y], sum, W{});
+                                if constexpr (kSums && !kOnce) here = mfma16(ones, part[y], here, W{});
                             }
+                        }
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                float e = sum[r];
-                                if constexpr (kSums) e = fmaf(less[r], here[r], e);
-                                acc[i][s][r] = fmaf(scale[r], e, acc[i][s][r]);
-                            }
+                        for (int r = 0; r < 4; ++r) {
+                            float e = sum[r];
+                            if constexpr (kSums) e = fmaf(less[r], here[r], e);
+                            acc[s][r] = fmaf(scale[r], e, acc[s][r]);
                         }
                     }
                 }
@@ -329,11 +308,9 @@ __global__ __launch_bounds__((Shape<X, MT, R, PER, ZEROS, EXACT>::kThreads)) voi
     }
     // the wave's sums take the place of its scales
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int s = 0; s < R; ++s) *reinterpret_cast<v4f*>(mine + (i * 16 + x16) * (16 * R) + s * 16 + q * 4) = acc[i][s];
+    for (int s = 0; s < R; ++s) *reinterpret_cast<v4f*>(mine + x16 * (16 * R) + s * 16 + q * 4) = acc[s];
     __syncthreads();
-    for (int x = threadIdx.x; x < MT * 64 * R; x += blockDim.x) {
+    for (int x = threadIdx.x; x < 64 * R; x += blockDim.x) {
         const int r = x / (4 * R), c = (x % (4 * R)) * 4;
         if (r >= rows || c >= cols) continue;
         v4f s = {0, 0, 0, 0};
@@ -371,27 +348,25 @@ __global__ __launch_bounds__(256) void packed_gemm_short_kernel(PackedGemm g) {
     store_results(g, row * g.ldy + col, 1, v4f{sum, 0, 0, 0});
 }
 
-template <typename X, int MT, int R>
-void launch_rows(hipStream_t st, const PackedGemm& g, int waves) {
-    const int strips = (g.n + 16 * R - 1) / (16 * R);
-    const int64_t tiles = packed_tiles(g.m, g.offsets ? g.groups : 0, MT * 16);
-    const dim3 grid(unsigned(tiles * strips)), block(64 * waves);
+}  // namespace
+
+}  // namespace oz
+
+#include "oz_packed_gemm_staged.h"
+
+namespace oz {
+
+namespace {
+
+// f(groups in a block, zero points or not, exact codes or not)
+template <typename X, typename F>
+void with_kind(const PackedGemm& g, F&& f) {
     const std::true_type yes;
     const std::false_type no;
-    auto launch = [&](auto per, auto zeros, auto exact) {
-        constexpr int kPer = decltype(per)::value;
-        constexpr bool kZeros = decltype(zeros)::value, kExact = decltype(exact)::value;
-        const size_t bytes = size_t(waves) * Shape<X, MT, R, kPer, kZeros, kExact>::kWaveBytes;
-        hipLaunchKernelGGL((packed_gemm_kernel<X, MT, R, kPer, kZeros, kExact>), grid, block, bytes, st, g, strips);
-    };
     auto of_group = [&](auto zeros, auto exact) {
-        if constexpr (R < 4 && MT * R < 8) {
-            if (g.w.shift == 5) return launch(std::integral_constant<int, 4>{}, zeros, exact);
-        }
-        if constexpr (MT * R < 8) {
-            if (g.w.shift == 6) return launch(std::integral_constant<int, 2>{}, zeros, exact);
-        }
-        launch(std::integral_constant<int, 1>{}, zeros, exact);
+        if (g.w.shift == 5) f(std::integral_constant<int, 4>{}, zeros, exact);
+        else if (g.w.shift == 6) f(std::integral_constant<int, 2>{}, zeros, exact);
+        else f(std::integral_constant<int, 1>{}, zeros, exact);
     };
     auto of_shift = [&](auto exact) {
         if (g.w.zero) of_group(yes, exact);
@@ -403,29 +378,71 @@ void launch_rows(hipStream_t st, const PackedGemm& g, int waves) {
     of_shift(yes);
 }
 
+template <typename X, int MT, int R>
+void launch_staged(hipStream_t st, const PackedGemm& g, int waves) {
+    const int strips = (g.n + 16 * R - 1) / (16 * R);
+    const dim3 grid(unsigned(packed_tiles(g.m, g.offsets ? g.groups : 0, MT * 16) * strips)), block(64 * waves);
+    with_kind<X>(g, [&](auto per, auto zeros, auto exact) {
+        constexpr int kPer = decltype(per)::value;
+        constexpr bool kZeros = decltype(zeros)::value, kExact = decltype(exact)::value;
+        if constexpr (R < 4 || kPer == 1) {
+            const size_t bytes = size_t(waves) * Staged<X, MT, R, kPer, kZeros>::kWaveBytes;
+            hipLaunchKernelGGL((packed_gemm_staged_kernel<X, MT, R, kPer, kZeros, kExact>), grid, block, bytes, st, g, strips);
+        }
+    });
+}
+
+template <typename X, int R>
+void launch_few(hipStream_t st, const PackedGemm& g, int waves) {
+    const int strips = (g.n + 16 * R - 1) / (16 * R);
+    const dim3 grid(unsigned(packed_tiles(g.m, g.offsets ? g.groups : 0, 16) * strips)), block(64 * waves);
+    with_kind<X>(g, [&](auto per, auto zeros, auto exact) {
+        constexpr int kPer = decltype(per)::value;
+        constexpr bool kZeros = decltype(zeros)::value, kExact = decltype(exact)::value;
+        if constexpr (R < 4 || kPer < 4) {
+            const size_t bytes = size_t(waves) * Shape<X, R, kPer, kZeros, kExact>::kWaveBytes;
+            hipLaunchKernelGGL((packed_gemm_kernel<X, R, kPer, kZeros, kExact>), grid, block, bytes, st, g, strips);
+        }
+    });
+}
+
+// The kernels with more than 64 KB of LDS to a workgroup.
+template <typename X, int MT, int R, int PER, bool ZEROS, bool EXACT>
+bool allow_lds() {
+    constexpr int bytes = 8 * Staged<X, MT, R, PER, ZEROS>::kWaveBytes;
+    static_assert(bytes <= 160 * 1024, "LDS");
+    return bytes <= 64 * 1024 || hipFuncSetAttribute(reinterpret_cast<const void*>(packed_gemm_staged_kernel<X, MT, R, PER, ZEROS, EXACT>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+}
+template <typename X, int MT, int R, bool EXACT>
+bool allow_kinds() {
+    if constexpr (R == 4) return allow_lds<X, MT, R, 1, false, EXACT>() && allow_lds<X, MT, R, 1, true, EXACT>();
+    else return allow_lds<X, MT, R, 1, false, EXACT>() && allow_lds<X, MT, R, 2, false, EXACT>() && allow_lds<X, MT, R, 4, false, EXACT>() &&
+                allow_lds<X, MT, R, 1, true, EXACT>() && allow_lds<X, MT, R, 2, true, EXACT>() && allow_lds<X, MT, R, 4, true, EXACT>();
+}
+template <typename X, bool EXACT>
+bool allow_staged() {
+    return (sizeof(X) == 4 || allow_kinds<X, 1, 1, EXACT>()) && allow_kinds<X, 1, 2, EXACT>() && allow_kinds<X, 2, 2, EXACT>() && allow_kinds<X, 2, 4, EXACT>();
+}
+
 template <typename X>
 void launch_typed(hipStream_t st, const PackedGemm& g, int num_cu) {
     if (g.k < 8) {
         hipLaunchKernelGGL(packed_gemm_short_kernel<X>, dim3(unsigned((int64_t(g.m) * g.n + 255) / 256)), dim3(256), 0, st, g);
         return;
     }
-    const PackedPlan plan = packed_plan(g.m, g.n, g.k, g.offsets ? g.groups : 0, sizeof(X), g.w.shift, num_cu);
-    const int mt = plan.rows, r = plan.strips, waves = plan.waves;
-    if (mt == 1) {
-        if (r == 4) launch_rows<X, 1, 4>(st, g, waves);
-        else if (r == 2) launch_rows<X, 1, 2>(st, g, waves);
-        else launch_rows<X, 1, 1>(st, g, waves);
-    } else if (mt == 2) {
+    const PackedPlan p = packed_plan(g.m, g.n, g.k, g.offsets ? g.groups : 0, sizeof(X), g.w.shift, num_cu);
+    if (p.staged) {
+        if (p.strips == 4) return launch_staged<X, 2, 4>(st, g, p.waves);
+        if (p.rows == 2) return launch_staged<X, 2, 2>(st, g, p.waves);
         if constexpr (sizeof(X) == 2) {
-            if (r == 2) return launch_rows<X, 2, 2>(st, g, waves);
+            if (p.strips == 1) return launch_staged<X, 1, 1>(st, g, p.waves);
         }
-        launch_rows<X, 2, 1>(st, g, waves);
-    } else {
-        if constexpr (sizeof(X) == 2) {
-            if (r == 2) return launch_rows<X, 4, 2>(st, g, waves);
-        }
-        launch_rows<X, 4, 1>(st, g, waves);
+        return launch_staged<X, 1, 2>(st, g, p.waves);
     }
+    if (p.strips == 4) launch_few<X, 4>(st, g, p.waves);
+    else if (p.strips == 2) launch_few<X, 2>(st, g, p.waves);
+    else launch_few<X, 1>(st, g, p.waves);
 }
 
 }  // namespace

@@ -19,25 +19,27 @@ def plan(tmp_path_factory):
 
 
 def test_packed_products(plan):
-    for (rows, strips), sizes in lr.PACKED.items():
+    for route, sizes in lr.PACKED.items():
         for counts, behind, n, k, group, kinds in sizes:
             for size in kinds:
                 got = plan("packed", sum(counts) + behind, n, k, len(counts), size, int(math.log2(group)))
-                assert got[:2] == (rows, strips) and got[2] <= 16, (rows, strips, n, k, group, size, got)
+                assert got[:3] == route, (route, counts, behind, n, k, group, size, got)
 
 
 def test_packed_plans_hold_everywhere(plan):
-    # what the kernels are built for: 1, 2 or 4 strips only as far as registers reach, a power of two of waves, no more than k has blocks for
+    # what the kernels are built for: strips only as far as registers reach, a power of two of waves, no more than k has blocks for
     for m in (1, 16, 17, 64, 1000, 100000):
         for n in (1, 1000, 70000):
             for k in (8, 200, 5000):
                 for groups in (0, 1, 60):
                     for size in (2, 4):
                         for shift in (5, 6, 7):
-                            rows, strips, waves = plan("packed", m, n, k, groups, size, shift)
-                            assert rows in (1, 2, 4) and strips in (1, 2, 4) and waves in (1, 2, 4, 8, 16) and waves < 2 * max(1, -(-k // 128))
-                            assert strips <= (4 if rows == 1 and shift > 5 else 2 if rows == 1 or (size == 2 and (rows == 2 or shift == 7)) else 1)
-                            assert waves <= (16 if rows == 1 and strips * size <= 4 or rows == strips == 1 else 8)
+                            staged, rows, strips, waves = plan("packed", m, n, k, groups, size, shift)
+                            assert waves in (1, 2, 4, 8, 16) and waves < 2 * max(1, -(-k // 128))
+                            if staged:
+                                assert (rows, strips) in ((1, 2), (2, 2), (2, 4) if shift == 7 else (2, 2), (1, 1) if size == 2 else (1, 2)) and waves <= 8
+                            else:
+                                assert rows == 1 and strips in (1, 2, 4 if shift > 5 else 2) and waves <= (16 if strips == 1 or strips * size <= 4 else 8)
 
 
 def test_tiles_of_orthogonal_updates(plan):
