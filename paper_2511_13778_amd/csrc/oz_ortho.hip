@@ -79,21 +79,32 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(Ortho o) {
     const int b = blockIdx.z, i0 = int(blockIdx.y) * 64, j0 = int(blockIdx.x) * 64;
     const T* g = static_cast<const T*>(o.g) + b * o.stride_g;
     const int x = threadIdx.x & 63, y0 = threadIdx.x >> 6;
-    // the parts in one order, by every wave for itself
-    double sum = 0.0;
+    // all of a lane's elements are on their way before the first is used
+    T raw[16];
 #pragma unroll
-    for (int p = 0; p < kNormParts / 64; ++p) sum += o.norm[b * kNormParts + p * 64 + (threadIdx.x & 63)];
+    for (int i = 0; i < 16; ++i) {
+        const int y = y0 + 4 * i, r = min(o.tall ? j0 + y : i0 + y, o.rows - 1), c = min(o.tall ? i0 + x : j0 + x, o.cols - 1);
+        raw[i] = g[r * o.ldg + c];
+    }
+    // the parts in one order, by every wave for itself
+    double part[kNormParts / 64], sum = 0.0;
+#pragma unroll
+    for (int p = 0; p < kNormParts / 64; ++p) part[p] = o.norm[b * kNormParts + p * 64 + (threadIdx.x & 63)];
+#pragma unroll
+    for (int p = 0; p < kNormParts / 64; ++p) sum += part[p];
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     const double inverse = 1.0 / (sqrt(sum) + double(o.eps));
-    for (int y = y0; y < 64; y += 4) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
         // (y, x) along G's own rows
-        const int r = o.tall ? j0 + y : i0 + y, c = o.tall ? i0 + x : j0 + x;
-        const float v = r < o.rows && c < o.cols ? float(double(to_float(g[r * o.ldg + c])) * inverse) : 0.0f;
+        const int y = y0 + 4 * i, r = o.tall ? j0 + y : i0 + y, c = o.tall ? i0 + x : j0 + x;
+        const float v = r < o.rows && c < o.cols ? float(double(to_float(raw[i])) * inverse) : 0.0f;
         if (o.tall) tile[x][y] = v;
         else tile[y][x] = v;
     }
     __syncthreads();
     const int64_t size = int64_t(o.ldm) * o.ldn;
+#pragma unroll
     for (int y = y0; y < 64; y += 4) {
         const float v = tile[y][x] * kScaleX, w = tile[x][y] * kScaleX;
         const int64_t at = int64_t(i0 + y) * o.ldn + j0 + x, turned = int64_t(j0 + y) * o.ldm + i0 + x;
