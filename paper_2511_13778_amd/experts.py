@@ -225,6 +225,7 @@ class ExpertLayer:
         if w1.dim() != 3 or w2.shape != (w1.shape[0], w1.shape[2], w1.shape[1]):
             raise ValueError("w1 experts x inner x width and w2 experts x width x inner, not %s and %s" % (tuple(w1.shape), tuple(w2.shape)))
         self.h, self.w1, self.w2, self.scale_dtype, self.experts = h, w1, w2, scale_dtype, w1.shape[0]
+        self.p1 = self.p2 = None
         self.prepare_weights()
 
     def prepare_weights(self):
@@ -241,12 +242,14 @@ class ExpertLayer:
         return combine(h, out, routing, weights)
 
     def pack_weights(self, group=64, scale_dtype=torch.float16):
-        """The 4-bit copies that serve_packed reads: a quarter of bfloat16's bytes, for a value that is off by at most a fourteenth of its group's
-        largest."""
+        """The 4-bit copies that serve_packed reads, made anew when the weights have changed: a quarter of bfloat16's bytes, for a value that is off by at
+        most a fourteenth of its group's largest."""
         self.p1, self.p2 = (packed.quantize(self.h, w.detach(), group=group, scale_dtype=scale_dtype) for w in (self.w1, self.w2))
 
     def serve_packed(self, x, ids, weights):
         """serve on the 4-bit copies, activations as they are: for few tokens in flight, where the time is the weights'."""
+        if self.p1 is None:
+            raise ValueError("pack_weights() first")
         h = self.h
         routing = sort_tokens(h, ids, self.experts)
         inner = torch.nn.functional.silu(packed.gemm_grouped(h, gather(h, x, routing), self.p1, routing.offsets))

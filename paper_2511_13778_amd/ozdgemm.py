@@ -211,6 +211,8 @@ class Handle:
         if self._h:
             self.lib.oz_destroy(self._h)
             self._h = C.c_void_p()
+            # they hold the handle that is gone; the calls themselves refuse an empty one
+            self.choose_experts_workspace_bytes = self.orthogonalize_workspace_bytes = lambda *sizes: 0
 
     def __del__(self):
         try:

@@ -262,3 +262,14 @@ def test_the_types_largest_and_zeros_of_both_signs(h, dtype, experts):
         exact, size = ref.choose_grad(ids, w, p, f, counted, dw.double(), 0.5, normalize)
         d = ex.choose_backward(h, x.cuda(), c, dw.cuda(), 0.5)
         close(d, exact, 64 * F * size + ref.rounded(exact, dtype) + 16 * LEAST, "dscores")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_no_tokens_and_nothing_live(h, dtype):
+    from paper_2511_13778_amd import experts as ex
+    for tokens, live in ((0, None), (5, torch.zeros(5, dtype=torch.bool, device="cuda"))):
+        x = torch.full((tokens, 200), float("nan"), device="cuda", dtype=dtype)
+        c = ex.choose(h, x, 8, live=live)
+        assert (c.ids == -1).all() and not c.weights.any() and not c.counts.any() and c.counted.item() == 0 and not c.shares.any() and c.loss.item() == 0
+        d = ex.choose_backward(h, x, c, torch.ones((tokens, 8), device="cuda"), 1.0)
+        assert d.shape == x.shape and not d.any()

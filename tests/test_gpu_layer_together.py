@@ -76,6 +76,8 @@ def test_layer_serves_packed_and_moves(h):
     n, width, inner, topk = 5, 130, 260, 2
     w1, w2 = (torch.randn(s, generator=r, device="cuda") * s[-1] ** -0.5 for s in ((n, inner, width), (n, width, inner)))
     layer = ex.ExpertLayer(h, w1, w2)
+    with pytest.raises(ValueError, match="pack_weights"):
+        layer.serve_packed(torch.zeros((1, width), device="cuda"), torch.zeros((1, 1), dtype=torch.int32, device="cuda"), None)
     layer.pack_weights(group=32)
     for tokens in (1, 40):
         x = torch.randn((tokens, width), generator=r, device="cuda").bfloat16()
@@ -219,3 +221,19 @@ def test_refusals_with_a_status(h):
     with pytest.raises(OzError):
         orthogonal.orthogonalize(h, torch.zeros((1, 32769), device="cuda"))
     assert torch.equal(orthogonal.orthogonalize(h, x), x)
+
+
+def test_a_closed_handle_is_refused():
+    from paper_2511_13778_amd import experts as ex, orthogonal, packed
+    from paper_2511_13778_amd import ozdgemm as g
+    other = g.Handle(0)
+    x = torch.randn((8, 64), device="cuda")
+    w = packed.quantize(other, x)
+    ex.choose(other, x, 2)
+    orthogonal.orthogonalize(other, x)
+    torch.cuda.synchronize()
+    other.close()
+    for call in (lambda: ex.choose(other, x, 2), lambda: ex.choose(other, x[:4], 2), lambda: orthogonal.orthogonalize(other, x), lambda: orthogonal.orthogonalize(other, x[:4]),
+                 lambda: packed.quantize(other, x), lambda: packed.gemm(other, x, w)):
+        with pytest.raises(g.OzError):
+            call()
