@@ -421,7 +421,7 @@ oz_status_t oz_pack4(oz_handle_t handle, void* stream, int64_t rows, int64_t col
 oz_status_t oz_unpack4(oz_handle_t handle, void* stream, int64_t rows, int64_t cols, void* X, int64_t ldx, int32_t x_type, int64_t batch,
                        int64_t stride_x, const oz_packed_t* W);
 
-/* Y = X W^T, X m x k in OZ_F32, OZ_BF16 or OZ_F16, W n x k in 4 bits, Y m x n.  Made for few rows (a token, a few in flight): W is read once for every 64
+/* Y = X W^T, X m x k in OZ_F32, OZ_BF16 or OZ_F16, W n x k in 4 bits, Y m x n.  Made for few rows (a token, a few in flight): W is read once for every 16 or 32
  * rows of X.  offsets NULL, groups 0: one matrix.  Otherwise rows offsets[g] .. of Y = the same rows of X times W_g^T, and rows of Y behind the last
  * group are set to zero.  Sums are held in 32 bits, each group's of code - 8 before it is scaled (X and Y in OZ_BF16: of 128 + code, less 136 times the
  * sum of x, some 10^-5 of the largest terms, which the rounding of Y hides); the one rounding to fewer bits is the result's.

@@ -11,6 +11,10 @@
 //
 // O, offdiag(P) and X are kept with their rows padded by zeros to whole tiles, so no product has edges.  A and A^2 are symmetric: their tiles below the
 // diagonal are computed and written to both sides.
+//
+// What bounds it is the matrix units for large matrices (4096 x 4096 bfloat16, five steps: 1250 us, 1070 at the rate of the library's product of that size), memory at
+// the ends of the tiles for middling ones (16 of 1024 x 2048: 1040 us, of which P X takes 580 where its products alone would be 270: ten bytes for each element of
+// X), and the number of launches for small ones (4 of 200 x 300 float32: 108 us in 17).
 #include <algorithm>
 
 #include "oz_layer.h"

@@ -131,7 +131,7 @@ def _product(h, x, w, groups, offsets, dtype, out):
 
 
 def gemm(h: g.Handle, x, w: Packed, dtype=None, out=None):
-    """x W^T in `dtype` (or out's, or x's), summed in 32 bits.  Made for few rows of x: W is read once for every 64."""
+    """x W^T in `dtype` (or out's, or x's), summed in 32 bits.  Made for few rows of x: W is read once for every 16 or 32."""
     return _product(h, x, w, 0, None, dtype, out)
 
 
