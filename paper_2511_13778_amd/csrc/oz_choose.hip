@@ -501,7 +501,7 @@ __global__ __launch_bounds__(kThreads, 4) void choose_grad_kernel(ChooseGradCall
     auto chosen = [&](int64_t t, int j) {
         Chosen x{-1, 0.0f, 0.0f};
         if (of_weights) {
-            const int64_t at = min(t, c.tokens - 1) * c.topk + min(j, c.topk - 1);
+            const int64_t at = min(t, int64_t(c.tokens) - 1) * c.topk + min(j, c.topk - 1);
             x = Chosen{c.ids[at], c.weights[at], c.dweights[at]};
         }
         return x;
