@@ -5,7 +5,7 @@
 //   ds_i = w_i (dw_i - sum_j w_j dw_j) for the chosen (or p_i (dw_i - sum_j w_j dw_j), dw = 0 for the others) + dloss experts / tokens * p_i (f_i - sum_e f_e p_e)
 //
 // A token is a group of 16 lanes (64 beyond 256 experts), each with consecutive experts in registers: four tokens to a wave, so that maxima and sums over
-// the experts are four rotations of 16 lanes.  65000 tokens of 256 bfloat16 scores, 8 chosen: 23 us forward, 7 for the batch's sums, 24 for the gradient, where a
+// the experts are four rotations of 16 lanes.  65000 tokens of 256 bfloat16 scores, 8 chosen: 23 us forward, 7 for the batch's sums, 19 for the gradient, where a
 // copy of as many bytes takes 16 in all; 16384 tokens of 64 float32 scores: 6, 7 and 5; 24 tokens: a launch.
 #include <algorithm>
 #include <type_traits>
@@ -477,7 +477,8 @@ __global__ __launch_bounds__(kSumThreads) void balance_kernel(Partials q, int ex
 
 // The scores' gradient: p once more from the scores, and what the chosen experts get put into a row of LDS that is read as the scores are and cleared by
 // those who wrote.  What bounds it is half the vector instructions, four hundred for four tokens of 256 scores, and half memory; loads with a branch around
-// them, which made each wait for the one before, and instructions of cases that are not asked for took 28 us instead of 24.
+// them, which made each wait for the one before, and instructions of cases that are not asked for took 28 us instead of 24; counts loaded by each lane 24
+// instead of 19.
 enum Parts { kAny, kNormalized, kPlain };
 template <typename T, int L, int V, Parts P>
 __global__ __launch_bounds__(kThreads, 4) void choose_grad_kernel(ChooseGradCall c) {
@@ -516,14 +517,16 @@ __global__ __launch_bounds__(kThreads, 4) void choose_grad_kernel(ChooseGradCall
 #pragma unroll
     for (int v = 0; v < V; ++v) f[v] = 0.0f;
     if (of_loss) {
-        int n = 0, of[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) of[v] = c.counts[min(first + v, c.experts - 1)];
+        // through LDS: a lane's own are V apart from the next lane's, so that loads of them would share no line
+        __shared__ __align__(16) int32_t of_all[L * V];
+        for (int e = threadIdx.x; e < L * V; e += kThreads) of_all[e] = e < c.experts ? c.counts[e] : 0;
         const int tokens = *c.counted;
         const float dloss = c.dloss ? *c.dloss : 1.0f;
+        __syncthreads();
+        int n = 0, of[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            of[v] = first + v < c.experts ? of[v] : 0;
+            of[v] = of_all[first + v];
             n += of[v];
         }
         n = group_count<L>(n);
