@@ -464,14 +464,16 @@ __global__ __launch_bounds__(kSumThreads) void balance_kernel(Partials q, int ex
         last = __hip_atomic_fetch_add(q.arrived, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == int(gridDim.x) - 1;
     }
     __syncthreads();
-    if (last && threadIdx.x == 0) {
-        double l = 0.0;
-        int64_t all = 0;
-        for (int i = 0; i < int(gridDim.x); ++i) {
-            l += __hip_atomic_load(&q.loss[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            all += __hip_atomic_load(&q.choices[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (last && threadIdx.x < 64) {
+        // at most 64 workgroups
+        const bool there = threadIdx.x < gridDim.x;
+        double l = there ? __hip_atomic_load(&q.loss[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+        int64_t all = there ? __hip_atomic_load(&q.choices[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+        for (int d = 1; d < 64; d *= 2) {
+            l += __shfl_xor(l, d);
+            all += __shfl_xor(all, d);
         }
-        *loss = all > 0 ? float(l * double(experts) / double(all)) : 0.0f;
+        if (threadIdx.x == 0) *loss = all > 0 ? float(l * double(experts) / double(all)) : 0.0f;
     }
 }
 
