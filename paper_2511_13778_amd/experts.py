@@ -119,11 +119,12 @@ class Choice:
     expert was chosen, int32), counted (one int32: tokens that have an expert), shares (their mean probability of each expert, float32) and
     loss (float32, one value).  counts may be added up over several GPUs before choose_backward, in place or set to others."""
 
-    __slots__ = ("ids", "weights", "live", "normalize", "_parts", "_table")
+    # _made: ids and weights as choose made them, which need no second look
+    __slots__ = ("ids", "weights", "live", "normalize", "_parts", "_table", "_made", "_set")
 
     def __init__(self, ids, weights, counts=None, counted=None, shares=None, loss=None, live=None, normalize=True):
         self.ids, self.weights, self.live, self.normalize = ids, weights, live, normalize
-        self._parts, self._table = [counts, counted, shares, loss], None
+        self._parts, self._table, self._made, self._set = [counts, counted, shares, loss], None, None, False
 
     # choose leaves the four results of the whole batch in one table of float32, (2 experts + 2 values): cut out when they are asked for
     def _part(at, cut):
@@ -134,7 +135,7 @@ class Choice:
             return have
 
         def put(self, value):
-            self._parts[at] = value
+            self._parts[at], self._set = value, True
         return property(get, put)
 
     counts = _part(0, lambda table, n: table.narrow(0, 0, n).view(torch.int32))
@@ -162,6 +163,7 @@ def choose(h: g.Handle, scores, topk: int, live=None, normalize=True, balance=Tr
     if not 1 <= topk <= min(experts, 64):
         raise ValueError("topk 1 .. 64 of %d experts, not %s" % (experts, topk))
     c = Choice(scores.new_empty((tokens, topk), dtype=torch.int32), scores.new_empty((tokens, topk), dtype=torch.float32), live=live, normalize=bool(normalize))
+    c._made = c.ids, c.weights
     more = (None, None, None, None, None, 0)
     if balance:
         # one allocation: the four results of the batch and, behind them, the workspace
@@ -180,21 +182,33 @@ def choose_backward(h: g.Handle, scores, choice: Choice, dweights=None, dloss=No
     """The gradient of choose's scores, for dweights (tokens x topk, float32) and dloss (a number, or one float32 on the GPU); either may be None."""
     ld = check_matrix(scores, "scores")
     ids, weights, live = choice.ids, choice.weights, choice.live
-    check_device(h, scores, ids, weights, live, dweights)
+    check_device(h, scores, ids, live, dweights)
     tokens, experts = scores.shape
-    if ids.dim() != 2 or ids.shape[0] != tokens or weights.shape != ids.shape or weights.dtype != torch.float32 or not weights.is_contiguous():
+    made = choice._made
+    if made is None or made[0] is not ids or made[1] is not weights:
+        check_device(h, weights)
+        check_ints(ids, "ids")
+        if ids.dim() != 2 or weights.shape != ids.shape or weights.dtype != torch.float32 or not weights.is_contiguous():
+            raise ValueError("ids and weights: int32 and float32 of the same tokens x topk, not %s and %s" % (tuple(ids.shape), tuple(weights.shape)))
+    if ids.shape[0] != tokens:
         raise ValueError("scores %s do not belong to this choice of %s" % (tuple(scores.shape), tuple(ids.shape)))
-    check_ints(ids, "ids")
     if dweights is not None and (dweights.dtype != torch.float32 or dweights.shape != ids.shape or not dweights.is_contiguous()):
         raise ValueError("dweights: contiguous float32 of %s" % (tuple(ids.shape),))
     counts = counted = scalar = None
     factor = 1.0
     if dloss is not None:
-        counts, counted = choice.counts, choice.counted
-        if counts is None or counted is None:
-            raise ValueError("a gradient of the loss needs the choice's counts: choose(balance=True)")
-        check_device(h, counts, counted)
-        counts, counted = check_ints(counts, "counts", experts).data_ptr(), check_ints(counted, "counted", 1).data_ptr()
+        if choice._table is not None and not choice._set:
+            table, of = choice._table
+            if of != experts or table.device != scores.device:
+                raise ValueError("scores of %d experts do not belong to this choice of %d" % (experts, of))
+            counts = table.data_ptr()
+            counted = counts + 4 * experts
+        else:
+            counts, counted = choice.counts, choice.counted
+            if counts is None or counted is None:
+                raise ValueError("a gradient of the loss needs the choice's counts: choose(balance=True)")
+            check_device(h, counts, counted)
+            counts, counted = check_ints(counts, "counts", experts).data_ptr(), check_ints(counted, "counted", 1).data_ptr()
         if torch.is_tensor(dloss):
             check_device(h, dloss)
             if not dloss.is_cuda or dloss.dtype != torch.float32 or dloss.numel() != 1:
