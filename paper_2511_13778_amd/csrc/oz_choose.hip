@@ -5,8 +5,8 @@
 //   ds_i = w_i (dw_i - sum_j w_j dw_j) for the chosen (or p_i (dw_i - sum_j w_j dw_j), dw = 0 for the others) + dloss experts / tokens * p_i (f_i - sum_e f_e p_e)
 //
 // A token is a group of 16 lanes (64 beyond 256 experts), each with consecutive experts in registers: four tokens to a wave, so that maxima and sums over
-// the experts are four rotations of 16 lanes.  65000 tokens of 256 bfloat16 scores, 8 chosen: 23 us forward, 7 for the batch's sums, 19 for the gradient, where a
-// copy of as many bytes takes 16 in all; 16384 tokens of 64 float32 scores: 6, 7 and 5; 24 tokens: a launch.
+// the experts are four rotations of 16 lanes.  65000 tokens of 256 bfloat16 scores, 8 chosen: 23 us forward, 6 for the batch's sums, 19 for the gradient, where a
+// copy of as many bytes takes 16 in all; 16384 tokens of 64 float32 scores: 6, 6 and 5; 24 tokens: a launch.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(ChooseCall c, Partials
     }
 }
 
-// The workgroups' partial sums, added in their order: 16 experts to a workgroup; the one that is through last has the loss.  What bounds its 7 us is latency: a read
+// The workgroups' partial sums, added in their order: 16 experts to a workgroup; the one that is through last has the loss.  What bounds its 6 us is latency: a read
 // of the partial sums, one more of the parts of the loss.
 __global__ __launch_bounds__(kSumThreads) void balance_kernel(Partials q, int experts, int32_t* counts, int32_t* of_tokens, float* shares, float* loss) {
     constexpr int kRows = kSumThreads / kPiece, kWaves = kSumThreads / 64;
