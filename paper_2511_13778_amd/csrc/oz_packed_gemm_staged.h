@@ -124,6 +124,8 @@ __global__ __launch_bounds__(512) void packed_gemm_staged_kernel(PackedGemm g, i
 #pragma unroll
         for (int i = 0; i < 4; ++i) ones[i] = uint32_t(__builtin_bit_cast(uint16_t, static_cast<W>(1.0f))) * 0x10001u;
         for (int b = begin; b < end; ++b) {
+            // lanes read what others of their wave wrote: LDS is in order, and what the compiler moves is held here and at each stage
+            __builtin_amdgcn_wave_barrier();
             const int in = (b - begin) % S::kAhead;
             if (in == 0) {
                 // the next blocks' scales, [block, group][row]
@@ -150,6 +152,7 @@ __global__ __launch_bounds__(512) void packed_gemm_staged_kernel(PackedGemm g, i
             v4f sum[MT][R], here[MT];
             auto of_stage = [&](auto V) {
                 constexpr int v = decltype(V)::value;
+                __builtin_amdgcn_wave_barrier();
                 E x[MT];
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
