@@ -53,6 +53,13 @@ template <int L>
 __device__ __forceinline__ uint32_t group_max(uint32_t x) {
     return fold<L>(x, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
+// whether it holds for any of the group's lanes
+template <int L>
+__device__ __forceinline__ bool in_group(bool x) {
+    uint64_t has = __ballot(x) >> (int(threadIdx.x & 63) / L * L);
+    if (L < 64) has &= (uint64_t(1) << (L & 63)) - 1;
+    return has != 0;
+}
 
 // Scores as whole numbers that rise with them, the expert in the low bits (lower ones above higher ones), so that no two are equal.  16-bit scores
 // leave room for the expert in the same word; float32 takes two.  -0 counts as +0, a NaN is above all; what is not above `kNone` is an expert that
@@ -550,15 +557,25 @@ __global__ __launch_bounds__(kThreads, 4) void choose_grad_kernel(ChooseGradCall
 #pragma unroll
         for (int v = 0; v < V; ++v) m = fmaxf(m, to_float(now.e[v]));
         m = group_largest<L>(m);
-        const bool any = on && m != -INFINITY;
-        if (of_loss || !normalize) {
-            // a NaN is not seen by the maximum, but in the sum
+        // The maximum sees no NaN.  A token of NaN and -infinity alone has an expert all the same, so scores are looked at again where it found none
+        bool any = m != -INFINITY, odd = false;
+        const bool softmax = of_loss || !normalize;
+        if (!softmax || __any(!any)) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) odd = odd || to_float(now.e[v]) != to_float(now.e[v]);
+            odd = in_group<L>(odd);
+            any = any || odd;
+        }
+        any = any && on;
+        if (softmax) {
+            // a NaN, which the maximum does not see, is in the sum
             const float sum = exponentials<L>(now.e, m, p), inverse = 1.0f / sum;
 #pragma unroll
             for (int v = 0; v < V; ++v) p[v] *= inverse;
         } else {
+            // not needed, but for what NaN and +infinity make of all of them
 #pragma unroll
-            for (int v = 0; v < V; ++v) p[v] = 0.0f;
+            for (int v = 0; v < V; ++v) p[v] = odd || m == INFINITY ? NAN : 0.0f;
         }
         float s[V];
 #pragma unroll

@@ -273,3 +273,37 @@ def test_no_tokens_and_nothing_live(h, dtype):
         assert (c.ids == -1).all() and not c.weights.any() and not c.counts.any() and c.counted.item() == 0 and not c.shares.any() and c.loss.item() == 0
         d = ex.choose_backward(h, x, c, torch.ones((tokens, 8), device="cuda"), 1.0)
         assert d.shape == x.shape and not d.any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("experts,topk", [(1, 1), (20, 3), (200, 8), (300, 20)])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_not_a_number_in_all_of_a_row(h, dtype, experts, topk, normalize):
+    # NaN in every score, NaN beside -infinity alone, one NaN and one +infinity among numbers: probabilities that are NaN, so all of the token's gradient is
+    from paper_2511_13778_amd import experts as ex
+    nan, inf = float("nan"), float("inf")
+    x = scores_of(13, 9, experts, dtype)
+    x[1] = nan
+    x[2] = -inf
+    x[2, experts // 2] = nan
+    x[3] = -nan
+    x[4, experts - 1] = nan
+    x[5, experts // 3] = inf
+    x[6] = -inf                                # nobody to be had: padding, not NaN
+    x[7, :experts // 2] = -inf
+    bad = torch.tensor([False, True, True, True, True, True, False, False, False])
+    c = ex.choose(h, x.cuda(), topk, normalize=normalize)
+    ids, w = ref.choose(x, topk, None, normalize)[:2]
+    assert torch.equal(c.ids.cpu().long(), ids)
+    assert torch.equal(c.weights.isnan().any(1).cpu(), bad) and c.loss.isnan() and c.shares.isnan().all() and c.counted.item() == 8
+    dw = torch.randn((9, topk), generator=torch.Generator().manual_seed(1)).cuda()
+    for weights, dloss in ((dw, 0.5), (dw, None), (None, 0.5)):
+        d = ex.choose_backward(h, x.cuda(), c, weights, dloss).cpu()
+        assert d[bad].isnan().all(), (weights is None, dloss, d.isnan().sum(1).tolist())
+        assert d[~bad].isfinite().all() and not d[6].any() and not d[7, :experts // 2].any()
+    # a token that is not live may have any scores
+    live = torch.ones(9, dtype=torch.bool)
+    live[bad] = False
+    c = ex.choose(h, x.cuda(), topk, live=live.cuda(), normalize=normalize)
+    for weights, dloss in ((dw, 0.5), (dw, None), (None, 0.5)):
+        assert not ex.choose_backward(h, x.cuda(), c, weights, dloss).cpu()[bad].any()
