@@ -424,7 +424,9 @@ oz_status_t oz_unpack4(oz_handle_t handle, void* stream, int64_t rows, int64_t c
 /* Y = X W^T, X m x k in OZ_F32, OZ_BF16 or OZ_F16, W n x k in 4 bits, Y m x n.  Made for few rows (a token, a few in flight): W is read once for every 16 or 32
  * rows of X.  offsets NULL, groups 0: one matrix.  Otherwise rows offsets[g] .. of Y = the same rows of X times W_g^T, and rows of Y behind the last
  * group are set to zero.  Sums are held in 32 bits, each group's of code - 8 before it is scaled (X and Y in OZ_BF16: of 128 + code, less 136 times the
- * sum of x, some 10^-5 of the largest terms, which the rounding of Y hides); the one rounding to fewer bits is the result's.
+ * sum of x, some 10^-5 of the largest terms, which the rounding of Y hides); the one rounding to fewer bits is the result's.  A result that is not finite
+ * this way is computed once more as the sum of x * (scale * (code - zero)) in 64 bits: an infinity in X keeps its product's sign, NaN comes of a NaN, of
+ * infinities of both signs or of one times a value of zero alone, and no sum leaves the range on the way.
  * k == 0: Y = 0.  Limits: (ceil(m / 16) + groups + 1) * ceil(n / 16) < 2^22. */
 oz_status_t oz_packed_gemm(oz_handle_t handle, void* stream, int64_t groups, const int32_t* offsets, int64_t m, int64_t n, int64_t k, const void* X,
                            int64_t ldx, int32_t x_type, const oz_packed_t* W, void* Y, int64_t ldy, int32_t y_type);

@@ -230,10 +230,11 @@ __global__ __launch_bounds__(512) void packed_gemm_staged_kernel(PackedGemm g, i
     __syncthreads();
     for (int x = threadIdx.x; x < MT * 64 * R; x += blockDim.x) {
         const int r = x / (4 * R), c = (x % (4 * R)) * 4;
-        if (r >= rows || c >= cols) continue;
+        const bool in = r < rows && c < cols;
         v4f s = {0, 0, 0, 0};
         for (int w = 0; w < waves; ++w) s += *reinterpret_cast<const v4f*>(lds + w * (S::kWaveBytes / 4) + r * (16 * R) + c);
-        store_results(g, int64_t(row0 + r) * g.ldy + col0 + c, cols - c, s);
+        mend_results<X>(g, of, in, row0 + r, col0 + c, s);
+        if (in) store_results(g, int64_t(row0 + r) * g.ldy + col0 + c, cols - c, s);
     }
 }
 

@@ -7,7 +7,7 @@ torch = pytest.importorskip("torch")
 import layer_reference as ref  # noqa: E402
 import layer_routes as lr  # noqa: E402
 from test_gpu_orthogonal import EPS, QUINTIC, check_five, gradient, parts_of  # noqa: E402
-from test_gpu_packed import check_product, weights  # noqa: E402
+from test_gpu_packed import check_product, check_special, special, weights  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -65,3 +65,36 @@ def test_tiles_of_orthogonal_updates(h, dtype, at):
     assert torch.equal(five, orthogonal.orthogonalize(h, x))
     for i in (0, batch - 1):
         check_five(five[i], x[i])
+
+
+def product_of(h, x, w, counts):
+    from paper_2511_13778_amd import packed
+    if not counts:
+        return packed.gemm(h, x, w), torch.zeros(x.shape[0], dtype=torch.int64)
+    offsets = torch.tensor([0] + counts).cumsum(0).to(torch.int32).cuda()
+    return packed.gemm_grouped(h, x, w, offsets), torch.repeat_interleave(torch.arange(len(counts)), torch.tensor(counts))
+
+
+@pytest.mark.parametrize("at", sorted(lr.PACKED), ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_infinities_in_packed_products(h, at, dtype):
+    for counts, behind, n, k, group, kinds in lr.PACKED[at]:
+        if dtype.itemsize not in kinds:
+            continue
+        r = torch.Generator(device="cuda").manual_seed(n + k + group)
+        zeros = group != 64
+        w = weights(r, n, k, group, zeros, torch.float32, (len(counts),) if counts else ())
+        if zeros:
+            w.zero.copy_(w.zero.round())
+        m = sum(counts) + behind
+        x = torch.randn((m, k), generator=r, device="cuda").to(dtype)
+        x[::3, k - 1] = float("inf")
+        x[1::7, k // 2] = -float("inf")
+        x[5::11, 0] = float("nan")
+        y, of = product_of(h, x, w, counts)
+        for e in range(max(1, len(counts))):
+            mine = (of == e).nonzero()[:, 0].cuda()
+            pick = (lambda v: v[e]) if counts else (lambda v: v)
+            exact = special(x[mine], ref.codes_of(pick(w.data), k), pick(w.scale), pick(w.zero) if zeros else None, group)
+            check_special(y[mine], exact, (at, n, k, e))
+        assert not y[len(of):].any()

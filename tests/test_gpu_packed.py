@@ -221,3 +221,68 @@ def test_captured_and_replayed_with_other_inputs(h):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(step(), got)
+
+
+def special(x, codes, scale, zero, group):
+    """x W^T with the infinities and NaN that its 64-bit terms have."""
+    return x.double() @ ref.values(codes, scale, zero, group).T
+
+
+def check_special(got, exact, what):
+    got = got.double()
+    assert torch.equal(got.isnan(), exact.isnan()) and torch.equal(got == float("inf"), exact == float("inf")) and torch.equal(got == -float("inf"), exact == -float("inf")), what
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 9, 1), (2, 5, 7), (1, 40, 8), (3, 70, 300), (4, 33, 1000), (12, 50, 201), (20, 37, 330), (40, 90, 257), (70, 40, 129)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_infinities_keep_their_sign(h, m, n, k, group, zeros):
+    # an infinity times a value is an infinity of the product's sign; NaN where the value is zero (code = zero point) or infinities of both signs meet
+    from paper_2511_13778_amd import packed
+    r = torch.Generator(device="cuda").manual_seed(m + n + k)
+    inf = float("inf")
+    for dtype in FLOATS:
+        w = weights(r, n, k, group, zeros, torch.float32)
+        if zeros:
+            w.zero.copy_(w.zero.round())
+        x = torch.randn((m, k), generator=r, device="cuda").to(dtype)
+        y = packed.gemm(h, x, w)
+        x[0, k - 1] = inf
+        if m > 1:
+            x[m - 1, k // 2] = -inf
+        if m > 2:
+            x[m // 2, 0] = inf
+            x[m // 2, k - 1] = -inf
+        if m > 3:
+            x[1, k // 3] = float("nan")
+        if m > 4:
+            x[2, 0] = x[2, k - 1] = -inf
+        codes = ref.codes_of(w.data, k)
+        exact = special(x, codes, w.scale, w.zero, group)
+        assert exact.isinf().any()
+        for out in {dtype, torch.float32}:
+            check_special(packed.gemm(h, x, w, dtype=out), exact, (dtype, out))
+        rest = x.isfinite().all(1)
+        assert torch.equal(packed.gemm(h, x, w)[rest], y[rest])
+        # one row of W alone with a scale that is no number
+        w.scale[0, n // 2] = float("nan")
+        check_special(packed.gemm(h, x, w), special(x, codes, w.scale, w.zero, group), (dtype, "scale"))
+
+
+@pytest.mark.parametrize("m,n,k", [(2, 9, 5), (1, 40, 300), (4, 70, 1000), (12, 50, 201), (40, 90, 257)])
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sums_that_pass_the_range_on_the_way(h, m, n, k, zeros, dtype):
+    # x near the type's end, scales that bring the results back: 128 + code, codes or their sums alone would be infinite
+    from paper_2511_13778_amd import packed
+    r = torch.Generator(device="cuda").manual_seed(m + n + k)
+    w = weights(r, n, k, 64, zeros, torch.float32)
+    w.scale.copy_(w.scale.clamp(-2.0, 2.0) * 1e-6)
+    x = (torch.rand((m, k), generator=r, device="cuda") * 2.0 - 1.0).to(dtype)
+    x[::2] *= 1e36
+    x[0] *= 300.0
+    x[:, 0] = torch.finfo(dtype).max
+    codes = ref.codes_of(w.data, k)
+    assert x.isfinite().all()
+    for out in {dtype, torch.float32}:
+        check_product(packed.gemm(h, x, w, dtype=out), x, codes, w.scale, w.zero, 64, (dtype, out))
