@@ -237,3 +237,24 @@ def test_a_closed_handle_is_refused():
                  lambda: packed.quantize(other, x), lambda: packed.gemm(other, x, w)):
         with pytest.raises(g.OzError):
             call()
+
+
+def test_weights_that_moved_are_not_served_from_old_copies(h):
+    from paper_2511_13778_amd import experts as ex
+    r = torch.Generator(device="cuda").manual_seed(6)
+    n, width, inner, topk = 4, 96, 160, 2
+    w1, w2 = (torch.randn(s, generator=r, device="cuda") * s[-1] ** -0.5 for s in ((n, inner, width), (n, width, inner)))
+    layer = ex.ExpertLayer(h, w1, w2)
+    layer.pack_weights(group=32)
+    x = torch.randn((6, width), generator=r, device="cuda").bfloat16()
+    c = ex.choose(h, torch.randn((6, n), generator=r, device="cuda"), topk, balance=False)
+    layer.serve_packed(x, c.ids, c.weights)
+    layer.update(gradient(r, n, inner, width), gradient(r, n, width, inner), 0.5)
+    with pytest.raises(ValueError, match="pack_weights"):
+        layer.serve_packed(x, c.ids, c.weights)
+    layer.pack_weights(group=32)
+    fresh = ex.ExpertLayer(h, w1, w2)
+    fresh.pack_weights(group=32)
+    assert torch.equal(layer.serve_packed(x, c.ids, c.weights), fresh.serve_packed(x, c.ids, c.weights))
+    layer.prepare_weights()                   # the same weights: their copies stay
+    assert torch.equal(layer.serve_packed(x, c.ids, c.weights), fresh.serve_packed(x, c.ids, c.weights))
