@@ -166,13 +166,12 @@ def choose(h: g.Handle, scores, topk: int, live=None, normalize=True, balance=Tr
     c._made = c.ids, c.weights
     more = (None, None, None, None, None, 0)
     if balance:
-        # one allocation: the four results of the batch and, behind them, the workspace
+        # one allocation for the four results of the batch, which a kept loss holds on to, and another for the workspace, which goes back after the call
         need = h.choose_experts_workspace_bytes(tokens, experts)
-        first = (2 * experts + 65) // 64 * 64
-        table = scores.new_empty(first + (need + 3) // 4, dtype=torch.float32)
+        table, ws = scores.new_empty(2 * experts + 2, dtype=torch.float32), scores.new_empty(need, dtype=torch.uint8)
         c._table = table, experts
         at = table.data_ptr()
-        more = (at, at + 4 * experts, at + 4 * experts + 4, at + 8 * experts + 4, at + 4 * first, need)
+        more = (at, at + 4 * experts, at + 4 * experts + 4, at + 8 * experts + 4, ws.data_ptr(), need)
     h.call("oz_choose_experts", stream_of(scores), tokens, experts, topk, scores.data_ptr(), ld, float_type(scores.dtype), _live(live, tokens),
            int(c.normalize), c.ids.data_ptr(), c.weights.data_ptr(), *more)
     return c

@@ -307,3 +307,17 @@ def test_not_a_number_in_all_of_a_row(h, dtype, experts, topk, normalize):
     c = ex.choose(h, x.cuda(), topk, live=live.cuda(), normalize=normalize)
     for weights, dloss in ((dw, 0.5), (dw, None), (None, 0.5)):
         assert not ex.choose_backward(h, x.cuda(), c, weights, dloss).cpu()[bad].any()
+
+
+def test_results_hold_no_workspace(h):
+    from paper_2511_13778_amd import experts as ex
+    x = scores_of(14, 20000, 256, torch.bfloat16).cuda()
+    need = h.choose_experts_workspace_bytes(20000, 256)
+    assert need > 100000
+    c = ex.choose(h, x, 4)
+    for part in (c.counts, c.counted, c.shares, c.loss):
+        assert part.untyped_storage().nbytes() <= 4 * (2 * 256 + 64)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    kept = [ex.choose(h, x, 4).loss for _ in range(50)]
+    assert torch.cuda.memory_allocated() - before < 50 * 8192 and all(torch.equal(a, kept[0]) for a in kept)
