@@ -269,12 +269,13 @@ class ExpertLayer:
         return combine(h, packed.gemm_grouped(h, inner, self.p2, routing.offsets), routing, weights)
 
     @torch.no_grad()
-    def update(self, dw1, dw2, rate):
+    def update(self, dw1, dw2, rate, dtype=torch.bfloat16):
         """A step of the weights against their gradients (or running means of them) made orthogonal, then prepare_weights(): each expert's matrix moves by
         rate in every direction, by rate * sqrt(out / in) where it makes more values than it takes.  In bfloat16, whose rounding of
-        the direction (0.2 %) is far below what Newton-Schulz leaves open.  The 4-bit copies, which are the old weights', are dropped."""
+        the direction (0.2 %) is far below what Newton-Schulz leaves open, or, in some three times as long, dtype=torch.float32 (10^-6).  The 4-bit
+        copies, which are the old weights', are dropped."""
         for w, d in ((self.w1, dw1), (self.w2, dw2)):
-            w.sub_(orthogonal.orthogonalize(self.h, d.bfloat16()), alpha=rate * max(1.0, w.shape[1] / max(w.shape[2], 1)) ** 0.5)
+            w.sub_(orthogonal.orthogonalize(self.h, d.to(dtype)), alpha=rate * max(1.0, w.shape[1] / max(w.shape[2], 1)) ** 0.5)
         self.p1 = self.p2 = None
         self.prepare_weights()
 

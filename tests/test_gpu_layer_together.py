@@ -258,3 +258,21 @@ def test_weights_that_moved_are_not_served_from_old_copies(h):
     assert torch.equal(layer.serve_packed(x, c.ids, c.weights), fresh.serve_packed(x, c.ids, c.weights))
     layer.prepare_weights()                   # the same weights: their copies stay
     assert torch.equal(layer.serve_packed(x, c.ids, c.weights), fresh.serve_packed(x, c.ids, c.weights))
+
+
+def test_update_in_all_of_the_gradients_bits(h):
+    # float32 gradients as they are where that is asked for: off by the method's 22-bit operands and the difference of the weights, far below a rounding to bfloat16
+    from paper_2511_13778_amd import experts as ex
+    r = torch.Generator(device="cuda").manual_seed(7)
+    n, width, inner = 3, 60, 100
+    w1, w2 = (torch.randn(s, generator=r, device="cuda") * s[-1] ** -0.5 for s in ((n, inner, width), (n, width, inner)))
+    layer, before = ex.ExpertLayer(h, w1, w2), (w1.clone(), w2.clone())
+    dw1, dw2 = gradient(r, n, inner, width), gradient(r, n, width, inner)
+    layer.update(dw1, dw2, 0.5, dtype=torch.float32)
+    for w, old, d, s in ((w1, before[0], dw1, (inner / width) ** 0.5), (w2, before[1], dw2, 1.0)):
+        for i in range(n):
+            exact = ref.orthogonalize(d[i], 5, QUINTIC, 1e-7)
+            own = off(ref.orthogonalize_in_parts(d[i], 5, QUINTIC, 1e-7, 2), exact)
+            sums = 3 * max(d[i].shape) ** 0.5 * F * 3.4445 ** 2
+            last = 3 * F * (old[i].double().norm() + exact.norm()) / (0.5 * s * exact.norm())       # the product with the rate and the difference, in float32
+            assert off((old[i] - w[i]).double() / (0.5 * s), exact) <= 1.5 * own + sums + F + last.item() < 2.0 ** -12
