@@ -436,8 +436,9 @@ oz_status_t oz_packed_gemm(oz_handle_t handle, void* stream, int64_t groups, con
  * values above 0.003 |X| into 0.68 .. 1.13 or so: the direction of a weight update that keeps X's singular vectors.
  * Z is held as 4096 Z, elements of A off its diagonal as 16384 A and those of b A + c A^2 as 4096 of them, in 16-bit floating point (up to 65504): the
  * coefficients have to keep singular values below 2 and the last below 16, or elements become infinite (these do: 1.3 and 4).  X in OZ_BF16: operands
- * of the products have 11 bits, an error of about 0.002 of the result with its rounding; OZ_F32, OZ_F16: 22 bits, about 10^-6.  Everything else is in 32
- * bits, |X| in 64.  A matrix of zeros stays one if eps > 0; an infinity or a NaN makes NaN of its matrix.
+ * of the products have 11 bits, among them the off-diagonals of A, which have no more in b A either, and Z itself has 22: an error of about 0.002 of the
+ * result with its rounding.  OZ_F32, OZ_F16 (and values of OZ_BF16 given as OZ_F32): operands of 22 bits, Z of 32, about 10^-6, in some three times as long.
+ * Diagonals and sums are in 32 bits, |X| in 64.  A matrix of zeros stays one if eps > 0; an infinity or a NaN makes NaN of its matrix.
  * Y may be X, with the same strides.  Sums are in a fixed order.  Limits: rows, cols <= 32768, batch <= 65535, 1 <= steps <= 64.
  * workspace: 256-byte aligned, oz_orthogonalize_workspace_bytes(...) bytes (up to 24 per element of a few matrices, of which more are done in turn). */
 size_t oz_orthogonalize_workspace_bytes(oz_handle_t handle, int64_t batch, int64_t rows, int64_t cols, int32_t type);

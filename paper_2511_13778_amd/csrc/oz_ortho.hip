@@ -1,13 +1,15 @@
 // A matrix made orthogonal by Newton-Schulz steps: X0 = G / (|G| + eps), X <- a X + (b A + c A^2) X with A = X X^T.  X is m x n, m <= n (a tall G is
 // taken transposed).
 //
-// A step is three products on v_mfma_f32_16x16x32_f16.  X, in 32 bits, goes into them in 16; what makes that exact enough is that everything large and
-// regular stays in 32 bits: with A = diag(d) + O (O without a diagonal) and P = a I + b A + c A^2
+// A step is three products on v_mfma_f32_16x16x32_f16.  X goes into them in 16 bits; what makes that exact enough is that everything large and
+// regular keeps more: with A = diag(d) + O (O without a diagonal) and P = a I + b A + c A^2
 //     P_ij = b O_ij + c ((d_i + d_j) O_ij + (O O)_ij),   P_ii = a + b d_i + c (d_i^2 + (O O)_ii),   X <- diag(P_ii) X + offdiag(P) X
-// only O, off-diagonals of P and X are rounded to 16 bits as operands, in a power of two's scale.  A step multiplies an error in X by up to a, so
-// after five a single rounding to 16 bits in one of these places is 2e-4 to 1e-3 of the result (A's diagonal left in O: 2e-3): bfloat16 results, whose
-// own rounding is 1.7e-3, take one 16-bit part of each operand; float32 and float16 results take two, x = hi + lo with 22 bits, and the
-// products hi hi + hi lo + lo hi.
+// only O, off-diagonals of P and X are rounded to 16 bits as operands, in a power of two's scale; diagonals and sums have 32.  A step multiplies an error in X by up
+// to a, so after five a single rounding to 16 bits in one of these places is 2e-4 to 1e-3 of the result (A's diagonal left in O: 2e-3).
+//   bfloat16 results, whose own rounding is 1.7e-3, take one 16-bit part of each operand.  O is held in that part alone, so its linear terms in P have 11 bits as well:
+//   512 x 1024, before the result's rounding, 5.6e-4 instead of the 5.3e-4 that its rest would leave, for four bytes more of each element written and read.  X
+//   keeps its rest, 22 bits in all, since X <- diag(P_ii) X carries it on; 32 instead would leave the same 5.6e-4 for two bytes more.
+//   float32 and float16 results take two parts, x = hi + lo with 22 bits, and the products hi hi + hi lo + lo hi; X has 32 bits, O in its linear terms 22.
 //
 // O, offdiag(P) and X are kept with their rows padded by zeros to whole tiles, so no product has edges.  A and A^2 are symmetric: their tiles below the
 // diagonal are computed and written to both sides.

@@ -173,3 +173,23 @@ def orthogonalize_bound(x, coefficients, eps, n):
     dph = dp + u * p + tiny / 4096
     bound = dph @ z + p @ dzh + (m + 8) * 2 * f * (p @ z)
     return orthogonalize(x, 1, coefficients, eps), (bound.T if x.shape[0] > x.shape[1] else bound)
+
+
+def orthogonalize_as_run(x, steps, coefficients, eps, rounded):
+    """Steps on bfloat16 as they are made, in 64 bits but for the roundings: X in two parts, operands of one, and, if `rounded`, the off-diagonals of A in the linear
+    terms of b A + c A^2 the rounded ones that the product takes."""
+    a, b, c = coefficients
+    z = x.double()
+    z = (z / (z.square().sum().sqrt() + eps)).float().double()
+    z = z.T if z.shape[0] > z.shape[1] else z
+    for _ in range(steps):
+        z, zh = parts(z, 4096.0, 2), parts(z, 4096.0, 1)
+        gram = zh @ zh.T
+        d = gram.diagonal()
+        off = gram - torch.diag(d)
+        oh = parts(off, 16384.0, 1)
+        square = oh @ oh
+        p = (b + c * (d[:, None] + d[None, :])) * (oh if rounded else off) + c * square
+        e = a + b * d + c * (d * d + square.diagonal())
+        z = e[:, None] * z + parts(p - torch.diag(p.diagonal()), 4096.0, 1) @ zh
+    return z.T if x.shape[0] > x.shape[1] else z

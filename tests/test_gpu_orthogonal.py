@@ -140,3 +140,32 @@ def test_captured_and_replayed_with_other_inputs(h):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(orthogonal.orthogonalize(h, x), got)
+
+
+@pytest.mark.parametrize("coefficients", [QUINTIC, (0.0, -1.7, 0.0)])
+def test_one_step_of_bfloat16_as_described(h, coefficients):
+    # Off-diagonals of A are rounded to their 11 bits once, for both of the terms they are in; X is held in 22.  A step modelled so gives the same bfloat16 results but where
+    # a 32-bit sum of another order, off by some 2^-22, moves one of the six roundings of a matrix (a chance of 2^-22 / 2^-11 each, which then changes an eighth of its
+    # results) or the result's own (2^-22 / 2^-8): below 0.1 %.  Without the rounding of A in the linear terms 3 and 12 % differ.
+    from paper_2511_13778_amd import orthogonal
+    r = torch.Generator(device="cuda").manual_seed(8)
+    x = (torch.randn((200, 1, 500), generator=r, device="cuda") + 0.3 * torch.randn((200, 3, 500), generator=r, device="cuda")).bfloat16()
+    got = orthogonal.orthogonalize(h, x, steps=1, coefficients=coefficients, eps=EPS)
+    for rounded, least, most in ((True, 0.0, 0.01), (False, 0.02, 0.3)):
+        model = torch.stack([ref.orthogonalize_as_run(m, 1, coefficients, EPS, rounded) for m in x]).bfloat16()
+        other = (model != got).double().mean().item()
+        assert least <= other <= most, (rounded, other)
+
+
+@pytest.mark.parametrize("rows,cols", [(48, 48), (64, 200), (200, 64), (300, 513)])
+def test_five_steps_of_bfloat16_as_described(h, rows, cols):
+    # the model's loss where all of the kernel's roundings are in it: no half as much again
+    from paper_2511_13778_amd import orthogonal
+    r = torch.Generator(device="cuda").manual_seed(rows + cols)
+    x = torch.randn((rows, cols), generator=r, device="cuda").bfloat16()
+    exact = ref.orthogonalize(x, 5, QUINTIC, EPS)
+    own = off(ref.orthogonalize_as_run(x, 5, QUINTIC, EPS, True), exact)
+    sums = 3 * max(x.shape) ** 0.5 * 2.0 ** -24 * 3.4445 ** 2
+    got = off(orthogonal.orthogonalize(h, x).double(), exact)
+    # independent of the result's own rounding, whose square is at most 2^-16 / 3 of the result's
+    assert got <= ((1.1 * own + sums) ** 2 + 2.0 ** -16 / 3) ** 0.5, (got, own)
