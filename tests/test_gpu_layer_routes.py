@@ -98,3 +98,24 @@ def test_infinities_in_packed_products(h, at, dtype):
             exact = special(x[mine], ref.codes_of(pick(w.data), k), pick(w.scale), pick(w.zero) if zeros else None, group)
             check_special(y[mine], exact, (at, n, k, e))
         assert not y[len(of):].any()
+
+
+@pytest.mark.parametrize("at", sorted(lr.PACKED), ids=str)
+def test_float32_rows_lose_nothing(h, at):
+    # 1 in one column of W and nothing elsewhere: that column of x bit for bit, whichever block, part of a block, strip or wave it lies in
+    for counts, behind, n, k, group, kinds in lr.PACKED[at]:
+        if 4 not in kinds:
+            continue
+        r = torch.Generator(device="cuda").manual_seed(n + k)
+        w = weights(r, n, k, group, False, torch.float32, (len(counts),) if counts else ())
+        m = sum(counts) + behind
+        x = torch.randn((m, k), generator=r, device="cuda") * 10.0 ** torch.randint(-25, 30, (m, 1), generator=r, device="cuda")
+        w.data.fill_(0x88)
+        w.scale.fill_(1.0)
+        for col in {0, k // 2, k // 128 * 128 - 1, k // 128 * 128, k - 1}:
+            if not 0 <= col < k:
+                continue
+            w.data[..., col // 2] = 0x98 if col % 2 else 0x89
+            y, of = product_of(h, x, w, counts)
+            assert torch.equal(y[:len(of)], x[:len(of), col:col + 1].expand(-1, n)), (at, n, k, col)
+            w.data[..., col // 2] = 0x88
