@@ -3,7 +3,7 @@
 // A workgroup has 16 R rows of W and 16 rows of x; its waves share k, in runs of blocks of 128, and add up their sums through LDS in the waves'
 // order.  code - 8 is exact in x's 16-bit type, and goes with x into v_mfma_f32_16x16x32 (float32 x as three bfloat16 parts, exactly); scales
 // are applied to each group's sum, in 32 bits, so a result of 16 bits has one rounding, the last.  The sums of x that zero points need are one
-// more matrix instruction, with a matrix of ones.  One row of 4096 x 4096 bfloat16: 5.7 us, of which a launch is 2.4; of 8192 x 8192 11 (3.0 TB/s); 96 rows of 32
+// more matrix instruction, with a matrix of ones.  One row of 4096 x 4096 bfloat16: 5.1 us, of which a launch is 2.4; of 8192 x 8192 10 (3.4 TB/s); 96 rows of 32
 // experts, 2048 x 2048: 18 (3.9 TB/s).
 #pragma once
 
