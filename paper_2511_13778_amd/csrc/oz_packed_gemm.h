@@ -149,42 +149,41 @@ struct ScaleLoad {
 
 // Sums of code - 8 (or of 128 + code, less what is too much) say nothing where x has an infinity, or leave float32's range on the way to a result that lies
 // in it.  Results that are not finite are therefore computed once more as they are defined, in 64 bits: sums of x * (scale * (code - zero)), here of N columns
-// of the result from `col` on, over eight columns of x at a time, `step` apart.
+// of the result from `col` on, over the eight columns of x from l0 on.
 template <int N, typename X>
-__device__ __forceinline__ void defined_sums(const PackedGemm& g, int of, const X* x, int col, int first, int step, double (&sum)[N]) {
+__device__ __forceinline__ void add_defined(const PackedGemm& g, int of, const X* x, int col, int l0, double (&sum)[N]) {
+    if (l0 >= g.k) return;
     const ScaleLoad scales(g.w.scale, g.w.type), zeros(g.w.zero, g.w.type);
-    const uint8_t* const w = g.w.data + of * g.w.stride;
+    uint32_t codes[N];
+    double scale[N], zero[N];
 #pragma unroll
-    for (int c = 0; c < N; ++c) sum[c] = 0.0;
-#pragma unroll 1
-    for (int l0 = first; l0 < g.k; l0 += step) {
-        uint32_t codes[N];
-        double scale[N], zero[N];
-#pragma unroll
-        for (int c = 0; c < N; ++c) {
-            const int64_t row = min(col + c, g.n - 1), at = of * g.w.scale_stride + int64_t(l0 >> g.w.shift) * g.w.scale_ld + row;
-            codes[c] = *reinterpret_cast<const uint32_t*>(w + row * g.w.ld + l0 / 2);
-            scale[c] = scales.value(scales.fetch(at));
-            zero[c] = g.w.zero ? zeros.value(zeros.fetch(at)) : 8.0f;
-        }
-        for (int i = 0; i < 8; ++i)
-            if (l0 + i < g.k) {
-                const double v = to_float(x[l0 + i]);
-#pragma unroll
-                for (int c = 0; c < N; ++c) sum[c] = fma(v, scale[c] * (double((codes[c] >> (4 * i)) & 15u) - zero[c]), sum[c]);
-            }
+    for (int c = 0; c < N; ++c) {
+        const int64_t row = min(col + c, g.n - 1), at = of * g.w.scale_stride + int64_t(l0 >> g.w.shift) * g.w.scale_ld + row;
+        codes[c] = *reinterpret_cast<const uint32_t*>(g.w.data + of * g.w.stride + row * g.w.ld + l0 / 2);
+        scale[c] = scales.value(scales.fetch(at));
+        zero[c] = g.w.zero ? zeros.value(zeros.fetch(at)) : 8.0f;
     }
+    for (int i = 0; i < 8; ++i)
+        if (l0 + i < g.k) {
+            const double v = to_float(x[l0 + i]);
+#pragma unroll
+            for (int c = 0; c < N; ++c) sum[c] = fma(v, scale[c] * (double((codes[c] >> (4 * i)) & 15u) - zero[c]), sum[c]);
+        }
 }
-// Every lane of a wave, with `s` the results of its row of x and four columns from `col` on.  One infinity among 64 x 8192 bfloat16 by 8192: 244 us instead of 27; a NaN 29.
+// Every lane of a wave, with `s` the results of its row of x and four columns from `col` on.  One infinity among 64 x 8192 bfloat16 by 8192: 250 us instead of 27,
+// one in each row 2260, many 280; a NaN 30.
 template <typename X>
 __device__ __forceinline__ void mend_results(const PackedGemm& g, int of, bool in, int row, int col, v4f& s) {
-    const bool odd = in && !(__builtin_isfinite(s[0]) && __builtin_isfinite(s[1]) && __builtin_isfinite(s[2]) && __builtin_isfinite(s[3]));
-    uint64_t left = __ballot(odd);
+    int odd = 0;                              // which of them
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd |= in && !__builtin_isfinite(s[i]) ? 1 << i : 0;
+    uint64_t left = __ballot(odd != 0);
     if (__builtin_expect(left == 0, true)) return;
     const int lane = threadIdx.x & 63;
     int seen = -1;
     while (left) {
         const int from = __builtin_ctzll(left), r = __builtin_amdgcn_readlane(row, from), c = __builtin_amdgcn_readlane(col, from);
+        const int which = __builtin_amdgcn_readlane(odd, from);
         const X* const x = static_cast<const X*>(g.x) + int64_t(r) * g.ldx;
         left &= left - 1;
         if (r != seen) {
@@ -201,12 +200,18 @@ __device__ __forceinline__ void mend_results(const PackedGemm& g, int of, bool i
             }
             seen = r;
         }
-        double sum[4];
-        defined_sums<4>(g, of, x, c, lane * 8, 512, sum);
+        double sum[4] = {0.0, 0.0, 0.0, 0.0};
+        // until all that are asked for are NaN, which they stay
+        for (int l0 = 0, open = which; l0 < g.k && open; l0 += 512) {
+            add_defined<4>(g, of, x, c, l0 + lane * 8, sum);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (__any(sum[i] != sum[i])) open &= ~(1 << i);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             for (int d = 1; d < 64; d *= 2) sum[i] += __shfl_xor(sum[i], d);
-            s[i] = lane == from && !__builtin_isfinite(s[i]) ? float(sum[i]) : s[i];
+            s[i] = lane == from && (which >> i & 1) ? float(sum[i]) : s[i];
         }
     }
 }
@@ -411,8 +416,8 @@ __global__ __launch_bounds__(256) void packed_gemm_short_kernel(PackedGemm g) {
         }
         sum = scale * (g.w.zero ? fmaf(8.0f - zero, all, sum) : sum);
         if (!__builtin_isfinite(sum)) {
-            double defined[1];
-            defined_sums<1>(g, of, x, int(col), 0, 8, defined);
+            double defined[1] = {0.0};
+            add_defined<1>(g, of, x, int(col), 0, defined);
             sum = float(defined[0]);
         }
     }
